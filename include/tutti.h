@@ -475,6 +475,135 @@ int tutti_kv_restore_layer_noalloc(const tutti_geom_t *geom, int device, uint32_
                                    tutti_cqe_t *cqe_out, void *stream);
 
 /* ------------------------------------------------------------------------- */
+/* Operators on the pool: what a model's layer does with it between restore    */
+/* and save.  (No counterpart in the paper, whose serving engine has them.)    */
+/* ------------------------------------------------------------------------- */
+
+#define TUTTI_DTYPE_BF16 0
+#define TUTTI_DTYPE_FP16 1
+
+#define TUTTI_ROPE_HALF 0  /* dimension i turns with i + rot_dim / 2 */
+#define TUTTI_ROPE_PAIRS 1 /* dimension 2 i turns with 2 i + 1       */
+
+/*
+ * One step's tokens against the pool: sequence s brings the rows [q_start[s], q_start[s+1]) of
+ * the step's token arrays (one row when it decodes, many when a prompt chunk is computed behind a
+ * restored prefix, none is allowed), which are the LAST of its ctx_len[s] tokens, and its
+ * tokens live in the pool blocks block_ids[blk_start[s] .. blk_start[s+1]) in logical order
+ * (extra entries are never read).  Row i of a sequence with n rows is at position
+ * ctx_len - n + i; a row whose position comes out negative (ctx_len smaller than n, as in a
+ * padded batch) is padding.  All five arrays are DEVICE pointers owned by the caller; they may
+ * change between calls and between replays of a captured graph, within the host-known sizes:
+ * n_tok rows in the token arrays (rows at and behind q_start[n_seq] are left as they are),
+ * n_blk entries in block_ids, max_new rows of one sequence at most.
+ * status (may be NULL): a device or mapped pinned int32 that the caller has set to 0; the first
+ * problem found is written to it.  TUTTI_EINVAL: a sequence's numbers contradict each other or
+ * the sizes; it is skipped, nothing is read or written for it.  TUTTI_EFAULT: a block id that is
+ * needed is outside the pool; that block is neither written nor attended to.
+ */
+typedef struct tutti_step {
+    uint32_t n_seq;
+    uint32_t n_tok;
+    uint32_t n_blk;
+    uint32_t max_new;
+    const uint32_t *q_start;   /* [n_seq + 1] */
+    const uint32_t *ctx_len;   /* [n_seq]     */
+    const uint32_t *blk_start; /* [n_seq + 1] */
+    const int32_t *block_ids;  /* [n_blk]     */
+    int32_t *status;
+} tutti_step_t;
+
+/* A step's projections, device pointers to [n_tok][heads][head_dim] elements of dtype; strides
+ * in elements from one token to the next, so that q, k and v may be parts of one packed row.
+ * Base addresses are 16-byte aligned, strides multiples of 8.  q and q_out may be the same
+ * array; both NULL (and n_q_heads 0) leaves the queries out. */
+typedef struct tutti_tokens {
+    uint32_t dtype; /* TUTTI_DTYPE_* */
+    uint32_t n_q_heads;
+    uint64_t q_stride, k_stride, v_stride, q_out_stride;
+    const void *q;
+    const void *k;
+    const void *v;
+    void *q_out;
+} tutti_tokens_t;
+
+/* Rotation of queries and keys: table is a device pointer to [n_pos][rot_dim] floats, the
+ * rot_dim / 2 cosines of a position and then its rot_dim / 2 sines, 16-byte aligned.  rot_dim is
+ * a multiple of 16 and at most head_dim; the dimensions behind it are copied. */
+typedef struct tutti_rope {
+    uint32_t style; /* TUTTI_ROPE_* */
+    uint32_t rot_dim;
+    uint64_t n_pos;
+    const float *table;
+} tutti_rope_t;
+
+/* Queries and outputs of one attention call; layout rules as for tutti_tokens_t.  lse (may be
+ * NULL) receives [n_tok][n_q_heads] natural logarithms of the softmax denominators. */
+typedef struct tutti_attend {
+    uint32_t dtype;
+    uint32_t n_q_heads;
+    uint64_t q_stride, out_stride;
+    const void *q;
+    void *out;
+    float *lse;
+    float scale; /* factor on q . k, finite */
+    uint32_t reserved;
+} tutti_attend_t;
+
+/*
+ * Scales of an 8-bit pool layer (geometry with elem_bytes = 1: e4m3 codes): k_scale and v_scale
+ * are device pointers to [n_blocks][n_kv_heads] floats, n_blocks that of the layer's
+ * tutti_pool_register (call it first; registering the pool again forgets the scales).  A stored
+ * key or value is code * scale of its block and head.  To move the scales with the blocks, give
+ * them a context of their own: a pool of n_blocks blocks of one token of n_kv_heads 4-byte
+ * elements (block_tokens 1, head_dim 1, n_kv_heads a multiple of 4) takes the same block ids.
+ */
+int tutti_scales_register(tutti_ctx_t *ctx, uint32_t layer, float *k_scale, float *v_scale,
+                          uint64_t n_blocks);
+
+/*
+ * Append a step's keys and values to layer `layer` of the pool, one launch: queries and keys
+ * are rotated by their positions on the way (rope NULL: not rotated), queries go to q_out, keys
+ * and values into their blocks.  Elements of a 16-bit pool have the type `dtype`.
+ * In an 8-bit pool a block and head has one scale for its keys and one for its values, a power
+ * of two: the smallest that brings the largest finite new value to 448 or less, at least the
+ * scale that the block has if it already holds earlier tokens of the sequence, and at least
+ * 2^-100.  Where the scale grows, the block's earlier codes are rounded again to the new one.
+ * Infinite values are stored as +-448 codes, NaN as NaN.
+ * A block that receives tokens must belong to one sequence of the step only (prefix blocks that
+ * several sequences share are only read by attention); two sequences that write the same rows,
+ * or in an 8-bit pool the same block, race.  Padding rows are skipped.  TUTTI_EINVAL in
+ * *status also for a sequence with ctx_len > rope->n_pos.
+ * Asynchronous on `stream`, graph-capturable.  TUTTI_EINVAL for a layer that is not registered,
+ * elem_bytes other than 2, or 1 with registered scales; head_dim not a multiple of 16 or above
+ * 256; n_q_heads not a multiple of n_kv_heads; a bad stride, alignment, type or rope.
+ */
+int tutti_kv_append_layer(tutti_ctx_t *ctx, uint32_t layer, const tutti_step_t *step,
+                          const tutti_tokens_t *tokens, const tutti_rope_t *rope, void *stream);
+
+/*
+ * Causal attention of a step's queries over layer `layer` of the pool: query head h reads KV
+ * head h / (n_q_heads / n_kv_heads); the row at position p attends to the keys at positions
+ * 0..p of its sequence (its own key included: append first).
+ *     out = sum_j softmax_j(scale * q . k_j) v_j,   lse = ln sum_j exp(scale * q . k_j)
+ * A row that sees no key (padding, or only blocks outside the pool) gets out = 0 and
+ * lse = -infinity.  Cache bytes behind a sequence's last token are never used, whatever they
+ * hold.  Sums and softmax statistics are 32-bit; probabilities are rounded to 16 bits for
+ * the product with the values.
+ * The handle holds the workspace in which parts of a long sequence are joined: calls on one
+ * handle must be ordered after each other (one stream, or events; replays of captured graphs
+ * too), calls that may overlap need a handle each.
+ * Asynchronous on `stream`, graph-capturable.  TUTTI_EINVAL for a layer that is not
+ * registered, head_dim other than 64 or 128, elem_bytes other than 2, or 1 with registered
+ * scales; n_q_heads not a multiple of n_kv_heads; a bad stride, alignment, type or scale.
+ */
+typedef struct tutti_attn tutti_attn_t;
+int tutti_attn_create(tutti_ctx_t *ctx, tutti_attn_t **out);
+int tutti_attn_destroy(tutti_attn_t *attn);
+int tutti_kv_attend_layer(tutti_attn_t *attn, uint32_t layer, const tutti_step_t *step,
+                          const tutti_attend_t *io, void *stream);
+
+/* ------------------------------------------------------------------------- */
 /* Slack-aware I/O scheduler (Section 3.3).  Pure host logic.                  */
 /* ------------------------------------------------------------------------- */
 #define TUTTI_PHASE_PREFILL 0

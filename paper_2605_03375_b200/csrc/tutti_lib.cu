@@ -7,9 +7,11 @@
 #include <new>
 #include <string>
 #include <thread>
+#include <utility>
 #include <vector>
 
 #include "tutti_internal.h"
+#include "tutti_paged.h"
 
 using namespace tutti;
 
@@ -72,6 +74,7 @@ struct tutti_ctx {
     void *partition = nullptr;   // SM partition state (tutti_partition.cu)
     bool pool_hnd = false;       // pool blocks are [head][token][dim]
     StoreTensorMaps maps;        // for the transposing bulk copies
+    std::vector<std::pair<float *, float *>> scales;   // K, V scales of an 8-bit pool layer
     PoolLayerDev *d_pools = nullptr;   // device copy of the pool table (multi-layer builds)
 };
 
@@ -113,6 +116,8 @@ extern "C" {
 // accessors for tutti_partition.cu
 void **tutti_ctx_partition_slot_(tutti_ctx_t *ctx) { return &ctx->partition; }
 int tutti_ctx_device_(tutti_ctx_t *ctx) { return ctx->device; }
+int tutti_ctx_sms_(tutti_ctx_t *ctx) { return ctx->device_sms; }
+const tutti_geom_t *tutti_ctx_geom_(tutti_ctx_t *ctx) { return &ctx->geom; }
 void tutti_set_cuda_error_(const char *msg) { g_last_cuda_error = msg; }
 
 uint32_t tutti_version(void) { return 0x000100; }
@@ -189,6 +194,7 @@ int tutti_ctx_create(const tutti_geom_t *geom, int device, tutti_ctx_t **out) {
     c->device = device;
     c->device_sms = prop.multiProcessorCount;
     c->pool.assign(geom->n_layers, PoolLayer{0, 0, 0, 0, false});
+    c->scales.assign(geom->n_layers, {nullptr, nullptr});
     for (auto &s : c->store) s = StoreDev{0, 0, 0, false, false};
     memset(&c->maps, 0, sizeof(c->maps));
     c->opt = CopyOptions{0, 2000000ull, 4, 0, 0, 0, 0, 0};   // 0 = chosen per launch
@@ -232,9 +238,35 @@ int tutti_pool_register(tutti_ctx_t *ctx, uint32_t layer, void *k_base, void *v_
     if ((k | v | block_stride) & 15) return TUTTI_EINVAL;
     if (block_stride < ctx->layout.block_bytes || n_blocks > 0x7fffffffull) return TUTTI_EINVAL;
     ctx->pool[layer] = PoolLayer{k, v, block_stride, n_blocks, true};
+    ctx->scales[layer] = {nullptr, nullptr};
     PoolLayerDev pl{k, v, block_stride, n_blocks};
     DeviceGuard guard(ctx->device);
     CK(cudaMemcpy(ctx->d_pools + layer, &pl, sizeof(pl), cudaMemcpyHostToDevice));
+    return TUTTI_OK;
+}
+
+int tutti_scales_register(tutti_ctx_t *ctx, uint32_t layer, float *k_scale, float *v_scale,
+                          uint64_t n_blocks) {
+    if (!ctx || layer >= ctx->geom.n_layers || !k_scale || !v_scale) return TUTTI_EINVAL;
+    if (ctx->geom.elem_bytes != 1 || !ctx->pool[layer].registered) return TUTTI_EINVAL;
+    if ((((uint64_t)k_scale | (uint64_t)v_scale) & 3) || n_blocks != ctx->pool[layer].n_blocks)
+        return TUTTI_EINVAL;
+    ctx->scales[layer] = {k_scale, v_scale};
+    return TUTTI_OK;
+}
+
+// The view that the operators on the pool compute with; TUTTI_EINVAL for a layer they cannot use.
+int tutti_ctx_pool_view_(tutti_ctx_t *ctx, uint32_t layer, PoolView *v, uint32_t *elem_bytes) {
+    if (layer >= ctx->geom.n_layers || !ctx->pool[layer].registered) return TUTTI_EINVAL;
+    const tutti_geom_t &g = ctx->geom;
+    if (g.elem_bytes != 2 && !(g.elem_bytes == 1 && ctx->scales[layer].first)) return TUTTI_EINVAL;
+    const PoolLayer &p = ctx->pool[layer];
+    const uint64_t row = (uint64_t)g.head_dim * g.elem_bytes;
+    *v = PoolView{p.k_base, p.v_base, p.block_stride, (uint32_t)p.n_blocks, g.block_tokens, g.n_kv_heads,
+                  g.head_dim, ctx->pool_hnd ? row : ctx->layout.token_bytes,
+                  ctx->pool_hnd ? row * g.block_tokens : row,
+                  ctx->scales[layer].first, ctx->scales[layer].second};
+    *elem_bytes = g.elem_bytes;
     return TUTTI_OK;
 }
 

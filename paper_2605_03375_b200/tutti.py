@@ -23,6 +23,8 @@ OPT_COPY_ENGINE, OPT_WAIT_NS, OPT_CTAS_PER_SM, OPT_BULK_WARPS, OPT_BULK_STAGES, 
 POOL_NHD, POOL_HND = 0, 1
 OP_FLAG_HND = 0x100
 ENGINE_AUTO, ENGINE_LDST, ENGINE_BULK = 0, 1, 2
+DTYPE_BF16, DTYPE_FP16 = 0, 1
+ROPE_HALF, ROPE_PAIRS = 0, 1
 
 
 class Geom(C.Structure):
@@ -42,6 +44,29 @@ class Batch(C.Structure):
     _fields_ = [("n_req", C.c_uint32), ("n_obj", C.c_uint32), ("n_blk", C.c_uint32),
                 ("plan_epoch", C.c_uint32), ("hit_tokens", C.c_void_p), ("obj_start", C.c_void_p),
                 ("obj_slot", C.c_void_p), ("blk_start", C.c_void_p), ("block_ids", C.c_void_p)]
+
+
+class Step(C.Structure):
+    _fields_ = [("n_seq", C.c_uint32), ("n_tok", C.c_uint32), ("n_blk", C.c_uint32),
+                ("max_new", C.c_uint32), ("q_start", C.c_void_p), ("ctx_len", C.c_void_p),
+                ("blk_start", C.c_void_p), ("block_ids", C.c_void_p), ("status", C.c_void_p)]
+
+
+class Tokens(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("n_q_heads", C.c_uint32), ("q_stride", C.c_uint64),
+                ("k_stride", C.c_uint64), ("v_stride", C.c_uint64), ("q_out_stride", C.c_uint64),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("style", C.c_uint32), ("rot_dim", C.c_uint32), ("n_pos", C.c_uint64),
+                ("table", C.c_void_p)]
+
+
+class Attend(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("n_q_heads", C.c_uint32), ("q_stride", C.c_uint64),
+                ("out_stride", C.c_uint64), ("q", C.c_void_p), ("out", C.c_void_p),
+                ("lse", C.c_void_p), ("scale", C.c_float), ("reserved", C.c_uint32)]
 
 
 class Cqe(C.Structure):
@@ -82,6 +107,8 @@ EXPORTS = [
     "tutti_stream_wait_iocb", "tutti_ring_last_launch_sms", "tutti_ring_poll_range",
     "tutti_ring_set_iocb_bytes", "tutti_sched_profile",
     "tutti_stage_plan", "tutti_stage_copy_layer", "tutti_build_sqes_staged",
+    "tutti_scales_register", "tutti_kv_append_layer", "tutti_attn_create", "tutti_attn_destroy",
+    "tutti_kv_attend_layer",
 ]
 
 _lib: Optional[C.CDLL] = None
@@ -154,6 +181,11 @@ def load(path: Optional[str] = None) -> C.CDLL:
         "tutti_filepool_pin": (C.c_int, [vp, u32, C.c_int]),
         "tutti_filepool_remove": (C.c_int, [vp, u64]),
         "tutti_filepool_stats": (C.c_int, [vp, P(u64), P(u64), P(u64), P(u64), P(u64)]),
+        "tutti_scales_register": (C.c_int, [vp, u32, vp, vp, u64]),
+        "tutti_kv_append_layer": (C.c_int, [vp, u32, P(Step), P(Tokens), P(Rope), vp]),
+        "tutti_attn_create": (C.c_int, [vp, P(vp)]),
+        "tutti_attn_destroy": (C.c_int, [vp]),
+        "tutti_kv_attend_layer": (C.c_int, [vp, u32, P(Step), P(Attend), vp]),
         "tutti_kv_restore_layer_noalloc": (C.c_int, [P(Geom), C.c_int, u32, P(Batch), vp, vp, u64,
                                                      u64, P(vp), P(u64), vp, vp]),
     }
@@ -228,6 +260,18 @@ class Context:
         _check(self.lib.tutti_store_register(self.h, dev, base, nbytes, kind),
                "tutti_store_register")
 
+    def tutti_scales_register(self, layer: int, k_scale: int, v_scale: int, n_blocks: int):
+        """Scales [n_blocks][n_kv_heads] (float32) of an 8-bit pool layer."""
+        _check(self.lib.tutti_scales_register(self.h, layer, k_scale, v_scale, n_blocks),
+               "tutti_scales_register")
+
+    def tutti_kv_append_layer(self, layer: int, step: Step, tokens: Tokens, rope: Optional[Rope] = None,
+                              stream=None, allow: Sequence[int] = ()) -> int:
+        """Write a step's keys and values into the pool, rotating queries and keys on the way."""
+        return _check(self.lib.tutti_kv_append_layer(self.h, layer, step, tokens, rope,
+                                                     _stream_ptr(stream)),
+                      "tutti_kv_append_layer", allow)
+
     def tutti_set_option(self, option: int, value: int):
         _check(self.lib.tutti_set_option(self.h, option, value), "tutti_set_option")
 
@@ -252,6 +296,81 @@ def make_batch(hit_tokens, obj_start, obj_slot, blk_start, block_ids, plan_epoch
               blk_start.data_ptr(), block_ids.data_ptr())
     b._keep = (hit_tokens, obj_start, obj_slot, blk_start, block_ids)
     return b
+
+
+def make_step(q_start, ctx_len, blk_start, block_ids, n_tok: int, max_new: int, status=None) -> Step:
+    """Step struct over device tensors (int32): one step's tokens against the pool."""
+    s = Step(int(ctx_len.numel()), n_tok, int(block_ids.numel()), max_new, q_start.data_ptr(),
+             ctx_len.data_ptr(), blk_start.data_ptr(), block_ids.data_ptr(),
+             None if status is None else status.data_ptr())
+    s._keep = (q_start, ctx_len, blk_start, block_ids, status)
+    return s
+
+
+def _dtype_code(t) -> int:
+    name = str(t.dtype)
+    if name == "torch.bfloat16":
+        return DTYPE_BF16
+    if name == "torch.float16":
+        return DTYPE_FP16
+    raise TuttiError(EINVAL, f"tensor of type {name}")
+
+
+def _rows(t, like) -> int:
+    """Token stride of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
+    heads, dim = t.shape[1], t.shape[2]
+    by_token, by_head, by_dim = t.stride()
+    if t.dtype != like.dtype or by_dim != 1 or (by_head != dim and heads > 1):
+        raise TuttiError(EINVAL, "token tensor (type or strides)")
+    return by_token
+
+
+def make_tokens(k, v, q=None, q_out=None) -> Tokens:
+    """Token struct over [tokens, heads, head_dim] device tensors (bf16 or fp16; views of a packed
+    projection are fine).  The struct does not keep the tensors alive."""
+    t = Tokens(_dtype_code(k), 0, 0, _rows(k, k), _rows(v, k), 0, None, k.data_ptr(), v.data_ptr(), None)
+    if q is not None:
+        t.n_q_heads, t.q_stride, t.q_out_stride = q.shape[1], _rows(q, k), _rows(q_out, k)
+        t.q, t.q_out = q.data_ptr(), q_out.data_ptr()
+    return t
+
+
+def make_rope(table, style: int = ROPE_HALF) -> Rope:
+    """Rotation over a [positions, rot_dim] float32 device table: cosines, then sines."""
+    if str(table.dtype) != "torch.float32" or not table.is_contiguous():
+        raise TuttiError(EINVAL, "rotation table (float32, contiguous)")
+    return Rope(style, table.shape[1], table.shape[0], table.data_ptr())
+
+
+def make_attend(q, out, lse=None) -> Attend:
+    """Attention struct over [tokens, heads, head_dim] queries and outputs; lse [tokens, heads] float32."""
+    if lse is not None and (str(lse.dtype) != "torch.float32" or not lse.is_contiguous()):
+        raise TuttiError(EINVAL, "lse (float32, contiguous)")
+    return Attend(_dtype_code(q), q.shape[1], _rows(q, q), _rows(out, q), q.data_ptr(), out.data_ptr(),
+                  None if lse is None else lse.data_ptr(), 0.0, 0)
+
+
+class Attn:
+    """tutti_attn_t: the workspace of attention calls that are ordered after each other."""
+
+    def __init__(self, ctx: Context):
+        self.ctx = ctx
+        self.lib = ctx.lib
+        h = C.c_void_p()
+        _check(self.lib.tutti_attn_create(ctx.h, C.byref(h)), "tutti_attn_create")
+        self.h = h
+
+    def close(self):
+        if self.h:
+            self.lib.tutti_attn_destroy(self.h)
+            self.h = None
+
+    def tutti_kv_attend_layer(self, layer: int, step: Step, io: Attend, scale: float, stream=None,
+                              allow: Sequence[int] = ()) -> int:
+        """Causal attention of the step's queries over the pool layer."""
+        io.scale = scale
+        return _check(self.lib.tutti_kv_attend_layer(self.h, layer, step, io, _stream_ptr(stream)),
+                      "tutti_kv_attend_layer", allow)
 
 
 class Ring:

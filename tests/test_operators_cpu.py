@@ -1,0 +1,152 @@
+"""What the operators on the pool refuse, and how they see a step's tables, without a GPU: the
+checks of arguments, of a sequence's numbers and of block ids are the library's own."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from paper_2605_03375_b200 import tutti as T
+
+
+def check_fn(name):
+    f = getattr(T.load(), name)
+    f.restype = C.c_int
+    return f
+
+
+def geom(**kw):
+    g = dict(n_layers=1, n_kv_heads=2, head_dim=128, elem_bytes=2, block_tokens=16, obj_tokens=16, n_devices=1, layout=1, n_slots=1)
+    g.update(kw)
+    return T.Geom(*g.values())
+
+
+def step(**kw):
+    s = T.Step(2, 4, 8, 3, 0x1000, 0x2000, 0x3000, 0x4000, None)
+    for k, v in kw.items():
+        setattr(s, k, v)
+    return s
+
+
+def tokens(**kw):
+    t = T.Tokens(T.DTYPE_BF16, 8, 1536, 1536, 1536, 1024, 0x10000, 0x20000, 0x30000, 0x40000)
+    for k, v in kw.items():
+        setattr(t, k, v)
+    return t
+
+
+def rope(**kw):
+    r = T.Rope(T.ROPE_HALF, 128, 100, 0x50000)
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+def attend(**kw):
+    a = T.Attend(T.DTYPE_FP16, 8, 1536, 1024, 0x10000, 0x20000, 0x30000, 0.1, 0)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def append_rc(g=None, s=None, t=None, r=None):
+    return check_fn("tutti_append_check_")(C.byref(g or geom()), C.byref(s or step()), C.byref(t or tokens()), C.byref(r) if r else None)
+
+
+def attend_rc(g=None, s=None, a=None):
+    return check_fn("tutti_attend_check_")(C.byref(g or geom()), C.byref(s or step()), C.byref(a or attend()))
+
+
+BAD_STEPS = [dict(q_start=None), dict(ctx_len=None), dict(blk_start=None), dict(block_ids=None), dict(max_new=0),
+             dict(q_start=0x1001), dict(ctx_len=0x2002), dict(block_ids=0x4003), dict(status=0x5001), dict(n_tok=1 << 31)]
+
+
+@pytest.mark.parametrize("kw", BAD_STEPS)
+def test_steps_that_are_refused(kw):
+    assert append_rc(s=step(**kw)) == T.EINVAL
+    assert attend_rc(s=step(**kw)) == T.EINVAL
+
+
+def test_calls_that_are_taken():
+    assert append_rc() == T.OK and append_rc(r=rope()) == T.OK and append_rc(r=rope(rot_dim=16, style=T.ROPE_PAIRS)) == T.OK
+    assert append_rc(geom(head_dim=80, elem_bytes=1)) == T.OK
+    assert append_rc(t=tokens(n_q_heads=0, q=None, q_out=None, q_stride=0, q_out_stride=0)) == T.OK
+    assert append_rc(s=step(n_tok=0)) == T.OK and append_rc(s=T.Step()) == T.OK
+    assert attend_rc() == T.OK and attend_rc(geom(head_dim=64, elem_bytes=1)) == T.OK and attend_rc(a=attend(lse=None)) == T.OK
+    assert attend_rc(s=T.Step()) == T.OK and attend_rc(a=attend(scale=-1.0)) == T.OK
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype=2), dict(n_q_heads=7), dict(q_stride=1020), dict(k_stride=128), dict(v_stride=1540), dict(q_out_stride=1016),
+    dict(k=None), dict(v=None), dict(q=None), dict(q_out=None), dict(k=0x20008), dict(q_out=0x40002), dict(n_q_heads=0)])
+def test_tokens_that_are_refused(kw):
+    assert append_rc(t=tokens(**kw)) == T.EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(style=2), dict(rot_dim=0), dict(rot_dim=24), dict(rot_dim=144), dict(table=None),
+                                dict(table=0x50008), dict(n_pos=0)])
+def test_rotations_that_are_refused(kw):
+    assert append_rc(r=rope(**kw)) == T.EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(elem_bytes=4), dict(head_dim=72), dict(head_dim=272)])
+def test_geometries_that_append_refuses(kw):
+    assert append_rc(geom(**kw), t=tokens(q_stride=4096, k_stride=4096, v_stride=4096, q_out_stride=4096)) == T.EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(elem_bytes=4), dict(head_dim=96), dict(head_dim=256), dict(n_kv_heads=3)])
+def test_geometries_that_attend_refuses(kw):
+    assert attend_rc(geom(**kw), a=attend(q_stride=4096, out_stride=4096)) == T.EINVAL
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=3), dict(n_q_heads=0), dict(n_q_heads=5), dict(q_stride=1000), dict(out_stride=1020),
+                                dict(q=None), dict(out=None), dict(q=0x10008), dict(lse=0x30002), dict(scale=float("inf")),
+                                dict(scale=float("nan")), dict(reserved=1)])
+def test_attends_that_are_refused(kw):
+    assert attend_rc(a=attend(**kw)) == T.EINVAL
+
+
+def test_null_handles():
+    lib = T.load()
+    assert lib.tutti_kv_append_layer(None, 0, step(), tokens(), None, None) == T.EINVAL
+    assert lib.tutti_kv_attend_layer(None, 0, step(), attend(), None) == T.EINVAL
+    assert lib.tutti_attn_create(None, None) == T.EINVAL and lib.tutti_attn_destroy(None) == T.EINVAL
+    assert lib.tutti_scales_register(None, 0, None, None, 0) == T.EINVAL
+    assert check_fn("tutti_append_check_")(None, C.byref(step()), C.byref(tokens()), None) == T.EINVAL
+    assert check_fn("tutti_append_check_")(C.byref(geom()), None, C.byref(tokens()), None) == T.EINVAL
+    assert check_fn("tutti_append_check_")(C.byref(geom()), C.byref(step()), None, None) == T.EINVAL
+    assert check_fn("tutti_attend_check_")(C.byref(geom()), C.byref(step()), None) == T.EINVAL
+
+
+def test_struct_sizes_match_the_header():
+    assert C.sizeof(T.Step) == 56 and C.sizeof(T.Tokens) == 72 and C.sizeof(T.Rope) == 24 and C.sizeof(T.Attend) == 56
+
+
+def views(q_start, ctx, blk_start, n_tok, n_blk, max_new, bs=16):
+    a = [np.asarray(x, dtype=np.uint32) for x in (q_start, ctx, blk_start)]
+    s = T.Step(len(ctx), n_tok, n_blk, max_new, *(x.ctypes.data for x in a), None, None)
+    f, out, got = check_fn("tutti_seq_view_"), (C.c_uint32 * 4)(), []
+    for i in range(len(ctx)):
+        rc = f(C.byref(s), bs, i, out)
+        got.append((rc, *out) if rc == T.OK else rc)
+    return got
+
+
+def test_sequences_that_contradict_their_sizes():
+    ok = T.OK
+    assert views([0, 1, 3], [16, 20], [0, 1, 3], 3, 3, 2) == [(ok, 0, 1, 16, 0), (ok, 1, 2, 20, 1)]
+    assert views([0, 1, 3], [17, 20], [0, 1, 3], 3, 3, 2)[0] == T.EINVAL           # more tokens than its blocks hold
+    assert views([0, 1, 3], [16, 20], [0, 1, 3], 2, 3, 2)[1] == T.EINVAL           # rows behind the arrays
+    assert views([0, 1, 3], [16, 20], [0, 1, 3], 3, 2, 2)[1] == T.EINVAL           # blocks behind the array
+    assert views([0, 1, 3], [16, 20], [0, 1, 3], 3, 3, 1)[1] == T.EINVAL           # more rows than max_new
+    assert views([2, 1, 3], [16, 20], [0, 1, 3], 3, 3, 2)[0] == T.EINVAL           # starts that go back
+    assert views([0, 1, 3], [16, 20], [2, 1, 3], 3, 3, 2)[0] == T.EINVAL
+    assert views([0, 1, 3], [0xffffffff, 0], [0, 1, 1], 3, 3, 2) == [T.EINVAL, (ok, 1, 2, 0, 1)]
+    assert views([0, 0], [0], [0, 0], 0, 0, 1) == [(ok, 0, 0, 0, 0)]
+    assert views([0, 1], [5], [0, 5], 1, 5, 1, bs=1) == [(ok, 0, 1, 5, 0)]
+
+
+def test_block_ids_outside_the_pool():
+    f = check_fn("tutti_block_offset_")
+    f.restype, f.argtypes = C.c_int64, [C.c_uint32, C.c_uint64, C.c_int32]
+    assert [f(10, 4096, i) for i in (0, 9, 10, -1, -(1 << 31), (1 << 31) - 1)] == [0, 9 * 4096, -1, -1, -1, -1]
+    assert f(1 << 30, 32768, (1 << 30) - 1) == ((1 << 30) - 1) * 32768            # offsets pass 32 bits
