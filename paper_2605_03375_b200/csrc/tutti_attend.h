@@ -1,0 +1,68 @@
+// Shared by the attention kernels: the call's parameters and a few instructions.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "tutti_paged.h"
+
+namespace tutti {
+
+struct AttendParams {
+    StepDev step;
+    PoolView pool;
+    uint32_t n_q_heads, group;
+    uint64_t q_stride, out_stride;    // elements
+    const void *q;
+    void *out;
+    float *lse;
+    float scale;
+};
+
+// Where parts of a tile that several workers share are left for the last of them to join.
+struct Workspace {
+    float *part;            // two slots a worker: rows x D sums, then behind them all maximum and denominator
+    uint32_t *count;        // parts that have arrived at the tile that starts in a worker; zero between calls
+    uint32_t workers;
+};
+
+#ifdef __CUDACC__
+__device__ inline float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ inline uint32_t smem_addr(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ inline void cp16(uint32_t dst, const void *src, bool there) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ inline void cp4(uint32_t dst, const void *src, bool there) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+__device__ inline void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ inline void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ inline uint32_t pack2(float a, float b, __nv_bfloat16) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+__device__ inline uint32_t pack2(float a, float b, __half) {
+    __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+#endif
+
+// 16 rows a tile (tutti_attend_few.cu).
+constexpr int FEW_ROWS = 16;
+cudaError_t few_setup();
+cudaError_t few_launch(const AttendParams &p, const Workspace &ws, bool c8, bool bf, cudaStream_t st);
+size_t few_part_bytes(uint32_t workers);
+uint32_t few_workers(int sms);
+
+// 256 rows a tile (tutti_attend_many.cu).
+cudaError_t many_setup();
+cudaError_t many_launch(const AttendParams &p, const Workspace &ws, bool c8, bool bf, cudaStream_t st);
+size_t many_part_bytes(uint32_t workers);
+uint32_t many_workers(int sms);
+
+}  // namespace tutti

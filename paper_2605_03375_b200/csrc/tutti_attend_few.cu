@@ -1,0 +1,604 @@
+// Attention of few rows per sequence (a decode step).
+#include <type_traits>
+
+#include "tutti_attend.h"
+
+namespace tutti {
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------
+// Few rows per sequence (decode): one pass over the cache at HBM speed.
+//
+// A *tile* is 16 rows of one sequence and KV head: (new token, query head of the group) pairs,
+// one A fragment of the warp-level matrix instruction.  Its keys are cut into units of WARPS x KW
+// keys; all units of all tiles of the step, laid end to end, are dealt out evenly over a fixed
+// number of workers (CTAs), so ragged batches, one long sequence and captured graphs whose lengths
+// change all load every SM alike and the host needs no length.  A worker's share is a run of
+// units: at most its first and its last tile are shared with neighbours.  Those parts go to the
+// workspace (two slots a worker) and whoever arrives last at a tile joins its parts in worker
+// order: the result does not depend on the order of arrival.
+//
+// Inside a worker each warp takes KW keys of a unit on its own: gather through the block table
+// with cp.async into its ring of STAGES x 8 KiB (a row of one head is the largest piece that is
+// contiguous in every pool layout), S = Q K^T, running maximum and sum, O += P V, all in
+// registers; no CTA barrier until a tile ends.  8-bit caches are multiplied as f16 codes
+// (exact); the scale of a key goes onto its score, the scale of a value onto its probability.
+constexpr int WARPS = 4;
+constexpr int STAGES = 3;
+constexpr uint32_t STAGE_BYTES = 8192;      // keys and values of one warp's KW keys
+constexpr int WORKERS_PER_SM = 2;
+
+__device__ inline void ldm4(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ inline void ldm4t(uint32_t (&r)[4], uint32_t a) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ inline void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ inline void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// two e4m3 codes (low 16 bits) as two f16
+__device__ inline uint32_t codes2(uint32_t x) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffff), __NV_E4M3);
+    return (uint32_t)h.x | (uint32_t)h.y << 16;
+}
+
+// A place in the step's units laid end to end: unit u of tile c of sequence s.
+struct Cursor {
+    uint32_t s, c, u;
+    uint32_t n_tiles, n_units;      // of the sequence
+    SeqView v;
+};
+
+
+// Tiles and units of a sequence (0 tiles: nothing to do); the error code, if any.
+__device__ inline int seq_shape(const AttendParams &p, uint32_t unit_keys, uint32_t s, Cursor &k) {
+    const int code = seq_view(p.step, p.pool.block_tokens, s, k.v);
+    k.n_tiles = code == TUTTI_OK ? (k.v.n_new * p.group + FEW_ROWS - 1) / FEW_ROWS * p.pool.n_kv_heads : 0;
+    k.n_units = code == TUTTI_OK && k.v.ctx ? (k.v.ctx + unit_keys - 1) / unit_keys : 1;
+    return code;
+}
+
+__device__ inline void advance(const AttendParams &p, uint32_t unit_keys, Cursor &k) {
+    if (++k.u < k.n_units) return;
+    k.u = 0;
+    if (++k.c < k.n_tiles) return;
+    k.c = 0;
+    do {
+        if (++k.s >= p.step.n_seq) return;      // behind the last unit: not used
+        seq_shape(p, unit_keys, k.s, k);
+    } while (k.n_tiles == 0);
+}
+
+// Q, K and V have the type T; 8-bit caches (C8) are multiplied as f16.
+template <typename T, bool C8, int D>
+struct Few {
+    using M = typename std::conditional<C8, __half, T>::type;        // type of the matrix instructions
+    static constexpr int RB = D * (C8 ? 1 : 2);                      // bytes of a row
+    static constexpr int KW = STAGE_BYTES / (2 * RB);                // keys of a warp's step
+    static constexpr int UNIT = WARPS * KW;
+    static constexpr int NT = KW / 8;                                // score fragments
+    static constexpr int DT = D / 8;                                 // output fragments
+    static constexpr int KPL = (KW + 31) / 32;                       // keys whose address a lane knows
+    static constexpr int CH = RB / 16;                               // 16-byte chunks of a row
+    static constexpr uint32_t SCALES = C8 ? KW * 8 : 0;              // scales of the stage's keys, then values
+    static constexpr uint32_t STAGE = STAGE_BYTES + SCALES;
+    // probabilities are kept 2^OFF times too large where they are rounded to f16: full precision
+    // down to 2^-28 of the largest instead of 2^-14
+    static constexpr float OFF = std::is_same<M, __half>::value ? 14.0f : 0.0f;
+    static constexpr uint32_t OFF_MASK = WARPS * STAGES * STAGE;     // uint64 keys that exist, by warp and stage
+    static constexpr uint32_t OFF_ML = OFF_MASK + WARPS * STAGES * 8;
+    static constexpr uint32_t OFF_PLAN = OFF_ML + WARPS * FEW_ROWS * 8;
+    static constexpr uint32_t SMEM = OFF_PLAN + 128;
+
+    // Where 16-byte chunk `ch` of row `row` lies: rotated so that the loads below meet no bank twice.
+    __device__ static uint32_t place(uint32_t row, uint32_t ch, bool value) {
+        if (!C8) return row * RB + ((ch ^ (row & 7)) * 16);
+        if (RB == 64) return (row / 2) * 128 + ((((row & 1) * 4 + ch) ^ ((row >> 1 & 3) << 1)) * 16);
+        return row * RB + ((ch ^ (value ? (row >> 1 & 3) << 1 : (row & 1) << 2)) * 16);
+    }
+};
+
+template <typename T, bool C8, int D>
+__global__ void __launch_bounds__(WARPS * 32, WORKERS_PER_SM)
+attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
+    using F = Few<T, C8, D>;
+    using M = typename F::M;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, c = lane % 4;
+    unsigned char *ring = smem + warp * STAGES * F::STAGE;
+    uint64_t *exists = reinterpret_cast<uint64_t *>(smem + F::OFF_MASK) + warp * STAGES;
+    float2 *ml = reinterpret_cast<float2 *>(smem + F::OFF_ML);
+    uint32_t *plan = reinterpret_cast<uint32_t *>(smem + F::OFF_PLAN);
+
+    // ---- this worker's share: a prefix sum over the sequences' units ----
+    const uint32_t per = (p.step.n_seq + WARPS * 32 - 1) / (WARPS * 32);
+    unsigned long long mine = 0;
+    for (uint32_t s = threadIdx.x * per; s < min((threadIdx.x + 1) * per, p.step.n_seq); ++s) {
+        Cursor k;
+        const int code = seq_shape(p, F::UNIT, s, k);
+        if (code != TUTTI_OK && blockIdx.x == 0) report(p.step, code);
+        mine += (unsigned long long)k.n_tiles * k.n_units;
+    }
+    unsigned long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned long long x = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += x;
+    }
+    unsigned long long *sums = reinterpret_cast<unsigned long long *>(plan);
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    unsigned long long total = 0, before = 0;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+        if (i < (int)warp) before += sums[i];
+        total += sums[i];
+    }
+    const unsigned long long workers = total < ws.workers ? total : ws.workers;
+    const uint32_t w = blockIdx.x;
+    if (w >= workers) return;
+    const unsigned long long x0 = w * total / workers, x1 = (w + 1) * total / workers;
+    before += incl - mine;
+    __syncthreads();
+    if (x0 >= before && x0 < before + mine) {      // one thread's sequences hold the first unit
+        unsigned long long at = before;
+        for (uint32_t s = threadIdx.x * per;; ++s) {
+            Cursor k;
+            seq_shape(p, F::UNIT, s, k);
+            const unsigned long long n = (unsigned long long)k.n_tiles * k.n_units;
+            if (x0 < at + n) {
+                plan[0] = s;
+                plan[1] = (uint32_t)((x0 - at) / k.n_units);
+                plan[2] = (uint32_t)((x0 - at) % k.n_units);
+                break;
+            }
+            at += n;
+        }
+    }
+    __syncthreads();
+    Cursor get;
+    get.s = plan[0];
+    get.c = plan[1];
+    get.u = plan[2];
+    seq_shape(p, F::UNIT, get.s, get);
+    Cursor put = get;                              // runs ahead: the unit whose loads are issued next
+    unsigned long long put_x = x0;
+
+    // ---- gathering ----
+    int64_t off[F::KPL];                           // of the lane's keys in the unit at `put`; -1: not there
+    auto locate = [&]() {
+#pragma unroll
+        for (int i = 0; i < F::KPL; ++i) {
+            const uint32_t key = (put.u * WARPS + warp) * F::KW + i * 32 + lane;
+            off[i] = -1;
+            if (put_x < x1 && i * 32 + lane < F::KW && key < put.v.ctx) {
+                const int32_t id = __ldg(p.step.block_ids + put.v.b0 + key / p.pool.block_tokens);
+                // offset and, for the scales, the id; the row inside the block is added when it is used
+                off[i] = (uint32_t)id < p.pool.n_blocks ? (int64_t)id : -2;
+            }
+        }
+    };
+    locate();
+    auto fetch = [&](uint32_t stage) {             // issues the loads of the unit at `put`, then looks up the next ids
+        if (put_x < x1) {
+            unsigned char *st = ring + stage * F::STAGE;
+            const uint32_t kst = smem_addr(st), vst = kst + F::KW * F::RB;
+            const uint32_t h = put.c / (put.n_tiles / p.pool.n_kv_heads);
+            uint64_t mask = 0;
+#pragma unroll
+            for (int i = 0; i < F::KPL; ++i) {
+                const uint32_t key = (put.u * WARPS + warp) * F::KW + i * 32 + lane;
+                if (off[i] == -2) report(p.step, TUTTI_EFAULT);
+                const bool ok = off[i] >= 0;
+                mask |= (uint64_t)__ballot_sync(0xffffffffu, ok) << (32 * i);
+                if (C8 && i * 32 + lane < F::KW) {
+                    const uint64_t at = ok ? (uint64_t)off[i] * p.pool.n_kv_heads + h : 0;
+                    cp4(kst + STAGE_BYTES + (i * 32 + lane) * 4, p.pool.k_scale + at, ok);
+                    cp4(kst + STAGE_BYTES + (F::KW + i * 32 + lane) * 4, p.pool.v_scale + at, ok);
+                }
+                if (ok) off[i] = block_offset(p.pool, (int32_t)off[i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + h * p.pool.head_stride);
+            }
+            if (lane == 0) exists[stage] = mask;
+#pragma unroll
+            for (int i = 0; i < F::KW * F::CH / 32; ++i) {
+                const uint32_t row = (i * 32 + lane) / F::CH, ch = lane % F::CH;
+                const int64_t o = __shfl_sync(0xffffffffu, off[(i * 32 / F::CH) / 32], row % 32);
+                const bool ok = o >= 0;
+                const uint64_t a = (ok ? (uint64_t)o : 0) + ch * 16;
+                cp16(kst + F::place(row, ch, false), (const void *)(p.pool.k_base + a), ok);
+                cp16(vst + F::place(row, ch, true), (const void *)(p.pool.v_base + a), ok);
+            }
+            ++put_x;
+            if (put_x < x1) advance(p, F::UNIT, put);
+            locate();
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+
+    // ---- the worker's tiles ----
+    uint32_t stage = 0;
+    for (unsigned long long x = x0; x < x1;) {
+        const uint32_t rts = get.n_tiles / p.pool.n_kv_heads, h = get.c / rts, row0 = (get.c % rts) * FEW_ROWS;
+        const uint32_t n_rows = get.v.n_new * p.group;
+        const int64_t first = (int64_t)get.v.ctx - get.v.n_new;
+        const unsigned long long tile0 = x - get.u;                       // the tile's units: [tile0, tile0 + n_units)
+        const unsigned long long seg_end = min(x1, tile0 + get.n_units);
+        // rows g and g + 8 of the tile: token, position (last key seen), query fragment
+        int64_t pos[2];
+        float rowscale[2];
+        uint32_t qf[D / 16][4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const uint32_t row = row0 + g + 8 * r;
+            const bool ok = row < n_rows;
+            const uint32_t i = ok ? row / p.group : 0, qh = h * p.group + (ok ? row % p.group : 0);
+            pos[r] = ok ? first + i : -1;
+            const T *q = (const T *)p.q + (uint64_t)(get.v.q0 + i) * p.q_stride + (uint64_t)qh * D;
+            rowscale[r] = p.scale * 1.4426950408889634f;
+            if constexpr (!C8) {
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        qf[k][r + 2 * j] = ok ? *reinterpret_cast<const uint32_t *>(q + k * 16 + j * 8 + 2 * c) : 0;
+            } else {
+                // the k index of step t is permuted: a thread's 16 elements are 16 neighbouring dimensions
+                float x[D / 4], top = 0;
+#pragma unroll
+                for (int b = 0; b < D / 64; ++b) {
+                    uint4 u[2] = {};
+                    if (ok) {
+                        u[0] = *reinterpret_cast<const uint4 *>(q + b * 64 + c * 16);
+                        u[1] = *reinterpret_cast<const uint4 *>(q + b * 64 + c * 16 + 8);
+                    }
+                    const T *e = reinterpret_cast<const T *>(u);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        x[b * 16 + j] = (float)e[j];
+                        top = fmaxf(top, fabsf(x[b * 16 + j]));
+                    }
+                }
+                // a row of bf16 queries is scaled by a power of two so that f16 holds it: exactly,
+                // but for elements below 2^-14 of the row's largest, which keep an error of 2^-25 of it
+                float down = 1.0f;
+                if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -60), 126);
+                    down = __uint_as_float((uint32_t)(127 - e) << 23);
+                    rowscale[r] *= __uint_as_float((uint32_t)(127 + e) << 23);
+                }
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int at = (k / 4) * 16 + (k % 4) * 4 + 2 * j;
+                        qf[k][r + 2 * j] = pack2(x[at] * down, x[at + 1] * down, __half());
+                    }
+            }
+        }
+        float o[F::DT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0, 0};
+        float vtop = 0;                      // 8-bit: power of two at or above no value scale so far; O is in its units
+#pragma unroll
+        for (int i = 0; i < F::DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0;
+        const int64_t last_all = first + row0 / p.group;        // keys up to here are seen by every row of the tile
+
+        for (; x < seg_end; ++x) {
+            cp_wait<STAGES - 2>();
+            __syncwarp();
+            fetch(stage == 0 ? STAGES - 1 : stage - 1);      // the stage before this one is free
+            unsigned char *st = ring + stage * F::STAGE;
+            const uint32_t kst = smem_addr(st), vst = kst + F::KW * F::RB;
+            const uint64_t there = exists[stage];
+            const int64_t key0 = (int64_t)(get.u * WARPS + warp) * F::KW;
+            constexpr uint64_t ALL = F::KW == 64 ? ~0ull : (1ull << (F::KW & 63)) - 1;
+            if (there) {
+                // scores
+                float s[F::NT][4];
+#pragma unroll
+                for (int n = 0; n < F::NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0;
+                if constexpr (!C8) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                        for (int n = 0; n < F::NT; n += 2) {
+                            // 16 keys x 16 dimensions: lanes 0-7 and 8-15 the two dimension halves of the first 8 keys
+                            uint32_t b[4];
+                            ldm4(b, kst + F::place(n * 8 + (lane & 7) + (lane >> 4) * 8, k * 2 + (lane >> 3 & 1), false));
+                            mma(s[n], qf[k], b[0], b[1], M());
+                            mma(s[n + 1], qf[k], b[2], b[3], M());
+                        }
+                } else {
+#pragma unroll
+                    for (int n = 0; n < F::NT; ++n)
+#pragma unroll
+                        for (int b = 0; b < D / 64; ++b) {
+                            const uint4 u = *reinterpret_cast<const uint4 *>(st + F::place(n * 8 + g, b * 4 + c, false));
+                            const uint32_t word[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) mma(s[n], qf[b * 4 + k], codes2(word[k]), codes2(word[k] >> 16), M());
+                        }
+                }
+                const bool masked = there != ALL || key0 + F::KW - 1 > last_all;
+                float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int n = 0; n < F::NT; ++n) {
+                    float2 ks = {1, 1};
+                    if constexpr (C8) ks = *reinterpret_cast<const float2 *>(st + STAGE_BYTES + (n * 8 + 2 * c) * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[n][e] *= rowscale[e / 2] * (C8 ? (e & 1 ? ks.y : ks.x) : 1.0f);
+                        if (masked) {
+                            const int key = n * 8 + 2 * c + (e & 1);
+                            if (!(there >> key & 1) || key0 + key > pos[e / 2]) s[n][e] = -INFINITY;
+                        }
+                        top[e / 2] = fmaxf(top[e / 2], s[n][e]);
+                    }
+                }
+                float alpha[2], sub[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+                    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+                    const float m2 = fmaxf(m[r], top[r]);
+                    sub[r] = m2 == -INFINITY ? 0 : m2;       // a row that has seen nothing yet
+                    alpha[r] = ex2(m[r] - sub[r]);
+                    m[r] = m2;
+                    l[r] *= alpha[r];
+                    sub[r] -= F::OFF;
+                }
+                float vinv = 1.0f;
+                if constexpr (C8) {
+                    float vs = 0;
+#pragma unroll
+                    for (int n = 0; n < F::NT; ++n) {
+                        const float2 v2 = *reinterpret_cast<const float2 *>(st + STAGE_BYTES + (F::KW + n * 8 + 2 * c) * 4);
+                        vs = fmaxf(vs, fmaxf(v2.x, v2.y));
+                    }
+                    vs = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, 1));
+                    vs = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, 2));
+                    vs = __uint_as_float(min(max(__float_as_uint(vs) >> 23, 1u), 253u) << 23);
+                    if (vs > vtop) {
+                        const float f = vtop / vs;
+                        alpha[0] *= f;
+                        alpha[1] *= f;
+                        vtop = vs;
+                    }
+                    vinv = 1.0f / vtop;
+                }
+                if (__any_sync(0xffffffffu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
+#pragma unroll
+                    for (int i = 0; i < F::DT; ++i) {
+                        o[i][0] *= alpha[0];
+                        o[i][1] *= alpha[0];
+                        o[i][2] *= alpha[1];
+                        o[i][3] *= alpha[1];
+                    }
+                }
+                uint32_t pf[F::NT / 2][4];
+#pragma unroll
+                for (int n = 0; n < F::NT; ++n) {
+                    float2 vs = {1, 1};
+                    if constexpr (C8) {
+                        vs = *reinterpret_cast<const float2 *>(st + STAGE_BYTES + (F::KW + n * 8 + 2 * c) * 4);
+                        vs.x *= vinv;
+                        vs.y *= vinv;
+                    }
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const float a = ex2(s[n][2 * r] - sub[r]), b = ex2(s[n][2 * r + 1] - sub[r]);
+                        l[r] += a + b;
+                        pf[n / 2][(n & 1) * 2 + r] = C8 ? pack2(a * vs.x, b * vs.y, M()) : pack2(a, b, M());
+                    }
+                }
+                // values
+                if constexpr (!C8) {
+#pragma unroll
+                    for (int k = 0; k < F::KW / 16; ++k)
+#pragma unroll
+                        for (int i = 0; i < F::DT; i += 2) {
+                            uint32_t b[4];
+                            ldm4t(b, vst + F::place(k * 16 + (lane & 15), i + (lane >> 4), true));
+                            mma(o[i], pf[k], b[0], b[1], M());
+                            mma(o[i + 1], pf[k], b[2], b[3], M());
+                        }
+                } else {
+                    // fragment i, column n stands for dimension n * DT + i: a thread's codes of a key are neighbours
+                    const unsigned char *vrow = st + F::KW * F::RB;
+#pragma unroll
+                    for (int k = 0; k < F::KW / 16; ++k) {
+                        uint32_t word[4][F::DT / 4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t row = k * 16 + 2 * c + (j & 1) + (j >> 1) * 8;
+                            if constexpr (D == 128) {
+                                const uint4 u = *reinterpret_cast<const uint4 *>(vrow + F::place(row, g, true));
+                                word[j][0] = u.x, word[j][1] = u.y, word[j][2] = u.z, word[j][3] = u.w;
+                            } else {
+                                const uint2 u = *reinterpret_cast<const uint2 *>(vrow + F::place(row, g / 2, true) + (g & 1) * 8);
+                                word[j][0] = u.x, word[j][1] = u.y;
+                            }
+                        }
+#pragma unroll
+                        for (int q = 0; q < F::DT / 4; ++q) {
+                            const uint32_t lo0 = __byte_perm(word[0][q], word[1][q], 0x5140), hi0 = __byte_perm(word[0][q], word[1][q], 0x7362);
+                            const uint32_t lo1 = __byte_perm(word[2][q], word[3][q], 0x5140), hi1 = __byte_perm(word[2][q], word[3][q], 0x7362);
+                            mma(o[q * 4 + 0], pf[k], codes2(lo0), codes2(lo1), M());
+                            mma(o[q * 4 + 1], pf[k], codes2(lo0 >> 16), codes2(lo1 >> 16), M());
+                            mma(o[q * 4 + 2], pf[k], codes2(hi0), codes2(hi1), M());
+                            mma(o[q * 4 + 3], pf[k], codes2(hi0 >> 16), codes2(hi1 >> 16), M());
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (x + 1 < seg_end) {
+                stage = stage + 1 == STAGES ? 0 : stage + 1;
+                ++get.u;
+            }
+        }
+
+        // ---- join the warps: O goes through the stage just used, which no load is aimed at ----
+        const bool whole = get.u + 1 == get.n_units && tile0 >= x0;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+            if (c == 0) ml[warp * FEW_ROWS + g + 8 * r] = make_float2(m[r], l[r]);
+        }
+        __syncthreads();
+        float *mine_o = reinterpret_cast<float *>(ring + stage * F::STAGE);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) top = fmaxf(top, ml[i * FEW_ROWS + g + 8 * r].x);
+            const float f = top == -INFINITY ? 0 : ex2(m[r] - top) * (C8 ? vtop : 1.0f);
+            float *dst = mine_o + (g + 8 * r) * D;
+#pragma unroll
+            for (int i = 0; i < F::DT; ++i) {
+                if constexpr (!C8) {
+                    *reinterpret_cast<float2 *>(dst + ((i * 8 + 2 * c) ^ ((g & 3) * 8))) = make_float2(o[i][2 * r] * f, o[i][2 * r + 1] * f);
+                } else {
+                    dst[(2 * c * F::DT + i) ^ ((g & 3) * 8)] = o[i][2 * r] * f;
+                    dst[((2 * c + 1) * F::DT + i) ^ ((g & 3) * 8)] = o[i][2 * r + 1] * f;
+                }
+            }
+        }
+        __syncthreads();
+        // thread t: row t / 8, every 8th group of four dimensions
+        const uint32_t row = threadIdx.x / 8, lanec = threadIdx.x % 8;
+        float M_ = -INFINITY, L = 0;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) M_ = fmaxf(M_, ml[i * FEW_ROWS + row].x);
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) {
+            const float2 e = ml[i * FEW_ROWS + row];
+            L += M_ == -INFINITY ? 0 : e.y * ex2(e.x - M_);
+        }
+        float acc[D / 8];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+            float4 a = make_float4(0, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) {
+                const float *src = reinterpret_cast<const float *>(smem + (i * STAGES + stage) * F::STAGE) + row * D;
+                const float4 b = *reinterpret_cast<const float4 *>(src + (((j * 8 + lanec) * 4) ^ ((row & 3) * 8)));
+                a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w;
+            }
+            acc[j * 4] = a.x, acc[j * 4 + 1] = a.y, acc[j * 4 + 2] = a.z, acc[j * 4 + 3] = a.w;
+        }
+        bool write = whole;
+        if (!whole) {
+            // this worker's part, and whoever brings the last part of the tile joins them
+            const uint32_t w0 = (uint32_t)(((tile0 + 1) * workers - 1) / total);
+            const uint32_t w1 = (uint32_t)(((tile0 + get.n_units) * workers - 1) / total);
+            auto slot = [&](uint32_t i) { return i == w0 ? 2 * i + 1 : 2 * i; };
+            float *part_o = ws.part, *part_ml = ws.part + (uint64_t)2 * ws.workers * FEW_ROWS * D;
+            float4 *po = reinterpret_cast<float4 *>(part_o + ((uint64_t)slot(w) * FEW_ROWS + row) * D);
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) po[j * 8 + lanec] = make_float4(acc[j * 4], acc[j * 4 + 1], acc[j * 4 + 2], acc[j * 4 + 3]);
+            if (lanec == 0) reinterpret_cast<float2 *>(part_ml)[slot(w) * FEW_ROWS + row] = make_float2(M_, L);
+            __threadfence();
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                const uint32_t old = atomicAdd(ws.count + w0, 1);
+                if (old == w1 - w0) ws.count[w0] = 0;          // ready for the next call
+                plan[0] = old == w1 - w0;
+            }
+            __syncthreads();
+            write = plan[0];
+            if (write) {
+                __threadfence();
+                M_ = -INFINITY;
+                L = 0;
+                for (uint32_t i = w0; i <= w1; ++i) M_ = fmaxf(M_, __ldcg(reinterpret_cast<const float2 *>(part_ml) + slot(i) * FEW_ROWS + row).x);
+#pragma unroll
+                for (int j = 0; j < D / 8; ++j) acc[j] = 0;
+                for (uint32_t i = w0; i <= w1; ++i) {
+                    const float2 e = __ldcg(reinterpret_cast<const float2 *>(part_ml) + slot(i) * FEW_ROWS + row);
+                    const float f = M_ == -INFINITY ? 0 : ex2(e.x - M_);
+                    L += e.y * f;
+                    const float4 *src = reinterpret_cast<const float4 *>(part_o + ((uint64_t)slot(i) * FEW_ROWS + row) * D);
+#pragma unroll
+                    for (int j = 0; j < D / 32; ++j) {
+                        const float4 b = __ldcg(src + j * 8 + lanec);
+                        acc[j * 4] += b.x * f, acc[j * 4 + 1] += b.y * f, acc[j * 4 + 2] += b.z * f, acc[j * 4 + 3] += b.w * f;
+                    }
+                }
+            }
+        }
+        if (write && row0 + row < n_rows) {
+            const uint32_t i = (row0 + row) / p.group, qh = h * p.group + (row0 + row) % p.group;
+            const uint64_t tok = get.v.q0 + i;
+            const float inv = M_ == -INFINITY ? 0.0f : 1.0f / L;
+            T *out = (T *)p.out + tok * p.out_stride + (uint64_t)qh * D;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+                *reinterpret_cast<uint2 *>(out + (j * 8 + lanec) * 4) =
+                    make_uint2(pack2(acc[j * 4] * inv, acc[j * 4 + 1] * inv, T()), pack2(acc[j * 4 + 2] * inv, acc[j * 4 + 3] * inv, T()));
+            if (p.lse && lanec == 0)
+                p.lse[tok * p.n_q_heads + qh] = M_ == -INFINITY ? -INFINITY : (M_ - F::OFF + log2f(L)) * 0.6931471805599453f;
+        }
+        __syncthreads();                     // the stage and the small arrays may be written again
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        if (x < x1) advance(p, F::UNIT, get);
+    }
+    cp_wait<0>();
+}
+
+template <typename T, bool C8, int D>
+cudaError_t launch_few(const AttendParams &p, const Workspace &ws, cudaStream_t st) {
+    attend_few_kernel<T, C8, D><<<ws.workers, WARPS * 32, Few<T, C8, D>::SMEM, st>>>(p, ws);
+    return cudaGetLastError();
+}
+
+template <bool C8>
+cudaError_t launch_few(const AttendParams &p, const Workspace &ws, bool bf, cudaStream_t st) {
+    if (p.pool.head_dim == 128)
+        return bf ? launch_few<__nv_bfloat16, C8, 128>(p, ws, st) : launch_few<__half, C8, 128>(p, ws, st);
+    return bf ? launch_few<__nv_bfloat16, C8, 64>(p, ws, st) : launch_few<__half, C8, 64>(p, ws, st);
+}
+
+template <typename T, bool C8, int D>
+cudaError_t setup_few() {
+    return cudaFuncSetAttribute(attend_few_kernel<T, C8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<T, C8, D>::SMEM);
+}
+
+template <typename T>
+cudaError_t setup_type() {
+    cudaError_t e = setup_few<T, false, 128>();
+    if (e == cudaSuccess) e = setup_few<T, true, 128>();
+    if (e == cudaSuccess) e = setup_few<T, false, 64>();
+    if (e == cudaSuccess) e = setup_few<T, true, 64>();
+    return e;
+}
+
+}  // namespace
+
+cudaError_t few_setup() {
+    const cudaError_t e = setup_type<__nv_bfloat16>();
+    return e == cudaSuccess ? setup_type<__half>() : e;
+}
+
+cudaError_t few_launch(const AttendParams &p, const Workspace &ws, bool c8, bool bf, cudaStream_t st) {
+    return c8 ? launch_few<true>(p, ws, bf, st) : launch_few<false>(p, ws, bf, st);
+}
+
+uint32_t few_workers(int sms) { return (uint32_t)sms * WORKERS_PER_SM; }
+size_t few_part_bytes(uint32_t workers) { return (size_t)2 * workers * FEW_ROWS * (128 + 2) * sizeof(float); }
+
+}  // namespace tutti

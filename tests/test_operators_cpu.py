@@ -150,3 +150,25 @@ def test_block_ids_outside_the_pool():
     f.restype, f.argtypes = C.c_int64, [C.c_uint32, C.c_uint64, C.c_int32]
     assert [f(10, 4096, i) for i in (0, 9, 10, -1, -(1 << 31), (1 << 31) - 1)] == [0, 9 * 4096, -1, -1, -1, -1]
     assert f(1 << 30, 32768, (1 << 30) - 1) == ((1 << 30) - 1) * 32768            # offsets pass 32 bits
+
+
+@pytest.mark.parametrize("group", [1, 2, 3, 5, 7, 8, 64, 300])
+def test_units_of_causal_tiles_in_closed_form(group):
+    """The number of 128-key units that 256-row tiles of a sequence see, against counting them."""
+    f = check_fn("tutti_many_units_")
+    f.argtypes = [C.c_uint32] * 4 + [C.POINTER(C.c_uint64)]
+    rng = np.random.default_rng(group)
+    out = (C.c_uint64 * 2)()
+    for ctx, new in [(1, 1), (128, 128), (129, 1), (5000, 700), (2000, 2000), (40000, 3), (10, 30), (0, 5), (131072, 1000)] + \
+            [(int(c), int(n)) for c, n in zip(rng.integers(0, 3000, 30), rng.integers(1, 900, 30))]:
+        rows, first = new * group, ctx - new
+        tiles = -(-rows // 256)
+        total = 0
+        for q in range(tiles):
+            last = first + (min(rows, (q + 1) * 256) - 1) // group
+            want = last // 128 + 1 if first >= 0 and ctx else max(1, -(-ctx // 128))
+            assert f(ctx, new, group, q, out) == tiles
+            assert (out[0], out[1]) == (want, total), (ctx, new, group, q)
+            total += want
+        f(ctx, new, group, tiles, out)
+        assert out[1] == total
