@@ -102,12 +102,15 @@ int tutti_kv_attend_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *s
     p.out = io->out;
     p.lse = io->lse;
     p.scale = io->scale;
+    p.hnd = p.pool.head_stride > p.pool.tok_stride;
     OnDevice on(tutti_ctx_device_(a->ctx));
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const bool bf = io->dtype == TUTTI_DTYPE_BF16;
     const bool few = (uint64_t)step->max_new * p.group <= FEW_ROWS;
+    PoolMaps maps;
+    if (!few) maps.valid = tutti_ctx_pool_maps_(a->ctx, layer, &maps.k, &maps.v);
     const cudaError_t e = few ? few_launch(p, a->few, elem_bytes == 1, bf, (cudaStream_t)stream)
-                              : many_launch(p, a->many, elem_bytes == 1, bf, (cudaStream_t)stream);
+                              : many_launch(p, maps, a->many, elem_bytes == 1, bf, (cudaStream_t)stream);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "attend launch");
 }
 

@@ -17,6 +17,13 @@ struct AttendParams {
     void *out;
     float *lse;
     float scale;
+    bool hnd;                         // head-major pool blocks
+};
+
+// Tile loads of the layer's keys and values.
+struct PoolMaps {
+    CUtensorMap k, v;
+    bool valid;
 };
 
 // Where parts of a tile that several workers share are left for the last of them to join.
@@ -61,7 +68,7 @@ uint32_t few_workers(int sms);
 
 // 256 rows a tile (tutti_attend_many.cu).
 cudaError_t many_setup();
-cudaError_t many_launch(const AttendParams &p, const Workspace &ws, bool c8, bool bf, cudaStream_t st);
+cudaError_t many_launch(const AttendParams &p, const PoolMaps &maps, const Workspace &ws, bool c8, bool bf, cudaStream_t st);
 size_t many_part_bytes(uint32_t workers);
 uint32_t many_workers(int sms);
 

@@ -7,17 +7,22 @@
 // is joined by the last of them; a causal tile's units are counted in closed form (floor_sum), so
 // a captured graph follows lengths that change.
 //
-// Roles of a worker's 12 warps:
+// Roles of a worker's 16 warps:
 //   0-3, 4-7  softmax of half 0 / half 1: a thread owns a row, reads its scores from TMEM, writes
 //             its probabilities back over them (16 bits), rescales the output when the running
 //             maximum has grown by more than 2^8, and writes the row out at the end;
 //   8         issues the matrix instructions: S = Q K^T (both operands in shared memory),
 //             O += P V (P from TMEM).  The halves alternate, so the tensor cores work on one
 //             while the other is in its softmax;
-//   9-11      gather keys and values through the block table into a ring of four 128-row tiles
+//   9-11      bring the queries of the next tile;
+//   12-15     gather keys and values through the block table into a ring of four 128-row tiles
 //             in the 128-byte swizzle (K: K-major B operand, V: the same bytes read as an
-//             MN-major B operand).  8-bit codes become 16-bit elements on the way: code * scale,
-//             exact for the powers of two that append writes.
+//             MN-major B operand): one tensor copy per block and 128 bytes of its rows, or, where a
+//             sequence ends inside the unit, a block is missing or blocks do not tile 64 rows, row
+//             by row with zeros in place of what is not there.  Two groups of two warps take the
+//             units in turn, so a group waits for its own loads while the other's are in flight.
+//             8-bit codes are widened in place to 16 bits: code * scale, exact for the powers of
+//             two that append writes.
 // Bound: the tensor cores (2 x 128 x 128 x D multiply-adds a half and unit) and, as close,
 // the 128 x 128 exponentials on 16 lanes a clock.
 #include <type_traits>
@@ -32,8 +37,8 @@ constexpr int HALF_ROWS = 128;
 constexpr int TILE_ROWS = 256;
 constexpr int BN = 128;                 // keys of a unit
 constexpr int RING = 4;                 // K and V tiles in flight
-constexpr int THREADS = 384;
-constexpr int MMA_WARP = 8, PROD_WARP = 9, PROD_WARPS = 3;
+constexpr int THREADS = 512;
+constexpr int MMA_WARP = 8, Q_WARP = 9, Q_WARPS = 3, KV_WARP = 12, KV_WARPS = 2;      // KV_WARPS: of a group
 constexpr uint32_t ATOM = BN * 128;     // 128 rows of 128 bytes
 constexpr float GROW = 8.0f;            // log2 of how far probabilities may exceed 1
 constexpr long long WAIT_CLOCKS = 3000000000ll;   // about 1.5 s: a wait that takes longer is given up
@@ -148,6 +153,13 @@ __device__ inline bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_
     }
     return true;
 }
+__device__ inline void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ inline void tile_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t c0, int32_t c1, int32_t c2, int32_t c3) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
 __device__ inline void tc_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -196,42 +208,35 @@ __device__ inline uint64_t operand(uint32_t addr) {
     return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(ATOM >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
-// code * scale of two (low and high half) pairs of codes, as two 16-bit pairs
-__device__ inline uint2 widen(uint32_t codes, __half2 s1, __half2 s2) {
-    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes & 0xffff), __NV_E4M3);
-    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> 16), __NV_E4M3);
-    const __half2 x = __hmul2(__hmul2(__half2(a), s1), s2), y = __hmul2(__hmul2(__half2(b), s1), s2);
-    return make_uint2(*reinterpret_cast<const uint32_t *>(&x), *reinterpret_cast<const uint32_t *>(&y));
+// Four codes as 16-bit elements in the order 0, 2 | 1, 3 (the queries are brought in the same order
+// and the outputs leave in it), not yet at their scale: the magnitude's 7 bits are moved to
+// where they are the value times 2^-8 (f16) or 2^-120 (bf16), subnormal codes included.
+__device__ inline uint2 spread(uint32_t w, __half) {
+    return make_uint2(((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u), ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u));
 }
-__device__ inline uint2 widen(uint32_t codes, __nv_bfloat162 s1, __nv_bfloat162 s2) {
-    // A code's 7 magnitude bits moved to bits 4..10 of a bf16 are the value times 2^-120, also
-    // where it is subnormal; s1 is 2^120.
-    uint32_t lo = __byte_perm(codes, 0, 0x1404), hi = __byte_perm(codes, 0, 0x3424);
-    lo = (lo & 0x80008000u) | ((lo >> 4) & 0x07f007f0u);
-    hi = (hi & 0x80008000u) | ((hi >> 4) & 0x07f007f0u);
-    __nv_bfloat162 x = __hmul2(__hmul2(*reinterpret_cast<__nv_bfloat162 *>(&lo), s1), s2);
-    __nv_bfloat162 y = __hmul2(__hmul2(*reinterpret_cast<__nv_bfloat162 *>(&hi), s1), s2);
-    uint2 r = make_uint2(*reinterpret_cast<uint32_t *>(&x), *reinterpret_cast<uint32_t *>(&y));
-    if (((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) {        // a NaN code among the four
-        if ((codes & 0x7fu) == 0x7fu) r.x |= 0x7fffu;
-        if ((codes & 0x7f00u) == 0x7f00u) r.x |= 0x7fff0000u;
-        if ((codes & 0x7f0000u) == 0x7f0000u) r.y |= 0x7fffu;
-        if ((codes & 0x7f000000u) == 0x7f000000u) r.y |= 0x7fff0000u;
-    }
-    return r;
+__device__ inline uint2 spread(uint32_t w, __nv_bfloat16) {
+    return make_uint2(((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u), ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u));
 }
-// A scale as the two factors that widen() multiplies by.  f16: half the scale, so that nothing
-// that came from f16 overflows, with a second factor for scales below the type's normal range.
-__device__ inline void factors(float s, __half2 &s1, __half2 &s2) {
-    s *= 0.5f;
-    const float low = fabsf(s) < 6.103515625e-05f ? 5.9604644775390625e-08f : 1.0f;
-    s1 = __float2half2_rn(s / low);
-    s2 = __float2half2_rn(low);
+// A scale as the two factors that finish spread(); the second is 1 wherever the first can be held.
+// f16: half the value, so that nothing that came from f16 overflows.
+__device__ inline void factors(float s, float &s1, float &s2, __half) {
+    s *= 128.0f;
+    s2 = fabsf(s) < 6.103515625e-05f ? 5.9604644775390625e-08f : 1.0f;      // below the normal range
+    s1 = s / s2;
 }
-__device__ inline void factors(float s, __nv_bfloat162 &s1, __nv_bfloat162 &s2) {
-    s1 = __float2bfloat162_rn(1.329227995784916e+36f);                 // 2^120
-    s2 = __float2bfloat162_rn(s);
+__device__ inline void factors(float s, float &s1, float &s2, __nv_bfloat16) {
+    s2 = fabsf(s) < 128.0f ? 1.0f : s;
+    s1 = 1.329227995784916e+36f * (s / s2);                                   // 2^120
 }
+__device__ inline __half2 twice(float x, __half) { return __float2half2_rn(x); }
+__device__ inline __nv_bfloat162 twice(float x, __nv_bfloat16) { return __float2bfloat162_rn(x); }
+template <typename P>
+__device__ inline uint32_t times(uint32_t x, P s) {
+    const P y = __hmul2(*reinterpret_cast<const P *>(&x), s);
+    return *reinterpret_cast<const uint32_t *>(&y);
+}
+// NaN codes (magnitude bits all ones) among four
+__device__ inline uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
 template <typename T, bool C8, int D>
 struct Many {
@@ -245,7 +250,6 @@ struct Many {
     static constexpr float VALUE = C8 && std::is_same<T, __half>::value ? 2.0f : 1.0f;
     // f16 probabilities are kept 2^6 times too large (at most 2^14): full precision down to 2^-20
     static constexpr float OFF = std::is_same<T, __half>::value ? 6.0f : 0.0f;
-    using Pair = typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type;
     // byte offset of 16-byte chunk `ch` of row `row` in a tile
     __device__ static uint32_t place(uint32_t row, uint32_t ch) {
         return (ch >> 3) * ATOM + row * 128 + (((ch ^ row) & 7) << 4);
@@ -253,7 +257,7 @@ struct Many {
 };
 
 template <typename T, bool C8, int D>
-__global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
+__global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ PoolMaps maps, const Workspace ws) {
     using C = Many<T, C8, D>;
     extern __shared__ unsigned char raw[];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
@@ -264,7 +268,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     volatile uint32_t *dead = misc + 60;
     const uint32_t bars = base + C::OFF_BAR;
     const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, s_full = bars + 80,
-                   p_full = bars + 96, o_full = bars + 112, o_empty = bars + 128, joined = bars + 144, drain = bars + 160;
+                   p_full = bars + 96, o_full = bars + 112, o_empty = bars + 128, joined = bars + 144, drain = bars + 160, raw_full = bars + 168;
 
     // ---- this worker's share ----
     unsigned long long *sums = reinterpret_cast<unsigned long long *>(misc);
@@ -303,8 +307,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             tile_seq(p, s, t);
             const unsigned long long n = t.r.before(t.r.n_tiles) * p.pool.n_kv_heads;
             if (x0 < at + n) {
-                misc[32] = s;
-                sums[14] = x0 - at;
+                misc[40] = s;
+                sums[18] = x0 - at;
                 break;
             }
             at += n;
@@ -312,10 +316,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     }
     if (threadIdx.x == 0) {
         for (int i = 0; i < RING; ++i) {
-            mbar_init(full + 8 * i, PROD_WARPS);
+            mbar_init(full + 8 * i, KV_WARPS);
             mbar_init(empty + 8 * i, 1);
         }
-        mbar_init(q_full, PROD_WARPS);
+        mbar_init(q_full, Q_WARPS);
         mbar_init(q_empty, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(s_full + 8 * i, 1);
@@ -325,6 +329,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             mbar_init(joined + 8 * i, 4);
         }
         mbar_init(drain, 1);
+        for (int i = 0; i < 2 * RING; ++i) mbar_init(raw_full + 8 * i, 1);
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async();
@@ -338,9 +343,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     tc_after();
     const uint32_t tmem = misc[61];
     Tile t;
-    tile_seq(p, misc[32], t);
+    tile_seq(p, misc[40], t);
     {
-        const unsigned long long in_seq = sums[14], head = t.r.before(t.r.n_tiles);
+        const unsigned long long in_seq = sums[18], head = t.r.before(t.r.n_tiles);
         t.h = (uint32_t)(in_seq / head);
         const unsigned long long rest = in_seq % head;
         const Rows r = t.r;
@@ -360,198 +365,184 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     auto S = [&](int i) { return tmem + i * 128; };
     auto O = [&](int i) { return tmem + 256 + i * D; };
 
-    // Registers: 384 x 168 at launch = 256 x 192 + 128 x 120; a softmax thread holds its row's 128 scores.
+    // Registers: 512 x 128 at launch = 256 x 192 + 256 x 64; a softmax thread holds its row's 128 scores.
     if (warp >= MMA_WARP) {
-        setmaxnreg_dec<120>();
-        if (warp >= PROD_WARP) {
-        // =================================== gathering ===================================
-        const uint32_t pw = warp - PROD_WARP;
-        uint32_t n_put = 0, n_sig = 0, q_at = ~0u, segs = 0, n_unit = 0;
+        setmaxnreg_dec<64>();
+        if (warp >= KV_WARP) {
+        // =================================== keys and values ===================================
+        const uint32_t group = (warp - KV_WARP) / KV_WARPS, half = (warp - KV_WARP) % KV_WARPS;     // rows [64 half, 64 half + 64)
+        constexpr int RB = D * (C8 ? 1 : 2);            // bytes of a row in the pool
+        constexpr int CH = RB / 16, RPI = 32 / CH;      // its 16-byte chunks; rows a warp takes at once
+        const uint32_t ch = lane % CH, sub = lane / CH;
+        const uint32_t kslot = base + C::OFF_RING + 2 * group * C::KV;
+        int32_t id[2];                                  // of rows lane and lane + 32; -1 behind the end
+        // tile loads: lane = (128-byte part of the rows) x (box of `box_rows` rows)
+        const uint32_t bs = p.pool.block_tokens, box_rows = min(bs, 64u), boxes = 64 / box_rows;
+        const uint32_t my_box = lane % boxes, my_part = lane / boxes;
+        uint32_t raw_phase[2] = {0, 0};
         bool ok = true;
-        int64_t off[4];                                 // rows lane, lane + 32, ...: block id, -1 behind the end, -2 outside the pool
-        float ks[4], vs[4];
-        Tile f = t;                                     // the unit whose block ids are being looked up
         unsigned long long fx = x0;
-        auto locate = [&]() {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t key = f.u * BN + i * 32 + lane;
-                off[i] = -1;
-                if (fx < x1 && key < f.v.ctx) {
-                    const int32_t id = __ldg(p.step.block_ids + f.v.b0 + key / p.pool.block_tokens);
-                    off[i] = (uint32_t)id < p.pool.n_blocks ? (int64_t)id : -2;
-                }
-            }
-        };
-        auto resolve = [&]() {                          // ids to byte offsets, scales; writes down which keys exist
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t key = f.u * BN + i * 32 + lane;
-                if (off[i] == -2 && pw == 0) report(p.step, TUTTI_EFAULT);
-                const bool there = off[i] >= 0;
-                const uint32_t mask = __ballot_sync(0xffffffffu, off[i] != -2);   // keys behind the end are masked by position
-                if (pw == 0 && lane == 0) exists[(n_unit & 7) * 4 + i] = mask;
-                if (C8) {
-                    const uint64_t at = there ? (uint64_t)off[i] * p.pool.n_kv_heads + f.h : 0;
-                    ks[i] = there ? p.pool.k_scale[at] : 0.0f;
-                    vs[i] = there ? p.pool.v_scale[at] : 0.0f;
-                }
-                if (there) off[i] = block_offset(p.pool, (int32_t)off[i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + f.h * p.pool.head_stride);
-            }
-            ++n_unit;
-        };
         auto step_unit = [&]() {
             ++fx;
-            if (fx < x1 && ++f.u == f.n_units) next_tile(p, f);
+            if (fx < x1 && ++t.u == t.n_units) next_tile(p, t);
         };
-        auto signal = [&](uint32_t upto) {              // tiles [n_sig, upto) have landed
-            while (n_sig < upto) {
-                fence_async();
-                __syncwarp();
-                if (lane == 0) {
-                    if (n_sig == q_at) mbar_arrive(q_full);
-                    mbar_arrive(full + 8 * (n_sig % RING));
-                }
-                ++n_sig;
+        auto locate = [&]() {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t key = t.u * BN + half * 64 + i * 32 + lane;
+                id[i] = fx < x1 && key < t.v.ctx ? __ldg(p.step.block_ids + t.v.b0 + key / p.pool.block_tokens) : -1;
             }
         };
-        auto room = [&]() { return n_put < RING || mbar_wait(empty + 8 * (n_put % RING), (n_put / RING - 1) & 1, dead); };
-        auto load_q = [&]() {                           // cp.async of the tile's rows, zeros behind the last
-            constexpr int CH = D / 8;
-            for (uint32_t i = pw; i < TILE_ROWS * CH / 32; i += PROD_WARPS) {
-                const uint32_t r = (i * 32 + lane) / CH, ch = lane % CH, row = t.q * TILE_ROWS + r;
-                const bool in = row < t.r.n_rows;
-                const uint32_t n = in ? row / p.group : 0, h = t.h * p.group + (in ? row % p.group : 0);
-                const T *src = (const T *)p.q + (uint64_t)(t.v.q0 + n) * p.q_stride + (uint64_t)h * D + ch * 8;
-                cp16(base + r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch), src, in);
-            }
-        };
-        constexpr int CH = D * (C8 ? 1 : 2) / 16;       // 16-byte chunks of a row in the pool
-        constexpr int RPI = 32 / CH;                    // rows a warp takes at once
-        constexpr int PER = 32 / RPI;                   // such steps in 32 rows
-        constexpr int N = (PER + PROD_WARPS - 1) / PROD_WARPS;
-        const uint32_t ch = lane % CH, sub = lane / CH;
+        if (group == 1) step_unit();
         locate();
-        uint4 rk[C8 ? 4 : 1][C8 ? N : 1], rv[C8 ? 4 : 1][C8 ? N : 1];
-        float cs[4];
-        auto fetch8 = [&](uint4 (&r)[C8 ? 4 : 1][C8 ? N : 1], uint64_t from) {
-            if constexpr (C8) {
+        for (uint32_t n = group; fx < x1; n += 2) {     // n: unit of the worker
+            const int32_t id0 = id[0], id1 = id[1];
+            const uint32_t key_unit = t.u * BN, head = t.h;
+            int64_t off[2];
+            float sc[2][2];
+            bool tiled = maps.valid;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int k = 0; k < N; ++k) {
-                        const uint32_t it = (pw + i) % PROD_WARPS + PROD_WARPS * k;
-                        r[i][k] = make_uint4(0, 0, 0, 0);
-                        if (it < PER) {
-                            const int64_t o = __shfl_sync(0xffffffffu, off[i], it * RPI + sub);
-                            if (o >= 0) r[i][k] = __ldg(reinterpret_cast<const uint4 *>(from + o + ch * 16));
-                        }
-                    }
-            }
-        };
-        auto store8 = [&](const uint4 (&r)[C8 ? 4 : 1][C8 ? N : 1], const float (&sc)[4], uint32_t slot) {
-            if constexpr (C8) {
-                const uint32_t dst = C::OFF_RING + slot * C::KV;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int k = 0; k < N; ++k) {
-                        const uint32_t it = (pw + i) % PROD_WARPS + PROD_WARPS * k;
-                        if (it < PER) {
-                            const uint32_t row = i * 32 + it * RPI + sub;
-                            typename C::Pair s1, s2;
-                            factors(__shfl_sync(0xffffffffu, sc[i], it * RPI + sub), s1, s2);
-                            const uint2 a = widen(r[i][k].x, s1, s2), b = widen(r[i][k].y, s1, s2);
-                            const uint2 c = widen(r[i][k].z, s1, s2), d = widen(r[i][k].w, s1, s2);
-                            *reinterpret_cast<uint4 *>(sm + dst + C::place(row, 2 * ch)) = make_uint4(a.x, a.y, b.x, b.y);
-                            *reinterpret_cast<uint4 *>(sm + dst + C::place(row, 2 * ch + 1)) = make_uint4(c.x, c.y, d.x, d.y);
-                        }
-                    }
-            }
-        };
-        if constexpr (C8) {
-            resolve();
-            fetch8(rk, p.pool.k_base);
-        }
-        for (unsigned long long x = x0; x < x1 && ok;) {
-            const uint32_t n = (uint32_t)min(x1 - x, (unsigned long long)(t.n_units - t.u));
-            if (segs) {
-                cp_wait<0>();
-                signal(n_put);
-                ok = mbar_wait(q_empty, (segs - 1) & 1, dead);
-                if (!ok) break;
-            }
-            load_q();
-            if constexpr (C8) {
-                cp_commit();
-                cp_wait<0>();
-                fence_async();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(q_full);
-            } else {
-                q_at = n_put;
-            }
-            for (uint32_t j = 0; j < n && ok; ++j) {
-                if constexpr (!C8) {
-                    resolve();
-                    for (int half = 0; half < 2 && ok; ++half) {
-                        ok = room();
-                        if (!ok) break;
-                        const uint32_t dst = base + C::OFF_RING + (n_put % RING) * C::KV;
-                        const uint64_t from = half ? p.pool.v_base : p.pool.k_base;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int k = 0; k < N; ++k) {
-                                const uint32_t it = (pw + i) % PROD_WARPS + PROD_WARPS * k;
-                                if (it < PER) {
-                                    const uint32_t row = it * RPI + sub;
-                                    const int64_t o = __shfl_sync(0xffffffffu, off[i], row);
-                                    cp16(dst + C::place(i * 32 + row, ch), (const void *)(from + (o >= 0 ? o : 0) + ch * 16), o >= 0);
-                                }
-                            }
-                        cp_commit();
-                        ++n_put;
-                        cp_wait<2>();
-                        if (n_put >= 2) signal(n_put - 2);
-                    }
-                    step_unit();
-                    locate();
-                } else {
-                    fetch8(rv, p.pool.v_base);
-                    ok = room();
-                    if (!ok) break;
-                    store8(rk, ks, n_put % RING);
-                    ++n_put;
-                    signal(n_put);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) cs[i] = vs[i];
-                    step_unit();
-                    locate();
-                    if (fx < x1) {
-                        resolve();
-                        fetch8(rk, p.pool.k_base);
-                    }
-                    ok = room();
-                    if (!ok) break;
-                    store8(rv, cs, n_put % RING);
-                    ++n_put;
-                    signal(n_put);
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t key = t.u * BN + half * 64 + i * 32 + lane;
+                const bool there = (uint32_t)id[i] < p.pool.n_blocks, bad = !there && key < t.v.ctx;
+                if (bad) report(p.step, TUTTI_EFAULT);
+                const uint32_t mask = __ballot_sync(0xffffffffu, !bad);       // keys behind the end are masked by position
+                if (lane == 0) exists[(n & 7) * 4 + half * 2 + i] = mask;
+                tiled = tiled && __all_sync(0xffffffffu, there);
+                off[i] = there ? block_offset(p.pool, id[i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + t.h * p.pool.head_stride) : -1;
+                if constexpr (C8) {
+                    const uint64_t at = there ? (uint64_t)id[i] * p.pool.n_kv_heads + t.h : 0;
+                    sc[0][i] = there ? p.pool.k_scale[at] : 0.0f;
+                    sc[1][i] = there ? p.pool.v_scale[at] : 0.0f;
                 }
             }
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                if (n >= 2) ok = mbar_wait(empty + 8 * (2 * group + kv), (n / 2 - 1) & 1, dead);
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                const uint64_t from = kv ? p.pool.v_base : p.pool.k_base;
+                // 8-bit rows wait in the upper half of the place that they will fill
+                const uint32_t dst = kslot + kv * C::KV + (C8 && D == 128 ? ATOM : 0);
+                if (tiled) {
+                    constexpr uint32_t PARTS = RB / 128 ? RB / 128 : 1;
+                    const uint32_t row = half * 64 + my_box * box_rows;
+                    const uint32_t bar = C8 ? raw_full + 8 * (warp - KV_WARP + 4 * kv) : full + 8 * (2 * group + kv);
+                    const uint32_t from_lane = my_box * box_rows % 32;
+                    const int32_t lo = __shfl_sync(0xffffffffu, id0, from_lane), hi = __shfl_sync(0xffffffffu, id1, from_lane);
+                    const int32_t block = my_box * box_rows < 32 ? lo : hi;
+                    if (lane == 0) mbar_expect(bar, 64 * RB);
+                    __syncwarp();
+                    if (my_part < PARTS) {
+                        const int32_t token = (int32_t)((key_unit + row) % bs), x0_ = (int32_t)(my_part * (128 / (C8 ? 1 : 2)));
+                        tile_load(dst + my_part * ATOM + row * 128, kv ? &maps.v : &maps.k, bar, x0_, p.hnd ? token : (int32_t)head,
+                                  p.hnd ? (int32_t)head : token, block);
+                    }
+                    continue;
+                }
+#pragma unroll
+                for (int it = 0; it < 64 / RPI; ++it) {
+                    const uint32_t r = it * RPI + sub, row = half * 64 + r;
+                    const int64_t o = __shfl_sync(0xffffffffu, off[it * RPI / 32], r % 32);
+                    cp16(dst + (C8 ? row * 128 + (((ch ^ row) & (CH - 1)) << 4) : C::place(row, ch)), (const void *)(from + (o >= 0 ? o : 0) + ch * 16), o >= 0);
+                }
+                cp_commit();
+            }
+            if (!ok) break;
+            step_unit();
+            step_unit();
+            locate();                                   // the next unit's ids arrive while this one's rows do
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv) {
+                if (tiled && !C8) break;                // the tensor copies arrive at `full` by themselves
+                if (tiled) {
+                    ok = mbar_wait(raw_full + 8 * (warp - KV_WARP + 4 * kv), raw_phase[kv]++ & 1, dead);
+                    if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                } else if (kv == 0) {
+                    cp_wait<1>();
+                } else {
+                    cp_wait<0>();
+                }
+                if constexpr (C8) {
+                    __syncwarp();                       // the warp's rows, brought by all its lanes
+                    unsigned char *slot = sm + C::OFF_RING + (2 * group + kv) * C::KV;
+#pragma unroll 2
+                    for (int it = 0; it < 64 / RPI; ++it) {
+                        const uint32_t r = it * RPI + sub, row = half * 64 + r;
+                        float s1, s2;
+                        factors(__shfl_sync(0xffffffffu, it * RPI >= 32 ? sc[kv][1] : sc[kv][0], r % 32), s1, s2, T());
+                        const uint4 c = *reinterpret_cast<const uint4 *>(slot + (D == 128 ? ATOM : 0) + row * 128 + (((ch ^ row) & (CH - 1)) << 4));
+                        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+                        uint32_t e[8];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint2 x = spread(w[k], T());
+                            e[2 * k] = times(x.x, twice(s1, T()));
+                            e[2 * k + 1] = times(x.y, twice(s1, T()));
+                        }
+                        if (__any_sync(0xffffffffu, s2 != 1.0f)) {
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) e[k] = times(e[k], twice(s2, T()));
+                        }
+                        if (nan_codes(w[0]) | nan_codes(w[1]) | nan_codes(w[2]) | nan_codes(w[3])) {
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t z = nan_codes(w[k]);
+                                if (z & 0x80u) e[2 * k] |= 0x7fffu;
+                                if (z & 0x800000u) e[2 * k] |= 0x7fff0000u;
+                                if (z & 0x8000u) e[2 * k + 1] |= 0x7fffu;
+                                if (z & 0x80000000u) e[2 * k + 1] |= 0x7fff0000u;
+                            }
+                        }
+                        __syncwarp();                   // every lane has read its part of these rows
+                        *reinterpret_cast<uint4 *>(slot + C::place(row, 2 * ch)) = make_uint4(e[0], e[1], e[2], e[3]);
+                        *reinterpret_cast<uint4 *>(slot + C::place(row, 2 * ch + 1)) = make_uint4(e[4], e[5], e[6], e[7]);
+                    }
+                }
+                fence_async();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full + 8 * (2 * group + kv));
+            }
+            if (!ok) break;
+        }
+        cp_wait<0>();
+        } else if (warp >= Q_WARP) {
+        // =================================== queries ===================================
+        uint32_t segs = 0;
+        for (unsigned long long x = x0; x < x1; ++segs) {
+            const uint32_t n = (uint32_t)min(x1 - x, (unsigned long long)(t.n_units - t.u));
+            bool ok = !segs || mbar_wait(q_empty, (segs - 1) & 1, dead);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            constexpr int CH = D / 8;
+            for (uint32_t i = warp - Q_WARP; i < TILE_ROWS * CH / 32; i += Q_WARPS) {
+                const uint32_t r = (i * 32 + lane) / CH, ch = lane % CH, row = t.q * TILE_ROWS + r;
+                const bool in = row < t.r.n_rows;           // zeros behind the last row
+                const uint32_t k = in ? row / p.group : 0, h = t.h * p.group + (in ? row % p.group : 0);
+                const T *src = (const T *)p.q + (uint64_t)(t.v.q0 + k) * p.q_stride + (uint64_t)h * D + ch * 8;
+                const uint32_t dst = r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch);
+                if constexpr (!C8) {
+                    cp16(base + dst, src, in);
+                } else {
+                    const uint4 u = in ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4 *>(sm + dst) = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.x, u.y, 0x7632),
+                                                                      __byte_perm(u.z, u.w, 0x5410), __byte_perm(u.z, u.w, 0x7632));
+                }
+            }
+            cp_commit();
+            cp_wait<0>();
+            fence_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full);
             x += n;
-            ++segs;
             if (x < x1) next_tile(p, t);
         }
         cp_wait<0>();
-        if (ok) signal(n_put);
         } else {
         // =================================== matrix instructions ===================================
         if (lane == 0) {
             constexpr uint32_t FMT = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
             constexpr uint32_t IDESC = 1u << 4 | FMT << 7 | FMT << 10 | (uint32_t)(HALF_ROWS / 16) << 24;
             constexpr uint32_t ID_QK = IDESC | (uint32_t)(BN / 8) << 17, ID_PV = IDESC | 1u << 16 | (uint32_t)(D / 8) << 17;
-            uint32_t kv = 0, segs = 0, np[2] = {0, 0}, ns[2] = {0, 0};
+            uint32_t n_unit = 0, segs = 0, np[2] = {0, 0}, ns[2] = {0, 0};
             bool ok = true;
             auto qk = [&](int i, uint32_t slot) {
                 const uint64_t a = operand(base + i * C::KV), b = operand(base + C::OFF_RING + slot * C::KV);
@@ -568,31 +559,31 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 for (int k = 0; k < BN / 16; ++k) mma_ts(O(i), S(i) + k * 8, b + ((k * 2048) >> 4), ID_PV, acc || k > 0);
                 tc_commit(o_full + 8 * i);
             };
-            auto landed = [&](uint32_t i) { return mbar_wait(full + 8 * (i % RING), (i / RING) & 1, dead); };
+            // K (0) or V (1) of unit u of the worker
+            auto slot = [](uint32_t u, uint32_t kv) { return (u & 1) * 2 + kv; };
+            auto landed = [&](uint32_t u, uint32_t kv) { return mbar_wait(full + 8 * slot(u, kv), (u / 2) & 1, dead); };
             for (unsigned long long x = x0; x < x1 && ok;) {
                 const uint32_t n = (uint32_t)min(x1 - x, (unsigned long long)(t.n_units - t.u));
                 const int halves = t.r.n_rows - t.q * TILE_ROWS > HALF_ROWS ? 2 : 1;
-                ok = mbar_wait(q_full, segs & 1, dead) && landed(kv);
+                ok = mbar_wait(q_full, segs & 1, dead) && landed(n_unit, 0);
                 if (!ok) break;
                 tc_after();
-                for (int i = 0; i < halves; ++i) qk(i, kv % RING);
-                tc_commit(empty + 8 * (kv % RING));
-                ++kv;
-                for (uint32_t j = 0; j < n && ok; ++j) {
+                for (int i = 0; i < halves; ++i) qk(i, slot(n_unit, 0));
+                tc_commit(empty + 8 * slot(n_unit, 0));
+                for (uint32_t j = 0; j < n && ok; ++j, ++n_unit) {
                     const bool more = j + 1 < n;
-                    ok = landed(kv) && (!more || landed(kv + 1));
+                    ok = landed(n_unit, 1) && (!more || landed(n_unit + 1, 0));
                     for (int i = 0; i < halves && ok; ++i) {
                         ok = mbar_wait(p_full + 8 * i, np[i]++ & 1, dead);
                         if (ok && j == 0 && ns[i]) ok = mbar_wait(o_empty + 8 * i, (ns[i] - 1) & 1, dead);
                         if (!ok) break;
                         tc_after();
-                        pv(i, kv % RING, j > 0);
-                        if (more) qk(i, (kv + 1) % RING);
+                        pv(i, slot(n_unit, 1), j > 0);
+                        if (more) qk(i, slot(n_unit + 1, 0));
                     }
                     if (!ok) break;
-                    tc_commit(empty + 8 * (kv % RING));
-                    if (more) tc_commit(empty + 8 * ((kv + 1) % RING));
-                    kv += more ? 2 : 1;
+                    tc_commit(empty + 8 * slot(n_unit, 1));
+                    if (more) tc_commit(empty + 8 * slot(n_unit + 1, 0));
                 }
                 if (!ok) break;
                 for (int i = 0; i < halves; ++i) ++ns[i];
@@ -744,10 +735,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     if (r == 0) {
                         const uint32_t old = atomicAdd(ws.count + 2 * w0 + i, 1);
                         if (old == w1 - w0) ws.count[2 * w0 + i] = 0;            // ready for the next call
-                        misc[40 + i] = old == w1 - w0;
+                        misc[42 + i] = old == w1 - w0;
                     }
                     if (!(ok = join())) break;
-                    write = *(volatile uint32_t *)(misc + 40 + i);
+                    write = *(volatile uint32_t *)(misc + 42 + i);
                     if (write) {
                         __threadfence();
                         m = -INFINITY;
@@ -773,9 +764,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     const float inv = m == -INFINITY ? 0.0f : C::VALUE / l;
                     uint4 *out = reinterpret_cast<uint4 *>((T *)p.out + token * p.out_stride + (uint64_t)qh * D);
 #pragma unroll
-                    for (int d = 0; d < D / 8; ++d)
-                        out[d] = make_uint4(pack2(o[8 * d] * inv, o[8 * d + 1] * inv, T()), pack2(o[8 * d + 2] * inv, o[8 * d + 3] * inv, T()),
-                                            pack2(o[8 * d + 4] * inv, o[8 * d + 5] * inv, T()), pack2(o[8 * d + 6] * inv, o[8 * d + 7] * inv, T()));
+                    for (int d = 0; d < D / 8; ++d) {
+                        constexpr int B = C8 ? 2 : 1, E = C8 ? 1 : 2;      // where elements 1 and 2 of four are
+                        const float *e = o + 8 * d;
+                        out[d] = make_uint4(pack2(e[0] * inv, e[B] * inv, T()), pack2(e[E] * inv, e[3] * inv, T()),
+                                            pack2(e[4] * inv, e[4 + B] * inv, T()), pack2(e[4 + E] * inv, e[7] * inv, T()));
+                    }
                     if (p.lse) p.lse[token * p.n_q_heads + qh] = m == -INFINITY ? -INFINITY : (m - C::OFF + log2f(l)) * 0.6931471805599453f;
                 }
             }
@@ -792,14 +786,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 }
 
 template <typename T, bool C8, int D>
-cudaError_t launch(const AttendParams &p, const Workspace &ws, cudaStream_t st) {
-    attend_many_kernel<T, C8, D><<<ws.workers, THREADS, Many<T, C8, D>::SMEM, st>>>(p, ws);
+cudaError_t launch(const AttendParams &p, const PoolMaps &maps, const Workspace &ws, cudaStream_t st) {
+    attend_many_kernel<T, C8, D><<<ws.workers, THREADS, Many<T, C8, D>::SMEM, st>>>(p, maps, ws);
     return cudaGetLastError();
 }
 
 template <typename T, bool C8>
-cudaError_t launch(const AttendParams &p, const Workspace &ws, cudaStream_t st) {
-    return p.pool.head_dim == 128 ? launch<T, C8, 128>(p, ws, st) : launch<T, C8, 64>(p, ws, st);
+cudaError_t launch(const AttendParams &p, const PoolMaps &maps, const Workspace &ws, cudaStream_t st) {
+    return p.pool.head_dim == 128 ? launch<T, C8, 128>(p, maps, ws, st) : launch<T, C8, 64>(p, maps, ws, st);
 }
 
 template <typename T, bool C8, int D>
@@ -823,9 +817,9 @@ cudaError_t many_setup() {
     return e == cudaSuccess ? setup_type<__half>() : e;
 }
 
-cudaError_t many_launch(const AttendParams &p, const Workspace &ws, bool c8, bool bf, cudaStream_t st) {
-    if (c8) return bf ? launch<__nv_bfloat16, true>(p, ws, st) : launch<__half, true>(p, ws, st);
-    return bf ? launch<__nv_bfloat16, false>(p, ws, st) : launch<__half, false>(p, ws, st);
+cudaError_t many_launch(const AttendParams &p, const PoolMaps &maps, const Workspace &ws, bool c8, bool bf, cudaStream_t st) {
+    if (c8) return bf ? launch<__nv_bfloat16, true>(p, maps, ws, st) : launch<__half, true>(p, maps, ws, st);
+    return bf ? launch<__nv_bfloat16, false>(p, maps, ws, st) : launch<__half, false>(p, maps, ws, st);
 }
 
 uint32_t many_workers(int sms) { return (uint32_t)sms; }

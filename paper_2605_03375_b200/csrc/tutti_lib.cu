@@ -75,6 +75,7 @@ struct tutti_ctx {
     bool pool_hnd = false;       // pool blocks are [head][token][dim]
     StoreTensorMaps maps;        // for the transposing bulk copies
     std::vector<std::pair<float *, float *>> scales;   // K, V scales of an 8-bit pool layer
+    std::vector<PoolTensorMaps> pool_maps;             // for attention's tile loads
     PoolLayerDev *d_pools = nullptr;   // device copy of the pool table (multi-layer builds)
 };
 
@@ -195,6 +196,7 @@ int tutti_ctx_create(const tutti_geom_t *geom, int device, tutti_ctx_t **out) {
     c->device_sms = prop.multiProcessorCount;
     c->pool.assign(geom->n_layers, PoolLayer{0, 0, 0, 0, false});
     c->scales.assign(geom->n_layers, {nullptr, nullptr});
+    c->pool_maps.assign(geom->n_layers, PoolTensorMaps());
     for (auto &s : c->store) s = StoreDev{0, 0, 0, false, false};
     memset(&c->maps, 0, sizeof(c->maps));
     c->opt = CopyOptions{0, 2000000ull, 4, 0, 0, 0, 0, 0};   // 0 = chosen per launch
@@ -231,6 +233,48 @@ int tutti_ctx_destroy(tutti_ctx_t *ctx) {
     return TUTTI_OK;
 }
 
+typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                              const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                              CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+static encode_fn tensor_map_encoder() {
+    void *fp = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fp, cudaEnableDefault, &q) == cudaSuccess && fp &&
+                    q == cudaDriverEntryPointSuccess;
+    if (!ok) cudaGetLastError();
+    return ok ? (encode_fn)fp : nullptr;
+}
+
+// Tensor maps of a pool layer for attention: one box is 128 bytes of up to 64 tokens of one head and
+// block, in the 128-byte swizzle.  Token-major: [block][token][head][dim], head-major:
+// [block][head][token][dim].  Where the geometry does not fit, or the driver refuses the strides, the
+// rows are gathered one by one instead.
+static void encode_pool_maps(tutti_ctx *ctx, uint32_t layer) {
+    PoolTensorMaps &m = ctx->pool_maps[layer];
+    m.valid[0] = m.valid[1] = false;
+    const tutti_geom_t &g = ctx->geom;
+    const PoolLayer &p = ctx->pool[layer];
+    const uint32_t bs = g.block_tokens;
+    const uint64_t row = (uint64_t)g.head_dim * g.elem_bytes;
+    if (g.elem_bytes > 2 || row % 128 || row > 256 || bs % 8 || (64 % bs && bs % 64)) return;
+    const encode_fn encode = tensor_map_encoder();
+    if (!encode) return;
+    const uint32_t tokens = bs < 64 ? bs : 64;
+    for (int hnd = 0; hnd < 2; ++hnd) {
+        const cuuint64_t dims[4] = {g.head_dim, hnd ? bs : g.n_kv_heads, hnd ? g.n_kv_heads : bs, p.n_blocks};
+        const cuuint64_t strides[3] = {row, hnd ? row * bs : ctx->layout.token_bytes, p.block_stride};
+        const cuuint32_t box[4] = {128 / g.elem_bytes, hnd ? tokens : 1, hnd ? 1 : tokens, 1}, ones[4] = {1, 1, 1, 1};
+        const CUtensorMapDataType type = g.elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+        bool ok = true;
+        for (int v = 0; v < 2; ++v)
+            ok = ok && encode(v ? &m.v[hnd] : &m.k[hnd], type, 4, (void *)(v ? p.v_base : p.k_base), dims, strides, box, ones,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+        m.valid[hnd] = ok;
+    }
+}
+
 int tutti_pool_register(tutti_ctx_t *ctx, uint32_t layer, void *k_base, void *v_base,
                         uint64_t block_stride, uint64_t n_blocks) {
     if (!ctx || layer >= ctx->geom.n_layers || !k_base || !v_base || !n_blocks) return TUTTI_EINVAL;
@@ -239,6 +283,7 @@ int tutti_pool_register(tutti_ctx_t *ctx, uint32_t layer, void *k_base, void *v_
     if (block_stride < ctx->layout.block_bytes || n_blocks > 0x7fffffffull) return TUTTI_EINVAL;
     ctx->pool[layer] = PoolLayer{k, v, block_stride, n_blocks, true};
     ctx->scales[layer] = {nullptr, nullptr};
+    encode_pool_maps(ctx, layer);
     PoolLayerDev pl{k, v, block_stride, n_blocks};
     DeviceGuard guard(ctx->device);
     CK(cudaMemcpy(ctx->d_pools + layer, &pl, sizeof(pl), cudaMemcpyHostToDevice));
@@ -270,6 +315,15 @@ int tutti_ctx_pool_view_(tutti_ctx_t *ctx, uint32_t layer, PoolView *v, uint32_t
     return TUTTI_OK;
 }
 
+// K and V tensor maps of a layer in the layout that is set now; false where there are none.
+bool tutti_ctx_pool_maps_(tutti_ctx *ctx, uint32_t layer, CUtensorMap *k, CUtensorMap *v) {
+    const PoolTensorMaps &m = ctx->pool_maps[layer];
+    if (!m.valid[ctx->pool_hnd]) return false;
+    *k = m.k[ctx->pool_hnd];
+    *v = m.v[ctx->pool_hnd];
+    return true;
+}
+
 int tutti_store_register(tutti_ctx_t *ctx, uint32_t dev, void *base, uint64_t bytes, uint32_t kind) {
     if (!ctx || dev >= ctx->geom.n_devices || !base) return TUTTI_EINVAL;
     if (((uint64_t)base & 15) || bytes < ctx->layout.dev_bytes) return TUTTI_EINVAL;
@@ -288,20 +342,14 @@ int tutti_store_register(tutti_ctx_t *ctx, uint32_t dev, void *base, uint64_t by
               ctx->layout.token_bytes % 16 == 0 &&
               (ctx->geom.block_tokens * row_bytes) % 128 == 0;   // a head's slab in the stage
     if (ok) {
-        typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *,
-                                      const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                      const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                      CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-        void *fp = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fp, cudaEnableDefault, &q) == cudaSuccess &&
-             fp && q == cudaDriverEntryPointSuccess;
+        const encode_fn encode = tensor_map_encoder();
+        ok = encode != nullptr;
         if (ok) {
             cuuint64_t dims[3] = {row_bytes / 4, ctx->geom.n_kv_heads, n_rows};
             cuuint64_t strides[2] = {row_bytes, ctx->layout.token_bytes};      // bytes, dims 1 and 2
             cuuint32_t box[3] = {(cuuint32_t)(row_bytes / 4), 1, ctx->geom.block_tokens};
             cuuint32_t estr[3] = {1, 1, 1};
-            CUresult r = ((encode_fn)fp)(&ctx->maps.map[dev], CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, base, dims,
+            CUresult r = encode(&ctx->maps.map[dev], CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, base, dims,
                                          strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                                          CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);

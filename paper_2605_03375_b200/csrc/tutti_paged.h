@@ -2,6 +2,7 @@
 // a registered pool layer and of a step's tables, and the checks that keep every access inside
 // them.  The checks are plain arithmetic, callable on the host too.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -14,6 +15,12 @@ struct PoolView {
     uint32_t n_blocks, block_tokens, n_kv_heads, head_dim;
     uint64_t tok_stride, head_stride;       // bytes between tokens / heads of a block
     float *k_scale, *v_scale;               // [n_blocks][n_kv_heads], 8-bit pools only
+};
+
+// Tensor maps of a pool layer, by pool layout (TUTTI_POOL_NHD, TUTTI_POOL_HND).
+struct PoolTensorMaps {
+    CUtensorMap k[2], v[2];
+    bool valid[2] = {false, false};
 };
 
 struct StepDev {
@@ -78,6 +85,7 @@ __device__ inline uint32_t warp_find(uint32_t n, uint32_t x, F start) {
 // The layer's view and the context's device, for the operators' entry points (tutti_lib.cu).
 struct tutti_ctx;
 extern "C" int tutti_ctx_pool_view_(tutti_ctx *ctx, uint32_t layer, tutti::PoolView *view, uint32_t *elem_bytes);
+extern "C" bool tutti_ctx_pool_maps_(tutti_ctx *ctx, uint32_t layer, CUtensorMap *k, CUtensorMap *v);
 extern "C" int tutti_ctx_device_(tutti_ctx *ctx);
 extern "C" int tutti_ctx_sms_(tutti_ctx *ctx);
 extern "C" const tutti_geom_t *tutti_ctx_geom_(tutti_ctx *ctx);
