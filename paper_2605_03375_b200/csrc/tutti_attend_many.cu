@@ -40,6 +40,7 @@ constexpr int RING = 4;                 // K and V tiles in flight
 constexpr int THREADS = 512;
 constexpr int MMA_WARP = 8, Q_WARP = 9, Q_WARPS = 3, KV_WARP = 12, KV_WARPS = 2;      // KV_WARPS: of a group
 constexpr uint32_t ATOM = BN * 128;     // 128 rows of 128 bytes
+constexpr int POLY_PAIRS = 5;           // of the 16 pairs in 32 scores: exponentials on the multiply-add units
 constexpr float GROW = 8.0f;            // log2 of how far probabilities may exceed 1
 constexpr long long WAIT_CLOCKS = 3000000000ll;   // about 1.5 s: a wait that takes longer is given up
 
@@ -192,14 +193,64 @@ __device__ inline void tc_ld32(uint32_t *r, uint32_t a) {
 __device__ inline void tc_loaded(uint32_t *r) {
     asm volatile("" : P4(r, 0), P4(r, 4), P4(r, 8), P4(r, 12), P4(r, 16), P4(r, 20), P4(r, 24), P4(r, 28));
 }
-__device__ inline void tc_st32(const uint32_t *r, uint32_t a) {
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};"
-                 ::I4(r, 0), I4(r, 4), I4(r, 8), I4(r, 12), I4(r, 16), I4(r, 20), I4(r, 24), I4(r, 28), "r"(a) : "memory");
-}
 __device__ inline void tc_st16(const uint32_t *r, uint32_t a) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"
                  ::I4(r, 0), I4(r, 4), I4(r, 8), I4(r, 12), "r"(a) : "memory");
+}
+
+__device__ inline void tc_ld16(uint32_t *r, uint32_t a) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : O4(r, 0), O4(r, 4), O4(r, 8), O4(r, 12) : "r"(a));
+}
+
+__device__ inline bool elect() {
+    uint32_t x;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(x));
+    return x;
+}
+
+// ---- arithmetic on pairs ----
+typedef unsigned long long f2;
+__device__ inline f2 pair(float a, float b) {
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ inline void unpair(f2 x, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ inline f2 fma2(f2 a, f2 b, f2 c) {
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ inline f2 add2(f2 a, f2 b) {
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ inline float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x of a pair on the multiply-add units, x <= 127: x = n + f with |f| <= 1/2, 2^f by its minimax
+// polynomial of degree 4 (fitted to a relative error of 2.6e-6, well under the 16 bits that
+// probabilities are rounded to), n added to the exponent.  Below -125 the result stays 2^-125.
+__device__ inline void ex2_poly(f2 x, float &a, float &b) {
+    const f2 magic = pair(12582912.0f, 12582912.0f);            // 1.5 * 2^23: rounds to an integer
+    unpair(x, a, b);
+    x = pair(fmaxf(a, -125.0f), fmaxf(b, -125.0f));
+    const f2 t = add2(x, magic);
+    const f2 f = fma2(add2(t, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), x);
+    f2 y = pair(0.009567738510668278f, 0.009567738510668278f);
+    y = fma2(y, f, pair(0.05591749772429466f, 0.05591749772429466f));
+    y = fma2(y, f, pair(0.24024811387062073f, 0.24024811387062073f));
+    y = fma2(y, f, pair(0.6931219100952148f, 0.6931219100952148f));
+    y = fma2(y, f, pair(0.9999992251396179f, 0.9999992251396179f));
+    float ta, tb, ya, yb;
+    unpair(t, ta, tb);
+    unpair(y, ya, yb);
+    a = __uint_as_float(__float_as_uint(ta) * 0x800000u + __float_as_uint(ya));
+    b = __uint_as_float(__float_as_uint(tb) * 0x800000u + __float_as_uint(yb));
 }
 
 // Shared-memory operand in the 128-byte swizzle: start, offset between 64-element groups of an
@@ -217,26 +268,32 @@ __device__ inline uint2 spread(uint32_t w, __half) {
 __device__ inline uint2 spread(uint32_t w, __nv_bfloat16) {
     return make_uint2(((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u), ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u));
 }
-// A scale as the two factors that finish spread(); the second is 1 wherever the first can be held.
-// f16: half the value, so that nothing that came from f16 overflows.
-__device__ inline void factors(float s, float &s1, float &s2, __half) {
-    s *= 128.0f;
-    s2 = fabsf(s) < 6.103515625e-05f ? 5.9604644775390625e-08f : 1.0f;      // below the normal range
-    s1 = s / s2;
-}
-__device__ inline void factors(float s, float &s1, float &s2, __nv_bfloat16) {
-    s2 = fabsf(s) < 128.0f ? 1.0f : s;
-    s1 = 1.329227995784916e+36f * (s / s2);                                   // 2^120
-}
-__device__ inline __half2 twice(float x, __half) { return __float2half2_rn(x); }
-__device__ inline __nv_bfloat162 twice(float x, __nv_bfloat16) { return __float2bfloat162_rn(x); }
-template <typename P>
-__device__ inline uint32_t times(uint32_t x, P s) {
-    const P y = __hmul2(*reinterpret_cast<const P *>(&x), s);
+__device__ inline uint32_t twice(float x, __half) { return pack2(x, x, __half()); }
+__device__ inline uint32_t twice(float x, __nv_bfloat16) { return pack2(x, x, __nv_bfloat16()); }
+__device__ inline uint32_t times(uint32_t x, uint32_t s, __half) {
+    const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&s));
     return *reinterpret_cast<const uint32_t *>(&y);
 }
-// NaN codes (magnitude bits all ones) among four
-__device__ inline uint32_t nan_codes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ inline uint32_t times(uint32_t x, uint32_t s, __nv_bfloat16) {
+    const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&s));
+    return *reinterpret_cast<const uint32_t *>(&y);
+}
+// A scale as the two factors that finish spread(), each rounded to the type (powers of two are
+// exact) and twice in a register; true if the second is not 1.  f16: half the value, so that
+// nothing that came from f16 overflows, and a second factor for what is below the normal range.
+__device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __half) {
+    s *= 128.0f;
+    const bool low = s != 0 && fabsf(s) < 6.103515625e-05f;
+    f1 = twice(low ? s * 16777216.0f : s, __half());
+    f2 = twice(low ? 5.9604644775390625e-08f : 1.0f, __half());               // 2^-24
+    return low;
+}
+__device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __nv_bfloat16) {
+    const bool high = fabsf(s) >= 128.0f;                                     // 2^120 * s would overflow
+    f1 = twice(high ? 1.329227995784916e+36f : 1.329227995784916e+36f * s, __nv_bfloat16());
+    f2 = twice(high ? s : 1.0f, __nv_bfloat16());
+    return high;
+}
 
 template <typename T, bool C8, int D>
 struct Many {
@@ -399,7 +456,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             const int32_t id0 = id[0], id1 = id[1];
             const uint32_t key_unit = t.u * BN, head = t.h;
             int64_t off[2];
-            float sc[2][2];
+            uint32_t fac[2][2], sec[2][2];              // 8-bit: the scales' two factors, twice 16 bits
+            bool small = false;
             bool tiled = maps.valid;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -412,10 +470,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 off[i] = there ? block_offset(p.pool, id[i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + t.h * p.pool.head_stride) : -1;
                 if constexpr (C8) {
                     const uint64_t at = there ? (uint64_t)id[i] * p.pool.n_kv_heads + t.h : 0;
-                    sc[0][i] = there ? p.pool.k_scale[at] : 0.0f;
-                    sc[1][i] = there ? p.pool.v_scale[at] : 0.0f;
+                    const float ks = there ? p.pool.k_scale[at] : 0.0f, vs = there ? p.pool.v_scale[at] : 0.0f;
+                    small = factors(ks, fac[0][i], sec[0][i], T()) || small;
+                    small = factors(vs, fac[1][i], sec[1][i], T()) || small;
                 }
             }
+            small = C8 && __any_sync(0xffffffffu, small);
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 if (n >= 2) ok = mbar_wait(empty + 8 * (2 * group + kv), (n / 2 - 1) & 1, dead);
@@ -465,37 +525,47 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if constexpr (C8) {
                     __syncwarp();                       // the warp's rows, brought by all its lanes
                     unsigned char *slot = sm + C::OFF_RING + (2 * group + kv) * C::KV;
-#pragma unroll 2
-                    for (int it = 0; it < 64 / RPI; ++it) {
-                        const uint32_t r = it * RPI + sub, row = half * 64 + r;
-                        float s1, s2;
-                        factors(__shfl_sync(0xffffffffu, it * RPI >= 32 ? sc[kv][1] : sc[kv][0], r % 32), s1, s2, T());
-                        const uint4 c = *reinterpret_cast<const uint4 *>(slot + (D == 128 ? ATOM : 0) + row * 128 + (((ch ^ row) & (CH - 1)) << 4));
-                        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-                        uint32_t e[8];
+                    constexpr int B = 4;                // steps whose codes are read before their rows are written over
+#pragma unroll 1
+                    for (int it0 = 0; it0 < 64 / RPI; it0 += B) {
+                        uint4 c[B];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            const uint2 x = spread(w[k], T());
-                            e[2 * k] = times(x.x, twice(s1, T()));
-                            e[2 * k + 1] = times(x.y, twice(s1, T()));
+                        for (int k = 0; k < B; ++k) {
+                            const uint32_t row = half * 64 + (it0 + k) * RPI + sub;
+                            c[k] = *reinterpret_cast<const uint4 *>(slot + (D == 128 ? ATOM : 0) + row * 128 + (((ch ^ row) & (CH - 1)) << 4));
                         }
-                        if (__any_sync(0xffffffffu, s2 != 1.0f)) {
+                        __syncwarp();
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) e[k] = times(e[k], twice(s2, T()));
-                        }
-                        if (nan_codes(w[0]) | nan_codes(w[1]) | nan_codes(w[2]) | nan_codes(w[3])) {
+                        for (int k = 0; k < B; ++k) {
+                            const uint32_t r = (it0 + k) * RPI + sub, row = half * 64 + r;
+                            const uint32_t f1 = __shfl_sync(0xffffffffu, r < 32 ? fac[kv][0] : fac[kv][1], r % 32);
+                            const uint32_t w[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
+                            uint32_t e[8], nan = 0;
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                const uint32_t z = nan_codes(w[k]);
-                                if (z & 0x80u) e[2 * k] |= 0x7fffu;
-                                if (z & 0x800000u) e[2 * k] |= 0x7fff0000u;
-                                if (z & 0x8000u) e[2 * k + 1] |= 0x7fffu;
-                                if (z & 0x80000000u) e[2 * k + 1] |= 0x7fff0000u;
+                            for (int i = 0; i < 4; ++i) {
+                                const uint2 x = spread(w[i], T());
+                                e[2 * i] = times(x.x, f1, T());
+                                e[2 * i + 1] = times(x.y, f1, T());
+                                nan |= (w[i] & 0x7f7f7f7fu) + 0x01010101u;
                             }
+                            if (small) {                // some scale of the unit needs its second factor
+                                const uint32_t f2 = __shfl_sync(0xffffffffu, r < 32 ? sec[kv][0] : sec[kv][1], r % 32);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) e[i] = times(e[i], f2, T());
+                            }
+                            if (nan & 0x80808080u) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint32_t z = (w[i] & 0x7f7f7f7fu) + 0x01010101u;
+                                    if (z & 0x80u) e[2 * i] |= 0x7fffu;
+                                    if (z & 0x800000u) e[2 * i] |= 0x7fff0000u;
+                                    if (z & 0x8000u) e[2 * i + 1] |= 0x7fffu;
+                                    if (z & 0x80000000u) e[2 * i + 1] |= 0x7fff0000u;
+                                }
+                            }
+                            *reinterpret_cast<uint4 *>(slot + C::place(row, 2 * ch)) = make_uint4(e[0], e[1], e[2], e[3]);
+                            *reinterpret_cast<uint4 *>(slot + C::place(row, 2 * ch + 1)) = make_uint4(e[4], e[5], e[6], e[7]);
                         }
-                        __syncwarp();                   // every lane has read its part of these rows
-                        *reinterpret_cast<uint4 *>(slot + C::place(row, 2 * ch)) = make_uint4(e[0], e[1], e[2], e[3]);
-                        *reinterpret_cast<uint4 *>(slot + C::place(row, 2 * ch + 1)) = make_uint4(e[4], e[5], e[6], e[7]);
                     }
                 }
                 fence_async();
@@ -538,7 +608,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         cp_wait<0>();
         } else {
         // =================================== matrix instructions ===================================
-        if (lane == 0) {
+        {
+            // the warp stays together; one elected lane issues, so operands live in uniform registers
             constexpr uint32_t FMT = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
             constexpr uint32_t IDESC = 1u << 4 | FMT << 7 | FMT << 10 | (uint32_t)(HALF_ROWS / 16) << 24;
             constexpr uint32_t ID_QK = IDESC | (uint32_t)(BN / 8) << 17, ID_PV = IDESC | 1u << 16 | (uint32_t)(D / 8) << 17;
@@ -546,54 +617,65 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             bool ok = true;
             auto qk = [&](int i, uint32_t slot) {
                 const uint64_t a = operand(base + i * C::KV), b = operand(base + C::OFF_RING + slot * C::KV);
+                if (elect()) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint64_t step = ((k / 4) * ATOM + (k % 4) * 32) >> 4;
-                    mma_ss(S(i), a + step, b + step, ID_QK, k > 0);
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint64_t step = ((k / 4) * ATOM + (k % 4) * 32) >> 4;
+                        mma_ss(S(i), a + step, b + step, ID_QK, k > 0);
+                    }
+                    tc_commit(s_full + 8 * i);
                 }
-                tc_commit(s_full + 8 * i);
+                __syncwarp();
             };
             auto pv = [&](int i, uint32_t slot, bool acc) {
                 const uint64_t b = operand(base + C::OFF_RING + slot * C::KV);
+                if (elect()) {
 #pragma unroll
-                for (int k = 0; k < BN / 16; ++k) mma_ts(O(i), S(i) + k * 8, b + ((k * 2048) >> 4), ID_PV, acc || k > 0);
-                tc_commit(o_full + 8 * i);
+                    for (int k = 0; k < BN / 16; ++k) mma_ts(O(i), S(i) + k * 8, b + ((k * 2048) >> 4), ID_PV, acc || k > 0);
+                    tc_commit(o_full + 8 * i);
+                }
+                __syncwarp();
+            };
+            auto commit = [&](uint32_t bar) {
+                if (elect()) tc_commit(bar);
+                __syncwarp();
             };
             // K (0) or V (1) of unit u of the worker
             auto slot = [](uint32_t u, uint32_t kv) { return (u & 1) * 2 + kv; };
+            auto all = [](bool x) { return (bool)__all_sync(0xffffffffu, x); };
             auto landed = [&](uint32_t u, uint32_t kv) { return mbar_wait(full + 8 * slot(u, kv), (u / 2) & 1, dead); };
             for (unsigned long long x = x0; x < x1 && ok;) {
                 const uint32_t n = (uint32_t)min(x1 - x, (unsigned long long)(t.n_units - t.u));
                 const int halves = t.r.n_rows - t.q * TILE_ROWS > HALF_ROWS ? 2 : 1;
-                ok = mbar_wait(q_full, segs & 1, dead) && landed(n_unit, 0);
+                ok = all(mbar_wait(q_full, segs & 1, dead) && landed(n_unit, 0));
                 if (!ok) break;
                 tc_after();
                 for (int i = 0; i < halves; ++i) qk(i, slot(n_unit, 0));
-                tc_commit(empty + 8 * slot(n_unit, 0));
+                commit(empty + 8 * slot(n_unit, 0));
                 for (uint32_t j = 0; j < n && ok; ++j, ++n_unit) {
                     const bool more = j + 1 < n;
-                    ok = landed(n_unit, 1) && (!more || landed(n_unit + 1, 0));
+                    ok = all(landed(n_unit, 1) && (!more || landed(n_unit + 1, 0)));
                     for (int i = 0; i < halves && ok; ++i) {
                         ok = mbar_wait(p_full + 8 * i, np[i]++ & 1, dead);
                         if (ok && j == 0 && ns[i]) ok = mbar_wait(o_empty + 8 * i, (ns[i] - 1) & 1, dead);
-                        if (!ok) break;
+                        if (!(ok = all(ok))) break;
                         tc_after();
                         pv(i, slot(n_unit, 1), j > 0);
                         if (more) qk(i, slot(n_unit + 1, 0));
                     }
                     if (!ok) break;
-                    tc_commit(empty + 8 * slot(n_unit, 1));
-                    if (more) tc_commit(empty + 8 * slot(n_unit + 1, 0));
+                    commit(empty + 8 * slot(n_unit, 1));
+                    if (more) commit(empty + 8 * slot(n_unit + 1, 0));
                 }
                 if (!ok) break;
                 for (int i = 0; i < halves; ++i) ++ns[i];
-                tc_commit(q_empty);
+                commit(q_empty);
                 ++segs;
                 x += n;
                 if (x < x1) next_tile(p, t);
             }
             // every matrix instruction has ended before TMEM is given back
-            tc_commit(drain);
+            commit(drain);
             const long long t0 = clock64();
             while (!mbar_try(drain, 0) && clock64() - t0 < WAIT_CLOCKS) {}
         }
@@ -650,15 +732,17 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         for (int k = 0; k < 128; ++k)
                             if (k > lim || !(word[k / 32] >> (k % 32) & 1)) s[k] = -INFINITY;
                     }
-                    float a0 = s[0], a1 = s[1], a2 = s[2], a3 = s[3];
+                    float a0 = max3(s[0], s[4], s[8]), a1 = max3(s[1], s[5], s[9]), a2 = max3(s[2], s[6], s[10]), a3 = max3(s[3], s[7], s[11]);
 #pragma unroll
-                    for (int k = 4; k < 128; k += 4) {
-                        a0 = fmaxf(a0, s[k]);
-                        a1 = fmaxf(a1, s[k + 1]);
-                        a2 = fmaxf(a2, s[k + 2]);
-                        a3 = fmaxf(a3, s[k + 3]);
+                    for (int k = 12; k < 124; k += 8) {
+                        a0 = max3(a0, s[k], s[k + 4]);
+                        a1 = max3(a1, s[k + 1], s[k + 5]);
+                        a2 = max3(a2, s[k + 2], s[k + 6]);
+                        a3 = max3(a3, s[k + 3], s[k + 7]);
                     }
-                    const float top = fmaxf(fmaxf(a0, a1), fmaxf(a2, a3)) * scl;
+                    a0 = max3(a0, s[124], s[125]);
+                    a1 = max3(a1, s[126], s[127]);
+                    const float top = max3(a0, a1, fmaxf(a2, a3)) * scl;
                     const bool grow = top > m + GROW || (m == -INFINITY && top > m);
                     if (__any_sync(0xffffffffu, grow)) {
                         const float alpha = grow ? ex2(m - top) : 1.0f;
@@ -670,33 +754,43 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                             if (!ok) break;
                             tc_after();
 #pragma unroll
-                            for (int q = 0; q < D / 32; ++q) {
-                                uint32_t o[32];
-                                tc_ld32(o, o_at + 32 * q);
+                            for (int q = 0; q < D / 16; ++q) {
+                                uint32_t o[16];
+                                tc_ld16(o, o_at + 16 * q);
                                 tc_wait_ld();
-                                tc_loaded(o);
+                                asm volatile("" : P4(o, 0), P4(o, 4), P4(o, 8), P4(o, 12));
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
-                                tc_st32(o, o_at + 32 * q);
+                                for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
+                                tc_st16(o, o_at + 16 * q);
                             }
                         }
                     }
                     const float sub = (m == -INFINITY ? 0.0f : m) - C::OFF;
-                    float l0 = 0, l1 = 0, l2 = 0, l3 = 0;
+                    const f2 scl2 = pair(scl, scl), sub2 = pair(-sub, -sub);
+                    f2 l0 = 0, l1 = 0;
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         uint32_t pk[16];
 #pragma unroll
-                        for (int k = 0; k < 32; k += 4) {
-                            const float e0 = ex2(fmaf(s[32 * q + k], scl, -sub)), e1 = ex2(fmaf(s[32 * q + k + 1], scl, -sub));
-                            const float e2 = ex2(fmaf(s[32 * q + k + 2], scl, -sub)), e3 = ex2(fmaf(s[32 * q + k + 3], scl, -sub));
-                            l0 += e0, l1 += e1, l2 += e2, l3 += e3;
-                            pk[k / 2] = pack2(e0, e1, T());
-                            pk[k / 2 + 1] = pack2(e2, e3, T());
+                        for (int k = 0; k < 16; ++k) {
+                            const f2 x = fma2(pair(s[32 * q + 2 * k], s[32 * q + 2 * k + 1]), scl2, sub2);
+                            float a, b;
+                            if (k * POLY_PAIRS / 16 != (k + 1) * POLY_PAIRS / 16) {       // spread over the 16
+                                ex2_poly(x, a, b);
+                            } else {
+                                unpair(x, a, b);
+                                a = ex2(a);
+                                b = ex2(b);
+                            }
+                            if (k & 1) l1 = add2(l1, pair(a, b));
+                            else l0 = add2(l0, pair(a, b));
+                            pk[k] = pack2(a, b, T());
                         }
                         tc_st16(pk, s_at + 16 * q);
                     }
-                    l += (l0 + l1) + (l2 + l3);
+                    float la, lb;
+                    unpair(add2(l0, l1), la, lb);
+                    l += la + lb;
                     tc_wait_st();
                     tc_before();
                     __syncwarp();
