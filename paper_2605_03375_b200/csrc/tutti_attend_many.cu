@@ -21,8 +21,9 @@
 //             sequence ends inside the unit, a block is missing or blocks do not tile 64 rows, row
 //             by row with zeros in place of what is not there.  Two groups of two warps take the
 //             units in turn, so a group waits for its own loads while the other's are in flight.
-//             8-bit codes are widened in place to 16 bits: code * scale, exact for the powers of
-//             two that append writes.
+//             8-bit codes are widened to 16 bits (code * scale, exact for the powers of two that
+//             append writes): keys where they landed, values out of a buffer of their own, so that
+//             they are fetched before the place they go to is free.
 // Bound: the tensor cores (2 x 128 x 128 x D multiply-adds a half and unit) and, as close,
 // the 128 x 128 exponentials on 16 lanes a clock.
 #include <type_traits>
@@ -259,15 +260,21 @@ __device__ inline uint64_t operand(uint32_t addr) {
     return (uint64_t)((addr & 0x3ffff) >> 4) | (uint64_t)(ATOM >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
 }
 
-// Four codes as 16-bit elements in the order 0, 2 | 1, 3 (the queries are brought in the same order
-// and the outputs leave in it), not yet at their scale: the magnitude's 7 bits are moved to
-// where they are the value times 2^-8 (f16) or 2^-120 (bf16), subnormal codes included.
+// Four codes as two pairs of 16-bit elements, not yet at their scale.  f16: the values, in order.
 __device__ inline uint2 spread(uint32_t w, __half) {
-    return make_uint2(((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u), ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u));
+    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffff), __NV_E4M3);
+    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
+    return make_uint2((uint32_t)a.x | (uint32_t)a.y << 16, (uint32_t)b.x | (uint32_t)b.y << 16);
 }
-__device__ inline uint2 spread(uint32_t w, __nv_bfloat16) {
-    return make_uint2(((w << 4) & 0x07f007f0u) | ((w << 8) & 0x80008000u), ((w >> 4) & 0x07f007f0u) | (w & 0x80008000u));
+// bf16: codes 0, 2 and 1, 3 (the queries are brought in the same order and the outputs leave in it),
+// the magnitude's 7 bits moved to where they are the value times 2^-120, subnormal codes included.
+// NaN codes become 480 * 2^-120, the largest magnitude there is: `top` collects the magnitudes.
+__device__ inline uint2 spread(uint32_t w, __nv_bfloat16, uint32_t &top) {
+    const uint32_t even = (w << 4) & 0x07f007f0u, odd = (w >> 4) & 0x07f007f0u;
+    top = __vmaxu2(__vmaxu2(top, even), odd);
+    return make_uint2(even | ((w << 8) & 0x80008000u), odd | (w & 0x80008000u));
 }
+__device__ inline uint2 spread(uint32_t w, __half, uint32_t &) { return spread(w, __half()); }
 __device__ inline uint32_t twice(float x, __half) { return pack2(x, x, __half()); }
 __device__ inline uint32_t twice(float x, __nv_bfloat16) { return pack2(x, x, __nv_bfloat16()); }
 __device__ inline uint32_t times(uint32_t x, uint32_t s, __half) {
@@ -282,7 +289,7 @@ __device__ inline uint32_t times(uint32_t x, uint32_t s, __nv_bfloat16) {
 // exact) and twice in a register; true if the second is not 1.  f16: half the value, so that
 // nothing that came from f16 overflows, and a second factor for what is below the normal range.
 __device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __half) {
-    s *= 128.0f;
+    s *= 0.5f;
     const bool low = s != 0 && fabsf(s) < 6.103515625e-05f;
     f1 = twice(low ? s * 16777216.0f : s, __half());
     f2 = twice(low ? 5.9604644775390625e-08f : 1.0f, __half());               // 2^-24
@@ -299,7 +306,8 @@ template <typename T, bool C8, int D>
 struct Many {
     static constexpr uint32_t KV = ATOM * (D / 64);         // bytes of a 128-row tile
     static constexpr uint32_t OFF_RING = 2 * KV;            // behind the two halves of Q
-    static constexpr uint32_t OFF_BAR = OFF_RING + RING * KV;
+    static constexpr uint32_t OFF_RAW = OFF_RING + RING * KV;          // 8-bit: codes of a group's values
+    static constexpr uint32_t OFF_BAR = OFF_RAW + (C8 ? 2 * ATOM : 0);
     static constexpr uint32_t OFF_EXISTS = OFF_BAR + 256;   // [8 units][4]: keys that exist
     static constexpr uint32_t OFF_MISC = OFF_EXISTS + 128;
     static constexpr uint32_t SMEM = OFF_MISC + 256 + 1024; // 1024: alignment of the dynamic part
@@ -307,6 +315,8 @@ struct Many {
     static constexpr float VALUE = C8 && std::is_same<T, __half>::value ? 2.0f : 1.0f;
     // f16 probabilities are kept 2^6 times too large (at most 2^14): full precision down to 2^-20
     static constexpr float OFF = std::is_same<T, __half>::value ? 6.0f : 0.0f;
+    // whether widened codes keep their order
+    static constexpr bool ORDERED = !C8 || std::is_same<T, __half>::value;
     // byte offset of 16-byte chunk `ch` of row `row` in a tile
     __device__ static uint32_t place(uint32_t row, uint32_t ch) {
         return (ch >> 3) * ATOM + row * 128 + (((ch ^ row) & 7) << 4);
@@ -431,148 +441,198 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         constexpr int RB = D * (C8 ? 1 : 2);            // bytes of a row in the pool
         constexpr int CH = RB / 16, RPI = 32 / CH;      // its 16-byte chunks; rows a warp takes at once
         const uint32_t ch = lane % CH, sub = lane / CH;
-        const uint32_t kslot = base + C::OFF_RING + 2 * group * C::KV;
-        int32_t id[2];                                  // of rows lane and lane + 32; -1 behind the end
-        // tile loads: lane = (128-byte part of the rows) x (box of `box_rows` rows)
+        const uint32_t slot0 = C::OFF_RING + 2 * group * C::KV;           // K's place; V's is the next
+        // Where the rows of the pool land: 16-bit ones in their places, 8-bit keys in the upper half
+        // of theirs, 8-bit values in the group's buffer (128 bytes from row to row, swizzled alike).
+        const uint32_t land[2] = {slot0 + (C8 && D == 128 ? ATOM : 0), C8 ? C::OFF_RAW + group * ATOM : slot0 + C::KV};
         const uint32_t bs = p.pool.block_tokens, box_rows = min(bs, 64u), boxes = 64 / box_rows;
-        const uint32_t my_box = lane % boxes, my_part = lane / boxes;
-        uint32_t raw_phase[2] = {0, 0};
+        const uint32_t my_box = lane % boxes, my_part = lane / boxes;    // of a lane's tensor copy
+        uint32_t raw_phase = 0;
         bool ok = true;
         unsigned long long fx = x0;
         auto step_unit = [&]() {
             ++fx;
             if (fx < x1 && ++t.u == t.n_units) next_tile(p, t);
         };
+        // The next unit: block ids of rows lane and lane + 32 (locate), then what follows from them.
+        int32_t id[2];
+        uint32_t key0 = 0, head = 0, ctx = 0;
+        int64_t off[2];
+        float ks[2], vs[2];
+        uint32_t missing[2];
+        bool tiled = false;
         auto locate = [&]() {
+            key0 = t.u * BN + half * 64;
+            head = t.h;
+            ctx = fx < x1 ? t.v.ctx : 0;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint32_t key = t.u * BN + half * 64 + i * 32 + lane;
-                id[i] = fx < x1 && key < t.v.ctx ? __ldg(p.step.block_ids + t.v.b0 + key / p.pool.block_tokens) : -1;
+                const uint32_t key = key0 + i * 32 + lane;
+                id[i] = key < ctx ? __ldg(p.step.block_ids + t.v.b0 + key / bs) : -1;
+            }
+        };
+        auto resolve = [&]() {
+            tiled = maps.valid;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t key = key0 + i * 32 + lane;
+                const bool there = (uint32_t)id[i] < p.pool.n_blocks, bad = !there && key < ctx;
+                if (bad) report(p.step, TUTTI_EFAULT);
+                missing[i] = __ballot_sync(0xffffffffu, bad);
+                tiled = tiled && __all_sync(0xffffffffu, there);
+                off[i] = there ? block_offset(p.pool, id[i]) + (int64_t)(key % bs * p.pool.tok_stride + head * p.pool.head_stride) : -1;
+                if constexpr (C8) {
+                    const uint64_t at = there ? (uint64_t)id[i] * p.pool.n_kv_heads + head : 0;
+                    ks[i] = there ? p.pool.k_scale[at] : 0.0f;
+                    vs[i] = there ? p.pool.v_scale[at] : 0.0f;
+                }
             }
         };
         if (group == 1) step_unit();
         locate();
+        resolve();
         for (uint32_t n = group; fx < x1; n += 2) {     // n: unit of the worker
-            const int32_t id0 = id[0], id1 = id[1];
-            const uint32_t key_unit = t.u * BN, head = t.h;
-            int64_t off[2];
+            // keys behind the end are masked by position, blocks outside the pool by this
+            if (lane < 2) exists[(n & 7) * 4 + half * 2 + lane] = ~(lane ? missing[1] : missing[0]);
             uint32_t fac[2][2], sec[2][2];              // 8-bit: the scales' two factors, twice 16 bits
             bool small = false;
-            bool tiled = maps.valid;
+            if constexpr (C8) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const uint32_t key = t.u * BN + half * 64 + i * 32 + lane;
-                const bool there = (uint32_t)id[i] < p.pool.n_blocks, bad = !there && key < t.v.ctx;
-                if (bad) report(p.step, TUTTI_EFAULT);
-                const uint32_t mask = __ballot_sync(0xffffffffu, !bad);       // keys behind the end are masked by position
-                if (lane == 0) exists[(n & 7) * 4 + half * 2 + i] = mask;
-                tiled = tiled && __all_sync(0xffffffffu, there);
-                off[i] = there ? block_offset(p.pool, id[i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + t.h * p.pool.head_stride) : -1;
-                if constexpr (C8) {
-                    const uint64_t at = there ? (uint64_t)id[i] * p.pool.n_kv_heads + t.h : 0;
-                    const float ks = there ? p.pool.k_scale[at] : 0.0f, vs = there ? p.pool.v_scale[at] : 0.0f;
-                    small = factors(ks, fac[0][i], sec[0][i], T()) || small;
-                    small = factors(vs, fac[1][i], sec[1][i], T()) || small;
+                for (int i = 0; i < 2; ++i) {
+                    small = factors(ks[i], fac[0][i], sec[0][i], T()) || small;
+                    small = factors(vs[i], fac[1][i], sec[1][i], T()) || small;
                 }
+                small = __any_sync(0xffffffffu, small);
             }
-            small = C8 && __any_sync(0xffffffffu, small);
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-                if (n >= 2) ok = mbar_wait(empty + 8 * (2 * group + kv), (n / 2 - 1) & 1, dead);
-                if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                const uint64_t from = kv ? p.pool.v_base : p.pool.k_base;
-                // 8-bit rows wait in the upper half of the place that they will fill
-                const uint32_t dst = kslot + kv * C::KV + (C8 && D == 128 ? ATOM : 0);
-                if (tiled) {
+            const bool by_tile = tiled;
+            const uint32_t raw_bar = raw_full + 16 * (warp - KV_WARP);
+            auto room = [&](int kv) {
+                const bool there = n < 2 || mbar_wait(empty + 8 * (2 * group + kv), (n / 2 - 1) & 1, dead);
+                return (bool)__all_sync(0xffffffffu, there);
+            };
+            auto fetch = [&](int kv) {                  // issues the loads of the warp's 64 rows
+                const uint32_t dst = base + land[kv];
+                if (by_tile) {
                     constexpr uint32_t PARTS = RB / 128 ? RB / 128 : 1;
-                    const uint32_t row = half * 64 + my_box * box_rows;
-                    const uint32_t bar = C8 ? raw_full + 8 * (warp - KV_WARP + 4 * kv) : full + 8 * (2 * group + kv);
-                    const uint32_t from_lane = my_box * box_rows % 32;
-                    const int32_t lo = __shfl_sync(0xffffffffu, id0, from_lane), hi = __shfl_sync(0xffffffffu, id1, from_lane);
-                    const int32_t block = my_box * box_rows < 32 ? lo : hi;
+                    const uint32_t row = my_box * box_rows, bar = C8 ? raw_bar + 8 * kv : full + 8 * (2 * group + kv);
+                    const int32_t lo = __shfl_sync(0xffffffffu, id[0], row % 32), hi = __shfl_sync(0xffffffffu, id[1], row % 32);
+                    __syncwarp();
                     if (lane == 0) mbar_expect(bar, 64 * RB);
                     __syncwarp();
                     if (my_part < PARTS) {
-                        const int32_t token = (int32_t)((key_unit + row) % bs), x0_ = (int32_t)(my_part * (128 / (C8 ? 1 : 2)));
-                        tile_load(dst + my_part * ATOM + row * 128, kv ? &maps.v : &maps.k, bar, x0_, p.hnd ? token : (int32_t)head,
-                                  p.hnd ? (int32_t)head : token, block);
+                        const int32_t token = (int32_t)((key0 + row) % bs);
+                        tile_load(dst + my_part * ATOM + (half * 64 + row) * 128, kv ? &maps.v : &maps.k, bar, (int32_t)(my_part * (C8 ? 128 : 64)),
+                                  p.hnd ? token : (int32_t)head, p.hnd ? (int32_t)head : token, row < 32 ? lo : hi);
                     }
-                    continue;
-                }
-#pragma unroll
-                for (int it = 0; it < 64 / RPI; ++it) {
-                    const uint32_t r = it * RPI + sub, row = half * 64 + r;
-                    const int64_t o = __shfl_sync(0xffffffffu, off[it * RPI / 32], r % 32);
-                    cp16(dst + (C8 ? row * 128 + (((ch ^ row) & (CH - 1)) << 4) : C::place(row, ch)), (const void *)(from + (o >= 0 ? o : 0) + ch * 16), o >= 0);
-                }
-                cp_commit();
-            }
-            if (!ok) break;
-            step_unit();
-            step_unit();
-            locate();                                   // the next unit's ids arrive while this one's rows do
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv) {
-                if (tiled && !C8) break;                // the tensor copies arrive at `full` by themselves
-                if (tiled) {
-                    ok = mbar_wait(raw_full + 8 * (warp - KV_WARP + 4 * kv), raw_phase[kv]++ & 1, dead);
-                    if (!(ok = __all_sync(0xffffffffu, ok))) break;
-                } else if (kv == 0) {
-                    cp_wait<1>();
                 } else {
-                    cp_wait<0>();
-                }
-                if constexpr (C8) {
-                    __syncwarp();                       // the warp's rows, brought by all its lanes
-                    unsigned char *slot = sm + C::OFF_RING + (2 * group + kv) * C::KV;
-                    constexpr int B = 4;                // steps whose codes are read before their rows are written over
-#pragma unroll 1
-                    for (int it0 = 0; it0 < 64 / RPI; it0 += B) {
-                        uint4 c[B];
+                    const uint64_t from = kv ? p.pool.v_base : p.pool.k_base;
 #pragma unroll
-                        for (int k = 0; k < B; ++k) {
-                            const uint32_t row = half * 64 + (it0 + k) * RPI + sub;
-                            c[k] = *reinterpret_cast<const uint4 *>(slot + (D == 128 ? ATOM : 0) + row * 128 + (((ch ^ row) & (CH - 1)) << 4));
-                        }
-                        __syncwarp();
-#pragma unroll
-                        for (int k = 0; k < B; ++k) {
-                            const uint32_t r = (it0 + k) * RPI + sub, row = half * 64 + r;
-                            const uint32_t f1 = __shfl_sync(0xffffffffu, r < 32 ? fac[kv][0] : fac[kv][1], r % 32);
-                            const uint32_t w[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
-                            uint32_t e[8], nan = 0;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint2 x = spread(w[i], T());
-                                e[2 * i] = times(x.x, f1, T());
-                                e[2 * i + 1] = times(x.y, f1, T());
-                                nan |= (w[i] & 0x7f7f7f7fu) + 0x01010101u;
-                            }
-                            if (small) {                // some scale of the unit needs its second factor
-                                const uint32_t f2 = __shfl_sync(0xffffffffu, r < 32 ? sec[kv][0] : sec[kv][1], r % 32);
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) e[i] = times(e[i], f2, T());
-                            }
-                            if (nan & 0x80808080u) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const uint32_t z = (w[i] & 0x7f7f7f7fu) + 0x01010101u;
-                                    if (z & 0x80u) e[2 * i] |= 0x7fffu;
-                                    if (z & 0x800000u) e[2 * i] |= 0x7fff0000u;
-                                    if (z & 0x8000u) e[2 * i + 1] |= 0x7fffu;
-                                    if (z & 0x80000000u) e[2 * i + 1] |= 0x7fff0000u;
-                                }
-                            }
-                            *reinterpret_cast<uint4 *>(slot + C::place(row, 2 * ch)) = make_uint4(e[0], e[1], e[2], e[3]);
-                            *reinterpret_cast<uint4 *>(slot + C::place(row, 2 * ch + 1)) = make_uint4(e[4], e[5], e[6], e[7]);
-                        }
+                    for (int it = 0; it < 64 / RPI; ++it) {
+                        const uint32_t r = it * RPI + sub, row = half * 64 + r;
+                        const int64_t o = __shfl_sync(0xffffffffu, off[it * RPI / 32], r % 32);
+                        cp16(dst + (C8 ? row * 128 + (((ch ^ row) & (CH - 1)) << 4) : C::place(row, ch)), (const void *)(from + (o >= 0 ? o : 0) + ch * 16), o >= 0);
                     }
+                    cp_commit();
                 }
+            };
+            auto arrive = [&](int kv) {                 // the warp's rows are in their places
                 fence_async();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(full + 8 * (2 * group + kv));
+            };
+            // 8-bit: four steps' codes are read before the rows they may lie in are written
+            auto widen = [&](int kv, auto two_factors) {
+                constexpr int B = 4;
+                const unsigned char *src = sm + land[kv];
+                unsigned char *dst = sm + slot0 + kv * C::KV;
+#pragma unroll 1
+                for (int it0 = 0; it0 < 64 / RPI; it0 += B) {
+                    uint4 c[B];
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int k = 0; k < B; ++k) {
+                        const uint32_t row = half * 64 + (it0 + k) * RPI + sub;
+                        c[k] = *reinterpret_cast<const uint4 *>(src + row * 128 + (((ch ^ row) & (CH - 1)) << 4));
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int k = 0; k < B; ++k) {
+                        const uint32_t r = (it0 + k) * RPI + sub, row = half * 64 + r;
+                        const uint32_t f1 = __shfl_sync(0xffffffffu, r < 32 ? fac[kv][0] : fac[kv][1], r % 32);
+                        const uint32_t w[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
+                        uint32_t e[8];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const uint2 x = spread(w[i], T(), top);
+                            e[2 * i] = times(x.x, f1, T());
+                            e[2 * i + 1] = times(x.y, f1, T());
+                        }
+                        if constexpr (two_factors.value) {
+                            const uint32_t f2 = __shfl_sync(0xffffffffu, r < 32 ? sec[kv][0] : sec[kv][1], r % 32);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) e[i] = times(e[i], f2, T());
+                        }
+                        *reinterpret_cast<uint4 *>(dst + C::place(row, 2 * ch)) = make_uint4(e[0], e[1], e[2], e[3]);
+                        *reinterpret_cast<uint4 *>(dst + C::place(row, 2 * ch + 1)) = make_uint4(e[4], e[5], e[6], e[7]);
+                    }
+                    if (C::ORDERED ? false : __vmaxu2(top, 0x07e007e0u) != 0x07e007e0u) {       // NaN codes: they are made NaN again
+#pragma unroll
+                        for (int k = 0; k < B; ++k) {
+                            const uint32_t row = half * 64 + (it0 + k) * RPI + sub;
+                            const uint32_t w[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                // code i of the 16 is element {0, 2, 1, 3}[i % 4] of its four
+                                const int e = (i & ~3) | (i & 1) << 1 | (i >> 1 & 1);
+                                if ((w[i / 4] >> (8 * (i & 3)) & 0x7f) == 0x7f)
+                                    *reinterpret_cast<uint16_t *>(dst + C::place(row, 2 * ch + e / 8) + (e % 8) * 2) = 0x7fff;
+                            }
+                        }
+                    }
+                }
+            };
+            if constexpr (!C8) {
+                if (!(ok = room(0))) break;
+                fetch(0);
+                if (!(ok = room(1))) break;
+                fetch(1);
+                step_unit();
+                step_unit();
+                locate();                               // the next unit's ids arrive while this one's rows do
+                if (!by_tile) {                         // tensor copies arrive at `full` by themselves
+                    cp_wait<1>();
+                    arrive(0);
+                    cp_wait<0>();
+                    arrive(1);
+                }
+                resolve();
+            } else {
+                fetch(1);
+                if (!(ok = room(0))) break;
+                fetch(0);
+                step_unit();
+                step_unit();
+                locate();
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    if (kv == 1) {
+                        resolve();                      // the next unit's scales arrive while this one's values are widened
+                        if (!(ok = room(1))) break;
+                    }
+                    if (by_tile) {
+                        ok = mbar_wait(raw_bar + 8 * kv, raw_phase & 1, dead);
+                        if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                    } else {
+                        cp_wait<0>();
+                        __syncwarp();                   // the warp's rows, brought by all its lanes
+                    }
+                    if (small) widen(kv, std::true_type());
+                    else widen(kv, std::false_type());
+                    arrive(kv);
+                }
+                if (!ok) break;
+                if (by_tile) ++raw_phase;
             }
-            if (!ok) break;
         }
         cp_wait<0>();
         } else if (warp >= Q_WARP) {
@@ -589,16 +649,19 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 const uint32_t k = in ? row / p.group : 0, h = t.h * p.group + (in ? row % p.group : 0);
                 const T *src = (const T *)p.q + (uint64_t)(t.v.q0 + k) * p.q_stride + (uint64_t)h * D + ch * 8;
                 const uint32_t dst = r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch);
-                if constexpr (!C8) {
-                    cp16(base + dst, src, in);
-                } else {
-                    const uint4 u = in ? *reinterpret_cast<const uint4 *>(src) : make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4 *>(sm + dst) = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.x, u.y, 0x7632),
-                                                                      __byte_perm(u.z, u.w, 0x5410), __byte_perm(u.z, u.w, 0x7632));
-                }
+                cp16(base + dst, src, in);
             }
             cp_commit();
             cp_wait<0>();
+            if constexpr (!C::ORDERED) {                    // each lane what it brought itself
+                for (uint32_t i = warp - Q_WARP; i < TILE_ROWS * CH / 32; i += Q_WARPS) {
+                    const uint32_t r = (i * 32 + lane) / CH, ch = lane % CH;
+                    uint4 *at = reinterpret_cast<uint4 *>(sm + r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch));
+                    const uint4 u = *at;
+                    *at = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.x, u.y, 0x7632),
+                                     __byte_perm(u.z, u.w, 0x5410), __byte_perm(u.z, u.w, 0x7632));
+                }
+            }
             fence_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full);
@@ -859,7 +922,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     uint4 *out = reinterpret_cast<uint4 *>((T *)p.out + token * p.out_stride + (uint64_t)qh * D);
 #pragma unroll
                     for (int d = 0; d < D / 8; ++d) {
-                        constexpr int B = C8 ? 2 : 1, E = C8 ? 1 : 2;      // where elements 1 and 2 of four are
+                        constexpr int B = C::ORDERED ? 1 : 2, E = C::ORDERED ? 2 : 1;      // where elements 1 and 2 of four are
                         const float *e = o + 8 * d;
                         out[d] = make_uint4(pack2(e[0] * inv, e[B] * inv, T()), pack2(e[E] * inv, e[3] * inv, T()),
                                             pack2(e[4] * inv, e[4 + B] * inv, T()), pack2(e[4 + E] * inv, e[7] * inv, T()));
