@@ -41,7 +41,7 @@ constexpr int RING = 4;                 // K and V tiles in flight
 constexpr int THREADS = 512;
 constexpr int MMA_WARP = 8, Q_WARP = 9, Q_WARPS = 3, KV_WARP = 12, KV_WARPS = 2;      // KV_WARPS: of a group
 constexpr uint32_t ATOM = BN * 128;     // 128 rows of 128 bytes
-constexpr int POLY_PAIRS = 5;           // of the 16 pairs in 32 scores: exponentials on the multiply-add units
+constexpr int EARLY = 3;                // of the 4 groups of 32 keys: probabilities handed over before the rest is done
 constexpr float GROW = 8.0f;            // log2 of how far probabilities may exceed 1
 constexpr long long WAIT_CLOCKS = 3000000000ll;   // about 1.5 s: a wait that takes longer is given up
 
@@ -233,27 +233,6 @@ __device__ inline float max3(float a, float b, float c) {
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// 2^x of a pair on the multiply-add units, x <= 127: x = n + f with |f| <= 1/2, 2^f by its minimax
-// polynomial of degree 4 (fitted to a relative error of 2.6e-6, well under the 16 bits that
-// probabilities are rounded to), n added to the exponent.  Below -125 the result stays 2^-125.
-__device__ inline void ex2_poly(f2 x, float &a, float &b) {
-    const f2 magic = pair(12582912.0f, 12582912.0f);            // 1.5 * 2^23: rounds to an integer
-    unpair(x, a, b);
-    x = pair(fmaxf(a, -125.0f), fmaxf(b, -125.0f));
-    const f2 t = add2(x, magic);
-    const f2 f = fma2(add2(t, pair(-12582912.0f, -12582912.0f)), pair(-1.0f, -1.0f), x);
-    f2 y = pair(0.009567738510668278f, 0.009567738510668278f);
-    y = fma2(y, f, pair(0.05591749772429466f, 0.05591749772429466f));
-    y = fma2(y, f, pair(0.24024811387062073f, 0.24024811387062073f));
-    y = fma2(y, f, pair(0.6931219100952148f, 0.6931219100952148f));
-    y = fma2(y, f, pair(0.9999992251396179f, 0.9999992251396179f));
-    float ta, tb, ya, yb;
-    unpair(t, ta, tb);
-    unpair(y, ya, yb);
-    a = __uint_as_float(__float_as_uint(ta) * 0x800000u + __float_as_uint(ya));
-    b = __uint_as_float(__float_as_uint(tb) * 0x800000u + __float_as_uint(yb));
-}
-
 // Shared-memory operand in the 128-byte swizzle: start, offset between 64-element groups of an
 // MN-major operand (not used by a K-major one), 1024 bytes from one group of 8 rows to the next.
 __device__ inline uint64_t operand(uint32_t addr) {
@@ -335,7 +314,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     volatile uint32_t *dead = misc + 60;
     const uint32_t bars = base + C::OFF_BAR;
     const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, s_full = bars + 80,
-                   p_full = bars + 96, o_full = bars + 112, o_empty = bars + 128, joined = bars + 144, drain = bars + 160, raw_full = bars + 168;
+                   p_full = bars + 96, o_full = bars + 112, o_empty = bars + 128, joined = bars + 144, drain = bars + 160, raw_full = bars + 168, p_late = bars + 232;
 
     // ---- this worker's share ----
     unsigned long long *sums = reinterpret_cast<unsigned long long *>(misc);
@@ -394,6 +373,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             mbar_init(o_full + 8 * i, 1);
             mbar_init(o_empty + 8 * i, 4);
             mbar_init(joined + 8 * i, 4);
+            mbar_init(p_late + 8 * i, 4);
         }
         mbar_init(drain, 1);
         for (int i = 0; i < 2 * RING; ++i) mbar_init(raw_full + 8 * i, 1);
@@ -690,12 +670,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 }
                 __syncwarp();
             };
-            auto pv = [&](int i, uint32_t slot, bool acc) {
+            // part 0: the keys whose probabilities come first; part 1: the others
+            auto pv = [&](int i, uint32_t slot, bool acc, int part) {
                 const uint64_t b = operand(base + C::OFF_RING + slot * C::KV);
                 if (elect()) {
 #pragma unroll
-                    for (int k = 0; k < BN / 16; ++k) mma_ts(O(i), S(i) + k * 8, b + ((k * 2048) >> 4), ID_PV, acc || k > 0);
-                    tc_commit(o_full + 8 * i);
+                    for (int k = 0; k < BN / 16; ++k)
+                        if ((k >= 2 * EARLY) == part) mma_ts(O(i), S(i) + k * 8, b + ((k * 2048) >> 4), ID_PV, acc || k > 0);
+                    if (part) tc_commit(o_full + 8 * i);
                 }
                 __syncwarp();
             };
@@ -723,7 +705,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         if (ok && j == 0 && ns[i]) ok = mbar_wait(o_empty + 8 * i, (ns[i] - 1) & 1, dead);
                         if (!(ok = all(ok))) break;
                         tc_after();
-                        pv(i, slot(n_unit, 1), j > 0);
+                        pv(i, slot(n_unit, 1), j > 0, 0);
+                        if (!(ok = all(mbar_wait(p_late + 8 * i, (np[i] - 1) & 1, dead)))) break;
+                        tc_after();
+                        pv(i, slot(n_unit, 1), true, 1);
                         if (more) qk(i, slot(n_unit + 1, 0));
                     }
                     if (!ok) break;
@@ -795,6 +780,28 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         for (int k = 0; k < 128; ++k)
                             if (k > lim || !(word[k / 32] >> (k % 32) & 1)) s[k] = -INFINITY;
                     }
+                    // Exponentials of groups [from, to) of 32 scores against the reference m; 16 bits of
+                    // each go back to TMEM, their 32-bit sums to l0 and l1.
+                    f2 l0, l1;
+                    auto exps = [&](int from, int to) {
+                        const float sub = C::OFF - (m == -INFINITY ? 0.0f : m);
+                        const f2 scl2 = pair(scl, scl), sub2 = pair(sub, sub);
+#pragma unroll
+                        for (int q = from; q < to; ++q) {
+                            uint32_t pk[16];
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) {
+                                float a, b;
+                                unpair(fma2(pair(s[32 * q + 2 * k], s[32 * q + 2 * k + 1]), scl2, sub2), a, b);
+                                a = ex2(a);
+                                b = ex2(b);
+                                if (k & 1) l1 = add2(l1, pair(a, b));
+                                else l0 = add2(l0, pair(a, b));
+                                pk[k] = pack2(a, b, T());
+                            }
+                            tc_st16(pk, s_at + 16 * q);
+                        }
+                    };
                     float a0 = max3(s[0], s[4], s[8]), a1 = max3(s[1], s[5], s[9]), a2 = max3(s[2], s[6], s[10]), a3 = max3(s[3], s[7], s[11]);
 #pragma unroll
                     for (int k = 12; k < 124; k += 8) {
@@ -807,7 +814,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     a1 = max3(a1, s[126], s[127]);
                     const float top = max3(a0, a1, fmaxf(a2, a3)) * scl;
                     const bool grow = top > m + GROW || (m == -INFINITY && top > m);
-                    if (__any_sync(0xffffffffu, grow)) {
+                    if (__any_sync(0xffffffffu, grow)) {          // rare: the reference has to move
                         const float alpha = grow ? ex2(m - top) : 1.0f;
                         if (grow) m = top;
                         l *= alpha;
@@ -828,36 +835,20 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                             }
                         }
                     }
-                    const float sub = (m == -INFINITY ? 0.0f : m) - C::OFF;
-                    const f2 scl2 = pair(scl, scl), sub2 = pair(-sub, -sub);
-                    f2 l0 = 0, l1 = 0;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t pk[16];
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const f2 x = fma2(pair(s[32 * q + 2 * k], s[32 * q + 2 * k + 1]), scl2, sub2);
-                            float a, b;
-                            if (k * POLY_PAIRS / 16 != (k + 1) * POLY_PAIRS / 16) {       // spread over the 16
-                                ex2_poly(x, a, b);
-                            } else {
-                                unpair(x, a, b);
-                                a = ex2(a);
-                                b = ex2(b);
-                            }
-                            if (k & 1) l1 = add2(l1, pair(a, b));
-                            else l0 = add2(l0, pair(a, b));
-                            pk[k] = pack2(a, b, T());
-                        }
-                        tc_st16(pk, s_at + 16 * q);
-                    }
+                    l0 = l1 = 0;
+                    exps(0, EARLY);
+                    tc_wait_st();
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(p_full + 8 * i);
+                    exps(EARLY, 4);
                     float la, lb;
                     unpair(add2(l0, l1), la, lb);
                     l += la + lb;
                     tc_wait_st();
                     tc_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(p_full + 8 * i);
+                    if (lane == 0) mbar_arrive(p_late + 8 * i);
                     ++n_s;
                 }
                 if (!ok) break;
