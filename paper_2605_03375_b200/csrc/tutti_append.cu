@@ -22,6 +22,12 @@ namespace tutti {
 namespace {
 
 constexpr int THREADS = 256;
+// Once a step has more rows than this, which fill the GPU's warps, a warp takes all rows of its
+// token (up to PASSES x (32 / jobs) of them): finding the sequence and the block costs it as much as
+// moving a few rows (16384 tokens of 48 rows: 169 us at 2 passes a warp, 108 at 4, 97 at 8, 76 at
+// 12, all of them).  Below, one pass, for latency.
+constexpr uint64_t ROWS_ENOUGH = 32768;
+constexpr uint32_t PASSES = 16;
 constexpr int SCALE_MIN_EXP = -100;     // never zero: dividing by a scale is exact and finite
 
 struct RopeDev {
@@ -155,36 +161,47 @@ __device__ void row_warp(const AppendParams &p, uint32_t w) {
     const uint32_t hk = p.pool.n_kv_heads, hd = p.pool.head_dim;
     const uint32_t n_rows = p.n_q_heads + (KV ? 2 * hk : 0);
     const uint32_t first = unit * p.row_passes * per + lane / p.jobs;
-#pragma unroll 4
-    for (uint32_t i = 0; i < p.row_passes; ++i) {
-        const uint32_t r = first + i * per;
-        if (r >= n_rows) break;
-        const char *src;
-        char *dst;
-        bool turn = b.turn;
-        if (r < p.n_q_heads) {
-            src = p.q + tok * p.q_stride + (uint64_t)r * hd * 2;
-            dst = p.q_out + tok * p.q_out_stride + (uint64_t)r * hd * 2;
-        } else {
-            if (at < 0) break;
-            const bool is_v = r >= p.n_q_heads + hk;
-            const uint32_t h = r - p.n_q_heads - (is_v ? hk : 0);
-            src = (is_v ? p.v + tok * p.v_stride : p.k + tok * p.k_stride) + (uint64_t)h * hd * 2;
-            dst = (char *)((is_v ? p.pool.v_base : p.pool.k_base) + at + h * p.pool.head_stride);
-            turn = turn && !is_v;
+    // Four rows' loads are issued before the first store: a store might alias a later load as far as
+    // the compiler knows, and one row in flight at a time leaves the memory idle.
+    for (uint32_t i0 = 0; i0 < p.row_passes; i0 += 4) {
+        uint4 u[4][2];
+        char *dst[4];
+        bool turn[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t r = first + (i0 + i) * per;
+            dst[i] = nullptr;
+            if (i0 + i >= p.row_passes || r >= n_rows) continue;
+            const char *src;
+            turn[i] = b.turn;
+            if (r < p.n_q_heads) {
+                src = p.q + tok * p.q_stride + (uint64_t)r * hd * 2;
+                dst[i] = p.q_out + tok * p.q_out_stride + (uint64_t)r * hd * 2;
+            } else {
+                if (at < 0) continue;
+                const bool is_v = r >= p.n_q_heads + hk;
+                const uint32_t h = r - p.n_q_heads - (is_v ? hk : 0);
+                src = (is_v ? p.v + tok * p.v_stride : p.k + tok * p.k_stride) + (uint64_t)h * hd * 2;
+                dst[i] = (char *)((is_v ? p.pool.v_base : p.pool.k_base) + at + h * p.pool.head_stride);
+                turn[i] = b.turn && !is_v;
+            }
+            u[i][0] = *reinterpret_cast<const uint4 *>(src + b.d0 * 2);
+            u[i][1] = *reinterpret_cast<const uint4 *>(src + b.d1 * 2);
         }
-        uint4 u0 = *reinterpret_cast<const uint4 *>(src + b.d0 * 2);
-        uint4 u1 = *reinterpret_cast<const uint4 *>(src + b.d1 * 2);
-        if (turn) {
-            float x[16];
-            unpack<T>(u0, x);
-            unpack<T>(u1, x + 8);
-            rotate(p.rope, t, x);
-            u0 = pack<T>(x);
-            u1 = pack<T>(x + 8);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!dst[i]) continue;
+            if (turn[i]) {
+                float x[16];
+                unpack<T>(u[i][0], x);
+                unpack<T>(u[i][1], x + 8);
+                rotate(p.rope, t, x);
+                u[i][0] = pack<T>(x);
+                u[i][1] = pack<T>(x + 8);
+            }
+            *reinterpret_cast<uint4 *>(dst[i] + b.d0 * 2) = u[i][0];
+            *reinterpret_cast<uint4 *>(dst[i] + b.d1 * 2) = u[i][1];
         }
-        *reinterpret_cast<uint4 *>(dst + b.d0 * 2) = u0;
-        *reinterpret_cast<uint4 *>(dst + b.d1 * 2) = u1;
     }
 }
 
@@ -212,8 +229,7 @@ __device__ inline uint2 codes_of(const float *x, float inv) {
 }
 
 // One touched block of one head, keys or values: the largest new value, the scale, the codes.
-// The block's rows belong to this warp alone.  Two passes over the new tokens (the second out of
-// L1/L2): a block of any number of tokens needs no more registers than a block of one.
+// The block's rows belong to this warp alone.
 template <typename T>
 __device__ void block_warp(const AppendParams &p, uint32_t w) {
     const uint32_t lane = threadIdx.x & 31, hk = p.pool.n_kv_heads, bs = p.pool.block_tokens;
@@ -248,56 +264,118 @@ __device__ void block_warp(const AppendParams &p, uint32_t w) {
     const Job b = job_of(p.rope, j);
     const bool turn = b.turn && !is_v;
 
-    auto load = [&](uint32_t pos, float *x) {
-        const char *src = in + (uint64_t)(row0 + (pos - first)) * in_stride;
-        unpack<T>(*reinterpret_cast<const uint4 *>(src + b.d0 * 2), x);
-        unpack<T>(*reinterpret_cast<const uint4 *>(src + b.d1 * 2), x + 8);
+    // Up to HELD passes stay in registers between finding the largest value and writing the codes;
+    // larger parts of a block are read twice (the second time out of L1/L2).
+    constexpr uint32_t HELD = 4;
+    const bool held_all = hi - lo <= HELD * per;
+    uint4 raw[HELD][2];
+    auto expand = [&](const uint4 (&v)[2], uint32_t pos, float *x) {
+        unpack<T>(v[0], x);
+        unpack<T>(v[1], x + 8);
         if (turn) {
             Turn t;
             load_turn(p.rope, pos, b.t0, t);
             rotate(p.rope, t, x);
         }
     };
+    auto load = [&](uint32_t pos, float *x) {
+        const char *src = in + (uint64_t)(row0 + (pos - first)) * in_stride;
+        const uint4 v[2] = {*reinterpret_cast<const uint4 *>(src + b.d0 * 2), *reinterpret_cast<const uint4 *>(src + b.d1 * 2)};
+        expand(v, pos, x);
+    };
+    // The block's earlier codes are fetched along: whether they have to be rounded again is known late.
+    const uint32_t held = lo - blk * bs;
+    const float old = held ? *scale : 0.0f;
+    uint2 was[HELD][2];
+    auto earlier = [&](uint32_t r, uint32_t c) { return reinterpret_cast<uint2 *>(rows + r * p.pool.tok_stride + (c ? b.d1 : b.d0)); };
+#pragma unroll
+    for (uint32_t i = 0; i < HELD; ++i) {
+        const uint32_t r = sub + i * per;
+        if (sub < per && r < held) {
+            was[i][0] = *earlier(r, 0);
+            was[i][1] = *earlier(r, 1);
+        }
+    }
     float amax = 0.0f;
-    if (sub < per)
+    if (held_all) {
+#pragma unroll
+        for (uint32_t i = 0; i < HELD; ++i) {
+            const uint32_t pos = lo + sub + i * per;
+            if (sub < per && pos < hi) {
+                const char *src = in + (uint64_t)(row0 + (pos - first)) * in_stride;
+                raw[i][0] = *reinterpret_cast<const uint4 *>(src + b.d0 * 2);
+                raw[i][1] = *reinterpret_cast<const uint4 *>(src + b.d1 * 2);
+            }
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < HELD; ++i) {
+            const uint32_t pos = lo + sub + i * per;
+            if (sub < per && pos < hi) {
+                float x[16];
+                expand(raw[i], pos, x);
+#pragma unroll
+                for (int k = 0; k < 16; ++k) amax = fmaxf(amax, finite_abs(x[k]));
+            }
+        }
+    } else if (sub < per) {
         for (uint32_t pos = lo + sub; pos < hi; pos += per) {
             float x[16];
             load(pos, x);
 #pragma unroll
             for (int i = 0; i < 16; ++i) amax = fmaxf(amax, finite_abs(x[i]));
         }
+    }
 #pragma unroll
     for (int o = 16; o; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
     float sc = pow2_scale(amax);
-    const uint32_t held = lo - blk * bs;
     if (held) {
-        const float old = *scale;
         sc = fmaxf(sc, old);
         if (sc != old && sub < per) {
             const float ratio = old / sc;
-            for (uint32_t r = sub; r < held; r += per) {
+            auto again = [&](const uint2 &codes) {
+                const __nv_fp8_e4m3 *e = reinterpret_cast<const __nv_fp8_e4m3 *>(&codes);
+                float x[8];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint2 *q = reinterpret_cast<uint2 *>(rows + r * p.pool.tok_stride + (c ? b.d1 : b.d0));
-                    const uint2 was = *q;
-                    const __nv_fp8_e4m3 *e = reinterpret_cast<const __nv_fp8_e4m3 *>(&was);
-                    float x[8];
+                for (int i = 0; i < 8; ++i) x[i] = (float)e[i];
+                return codes_of(x, ratio);
+            };
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = (float)e[i];
-                    *q = codes_of(x, ratio);
+            for (uint32_t i = 0; i < HELD; ++i) {
+                const uint32_t r = sub + i * per;
+                if (r < held) {
+                    *earlier(r, 0) = again(was[i][0]);
+                    *earlier(r, 1) = again(was[i][1]);
                 }
+            }
+            for (uint32_t r = sub + HELD * per; r < held; r += per) {
+                *earlier(r, 0) = again(*earlier(r, 0));
+                *earlier(r, 1) = again(*earlier(r, 1));
             }
         }
     }
     const float inv = 1.0f / sc;          // exact: a power of two
-    if (sub < per)
+    auto write = [&](uint32_t pos, const float *x) {
+        char *dst = rows + (pos - blk * bs) * p.pool.tok_stride;
+        *reinterpret_cast<uint2 *>(dst + b.d0) = codes_of(x, inv);
+        *reinterpret_cast<uint2 *>(dst + b.d1) = codes_of(x + 8, inv);
+    };
+    if (held_all) {
+#pragma unroll
+        for (uint32_t i = 0; i < HELD; ++i) {
+            const uint32_t pos = lo + sub + i * per;
+            if (sub < per && pos < hi) {
+                float x[16];
+                expand(raw[i], pos, x);
+                write(pos, x);
+            }
+        }
+    } else if (sub < per) {
         for (uint32_t pos = lo + sub; pos < hi; pos += per) {
             float x[16];
             load(pos, x);
-            char *dst = rows + (pos - blk * bs) * p.pool.tok_stride;
-            *reinterpret_cast<uint2 *>(dst + b.d0) = codes_of(x, inv);
-            *reinterpret_cast<uint2 *>(dst + b.d1) = codes_of(x + 8, inv);
+            write(pos, x);
         }
+    }
     __syncwarp();                         // every lane has read the old scale
     if (lane == 0) *scale = sc;
 }
@@ -404,8 +482,9 @@ int tutti_kv_append_layer(tutti_ctx_t *ctx, uint32_t layer, const tutti_step_t *
     p.jobs = p.pool.head_dim / 16;
     const uint32_t per = 32 / p.jobs;
     const uint32_t rows = t->n_q_heads + (elem_bytes == 2 ? 2 * p.pool.n_kv_heads : 0);
-    p.row_passes = 1;
-    p.row_units = (rows + per * p.row_passes - 1) / (per * p.row_passes);
+    const uint32_t passes = (rows + per - 1) / per;
+    p.row_units = (uint64_t)step->n_tok * rows > ROWS_ENOUGH ? (passes + PASSES - 1) / PASSES : passes;
+    p.row_passes = p.row_units ? (passes + p.row_units - 1) / p.row_units : 0;
     uint64_t warps = (uint64_t)step->n_tok * p.row_units;
     p.blk_units = 0;
     uint64_t blk_warps = 0;

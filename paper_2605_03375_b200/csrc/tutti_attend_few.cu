@@ -28,6 +28,7 @@ constexpr int WARPS = 4;
 constexpr int STAGES = 3;
 constexpr uint32_t STAGE_BYTES = 8192;      // keys and values of one warp's KW keys
 constexpr int WORKERS_PER_SM = 2;
+constexpr int MIN_UNITS = 2;                // of a worker: a worker more costs joining its part
 
 __device__ inline void ldm4(uint32_t (&r)[4], uint32_t a) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -124,11 +125,13 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     // ---- this worker's share: a prefix sum over the sequences' units ----
     const uint32_t per = (p.step.n_seq + WARPS * 32 - 1) / (WARPS * 32);
     unsigned long long mine = 0;
+    Cursor own;                                    // the thread's last sequence (its only one, mostly)
+    own.s = ~0u;
     for (uint32_t s = threadIdx.x * per; s < min((threadIdx.x + 1) * per, p.step.n_seq); ++s) {
-        Cursor k;
-        const int code = seq_shape(p, F::UNIT, s, k);
+        const int code = seq_shape(p, F::UNIT, s, own);
+        own.s = s;
         if (code != TUTTI_OK && blockIdx.x == 0) report(p.step, code);
-        mine += (unsigned long long)k.n_tiles * k.n_units;
+        mine += (unsigned long long)own.n_tiles * own.n_units;
     }
     unsigned long long incl = mine;
 #pragma unroll
@@ -145,7 +148,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         if (i < (int)warp) before += sums[i];
         total += sums[i];
     }
-    const unsigned long long workers = total < ws.workers ? total : ws.workers;
+    const unsigned long long wanted = (total + MIN_UNITS - 1) / MIN_UNITS, workers = wanted < ws.workers ? wanted : ws.workers;
     const uint32_t w = blockIdx.x;
     if (w >= workers) return;
     const unsigned long long x0 = w * total / workers, x1 = (w + 1) * total / workers;
@@ -154,60 +157,62 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     if (x0 >= before && x0 < before + mine) {      // one thread's sequences hold the first unit
         unsigned long long at = before;
         for (uint32_t s = threadIdx.x * per;; ++s) {
-            Cursor k;
-            seq_shape(p, F::UNIT, s, k);
-            const unsigned long long n = (unsigned long long)k.n_tiles * k.n_units;
+            if (s != own.s) seq_shape(p, F::UNIT, s, own);
+            const unsigned long long n = (unsigned long long)own.n_tiles * own.n_units;
             if (x0 < at + n) {
-                plan[0] = s;
-                plan[1] = (uint32_t)((x0 - at) / k.n_units);
-                plan[2] = (uint32_t)((x0 - at) % k.n_units);
+                own.s = s;
+                own.c = (uint32_t)((x0 - at) / own.n_units);
+                own.u = (uint32_t)((x0 - at) % own.n_units);
+                *reinterpret_cast<Cursor *>(plan) = own;
                 break;
             }
             at += n;
+            own.s = ~0u;
         }
     }
     __syncthreads();
-    Cursor get;
-    get.s = plan[0];
-    get.c = plan[1];
-    get.u = plan[2];
-    seq_shape(p, F::UNIT, get.s, get);
+    Cursor get = *reinterpret_cast<const Cursor *>(plan);
     Cursor put = get;                              // runs ahead: the unit whose loads are issued next
     unsigned long long put_x = x0;
 
     // ---- gathering ----
-    int64_t off[F::KPL];                           // of the lane's keys in the unit at `put`; -1: not there
-    auto locate = [&]() {
+    // The ids of a unit's blocks are looked up two units before its rows are fetched, and not touched
+    // until then (the first use waits for the load).
+    int32_t ids[2][F::KPL];                        // of the lane's keys, of the unit at `put` and the one behind it
+    Cursor look = get;
+    unsigned long long look_x = x0;
+    auto locate = [&](int32_t (&id)[F::KPL]) {
 #pragma unroll
         for (int i = 0; i < F::KPL; ++i) {
-            const uint32_t key = (put.u * WARPS + warp) * F::KW + i * 32 + lane;
-            off[i] = -1;
-            if (put_x < x1 && i * 32 + lane < F::KW && key < put.v.ctx) {
-                const int32_t id = __ldg(p.step.block_ids + put.v.b0 + key / p.pool.block_tokens);
-                // offset and, for the scales, the id; the row inside the block is added when it is used
-                off[i] = (uint32_t)id < p.pool.n_blocks ? (int64_t)id : -2;
-            }
+            const uint32_t key = (look.u * WARPS + warp) * F::KW + i * 32 + lane;
+            id[i] = -1;
+            if (look_x < x1 && i * 32 + lane < F::KW && key < look.v.ctx)
+                id[i] = __ldg(p.step.block_ids + look.v.b0 + key / p.pool.block_tokens);
         }
+        ++look_x;
+        if (look_x < x1) advance(p, F::UNIT, look);
     };
-    locate();
+    locate(ids[0]);
+    locate(ids[1]);
     auto fetch = [&](uint32_t stage) {             // issues the loads of the unit at `put`, then looks up the next ids
         if (put_x < x1) {
             unsigned char *st = ring + stage * F::STAGE;
             const uint32_t kst = smem_addr(st), vst = kst + F::KW * F::RB;
             const uint32_t h = put.c / (put.n_tiles / p.pool.n_kv_heads);
             uint64_t mask = 0;
+            int64_t off[F::KPL];
 #pragma unroll
             for (int i = 0; i < F::KPL; ++i) {
                 const uint32_t key = (put.u * WARPS + warp) * F::KW + i * 32 + lane;
-                if (off[i] == -2) report(p.step, TUTTI_EFAULT);
-                const bool ok = off[i] >= 0;
+                const bool held = i * 32 + lane < F::KW && key < put.v.ctx, ok = held && (uint32_t)ids[0][i] < p.pool.n_blocks;
+                if (held && !ok) report(p.step, TUTTI_EFAULT);
                 mask |= (uint64_t)__ballot_sync(0xffffffffu, ok) << (32 * i);
                 if (C8 && i * 32 + lane < F::KW) {
-                    const uint64_t at = ok ? (uint64_t)off[i] * p.pool.n_kv_heads + h : 0;
+                    const uint64_t at = ok ? (uint64_t)ids[0][i] * p.pool.n_kv_heads + h : 0;
                     cp4(kst + STAGE_BYTES + (i * 32 + lane) * 4, p.pool.k_scale + at, ok);
                     cp4(kst + STAGE_BYTES + (F::KW + i * 32 + lane) * 4, p.pool.v_scale + at, ok);
                 }
-                if (ok) off[i] = block_offset(p.pool, (int32_t)off[i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + h * p.pool.head_stride);
+                off[i] = ok ? block_offset(p.pool, ids[0][i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + h * p.pool.head_stride) : -1;
             }
             if (lane == 0) exists[stage] = mask;
 #pragma unroll
@@ -221,7 +226,9 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             }
             ++put_x;
             if (put_x < x1) advance(p, F::UNIT, put);
-            locate();
+#pragma unroll
+            for (int i = 0; i < F::KPL; ++i) ids[0][i] = ids[1][i];
+            locate(ids[1]);
         }
         cp_commit();
     };

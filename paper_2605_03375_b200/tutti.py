@@ -307,20 +307,24 @@ def make_step(q_start, ctx_len, blk_start, block_ids, n_tok: int, max_new: int, 
     return s
 
 
-def _dtype_code(t) -> int:
-    name = str(t.dtype)
-    if name == "torch.bfloat16":
-        return DTYPE_BF16
-    if name == "torch.float16":
-        return DTYPE_FP16
-    raise TuttiError(EINVAL, f"tensor of type {name}")
+_DTYPE_CODES = {}                           # torch dtype -> TUTTI_DTYPE_*
 
 
-def _rows(t, like) -> int:
+def _dtype_code(dtype) -> int:
+    code = _DTYPE_CODES.get(dtype)
+    if code is None:
+        code = {"torch.bfloat16": DTYPE_BF16, "torch.float16": DTYPE_FP16}.get(str(dtype))
+        if code is None:
+            raise TuttiError(EINVAL, f"tensor of type {dtype}")
+        _DTYPE_CODES[dtype] = code
+    return code
+
+
+def _rows(t, dtype) -> int:
     """Token stride of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
-    heads, dim = t.shape[1], t.shape[2]
+    _, heads, dim = t.shape
     by_token, by_head, by_dim = t.stride()
-    if t.dtype != like.dtype or by_dim != 1 or (by_head != dim and heads > 1):
+    if t.dtype is not dtype or by_dim != 1 or (by_head != dim and heads > 1):
         raise TuttiError(EINVAL, "token tensor (type or strides)")
     return by_token
 
@@ -328,25 +332,40 @@ def _rows(t, like) -> int:
 def make_tokens(k, v, q=None, q_out=None) -> Tokens:
     """Token struct over [tokens, heads, head_dim] device tensors (bf16 or fp16; views of a packed
     projection are fine).  The struct does not keep the tensors alive."""
-    t = Tokens(_dtype_code(k), 0, 0, _rows(k, k), _rows(v, k), 0, None, k.data_ptr(), v.data_ptr(), None)
-    if q is not None:
-        t.n_q_heads, t.q_stride, t.q_out_stride = q.shape[1], _rows(q, k), _rows(q_out, k)
-        t.q, t.q_out = q.data_ptr(), q_out.data_ptr()
-    return t
+    dtype = k.dtype
+    code = _dtype_code(dtype)
+    if q is None:
+        return Tokens(code, 0, 0, _rows(k, dtype), _rows(v, dtype), 0, None, k.data_ptr(), v.data_ptr(), None)
+    return Tokens(code, q.shape[1], _rows(q, dtype), _rows(k, dtype), _rows(v, dtype), _rows(q_out, dtype),
+                  q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr())
+
+
+_FLOAT32 = []                               # torch.float32, once seen (torch itself is not imported here)
+
+
+def _float32(t) -> bool:
+    if _FLOAT32:
+        return t.dtype is _FLOAT32[0]
+    if str(t.dtype) == "torch.float32":
+        _FLOAT32.append(t.dtype)
+        return True
+    return False
 
 
 def make_rope(table, style: int = ROPE_HALF) -> Rope:
     """Rotation over a [positions, rot_dim] float32 device table: cosines, then sines."""
-    if str(table.dtype) != "torch.float32" or not table.is_contiguous():
+    if not _float32(table) or not table.is_contiguous():
         raise TuttiError(EINVAL, "rotation table (float32, contiguous)")
-    return Rope(style, table.shape[1], table.shape[0], table.data_ptr())
+    n_pos, rot_dim = table.shape
+    return Rope(style, rot_dim, n_pos, table.data_ptr())
 
 
 def make_attend(q, out, lse=None) -> Attend:
     """Attention struct over [tokens, heads, head_dim] queries and outputs; lse [tokens, heads] float32."""
-    if lse is not None and (str(lse.dtype) != "torch.float32" or not lse.is_contiguous()):
+    if lse is not None and not (_float32(lse) and lse.is_contiguous()):
         raise TuttiError(EINVAL, "lse (float32, contiguous)")
-    return Attend(_dtype_code(q), q.shape[1], _rows(q, q), _rows(out, q), q.data_ptr(), out.data_ptr(),
+    dtype = q.dtype
+    return Attend(_dtype_code(dtype), q.shape[1], _rows(q, dtype), _rows(out, dtype), q.data_ptr(), out.data_ptr(),
                   None if lse is None else lse.data_ptr(), 0.0, 0)
 
 
