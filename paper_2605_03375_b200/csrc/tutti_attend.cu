@@ -56,7 +56,7 @@ int tutti_attn_create(tutti_ctx_t *ctx, tutti_attn_t **out) {
     if (!a) return TUTTI_ENOMEM;
     a->ctx = ctx;
     const uint32_t n_few = few_workers(tutti_ctx_sms_(ctx)), n_many = many_workers(tutti_ctx_sms_(ctx));
-    const size_t part = few_part_bytes(n_few) > many_part_bytes(n_many) ? few_part_bytes(n_few) : many_part_bytes(n_many);
+    const size_t few_part = few_part_bytes(tutti_ctx_sms_(ctx)), many_part = many_part_bytes(n_many), part = few_part > many_part ? few_part : many_part;
     const size_t counts = (n_few + 2 * n_many) * sizeof(uint32_t);
     float *parts = nullptr;
     uint32_t *count = nullptr;
@@ -109,7 +109,7 @@ int tutti_kv_attend_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *s
     const bool few = (uint64_t)step->max_new * p.group <= FEW_ROWS;
     PoolMaps maps;
     if (!few) maps.valid = tutti_ctx_pool_maps_(a->ctx, layer, &maps.k, &maps.v);
-    const cudaError_t e = few ? few_launch(p, a->few, elem_bytes == 1, bf, (cudaStream_t)stream)
+    const cudaError_t e = few ? few_launch(p, a->few, tutti_ctx_sms_(a->ctx), elem_bytes == 1, bf, (cudaStream_t)stream)
                               : many_launch(p, maps, a->many, elem_bytes == 1, bf, (cudaStream_t)stream);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "attend launch");
 }

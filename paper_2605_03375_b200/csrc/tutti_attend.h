@@ -59,11 +59,11 @@ __device__ inline uint32_t pack2(float a, float b, __half) {
 }
 #endif
 
-// 16 rows a tile (tutti_attend_few.cu).
+// 8 or 16 rows a tile (tutti_attend_few.cu).
 constexpr int FEW_ROWS = 16;
 cudaError_t few_setup();
-cudaError_t few_launch(const AttendParams &p, const Workspace &ws, bool c8, bool bf, cudaStream_t st);
-size_t few_part_bytes(uint32_t workers);
+cudaError_t few_launch(const AttendParams &p, const Workspace &ws, int sms, bool c8, bool bf, cudaStream_t st);
+size_t few_part_bytes(int sms);
 uint32_t few_workers(int sms);
 
 // 256 rows a tile (tutti_attend_many.cu).

@@ -10,8 +10,8 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 // Few rows per sequence (decode): one pass over the cache at HBM speed.
 //
-// A *tile* is 16 rows of one sequence and KV head: (new token, query head of the group) pairs,
-// one A fragment of the warp-level matrix instruction.  Its keys are cut into units of WARPS x KW
+// A *tile* is 8 or 16 rows of one sequence and KV head: (new token, query head of the group) pairs,
+// one or two B fragments of the warp-level matrix instruction.  Its keys are cut into units of WARPS x KW
 // keys; all units of all tiles of the step, laid end to end, are dealt out evenly over a fixed
 // number of workers (CTAs), so ragged batches, one long sequence and captured graphs whose lengths
 // change all load every SM alike and the host needs no length.  A worker's share is a run of
@@ -20,14 +20,14 @@ namespace {
 // order: the result does not depend on the order of arrival.
 //
 // Inside a worker each warp takes KW keys of a unit on its own: gather through the block table
-// with cp.async into its ring of STAGES x 8 KiB (a row of one head is the largest piece that is
-// contiguous in every pool layout), S = Q K^T, running maximum and sum, O += P V, all in
-// registers; no CTA barrier until a tile ends.  8-bit caches are multiplied as f16 codes
-// (exact); the scale of a key goes onto its score, the scale of a value onto its probability.
+// with cp.async into its ring of STAGES stages (a row of one head is the largest piece that is
+// contiguous in every pool layout), S^T = K Q^T, running maximum and sum, O^T += V^T P^T, all in
+// registers; no CTA barrier until a tile ends.  Keys and values are the A operand, so that the
+// few rows fill the N of 8 of one instruction: half the instructions and registers of the other
+// way round.  8-bit caches are multiplied as f16 codes (exact); the scale of a key goes onto
+// its score, the scale of a value onto its probability.
 constexpr int WARPS = 4;
 constexpr int STAGES = 3;
-constexpr uint32_t STAGE_BYTES = 8192;      // keys and values of one warp's KW keys
-constexpr int WORKERS_PER_SM = 2;
 constexpr int MIN_UNITS = 2;                // of a worker: a worker more costs joining its part
 
 __device__ inline void ldm4(uint32_t (&r)[4], uint32_t a) {
@@ -48,6 +48,12 @@ __device__ inline void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, u
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// an 8 x 8 block of 16-bit elements, thread (g, c) holding row g, columns 2 c and 2 c + 1
+__device__ inline uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 // two e4m3 codes (low 16 bits) as two f16
 __device__ inline uint32_t codes2(uint32_t x) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffff), __NV_E4M3);
@@ -63,33 +69,38 @@ struct Cursor {
 
 
 // Tiles and units of a sequence (0 tiles: nothing to do); the error code, if any.
-__device__ inline int seq_shape(const AttendParams &p, uint32_t unit_keys, uint32_t s, Cursor &k) {
+__device__ inline int seq_shape(const AttendParams &p, uint32_t rows, uint32_t unit_keys, uint32_t s, Cursor &k) {
     const int code = seq_view(p.step, p.pool.block_tokens, s, k.v);
-    k.n_tiles = code == TUTTI_OK ? (k.v.n_new * p.group + FEW_ROWS - 1) / FEW_ROWS * p.pool.n_kv_heads : 0;
+    k.n_tiles = code == TUTTI_OK ? (k.v.n_new * p.group + rows - 1) / rows * p.pool.n_kv_heads : 0;
     k.n_units = code == TUTTI_OK && k.v.ctx ? (k.v.ctx + unit_keys - 1) / unit_keys : 1;
     return code;
 }
 
-__device__ inline void advance(const AttendParams &p, uint32_t unit_keys, Cursor &k) {
+__device__ inline void advance(const AttendParams &p, uint32_t rows, uint32_t unit_keys, Cursor &k) {
     if (++k.u < k.n_units) return;
     k.u = 0;
     if (++k.c < k.n_tiles) return;
     k.c = 0;
     do {
         if (++k.s >= p.step.n_seq) return;      // behind the last unit: not used
-        seq_shape(p, unit_keys, k.s, k);
+        seq_shape(p, rows, unit_keys, k.s, k);
     } while (k.n_tiles == 0);
 }
 
-// Q, K and V have the type T; 8-bit caches (C8) are multiplied as f16.
-template <typename T, bool C8, int D>
+// Q, K and V have the type T; 8-bit caches (C8) are multiplied as f16.  NB: blocks of 8 rows.
+template <typename T, bool C8, int D, int NB>
 struct Few {
     using M = typename std::conditional<C8, __half, T>::type;        // type of the matrix instructions
+    static constexpr int ROWS = 8 * NB;
+    // 8-bit caches take more instructions a byte (widening): with 8 rows 128 registers are enough for
+    // 16 warps an SM instead of 8, each with half the bytes in flight.
+    static constexpr int WORKERS_PER_SM = C8 && NB == 1 ? 4 : 2;
+    static constexpr uint32_t STAGE_BYTES = C8 && NB == 1 ? 4096 : 8192;   // keys and values of one warp's KW keys
     static constexpr int RB = D * (C8 ? 1 : 2);                      // bytes of a row
     static constexpr int KW = STAGE_BYTES / (2 * RB);                // keys of a warp's step
     static constexpr int UNIT = WARPS * KW;
-    static constexpr int NT = KW / 8;                                // score fragments
-    static constexpr int DT = D / 8;                                 // output fragments
+    static constexpr int MT = KW / 16;                               // blocks of 16 keys
+    static constexpr int DT = D / 16;                                // blocks of 16 dimensions
     static constexpr int KPL = (KW + 31) / 32;                       // keys whose address a lane knows
     static constexpr int CH = RB / 16;                               // 16-byte chunks of a row
     static constexpr uint32_t SCALES = C8 ? KW * 8 : 0;              // scales of the stage's keys, then values
@@ -99,8 +110,9 @@ struct Few {
     static constexpr float OFF = std::is_same<M, __half>::value ? 14.0f : 0.0f;
     static constexpr uint32_t OFF_MASK = WARPS * STAGES * STAGE;     // uint64 keys that exist, by warp and stage
     static constexpr uint32_t OFF_ML = OFF_MASK + WARPS * STAGES * 8;
-    static constexpr uint32_t OFF_PLAN = OFF_ML + WARPS * FEW_ROWS * 8;
+    static constexpr uint32_t OFF_PLAN = OFF_ML + WARPS * ROWS * 8;
     static constexpr uint32_t SMEM = OFF_PLAN + 128;
+    static_assert(STAGE_BYTES >= ROWS * D * 4, "a warp's sums go through one of its stages");
 
     // Where 16-byte chunk `ch` of row `row` lies: rotated so that the loads below meet no bank twice.
     __device__ static uint32_t place(uint32_t row, uint32_t ch, bool value) {
@@ -110,10 +122,10 @@ struct Few {
     }
 };
 
-template <typename T, bool C8, int D>
-__global__ void __launch_bounds__(WARPS * 32, WORKERS_PER_SM)
+template <typename T, bool C8, int D, int NB>
+__global__ void __launch_bounds__(WARPS * 32, Few<T, C8, D, NB>::WORKERS_PER_SM)
 attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
-    using F = Few<T, C8, D>;
+    using F = Few<T, C8, D, NB>;
     using M = typename F::M;
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, c = lane % 4;
@@ -128,7 +140,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     Cursor own;                                    // the thread's last sequence (its only one, mostly)
     own.s = ~0u;
     for (uint32_t s = threadIdx.x * per; s < min((threadIdx.x + 1) * per, p.step.n_seq); ++s) {
-        const int code = seq_shape(p, F::UNIT, s, own);
+        const int code = seq_shape(p, F::ROWS, F::UNIT, s, own);
         own.s = s;
         if (code != TUTTI_OK && blockIdx.x == 0) report(p.step, code);
         mine += (unsigned long long)own.n_tiles * own.n_units;
@@ -157,7 +169,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     if (x0 >= before && x0 < before + mine) {      // one thread's sequences hold the first unit
         unsigned long long at = before;
         for (uint32_t s = threadIdx.x * per;; ++s) {
-            if (s != own.s) seq_shape(p, F::UNIT, s, own);
+            if (s != own.s) seq_shape(p, F::ROWS, F::UNIT, s, own);
             const unsigned long long n = (unsigned long long)own.n_tiles * own.n_units;
             if (x0 < at + n) {
                 own.s = s;
@@ -190,7 +202,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 id[i] = __ldg(p.step.block_ids + look.v.b0 + key / p.pool.block_tokens);
         }
         ++look_x;
-        if (look_x < x1) advance(p, F::UNIT, look);
+        if (look_x < x1) advance(p, F::ROWS, F::UNIT, look);
     };
     locate(ids[0]);
     locate(ids[1]);
@@ -209,8 +221,8 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 mask |= (uint64_t)__ballot_sync(0xffffffffu, ok) << (32 * i);
                 if (C8 && i * 32 + lane < F::KW) {
                     const uint64_t at = ok ? (uint64_t)ids[0][i] * p.pool.n_kv_heads + h : 0;
-                    cp4(kst + STAGE_BYTES + (i * 32 + lane) * 4, p.pool.k_scale + at, ok);
-                    cp4(kst + STAGE_BYTES + (F::KW + i * 32 + lane) * 4, p.pool.v_scale + at, ok);
+                    cp4(kst + F::STAGE_BYTES + (i * 32 + lane) * 4, p.pool.k_scale + at, ok);
+                    cp4(kst + F::STAGE_BYTES + (F::KW + i * 32 + lane) * 4, p.pool.v_scale + at, ok);
                 }
                 off[i] = ok ? block_offset(p.pool, ids[0][i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + h * p.pool.head_stride) : -1;
             }
@@ -225,7 +237,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 cp16(vst + F::place(row, ch, true), (const void *)(p.pool.v_base + a), ok);
             }
             ++put_x;
-            if (put_x < x1) advance(p, F::UNIT, put);
+            if (put_x < x1) advance(p, F::ROWS, F::UNIT, put);
 #pragma unroll
             for (int i = 0; i < F::KPL; ++i) ids[0][i] = ids[1][i];
             locate(ids[1]);
@@ -238,44 +250,44 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     // ---- the worker's tiles ----
     uint32_t stage = 0;
     for (unsigned long long x = x0; x < x1;) {
-        const uint32_t rts = get.n_tiles / p.pool.n_kv_heads, h = get.c / rts, row0 = (get.c % rts) * FEW_ROWS;
+        const uint32_t rts = get.n_tiles / p.pool.n_kv_heads, h = get.c / rts, row0 = (get.c % rts) * F::ROWS;
         const uint32_t n_rows = get.v.n_new * p.group;
         const int64_t first = (int64_t)get.v.ctx - get.v.n_new;
         const unsigned long long tile0 = x - get.u;                       // the tile's units: [tile0, tile0 + n_units)
         const unsigned long long seg_end = min(x1, tile0 + get.n_units);
-        // rows g and g + 8 of the tile: token, position (last key seen), query fragment
-        int64_t pos[2];
-        float rowscale[2];
-        uint32_t qf[D / 16][4];
+        // Query fragments: row g of each block of 8.  Scores: rows 2 c and 2 c + 1 of each block, their
+        // positions (the last key they see) and factors.
+        int64_t pos[NB][2];
+        float rowscale[NB][2];
+        uint32_t qf[NB][D / 16][2];
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            const uint32_t row = row0 + g + 8 * r;
+        for (int b = 0; b < NB; ++b) {
+            const uint32_t row = row0 + b * 8 + g;
             const bool ok = row < n_rows;
             const uint32_t i = ok ? row / p.group : 0, qh = h * p.group + (ok ? row % p.group : 0);
-            pos[r] = ok ? first + i : -1;
             const T *q = (const T *)p.q + (uint64_t)(get.v.q0 + i) * p.q_stride + (uint64_t)qh * D;
-            rowscale[r] = p.scale * 1.4426950408889634f;
+            float mul = p.scale * 1.4426950408889634f;
             if constexpr (!C8) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
 #pragma unroll
                     for (int j = 0; j < 2; ++j)
-                        qf[k][r + 2 * j] = ok ? *reinterpret_cast<const uint32_t *>(q + k * 16 + j * 8 + 2 * c) : 0;
+                        qf[b][k][j] = ok ? *reinterpret_cast<const uint32_t *>(q + k * 16 + j * 8 + 2 * c) : 0;
             } else {
-                // the k index of step t is permuted: a thread's 16 elements are 16 neighbouring dimensions
-                float x[D / 4], top = 0;
+                // the k index of a step is permuted: a thread's 16 elements are 16 neighbouring dimensions
+                float e16[D / 4], top = 0;
 #pragma unroll
-                for (int b = 0; b < D / 64; ++b) {
+                for (int d = 0; d < D / 64; ++d) {
                     uint4 u[2] = {};
                     if (ok) {
-                        u[0] = *reinterpret_cast<const uint4 *>(q + b * 64 + c * 16);
-                        u[1] = *reinterpret_cast<const uint4 *>(q + b * 64 + c * 16 + 8);
+                        u[0] = *reinterpret_cast<const uint4 *>(q + d * 64 + c * 16);
+                        u[1] = *reinterpret_cast<const uint4 *>(q + d * 64 + c * 16 + 8);
                     }
                     const T *e = reinterpret_cast<const T *>(u);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        x[b * 16 + j] = (float)e[j];
-                        top = fmaxf(top, fabsf(x[b * 16 + j]));
+                        e16[d * 16 + j] = (float)e[j];
+                        top = fmaxf(top, fabsf(e16[d * 16 + j]));
                     }
                 }
                 // a row of bf16 queries is scaled by a power of two so that f16 holds it: exactly,
@@ -286,21 +298,32 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                     const int e = min(max((int)(__float_as_uint(top) >> 23) - 127, -60), 126);
                     down = __uint_as_float((uint32_t)(127 - e) << 23);
-                    rowscale[r] *= __uint_as_float((uint32_t)(127 + e) << 23);
+                    mul *= __uint_as_float((uint32_t)(127 + e) << 23);
                 }
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const int at = (k / 4) * 16 + (k % 4) * 4 + 2 * j;
-                        qf[k][r + 2 * j] = pack2(x[at] * down, x[at + 1] * down, __half());
+                        qf[b][k][j] = pack2(e16[at] * down, e16[at + 1] * down, __half());
                     }
             }
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const uint32_t mine = row0 + b * 8 + 2 * c + r;
+                pos[b][r] = mine < n_rows ? first + mine / p.group : -1;
+                rowscale[b][r] = __shfl_sync(0xffffffffu, mul, (2 * c + r) * 4);
+            }
         }
-        float o[F::DT][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0, 0};
+        float o[NB][F::DT][4], m[NB][2], l[NB][2];
         float vtop = 0;                      // 8-bit: power of two at or above no value scale so far; O is in its units
 #pragma unroll
-        for (int i = 0; i < F::DT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0;
+        for (int b = 0; b < NB; ++b) {
+            m[b][0] = m[b][1] = -INFINITY;
+            l[b][0] = l[b][1] = 0;
+#pragma unroll
+            for (int i = 0; i < F::DT; ++i) o[b][i][0] = o[b][i][1] = o[b][i][2] = o[b][i][3] = 0;
+        }
         const int64_t last_all = first + row0 / p.group;        // keys up to here are seen by every row of the tile
 
         for (; x < seg_end; ++x) {
@@ -313,124 +336,127 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             const int64_t key0 = (int64_t)(get.u * WARPS + warp) * F::KW;
             constexpr uint64_t ALL = F::KW == 64 ? ~0ull : (1ull << (F::KW & 63)) - 1;
             if (there) {
-                // scores
-                float s[F::NT][4];
+                // scores: fragment element e is key 16 t + g + 8 (e / 2), row 2 c + e % 2
+                float s[NB][F::MT][4];
 #pragma unroll
-                for (int n = 0; n < F::NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0;
-                if constexpr (!C8) {
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
+                    for (int t = 0; t < F::MT; ++t) s[b][t][0] = s[b][t][1] = s[b][t][2] = s[b][t][3] = 0;
 #pragma unroll
-                        for (int n = 0; n < F::NT; n += 2) {
-                            // 16 keys x 16 dimensions: lanes 0-7 and 8-15 the two dimension halves of the first 8 keys
-                            uint32_t b[4];
-                            ldm4(b, kst + F::place(n * 8 + (lane & 7) + (lane >> 4) * 8, k * 2 + (lane >> 3 & 1), false));
-                            mma(s[n], qf[k], b[0], b[1], M());
-                            mma(s[n + 1], qf[k], b[2], b[3], M());
+                for (int t = 0; t < F::MT; ++t) {
+                    if constexpr (!C8) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) {
+                            uint32_t a[4];
+                            ldm4(a, kst + F::place(t * 16 + (lane & 15), k * 2 + (lane >> 4), false));
+#pragma unroll
+                            for (int b = 0; b < NB; ++b) mma(s[b][t], a, qf[b][k][0], qf[b][k][1], M());
                         }
-                } else {
+                    } else {
 #pragma unroll
-                    for (int n = 0; n < F::NT; ++n)
+                        for (int d = 0; d < D / 64; ++d) {
+                            const uint4 u = *reinterpret_cast<const uint4 *>(st + F::place(t * 16 + g, d * 4 + c, false));
+                            const uint4 v = *reinterpret_cast<const uint4 *>(st + F::place(t * 16 + g + 8, d * 4 + c, false));
+                            const uint32_t lo[4] = {u.x, u.y, u.z, u.w}, hi[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                        for (int b = 0; b < D / 64; ++b) {
-                            const uint4 u = *reinterpret_cast<const uint4 *>(st + F::place(n * 8 + g, b * 4 + c, false));
-                            const uint32_t word[4] = {u.x, u.y, u.z, u.w};
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t a[4] = {codes2(lo[k]), codes2(hi[k]), codes2(lo[k] >> 16), codes2(hi[k] >> 16)};
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) mma(s[n], qf[b * 4 + k], codes2(word[k]), codes2(word[k] >> 16), M());
+                                for (int b = 0; b < NB; ++b) mma(s[b][t], a, qf[b][d * 4 + k][0], qf[b][d * 4 + k][1], M());
+                            }
                         }
+                    }
                 }
                 const bool masked = there != ALL || key0 + F::KW - 1 > last_all;
-                float top[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                for (int n = 0; n < F::NT; ++n) {
-                    float2 ks = {1, 1};
-                    if constexpr (C8) ks = *reinterpret_cast<const float2 *>(st + STAGE_BYTES + (n * 8 + 2 * c) * 4);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        s[n][e] *= rowscale[e / 2] * (C8 ? (e & 1 ? ks.y : ks.x) : 1.0f);
-                        if (masked) {
-                            const int key = n * 8 + 2 * c + (e & 1);
-                            if (!(there >> key & 1) || key0 + key > pos[e / 2]) s[n][e] = -INFINITY;
-                        }
-                        top[e / 2] = fmaxf(top[e / 2], s[n][e]);
-                    }
-                }
-                float alpha[2], sub[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
-                    top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
-                    const float m2 = fmaxf(m[r], top[r]);
-                    sub[r] = m2 == -INFINITY ? 0 : m2;       // a row that has seen nothing yet
-                    alpha[r] = ex2(m[r] - sub[r]);
-                    m[r] = m2;
-                    l[r] *= alpha[r];
-                    sub[r] -= F::OFF;
-                }
-                float vinv = 1.0f;
+                float vs[F::MT][2], vinv = 1.0f, vdown = 1.0f;      // 8-bit: value scales of the lane's keys
                 if constexpr (C8) {
-                    float vs = 0;
+                    float vmax = 0;
 #pragma unroll
-                    for (int n = 0; n < F::NT; ++n) {
-                        const float2 v2 = *reinterpret_cast<const float2 *>(st + STAGE_BYTES + (F::KW + n * 8 + 2 * c) * 4);
-                        vs = fmaxf(vs, fmaxf(v2.x, v2.y));
-                    }
-                    vs = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, 1));
-                    vs = fmaxf(vs, __shfl_xor_sync(0xffffffffu, vs, 2));
-                    vs = __uint_as_float(min(max(__float_as_uint(vs) >> 23, 1u), 253u) << 23);
-                    if (vs > vtop) {
-                        const float f = vtop / vs;
-                        alpha[0] *= f;
-                        alpha[1] *= f;
-                        vtop = vs;
+                    for (int t = 0; t < F::MT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            vs[t][i] = *reinterpret_cast<const float *>(st + F::STAGE_BYTES + (F::KW + t * 16 + g + 8 * i) * 4);
+                            vmax = fmaxf(vmax, vs[t][i]);
+                        }
+                    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, 4));
+                    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, 8));
+                    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, 16));
+                    vmax = __uint_as_float(min(max(__float_as_uint(vmax) >> 23, 1u), 253u) << 23);
+                    if (vmax > vtop) {
+                        vdown = vtop / vmax;
+                        vtop = vmax;
                     }
                     vinv = 1.0f / vtop;
                 }
-                if (__any_sync(0xffffffffu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
+                uint32_t pf[NB][F::MT][2];
 #pragma unroll
-                    for (int i = 0; i < F::DT; ++i) {
-                        o[i][0] *= alpha[0];
-                        o[i][1] *= alpha[0];
-                        o[i][2] *= alpha[1];
-                        o[i][3] *= alpha[1];
-                    }
-                }
-                uint32_t pf[F::NT / 2][4];
+                for (int b = 0; b < NB; ++b) {
+                    float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-                for (int n = 0; n < F::NT; ++n) {
-                    float2 vs = {1, 1};
-                    if constexpr (C8) {
-                        vs = *reinterpret_cast<const float2 *>(st + STAGE_BYTES + (F::KW + n * 8 + 2 * c) * 4);
-                        vs.x *= vinv;
-                        vs.y *= vinv;
-                    }
+                    for (int t = 0; t < F::MT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float ks = rowscale[b][e & 1];
+                            const int key = t * 16 + g + 8 * (e / 2);
+                            if constexpr (C8) ks *= *reinterpret_cast<const float *>(st + F::STAGE_BYTES + key * 4);
+                            s[b][t][e] *= ks;
+                            if (masked && (!(there >> key & 1) || key0 + key > pos[b][e & 1])) s[b][t][e] = -INFINITY;
+                            top[e & 1] = fmaxf(top[e & 1], s[b][t][e]);
+                        }
+                    float alpha[2], sub[2];
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const float a = ex2(s[n][2 * r] - sub[r]), b = ex2(s[n][2 * r + 1] - sub[r]);
-                        l[r] += a + b;
-                        pf[n / 2][(n & 1) * 2 + r] = C8 ? pack2(a * vs.x, b * vs.y, M()) : pack2(a, b, M());
+                        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 4));
+                        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 8));
+                        top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 16));
+                        const float m2 = fmaxf(m[b][r], top[r]);
+                        sub[r] = m2 == -INFINITY ? 0 : m2;       // a row that has seen nothing yet
+                        alpha[r] = ex2(m[b][r] - sub[r]);
+                        m[b][r] = m2;
+                        l[b][r] *= alpha[r];
+                        alpha[r] *= vdown;
+                        sub[r] -= F::OFF;
                     }
+                    if (__any_sync(0xffffffffu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
+#pragma unroll
+                        for (int i = 0; i < F::DT; ++i) {
+                            o[b][i][0] *= alpha[0];
+                            o[b][i][1] *= alpha[1];
+                            o[b][i][2] *= alpha[0];
+                            o[b][i][3] *= alpha[1];
+                        }
+                    }
+#pragma unroll
+                    for (int t = 0; t < F::MT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float x0_ = ex2(s[b][t][2 * i] - sub[0]), x1_ = ex2(s[b][t][2 * i + 1] - sub[1]);
+                            l[b][0] += x0_;
+                            l[b][1] += x1_;
+                            const float f = C8 ? vs[t][i] * vinv : 1.0f;
+                            // from (key g, rows 2 c and 2 c + 1) to (row g, keys 2 c and 2 c + 1)
+                            pf[b][t][i] = transpose8(C8 ? pack2(x0_ * f, x1_ * f, M()) : pack2(x0_, x1_, M()));
+                        }
                 }
                 // values
-                if constexpr (!C8) {
 #pragma unroll
-                    for (int k = 0; k < F::KW / 16; ++k)
+                for (int t = 0; t < F::MT; ++t) {
+                    if constexpr (!C8) {
 #pragma unroll
-                        for (int i = 0; i < F::DT; i += 2) {
-                            uint32_t b[4];
-                            ldm4t(b, vst + F::place(k * 16 + (lane & 15), i + (lane >> 4), true));
-                            mma(o[i], pf[k], b[0], b[1], M());
-                            mma(o[i + 1], pf[k], b[2], b[3], M());
+                        for (int i = 0; i < F::DT; ++i) {
+                            uint32_t a[4];
+                            ldm4t(a, vst + F::place(t * 16 + (lane & 7) + (lane >> 4) * 8, i * 2 + (lane >> 3 & 1), true));
+#pragma unroll
+                            for (int b = 0; b < NB; ++b) mma(o[b][i], a, pf[b][t][0], pf[b][t][1], M());
                         }
-                } else {
-                    // fragment i, column n stands for dimension n * DT + i: a thread's codes of a key are neighbours
-                    const unsigned char *vrow = st + F::KW * F::RB;
-#pragma unroll
-                    for (int k = 0; k < F::KW / 16; ++k) {
-                        uint32_t word[4][F::DT / 4];
+                    } else {
+                        // rows g and g + 8 of fragment i are dimensions g * D / 8 + 2 i and + 1: a thread's codes of a key
+                        // are neighbours
+                        const unsigned char *vrow = st + F::KW * F::RB;
+                        uint32_t word[4][D / 32];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const uint32_t row = k * 16 + 2 * c + (j & 1) + (j >> 1) * 8;
+                            const uint32_t row = t * 16 + 2 * c + (j & 1) + (j >> 1) * 8;
                             if constexpr (D == 128) {
                                 const uint4 u = *reinterpret_cast<const uint4 *>(vrow + F::place(row, g, true));
                                 word[j][0] = u.x, word[j][1] = u.y, word[j][2] = u.z, word[j][3] = u.w;
@@ -440,13 +466,13 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                             }
                         }
 #pragma unroll
-                        for (int q = 0; q < F::DT / 4; ++q) {
-                            const uint32_t lo0 = __byte_perm(word[0][q], word[1][q], 0x5140), hi0 = __byte_perm(word[0][q], word[1][q], 0x7362);
-                            const uint32_t lo1 = __byte_perm(word[2][q], word[3][q], 0x5140), hi1 = __byte_perm(word[2][q], word[3][q], 0x7362);
-                            mma(o[q * 4 + 0], pf[k], codes2(lo0), codes2(lo1), M());
-                            mma(o[q * 4 + 1], pf[k], codes2(lo0 >> 16), codes2(lo1 >> 16), M());
-                            mma(o[q * 4 + 2], pf[k], codes2(hi0), codes2(hi1), M());
-                            mma(o[q * 4 + 3], pf[k], codes2(hi0 >> 16), codes2(hi1 >> 16), M());
+                        for (int i = 0; i < F::DT; ++i) {
+                            const uint32_t pick = i & 1 ? 0x7362 : 0x5140;       // two neighbouring dimensions of two keys
+                            const uint32_t x = __byte_perm(word[0][i / 2], word[1][i / 2], pick);
+                            const uint32_t y = __byte_perm(word[2][i / 2], word[3][i / 2], pick);
+                            const uint32_t a[4] = {codes2(x), codes2(x >> 16), codes2(y), codes2(y >> 16)};
+#pragma unroll
+                            for (int b = 0; b < NB; ++b) mma(o[b][i], a, pf[b][t][0], pf[b][t][1], M());
                         }
                     }
                 }
@@ -461,49 +487,53 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         // ---- join the warps: O goes through the stage just used, which no load is aimed at ----
         const bool whole = get.u + 1 == get.n_units && tile0 >= x0;
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
-            l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
-            if (c == 0) ml[warp * FEW_ROWS + g + 8 * r] = make_float2(m[r], l[r]);
-        }
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                l[b][r] += __shfl_xor_sync(0xffffffffu, l[b][r], 4);
+                l[b][r] += __shfl_xor_sync(0xffffffffu, l[b][r], 8);
+                l[b][r] += __shfl_xor_sync(0xffffffffu, l[b][r], 16);
+                if (g == 0) ml[warp * F::ROWS + b * 8 + 2 * c + r] = make_float2(m[b][r], l[b][r]);
+            }
         __syncthreads();
         float *mine_o = reinterpret_cast<float *>(ring + stage * F::STAGE);
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            float top = -INFINITY;
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < WARPS; ++i) top = fmaxf(top, ml[i * FEW_ROWS + g + 8 * r].x);
-            const float f = top == -INFINITY ? 0 : ex2(m[r] - top) * (C8 ? vtop : 1.0f);
-            float *dst = mine_o + (g + 8 * r) * D;
+            for (int r = 0; r < 2; ++r) {
+                const uint32_t row = b * 8 + 2 * c + r;
+                float top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < F::DT; ++i) {
-                if constexpr (!C8) {
-                    *reinterpret_cast<float2 *>(dst + ((i * 8 + 2 * c) ^ ((g & 3) * 8))) = make_float2(o[i][2 * r] * f, o[i][2 * r + 1] * f);
-                } else {
-                    dst[(2 * c * F::DT + i) ^ ((g & 3) * 8)] = o[i][2 * r] * f;
-                    dst[((2 * c + 1) * F::DT + i) ^ ((g & 3) * 8)] = o[i][2 * r + 1] * f;
+                for (int i = 0; i < WARPS; ++i) top = fmaxf(top, ml[i * F::ROWS + row].x);
+                const float f = top == -INFINITY ? 0 : ex2(m[b][r] - top) * (C8 ? vtop : 1.0f);
+                float *dst = mine_o + row * D;
+#pragma unroll
+                for (int i = 0; i < F::DT; ++i) {
+                    const uint32_t d0 = C8 ? g * (D / 8) + 2 * i : i * 16 + g, d1 = C8 ? d0 + 1 : d0 + 8;
+                    dst[d0 ^ (c * 8)] = o[b][i][r] * f;
+                    dst[d1 ^ (c * 8)] = o[b][i][2 + r] * f;
                 }
             }
-        }
         __syncthreads();
-        // thread t: row t / 8, every 8th group of four dimensions
-        const uint32_t row = threadIdx.x / 8, lanec = threadIdx.x % 8;
+        // TPR threads a row, each every TPR-th group of four dimensions
+        constexpr int TPR = WARPS * 32 / F::ROWS, GROUPS = D / 4 / TPR;
+        const uint32_t row = threadIdx.x / TPR, lanec = threadIdx.x % TPR;
         float M_ = -INFINITY, L = 0;
 #pragma unroll
-        for (int i = 0; i < WARPS; ++i) M_ = fmaxf(M_, ml[i * FEW_ROWS + row].x);
+        for (int i = 0; i < WARPS; ++i) M_ = fmaxf(M_, ml[i * F::ROWS + row].x);
 #pragma unroll
         for (int i = 0; i < WARPS; ++i) {
-            const float2 e = ml[i * FEW_ROWS + row];
+            const float2 e = ml[i * F::ROWS + row];
             L += M_ == -INFINITY ? 0 : e.y * ex2(e.x - M_);
         }
-        float acc[D / 8];
+        float acc[GROUPS * 4];
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
+        for (int j = 0; j < GROUPS; ++j) {
             float4 a = make_float4(0, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
                 const float *src = reinterpret_cast<const float *>(smem + (i * STAGES + stage) * F::STAGE) + row * D;
-                const float4 b = *reinterpret_cast<const float4 *>(src + (((j * 8 + lanec) * 4) ^ ((row & 3) * 8)));
+                const float4 b = *reinterpret_cast<const float4 *>(src + (((j * TPR + lanec) * 4) ^ ((row >> 1 & 3) * 8)));
                 a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w;
             }
             acc[j * 4] = a.x, acc[j * 4 + 1] = a.y, acc[j * 4 + 2] = a.z, acc[j * 4 + 3] = a.w;
@@ -514,11 +544,11 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             const uint32_t w0 = (uint32_t)(((tile0 + 1) * workers - 1) / total);
             const uint32_t w1 = (uint32_t)(((tile0 + get.n_units) * workers - 1) / total);
             auto slot = [&](uint32_t i) { return i == w0 ? 2 * i + 1 : 2 * i; };
-            float *part_o = ws.part, *part_ml = ws.part + (uint64_t)2 * ws.workers * FEW_ROWS * D;
-            float4 *po = reinterpret_cast<float4 *>(part_o + ((uint64_t)slot(w) * FEW_ROWS + row) * D);
+            float *part_o = ws.part, *part_ml = ws.part + (uint64_t)2 * ws.workers * F::ROWS * D;
+            float4 *po = reinterpret_cast<float4 *>(part_o + ((uint64_t)slot(w) * F::ROWS + row) * D);
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) po[j * 8 + lanec] = make_float4(acc[j * 4], acc[j * 4 + 1], acc[j * 4 + 2], acc[j * 4 + 3]);
-            if (lanec == 0) reinterpret_cast<float2 *>(part_ml)[slot(w) * FEW_ROWS + row] = make_float2(M_, L);
+            for (int j = 0; j < GROUPS; ++j) po[j * TPR + lanec] = make_float4(acc[j * 4], acc[j * 4 + 1], acc[j * 4 + 2], acc[j * 4 + 3]);
+            if (lanec == 0) reinterpret_cast<float2 *>(part_ml)[slot(w) * F::ROWS + row] = make_float2(M_, L);
             __threadfence();
             __syncthreads();
             if (threadIdx.x == 0) {
@@ -532,17 +562,17 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 __threadfence();
                 M_ = -INFINITY;
                 L = 0;
-                for (uint32_t i = w0; i <= w1; ++i) M_ = fmaxf(M_, __ldcg(reinterpret_cast<const float2 *>(part_ml) + slot(i) * FEW_ROWS + row).x);
+                for (uint32_t i = w0; i <= w1; ++i) M_ = fmaxf(M_, __ldcg(reinterpret_cast<const float2 *>(part_ml) + slot(i) * F::ROWS + row).x);
 #pragma unroll
-                for (int j = 0; j < D / 8; ++j) acc[j] = 0;
+                for (int j = 0; j < GROUPS * 4; ++j) acc[j] = 0;
                 for (uint32_t i = w0; i <= w1; ++i) {
-                    const float2 e = __ldcg(reinterpret_cast<const float2 *>(part_ml) + slot(i) * FEW_ROWS + row);
+                    const float2 e = __ldcg(reinterpret_cast<const float2 *>(part_ml) + slot(i) * F::ROWS + row);
                     const float f = M_ == -INFINITY ? 0 : ex2(e.x - M_);
                     L += e.y * f;
-                    const float4 *src = reinterpret_cast<const float4 *>(part_o + ((uint64_t)slot(i) * FEW_ROWS + row) * D);
+                    const float4 *src = reinterpret_cast<const float4 *>(part_o + ((uint64_t)slot(i) * F::ROWS + row) * D);
 #pragma unroll
-                    for (int j = 0; j < D / 32; ++j) {
-                        const float4 b = __ldcg(src + j * 8 + lanec);
+                    for (int j = 0; j < GROUPS; ++j) {
+                        const float4 b = __ldcg(src + j * TPR + lanec);
                         acc[j * 4] += b.x * f, acc[j * 4 + 1] += b.y * f, acc[j * 4 + 2] += b.z * f, acc[j * 4 + 3] += b.w * f;
                     }
                 }
@@ -554,58 +584,64 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             const float inv = M_ == -INFINITY ? 0.0f : 1.0f / L;
             T *out = (T *)p.out + tok * p.out_stride + (uint64_t)qh * D;
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j)
-                *reinterpret_cast<uint2 *>(out + (j * 8 + lanec) * 4) =
+            for (int j = 0; j < GROUPS; ++j)
+                *reinterpret_cast<uint2 *>(out + (j * TPR + lanec) * 4) =
                     make_uint2(pack2(acc[j * 4] * inv, acc[j * 4 + 1] * inv, T()), pack2(acc[j * 4 + 2] * inv, acc[j * 4 + 3] * inv, T()));
             if (p.lse && lanec == 0)
                 p.lse[tok * p.n_q_heads + qh] = M_ == -INFINITY ? -INFINITY : (M_ - F::OFF + log2f(L)) * 0.6931471805599453f;
         }
         __syncthreads();                     // the stage and the small arrays may be written again
         stage = stage + 1 == STAGES ? 0 : stage + 1;
-        if (x < x1) advance(p, F::UNIT, get);
+        if (x < x1) advance(p, F::ROWS, F::UNIT, get);
     }
     cp_wait<0>();
 }
 
-template <typename T, bool C8, int D>
-cudaError_t launch_few(const AttendParams &p, const Workspace &ws, cudaStream_t st) {
-    attend_few_kernel<T, C8, D><<<ws.workers, WARPS * 32, Few<T, C8, D>::SMEM, st>>>(p, ws);
+template <typename T, bool C8, int D, int NB>
+cudaError_t launch_few(const AttendParams &p, Workspace ws, int sms, cudaStream_t st) {
+    using F = Few<T, C8, D, NB>;
+    ws.workers = sms * F::WORKERS_PER_SM;
+    attend_few_kernel<T, C8, D, NB><<<ws.workers, WARPS * 32, F::SMEM, st>>>(p, ws);
     return cudaGetLastError();
 }
 
-template <bool C8>
-cudaError_t launch_few(const AttendParams &p, const Workspace &ws, bool bf, cudaStream_t st) {
-    if (p.pool.head_dim == 128)
-        return bf ? launch_few<__nv_bfloat16, C8, 128>(p, ws, st) : launch_few<__half, C8, 128>(p, ws, st);
-    return bf ? launch_few<__nv_bfloat16, C8, 64>(p, ws, st) : launch_few<__half, C8, 64>(p, ws, st);
-}
-
-template <typename T, bool C8, int D>
+template <typename T, bool C8, int D, int NB>
 cudaError_t setup_few() {
-    return cudaFuncSetAttribute(attend_few_kernel<T, C8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<T, C8, D>::SMEM);
+    return cudaFuncSetAttribute(attend_few_kernel<T, C8, D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<T, C8, D, NB>::SMEM);
 }
 
-template <typename T>
-cudaError_t setup_type() {
-    cudaError_t e = setup_few<T, false, 128>();
-    if (e == cudaSuccess) e = setup_few<T, true, 128>();
-    if (e == cudaSuccess) e = setup_few<T, false, 64>();
-    if (e == cudaSuccess) e = setup_few<T, true, 64>();
-    return e;
+// f(type, 8-bit, head_dim, row blocks) for one or for every instance
+template <typename F>
+cudaError_t pick(bool bf, bool c8, bool wide, bool two, F f) {
+    auto nb = [&](auto t, auto c, auto d) {
+        return two ? f(t, c, d, std::integral_constant<int, 2>()) : f(t, c, d, std::integral_constant<int, 1>());
+    };
+    auto dim = [&](auto t, auto c) {
+        return wide ? nb(t, c, std::integral_constant<int, 128>()) : nb(t, c, std::integral_constant<int, 64>());
+    };
+    auto cache = [&](auto t) { return c8 ? dim(t, std::true_type()) : dim(t, std::false_type()); };
+    return bf ? cache(__nv_bfloat16()) : cache(__half());
 }
 
 }  // namespace
 
 cudaError_t few_setup() {
-    const cudaError_t e = setup_type<__nv_bfloat16>();
-    return e == cudaSuccess ? setup_type<__half>() : e;
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < 16 && e == cudaSuccess; ++i)
+        e = pick(i & 1, i & 2, i & 4, i & 8, [](auto t, auto c, auto d, auto nb) { return setup_few<decltype(t), c.value, d.value, nb.value>(); });
+    return e;
 }
 
-cudaError_t few_launch(const AttendParams &p, const Workspace &ws, bool c8, bool bf, cudaStream_t st) {
-    return c8 ? launch_few<true>(p, ws, bf, st) : launch_few<false>(p, ws, bf, st);
+cudaError_t few_launch(const AttendParams &p, const Workspace &ws, int sms, bool c8, bool bf, cudaStream_t st) {
+    // one block of 8 rows where a step's tokens and the query heads of a KV head fit
+    const bool two = (uint64_t)p.step.max_new * p.group > 8;
+    return pick(bf, c8, p.pool.head_dim == 128, two, [&](auto t, auto c, auto d, auto nb) {
+        return launch_few<decltype(t), c.value, d.value, nb.value>(p, ws, sms, st);
+    });
 }
 
-uint32_t few_workers(int sms) { return (uint32_t)sms * WORKERS_PER_SM; }
-size_t few_part_bytes(uint32_t workers) { return (size_t)2 * workers * FEW_ROWS * (128 + 2) * sizeof(float); }
+// of the instance with the most
+uint32_t few_workers(int sms) { return (uint32_t)sms * 4; }
+size_t few_part_bytes(int sms) { return (size_t)2 * sms * 4 * 8 * (128 + 2) * sizeof(float); }
 
 }  // namespace tutti
