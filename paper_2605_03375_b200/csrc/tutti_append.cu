@@ -146,11 +146,11 @@ __device__ void row_warp(const AppendParams &p, uint32_t w) {
     if (pos < 0) return;
     int64_t at = 0;
     if (KV) {
-        at = block_offset(p.pool, __ldg(p.step.block_ids + v.b0 + (uint32_t)pos / p.pool.block_tokens));
+        at = block_offset(p.pool, __ldg(p.step.block_ids + v.b0 + p.pool.block_of((uint32_t)pos)));
         if (at < 0) {
             if (lane == 0) report(p.step, TUTTI_EFAULT);
         } else {
-            at += (int64_t)((uint32_t)pos % p.pool.block_tokens * p.pool.tok_stride);
+            at += (int64_t)(p.pool.row_of((uint32_t)pos) * p.pool.tok_stride);
         }
     }
     const uint32_t per = 32 / p.jobs, j = lane % p.jobs;

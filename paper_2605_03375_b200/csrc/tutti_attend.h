@@ -49,6 +49,10 @@ __device__ inline void cp4(uint32_t dst, const void *src, bool there) {
 __device__ inline void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ inline void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// four e4m3 codes as four f16
+__device__ inline void codes4(uint32_t w, uint32_t &lo, uint32_t &hi) {
+    asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
 __device__ inline uint32_t pack2(float a, float b, __nv_bfloat16) {
     __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<uint32_t *>(&h);

@@ -27,7 +27,7 @@ namespace {
 // way round.  8-bit caches are multiplied as f16 codes (exact); the scale of a key goes onto
 // its score, the scale of a value onto its probability.
 constexpr int WARPS = 4;
-constexpr int STAGES = 3;
+constexpr int STAGES = 3, STAGES_WIDE = 2;
 constexpr int MIN_UNITS = 2;                // of a worker: a worker more costs joining its part
 
 __device__ inline void ldm4(uint32_t (&r)[4], uint32_t a) {
@@ -54,24 +54,17 @@ __device__ inline uint32_t transpose8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-// two e4m3 codes (low 16 bits) as two f16
-__device__ inline uint32_t codes2(uint32_t x) {
-    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(x & 0xffff), __NV_E4M3);
-    return (uint32_t)h.x | (uint32_t)h.y << 16;
-}
-
-// A place in the step's units laid end to end: unit u of tile c of sequence s.
+// A place in the step's units laid end to end: unit u of row tile r and KV head h of sequence s.
 struct Cursor {
-    uint32_t s, c, u;
-    uint32_t n_tiles, n_units;      // of the sequence
+    uint32_t s, h, r, u;
+    uint32_t n_tiles, n_units;      // of the sequence: row tiles, units of each
     SeqView v;
 };
 
-
-// Tiles and units of a sequence (0 tiles: nothing to do); the error code, if any.
+// Row tiles and units of a sequence (0 tiles: nothing to do); the error code, if any.
 __device__ inline int seq_shape(const AttendParams &p, uint32_t rows, uint32_t unit_keys, uint32_t s, Cursor &k) {
     const int code = seq_view(p.step, p.pool.block_tokens, s, k.v);
-    k.n_tiles = code == TUTTI_OK ? (k.v.n_new * p.group + rows - 1) / rows * p.pool.n_kv_heads : 0;
+    k.n_tiles = code == TUTTI_OK ? (k.v.n_new * p.group + rows - 1) / rows : 0;
     k.n_units = code == TUTTI_OK && k.v.ctx ? (k.v.ctx + unit_keys - 1) / unit_keys : 1;
     return code;
 }
@@ -79,8 +72,10 @@ __device__ inline int seq_shape(const AttendParams &p, uint32_t rows, uint32_t u
 __device__ inline void advance(const AttendParams &p, uint32_t rows, uint32_t unit_keys, Cursor &k) {
     if (++k.u < k.n_units) return;
     k.u = 0;
-    if (++k.c < k.n_tiles) return;
-    k.c = 0;
+    if (++k.r < k.n_tiles) return;
+    k.r = 0;
+    if (++k.h < p.pool.n_kv_heads) return;
+    k.h = 0;
     do {
         if (++k.s >= p.step.n_seq) return;      // behind the last unit: not used
         seq_shape(p, rows, unit_keys, k.s, k);
@@ -93,9 +88,10 @@ struct Few {
     using M = typename std::conditional<C8, __half, T>::type;        // type of the matrix instructions
     static constexpr int ROWS = 8 * NB;
     // 8-bit caches take more instructions a byte (widening): with 8 rows 128 registers are enough for
-    // 16 warps an SM instead of 8, each with half the bytes in flight.
+    // 16 warps an SM instead of 8, each with a stage less.
     static constexpr int WORKERS_PER_SM = C8 && NB == 1 ? 4 : 2;
-    static constexpr uint32_t STAGE_BYTES = C8 && NB == 1 ? 4096 : 8192;   // keys and values of one warp's KW keys
+    static constexpr int STAGES = C8 && NB == 1 ? STAGES_WIDE : tutti::STAGES;
+    static constexpr uint32_t STAGE_BYTES = C8 && NB == 1 && D == 64 ? 4096 : 8192;  // keys and values of one warp's KW keys
     static constexpr int RB = D * (C8 ? 1 : 2);                      // bytes of a row
     static constexpr int KW = STAGE_BYTES / (2 * RB);                // keys of a warp's step
     static constexpr int UNIT = WARPS * KW;
@@ -129,8 +125,8 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     using M = typename F::M;
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, c = lane % 4;
-    unsigned char *ring = smem + warp * STAGES * F::STAGE;
-    uint64_t *exists = reinterpret_cast<uint64_t *>(smem + F::OFF_MASK) + warp * STAGES;
+    unsigned char *ring = smem + warp * F::STAGES * F::STAGE;
+    uint64_t *exists = reinterpret_cast<uint64_t *>(smem + F::OFF_MASK) + warp * F::STAGES;
     float2 *ml = reinterpret_cast<float2 *>(smem + F::OFF_ML);
     uint32_t *plan = reinterpret_cast<uint32_t *>(smem + F::OFF_PLAN);
 
@@ -143,7 +139,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         const int code = seq_shape(p, F::ROWS, F::UNIT, s, own);
         own.s = s;
         if (code != TUTTI_OK && blockIdx.x == 0) report(p.step, code);
-        mine += (unsigned long long)own.n_tiles * own.n_units;
+        mine += (unsigned long long)own.n_tiles * own.n_units * p.pool.n_kv_heads;
     }
     unsigned long long incl = mine;
 #pragma unroll
@@ -170,10 +166,12 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         unsigned long long at = before;
         for (uint32_t s = threadIdx.x * per;; ++s) {
             if (s != own.s) seq_shape(p, F::ROWS, F::UNIT, s, own);
-            const unsigned long long n = (unsigned long long)own.n_tiles * own.n_units;
+            const unsigned long long n = (unsigned long long)own.n_tiles * own.n_units * p.pool.n_kv_heads;
             if (x0 < at + n) {
                 own.s = s;
-                own.c = (uint32_t)((x0 - at) / own.n_units);
+                const unsigned long long tile = (x0 - at) / own.n_units;
+                own.h = (uint32_t)(tile / own.n_tiles);
+                own.r = (uint32_t)(tile % own.n_tiles);
                 own.u = (uint32_t)((x0 - at) % own.n_units);
                 *reinterpret_cast<Cursor *>(plan) = own;
                 break;
@@ -184,47 +182,52 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     }
     __syncthreads();
     Cursor get = *reinterpret_cast<const Cursor *>(plan);
-    Cursor put = get;                              // runs ahead: the unit whose loads are issued next
-    unsigned long long put_x = x0;
 
     // ---- gathering ----
     // The ids of a unit's blocks are looked up two units before its rows are fetched, and not touched
     // until then (the first use waits for the load).
-    int32_t ids[2][F::KPL];                        // of the lane's keys, of the unit at `put` and the one behind it
+    struct Pending {
+        uint32_t key0, ctx, h;                     // of a unit: the warp's first key, keys that exist, KV head
+        int32_t id[F::KPL];                        // of the lane's keys
+    } pend[2];
     Cursor look = get;
-    unsigned long long look_x = x0;
-    auto locate = [&](int32_t (&id)[F::KPL]) {
+    unsigned long long look_x = x0, put_x = x0;
+    auto locate = [&](Pending &u) {
+        u.key0 = (look.u * WARPS + warp) * F::KW;
+        u.ctx = look.v.ctx;
+        u.h = look.h;
+        if (look_x < x1) {
 #pragma unroll
-        for (int i = 0; i < F::KPL; ++i) {
-            const uint32_t key = (look.u * WARPS + warp) * F::KW + i * 32 + lane;
-            id[i] = -1;
-            if (look_x < x1 && i * 32 + lane < F::KW && key < look.v.ctx)
-                id[i] = __ldg(p.step.block_ids + look.v.b0 + key / p.pool.block_tokens);
+            for (int i = 0; i < F::KPL; ++i) {
+                const uint32_t key = u.key0 + i * 32 + lane;
+                u.id[i] = -1;
+                if (i * 32 + lane < F::KW && key < u.ctx) u.id[i] = __ldg(p.step.block_ids + look.v.b0 + p.pool.block_of(key));
+            }
+            advance(p, F::ROWS, F::UNIT, look);
         }
         ++look_x;
-        if (look_x < x1) advance(p, F::ROWS, F::UNIT, look);
     };
-    locate(ids[0]);
-    locate(ids[1]);
-    auto fetch = [&](uint32_t stage) {             // issues the loads of the unit at `put`, then looks up the next ids
+    locate(pend[0]);
+    locate(pend[1]);
+    auto fetch = [&](uint32_t stage) {             // issues the loads of the next unit, then looks up the ids two behind
         if (put_x < x1) {
             unsigned char *st = ring + stage * F::STAGE;
             const uint32_t kst = smem_addr(st), vst = kst + F::KW * F::RB;
-            const uint32_t h = put.c / (put.n_tiles / p.pool.n_kv_heads);
+            const Pending &u = pend[0];
             uint64_t mask = 0;
             int64_t off[F::KPL];
 #pragma unroll
             for (int i = 0; i < F::KPL; ++i) {
-                const uint32_t key = (put.u * WARPS + warp) * F::KW + i * 32 + lane;
-                const bool held = i * 32 + lane < F::KW && key < put.v.ctx, ok = held && (uint32_t)ids[0][i] < p.pool.n_blocks;
+                const uint32_t key = u.key0 + i * 32 + lane;
+                const bool held = i * 32 + lane < F::KW && key < u.ctx, ok = held && (uint32_t)u.id[i] < p.pool.n_blocks;
                 if (held && !ok) report(p.step, TUTTI_EFAULT);
                 mask |= (uint64_t)__ballot_sync(0xffffffffu, ok) << (32 * i);
                 if (C8 && i * 32 + lane < F::KW) {
-                    const uint64_t at = ok ? (uint64_t)ids[0][i] * p.pool.n_kv_heads + h : 0;
+                    const uint64_t at = ok ? (uint64_t)(uint32_t)u.id[i] * p.pool.n_kv_heads + u.h : 0;
                     cp4(kst + F::STAGE_BYTES + (i * 32 + lane) * 4, p.pool.k_scale + at, ok);
                     cp4(kst + F::STAGE_BYTES + (F::KW + i * 32 + lane) * 4, p.pool.v_scale + at, ok);
                 }
-                off[i] = ok ? block_offset(p.pool, ids[0][i]) + (int64_t)(key % p.pool.block_tokens * p.pool.tok_stride + h * p.pool.head_stride) : -1;
+                off[i] = ok ? block_offset(p.pool, u.id[i]) + (int64_t)(p.pool.row_of(key) * p.pool.tok_stride + u.h * p.pool.head_stride) : -1;
             }
             if (lane == 0) exists[stage] = mask;
 #pragma unroll
@@ -237,20 +240,18 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 cp16(vst + F::place(row, ch, true), (const void *)(p.pool.v_base + a), ok);
             }
             ++put_x;
-            if (put_x < x1) advance(p, F::ROWS, F::UNIT, put);
-#pragma unroll
-            for (int i = 0; i < F::KPL; ++i) ids[0][i] = ids[1][i];
-            locate(ids[1]);
+            pend[0] = pend[1];
+            locate(pend[1]);
         }
         cp_commit();
     };
 #pragma unroll
-    for (int i = 0; i < STAGES - 1; ++i) fetch(i);
+    for (int i = 0; i < F::STAGES - 1; ++i) fetch(i);
 
     // ---- the worker's tiles ----
     uint32_t stage = 0;
     for (unsigned long long x = x0; x < x1;) {
-        const uint32_t rts = get.n_tiles / p.pool.n_kv_heads, h = get.c / rts, row0 = (get.c % rts) * F::ROWS;
+        const uint32_t h = get.h, row0 = get.r * F::ROWS;
         const uint32_t n_rows = get.v.n_new * p.group;
         const int64_t first = (int64_t)get.v.ctx - get.v.n_new;
         const unsigned long long tile0 = x - get.u;                       // the tile's units: [tile0, tile0 + n_units)
@@ -327,9 +328,9 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         const int64_t last_all = first + row0 / p.group;        // keys up to here are seen by every row of the tile
 
         for (; x < seg_end; ++x) {
-            cp_wait<STAGES - 2>();
+            cp_wait<F::STAGES - 2>();
             __syncwarp();
-            fetch(stage == 0 ? STAGES - 1 : stage - 1);      // the stage before this one is free
+            fetch(stage == 0 ? F::STAGES - 1 : stage - 1);      // the stage before this one is free
             unsigned char *st = ring + stage * F::STAGE;
             const uint32_t kst = smem_addr(st), vst = kst + F::KW * F::RB;
             const uint64_t there = exists[stage];
@@ -360,7 +361,9 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                             const uint32_t lo[4] = {u.x, u.y, u.z, u.w}, hi[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                             for (int k = 0; k < 4; ++k) {
-                                const uint32_t a[4] = {codes2(lo[k]), codes2(hi[k]), codes2(lo[k] >> 16), codes2(hi[k] >> 16)};
+                                uint32_t a[4];
+                                codes4(lo[k], a[0], a[2]);
+                                codes4(hi[k], a[1], a[3]);
 #pragma unroll
                                 for (int b = 0; b < NB; ++b) mma(s[b][t], a, qf[b][d * 4 + k][0], qf[b][d * 4 + k][1], M());
                             }
@@ -468,9 +471,9 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
 #pragma unroll
                         for (int i = 0; i < F::DT; ++i) {
                             const uint32_t pick = i & 1 ? 0x7362 : 0x5140;       // two neighbouring dimensions of two keys
-                            const uint32_t x = __byte_perm(word[0][i / 2], word[1][i / 2], pick);
-                            const uint32_t y = __byte_perm(word[2][i / 2], word[3][i / 2], pick);
-                            const uint32_t a[4] = {codes2(x), codes2(x >> 16), codes2(y), codes2(y >> 16)};
+                            uint32_t a[4];
+                            codes4(__byte_perm(word[0][i / 2], word[1][i / 2], pick), a[0], a[1]);
+                            codes4(__byte_perm(word[2][i / 2], word[3][i / 2], pick), a[2], a[3]);
 #pragma unroll
                             for (int b = 0; b < NB; ++b) mma(o[b][i], a, pf[b][t][0], pf[b][t][1], M());
                         }
@@ -479,7 +482,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             }
             __syncwarp();
             if (x + 1 < seg_end) {
-                stage = stage + 1 == STAGES ? 0 : stage + 1;
+                stage = stage + 1 == F::STAGES ? 0 : stage + 1;
                 ++get.u;
             }
         }
@@ -532,7 +535,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             float4 a = make_float4(0, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
-                const float *src = reinterpret_cast<const float *>(smem + (i * STAGES + stage) * F::STAGE) + row * D;
+                const float *src = reinterpret_cast<const float *>(smem + (i * F::STAGES + stage) * F::STAGE) + row * D;
                 const float4 b = *reinterpret_cast<const float4 *>(src + (((j * TPR + lanec) * 4) ^ ((row >> 1 & 3) * 8)));
                 a.x += b.x, a.y += b.y, a.z += b.z, a.w += b.w;
             }
@@ -591,7 +594,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 p.lse[tok * p.n_q_heads + qh] = M_ == -INFINITY ? -INFINITY : (M_ - F::OFF + log2f(L)) * 0.6931471805599453f;
         }
         __syncthreads();                     // the stage and the small arrays may be written again
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        stage = stage + 1 == F::STAGES ? 0 : stage + 1;
         if (x < x1) advance(p, F::ROWS, F::UNIT, get);
     }
     cp_wait<0>();

@@ -241,9 +241,9 @@ __device__ inline uint64_t operand(uint32_t addr) {
 
 // Four codes as two pairs of 16-bit elements, not yet at their scale.  f16: the values, in order.
 __device__ inline uint2 spread(uint32_t w, __half) {
-    const __half2_raw a = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w & 0xffff), __NV_E4M3);
-    const __half2_raw b = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w >> 16), __NV_E4M3);
-    return make_uint2((uint32_t)a.x | (uint32_t)a.y << 16, (uint32_t)b.x | (uint32_t)b.y << 16);
+    uint2 r;
+    codes4(w, r.x, r.y);
+    return r;
 }
 // bf16: codes 0, 2 and 1, 3 (the queries are brought in the same order and the outputs leave in it),
 // the magnitude's 7 bits moved to where they are the value times 2^-120, subnormal codes included.
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint32_t key = key0 + i * 32 + lane;
-                id[i] = key < ctx ? __ldg(p.step.block_ids + t.v.b0 + key / bs) : -1;
+                id[i] = key < ctx ? __ldg(p.step.block_ids + t.v.b0 + p.pool.block_of(key)) : -1;
             }
         };
         auto resolve = [&]() {
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if (bad) report(p.step, TUTTI_EFAULT);
                 missing[i] = __ballot_sync(0xffffffffu, bad);
                 tiled = tiled && __all_sync(0xffffffffu, there);
-                off[i] = there ? block_offset(p.pool, id[i]) + (int64_t)(key % bs * p.pool.tok_stride + head * p.pool.head_stride) : -1;
+                off[i] = there ? block_offset(p.pool, id[i]) + (int64_t)(p.pool.row_of(key) * p.pool.tok_stride + head * p.pool.head_stride) : -1;
                 if constexpr (C8) {
                     const uint64_t at = there ? (uint64_t)id[i] * p.pool.n_kv_heads + head : 0;
                     ks[i] = there ? p.pool.k_scale[at] : 0.0f;
@@ -500,7 +500,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     if (lane == 0) mbar_expect(bar, 64 * RB);
                     __syncwarp();
                     if (my_part < PARTS) {
-                        const int32_t token = (int32_t)((key0 + row) % bs);
+                        const int32_t token = (int32_t)p.pool.row_of(key0 + row);
                         tile_load(dst + my_part * ATOM + (half * 64 + row) * 128, kv ? &maps.v : &maps.k, bar, (int32_t)(my_part * (C8 ? 128 : 64)),
                                   p.hnd ? token : (int32_t)head, p.hnd ? (int32_t)head : token, row < 32 ? lo : hi);
                     }

@@ -15,7 +15,20 @@ struct PoolView {
     uint32_t n_blocks, block_tokens, n_kv_heads, head_dim;
     uint64_t tok_stride, head_stride;       // bytes between tokens / heads of a block
     float *k_scale, *v_scale;               // [n_blocks][n_kv_heads], 8-bit pools only
+    uint32_t block_mul, block_shift;        // key / block_tokens = key * block_mul >> block_shift, for keys below 2^31
+
+    __host__ __device__ uint32_t block_of(uint32_t key) const { return (uint32_t)((uint64_t)key * block_mul >> block_shift); }
+    __host__ __device__ uint32_t row_of(uint32_t key) const { return key - block_of(key) * block_tokens; }
 };
+
+// n / d for n < 2^31 as a product and a shift (Granlund and Montgomery): with 2^s >= d the
+// multiplier floor(2^(31+s) / d) + 1 fits 32 bits and errs by less than 2^s / 2^31 a unit of n.
+inline void division_by(uint32_t d, uint32_t &mul, uint32_t &shift) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    shift = 31 + s;
+    mul = (uint32_t)((1ull << shift) / d + (d > 1 ? 1 : 0));
+}
 
 // Tensor maps of a pool layer, by pool layout (TUTTI_POOL_NHD, TUTTI_POOL_HND).
 struct PoolTensorMaps {
