@@ -27,7 +27,9 @@ namespace {
 // way round.  8-bit caches are multiplied as f16 codes (exact); the scale of a key goes onto
 // its score, the scale of a value onto its probability.
 constexpr int WARPS = 4;
-constexpr int STAGES = 3, STAGES_WIDE = 2;
+constexpr int STAGES = 3, STAGES_8 = 2;
+constexpr int WORKERS_8 = 3;
+constexpr uint32_t BYTES_8 = 8192;
 constexpr int MIN_UNITS = 2;                // of a worker: a worker more costs joining its part
 
 __device__ inline void ldm4(uint32_t (&r)[4], uint32_t a) {
@@ -89,9 +91,9 @@ struct Few {
     static constexpr int ROWS = 8 * NB;
     // 8-bit caches take more instructions a byte (widening): with 8 rows 128 registers are enough for
     // 16 warps an SM instead of 8, each with a stage less.
-    static constexpr int WORKERS_PER_SM = C8 && NB == 1 ? 4 : 2;
-    static constexpr int STAGES = C8 && NB == 1 ? STAGES_WIDE : tutti::STAGES;
-    static constexpr uint32_t STAGE_BYTES = C8 && NB == 1 && D == 64 ? 4096 : 8192;  // keys and values of one warp's KW keys
+    static constexpr int WORKERS_PER_SM = C8 && NB == 1 ? WORKERS_8 : 2;
+    static constexpr int STAGES = C8 && NB == 1 ? STAGES_8 : tutti::STAGES;
+    static constexpr uint32_t STAGE_BYTES = C8 && NB == 1 ? BYTES_8 : 8192;  // keys and values of one warp's KW keys
     static constexpr int RB = D * (C8 ? 1 : 2);                      // bytes of a row
     static constexpr int KW = STAGE_BYTES / (2 * RB);                // keys of a warp's step
     static constexpr int UNIT = WARPS * KW;
