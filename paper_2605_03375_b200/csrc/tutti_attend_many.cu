@@ -12,8 +12,12 @@
 //             its probabilities back over them (16 bits), rescales the output when the running
 //             maximum has grown by more than 2^8, and writes the row out at the end;
 //   8         issues the matrix instructions: S = Q K^T (both operands in shared memory),
-//             O += P V (P from TMEM).  The halves alternate, so the tensor cores work on one
-//             while the other is in its softmax;
+//             O += P V (P from TMEM).  Units are taken in two steps of 64 keys, each with
+//             its own columns of scores: a step's scores are ready before the softmax of the step
+//             before it has ended, so the softmax warps never wait for a product that depends on
+//             them (with one set of 128 columns a half, whose probabilities lie over its scores, they
+//             did: 3900 clocks a unit).  An instruction of 128 x 64 x 16 reads 6 KB of shared
+//             memory in the time of 4 KB, which makes Q K^T 1.5 times as long; P V is not touched;
 //   9-11      bring the queries of the next tile;
 //   12-15     gather keys and values through the block table into a ring of four 128-row tiles
 //             in the 128-byte swizzle (K: K-major B operand, V: the same bytes read as an
@@ -41,7 +45,8 @@ constexpr int RING = 4;                 // K and V tiles in flight
 constexpr int THREADS = 512;
 constexpr int MMA_WARP = 8, Q_WARP = 9, Q_WARPS = 3, KV_WARP = 12, KV_WARPS = 2;      // KV_WARPS: of a group
 constexpr uint32_t ATOM = BN * 128;     // 128 rows of 128 bytes
-constexpr int EARLY = 3;                // of the 4 groups of 32 keys: probabilities handed over before the rest is done
+constexpr int SUB_16 = 128, SUB_8 = 64;  // keys of a step, by the cache's bits
+constexpr int REGS_16 = 192, REGS_8 = 160;  // of a softmax thread; the other half of the threads has 256 less these
 constexpr float GROW = 8.0f;            // log2 of how far probabilities may exceed 1
 constexpr long long WAIT_CLOCKS = 3000000000ll;   // about 1.5 s: a wait that takes longer is given up
 
@@ -283,11 +288,13 @@ __device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __nv_bfloat1
 
 template <typename T, bool C8, int D>
 struct Many {
+    static constexpr int SUB = C8 ? SUB_8 : SUB_16, STEPS = BN / SUB;
+    static constexpr int SOFT_REGS = C8 ? REGS_8 : REGS_16;
     static constexpr uint32_t KV = ATOM * (D / 64);         // bytes of a 128-row tile
     static constexpr uint32_t OFF_RING = 2 * KV;            // behind the two halves of Q
     static constexpr uint32_t OFF_RAW = OFF_RING + RING * KV;          // 8-bit: codes of a group's values
     static constexpr uint32_t OFF_BAR = OFF_RAW + (C8 ? 2 * ATOM : 0);
-    static constexpr uint32_t OFF_EXISTS = OFF_BAR + 256;   // [8 units][4]: keys that exist
+    static constexpr uint32_t OFF_EXISTS = OFF_BAR + 288;   // [8 units][4]: keys that exist
     static constexpr uint32_t OFF_MISC = OFF_EXISTS + 128;
     static constexpr uint32_t SMEM = OFF_MISC + 256 + 1024; // 1024: alignment of the dynamic part
     // f16 codes are widened at half their value: scores and outputs make up for it
@@ -305,6 +312,7 @@ struct Many {
 template <typename T, bool C8, int D>
 __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ PoolMaps maps, const Workspace ws) {
     using C = Many<T, C8, D>;
+    constexpr int SUB = C::SUB, STEPS = C::STEPS;
     extern __shared__ unsigned char raw[];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
     unsigned char *sm = raw + (base - smem_addr(raw));
@@ -313,8 +321,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     uint32_t *exists = reinterpret_cast<uint32_t *>(sm + C::OFF_EXISTS);
     volatile uint32_t *dead = misc + 60;
     const uint32_t bars = base + C::OFF_BAR;
-    const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, s_full = bars + 80,
-                   p_full = bars + 96, o_full = bars + 112, o_empty = bars + 128, joined = bars + 144, drain = bars + 160, raw_full = bars + 168, p_late = bars + 232;
+    const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, o_full = bars + 80, o_empty = bars + 96,
+                   joined = bars + 112, drain = bars + 128, raw_full = bars + 136, s_full = bars + 200, p_full = bars + 232, o_done = bars + 264;
 
     // ---- this worker's share ----
     unsigned long long *sums = reinterpret_cast<unsigned long long *>(misc);
@@ -368,12 +376,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         mbar_init(q_full, Q_WARPS);
         mbar_init(q_empty, 1);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(s_full + 8 * i, 1);
-            mbar_init(p_full + 8 * i, 4);
             mbar_init(o_full + 8 * i, 1);
+            mbar_init(o_done + 8 * i, 1);
             mbar_init(o_empty + 8 * i, 4);
             mbar_init(joined + 8 * i, 4);
-            mbar_init(p_late + 8 * i, 4);
+        }
+        for (int i = 0; i < 4; ++i) {               // half x step of a unit
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_full + 8 * i, 4);
         }
         mbar_init(drain, 1);
         for (int i = 0; i < 2 * RING; ++i) mbar_init(raw_full + 8 * i, 1);
@@ -408,13 +418,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         t.u = (uint32_t)(rest - r.before(lo));
         t.n_units = r.units(lo);
     }
-    // scores (and probabilities over them) of the halves, then their outputs
-    auto S = [&](int i) { return tmem + i * 128; };
+    // scores (and probabilities over them) of a half and step, then the halves' outputs
+    auto S = [&](int i, int u) { return tmem + i * 128 + u * SUB; };
     auto O = [&](int i) { return tmem + 256 + i * D; };
 
-    // Registers: 512 x 128 at launch = 256 x 192 + 256 x 64; a softmax thread holds its row's 128 scores.
+    // Registers: 512 x 128 at launch = 256 x 160 + 256 x 96; a softmax thread holds 64 scores.
     if (warp >= MMA_WARP) {
-        setmaxnreg_dec<64>();
+        setmaxnreg_dec<256 - C::SOFT_REGS>();
         if (warp >= KV_WARP) {
         // =================================== keys and values ===================================
         const uint32_t group = (warp - KV_WARP) / KV_WARPS, half = (warp - KV_WARP) % KV_WARPS;     // rows [64 half, 64 half + 64)
@@ -655,29 +665,28 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             // the warp stays together; one elected lane issues, so operands live in uniform registers
             constexpr uint32_t FMT = std::is_same<T, __nv_bfloat16>::value ? 1 : 0;
             constexpr uint32_t IDESC = 1u << 4 | FMT << 7 | FMT << 10 | (uint32_t)(HALF_ROWS / 16) << 24;
-            constexpr uint32_t ID_QK = IDESC | (uint32_t)(BN / 8) << 17, ID_PV = IDESC | 1u << 16 | (uint32_t)(D / 8) << 17;
+            constexpr uint32_t ID_QK = IDESC | (uint32_t)(SUB / 8) << 17, ID_PV = IDESC | 1u << 16 | (uint32_t)(D / 8) << 17;
             uint32_t n_unit = 0, segs = 0, np[2] = {0, 0}, ns[2] = {0, 0};
             bool ok = true;
-            auto qk = [&](int i, uint32_t slot) {
-                const uint64_t a = operand(base + i * C::KV), b = operand(base + C::OFF_RING + slot * C::KV);
+            constexpr uint32_t STEP_BYTES = SUB * 128;          // from a step's rows to the next one's
+            auto qk = [&](int i, int u, uint32_t slot) {
+                const uint64_t a = operand(base + i * C::KV), b = operand(base + C::OFF_RING + slot * C::KV + u * STEP_BYTES);
                 if (elect()) {
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint64_t step = ((k / 4) * ATOM + (k % 4) * 32) >> 4;
-                        mma_ss(S(i), a + step, b + step, ID_QK, k > 0);
+                        mma_ss(S(i, u), a + step, b + step, ID_QK, k > 0);
                     }
-                    tc_commit(s_full + 8 * i);
+                    tc_commit(s_full + 8 * (2 * i + u));
                 }
                 __syncwarp();
             };
-            // part 0: the keys whose probabilities come first; part 1: the others
-            auto pv = [&](int i, uint32_t slot, bool acc, int part) {
-                const uint64_t b = operand(base + C::OFF_RING + slot * C::KV);
+            auto pv = [&](int i, int u, uint32_t slot, bool acc) {
+                const uint64_t b = operand(base + C::OFF_RING + slot * C::KV + u * STEP_BYTES);
                 if (elect()) {
 #pragma unroll
-                    for (int k = 0; k < BN / 16; ++k)
-                        if ((k >= 2 * EARLY) == part) mma_ts(O(i), S(i) + k * 8, b + ((k * 2048) >> 4), ID_PV, acc || k > 0);
-                    if (part) tc_commit(o_full + 8 * i);
+                    for (int k = 0; k < SUB / 16; ++k) mma_ts(O(i), S(i, u) + k * 8, b + ((k * 2048) >> 4), ID_PV, acc || k > 0);
+                    tc_commit(o_full + 8 * i);
                 }
                 __syncwarp();
             };
@@ -695,28 +704,31 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 ok = all(mbar_wait(q_full, segs & 1, dead) && landed(n_unit, 0));
                 if (!ok) break;
                 tc_after();
-                for (int i = 0; i < halves; ++i) qk(i, slot(n_unit, 0));
+                for (int u = 0; u < STEPS; ++u)
+                    for (int i = 0; i < halves; ++i) qk(i, u, slot(n_unit, 0));
                 commit(empty + 8 * slot(n_unit, 0));
                 for (uint32_t j = 0; j < n && ok; ++j, ++n_unit) {
                     const bool more = j + 1 < n;
                     ok = all(landed(n_unit, 1) && (!more || landed(n_unit + 1, 0)));
-                    for (int i = 0; i < halves && ok; ++i) {
-                        ok = mbar_wait(p_full + 8 * i, np[i]++ & 1, dead);
-                        if (ok && j == 0 && ns[i]) ok = mbar_wait(o_empty + 8 * i, (ns[i] - 1) & 1, dead);
-                        if (!(ok = all(ok))) break;
-                        tc_after();
-                        pv(i, slot(n_unit, 1), j > 0, 0);
-                        if (!(ok = all(mbar_wait(p_late + 8 * i, (np[i] - 1) & 1, dead)))) break;
-                        tc_after();
-                        pv(i, slot(n_unit, 1), true, 1);
-                        if (more) qk(i, slot(n_unit + 1, 0));
-                    }
+                    for (int u = 0; u < STEPS && ok; ++u)
+                        for (int i = 0; i < halves && ok; ++i) {
+                            ok = mbar_wait(p_full + 8 * (2 * i + u), np[i] & 1, dead);
+                            if (ok && j == 0 && u == 0 && ns[i]) ok = mbar_wait(o_empty + 8 * i, (ns[i] - 1) & 1, dead);
+                            if (!(ok = all(ok))) break;
+                            tc_after();
+                            pv(i, u, slot(n_unit, 1), j > 0 || u > 0);
+                            if (more) qk(i, u, slot(n_unit + 1, 0));
+                            np[i] += u == STEPS - 1;
+                        }
                     if (!ok) break;
                     commit(empty + 8 * slot(n_unit, 1));
                     if (more) commit(empty + 8 * slot(n_unit + 1, 0));
                 }
                 if (!ok) break;
-                for (int i = 0; i < halves; ++i) ++ns[i];
+                for (int i = 0; i < halves; ++i) {
+                    commit(o_done + 8 * i);
+                    ++ns[i];
+                }
                 commit(q_empty);
                 ++segs;
                 x += n;
@@ -731,12 +743,12 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         }
     } else {
         // =================================== softmax ===================================
-        setmaxnreg_inc<192>();
+        setmaxnreg_inc<C::SOFT_REGS>();
         const int i = warp / 4;                                   // half
-        const uint32_t lanes = (warp % 4) * 32 << 16, s_at = S(i) + lanes, o_at = O(i) + lanes, r = (warp % 4) * 32 + lane;
+        const uint32_t lanes = (warp % 4) * 32 << 16, o_at = O(i) + lanes, r = (warp % 4) * 32 + lane;
         const float scl = fmaxf(fabsf(p.scale) * 1.4426950408889634f * C::VALUE, 1e-30f);
         const bool negative = p.scale < 0;
-        uint32_t n_s = 0, n_unit = 0, n_join = 0;                 // scores seen by this half; units of the worker
+        uint32_t n_s = 0, n_seg = 0, n_unit = 0, n_join = 0;                 // steps of this half; units of the worker
         bool ok = true;
         auto join = [&]() {                                       // the half's four warps
             __syncwarp();
@@ -754,64 +766,49 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 const int64_t pos = t.r.first + tok;
                 const int64_t pos_low = __shfl_sync(0xffffffffu, pos, 0);
                 float m = -INFINITY, l = 0;
-                for (uint32_t j = 0; j < n && ok; ++j) {
-                    ok = mbar_wait(s_full + 8 * i, n_s & 1, dead);
+                const uint32_t steps = STEPS * n;
+                for (uint32_t j = 0; j < steps && ok; ++j) {
+                    const int u = j % STEPS;
+                    const uint32_t s_at = S(i, u) + lanes;
+                    ok = mbar_wait(s_full + 8 * (2 * i + u), n_s / STEPS & 1, dead);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     tc_after();
-                    uint32_t sr[128];
+                    uint32_t sr[SUB];
                     float *s = reinterpret_cast<float *>(sr);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) tc_ld32(sr + 32 * q, s_at + 32 * q);
-                    const uint4 ex = *reinterpret_cast<const uint4 *>(exists + ((n_unit + j) & 7) * 4);
+                    for (int q = 0; q < SUB / 32; ++q) tc_ld32(sr + 32 * q, s_at + 32 * q);
+                    uint32_t ex[SUB / 32], all = ~0u;             // keys that exist
+#pragma unroll
+                    for (int q = 0; q < SUB / 32; ++q) {
+                        ex[q] = exists[((n_unit + j / STEPS) & 7) * 4 + SUB / 32 * u + q];
+                        all &= ex[q];
+                    }
                     tc_wait_ld();
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) tc_loaded(sr + 32 * q);
-                    const int64_t key0 = (int64_t)(t.u + j) * BN;
+                    for (int q = 0; q < SUB / 32; ++q) tc_loaded(sr + 32 * q);
+                    const int64_t key0 = (int64_t)t.u * BN + j * SUB;
                     if (negative) {
 #pragma unroll
-                        for (int k = 0; k < 128; ++k) s[k] = -s[k];
+                        for (int k = 0; k < SUB; ++k) s[k] = -s[k];
                     }
-                    if (key0 + BN - 1 > pos_low || (ex.x & ex.y & ex.z & ex.w) != ~0u) {
+                    if (key0 + SUB - 1 > pos_low || all != ~0u) {
                         const int64_t d = pos - key0;
-                        const int lim = d < -1 ? -1 : d > BN ? BN : (int)d;
-                        const uint32_t word[4] = {ex.x, ex.y, ex.z, ex.w};
+                        const int lim = d < -1 ? -1 : d > SUB ? SUB : (int)d;
 #pragma unroll
-                        for (int k = 0; k < 128; ++k)
-                            if (k > lim || !(word[k / 32] >> (k % 32) & 1)) s[k] = -INFINITY;
+                        for (int k = 0; k < SUB; ++k)
+                            if (k > lim || !(ex[k / 32] >> (k % 32) & 1)) s[k] = -INFINITY;
                     }
-                    // Exponentials of groups [from, to) of 32 scores against the reference m; 16 bits of
-                    // each go back to TMEM, their 32-bit sums to l0 and l1.
-                    f2 l0, l1;
-                    auto exps = [&](int from, int to) {
-                        const float sub = C::OFF - (m == -INFINITY ? 0.0f : m);
-                        const f2 scl2 = pair(scl, scl), sub2 = pair(sub, sub);
-#pragma unroll
-                        for (int q = from; q < to; ++q) {
-                            uint32_t pk[16];
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                float a, b;
-                                unpair(fma2(pair(s[32 * q + 2 * k], s[32 * q + 2 * k + 1]), scl2, sub2), a, b);
-                                a = ex2(a);
-                                b = ex2(b);
-                                if (k & 1) l1 = add2(l1, pair(a, b));
-                                else l0 = add2(l0, pair(a, b));
-                                pk[k] = pack2(a, b, T());
-                            }
-                            tc_st16(pk, s_at + 16 * q);
-                        }
-                    };
                     float a0 = max3(s[0], s[4], s[8]), a1 = max3(s[1], s[5], s[9]), a2 = max3(s[2], s[6], s[10]), a3 = max3(s[3], s[7], s[11]);
 #pragma unroll
-                    for (int k = 12; k < 124; k += 8) {
+                    for (int k = 12; k < SUB - 4; k += 8) {
                         a0 = max3(a0, s[k], s[k + 4]);
                         a1 = max3(a1, s[k + 1], s[k + 5]);
                         a2 = max3(a2, s[k + 2], s[k + 6]);
                         a3 = max3(a3, s[k + 3], s[k + 7]);
                     }
-                    a0 = max3(a0, s[124], s[125]);
-                    a1 = max3(a1, s[126], s[127]);
+                    a0 = max3(a0, s[SUB - 4], s[SUB - 3]);
+                    a1 = max3(a1, s[SUB - 2], s[SUB - 1]);
                     const float top = max3(a0, a1, fmaxf(a2, a3)) * scl;
                     const bool grow = top > m + GROW || (m == -INFINITY && top > m);
                     if (__any_sync(0xffffffffu, grow)) {          // rare: the reference has to move
@@ -819,6 +816,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         if (grow) m = top;
                         l *= alpha;
                         if (j > 0) {
+                            // these scores were issued behind the product two steps back, so only the last one's may be open
                             ok = mbar_wait(o_full + 8 * i, (n_s - 1) & 1, dead);
                             ok = __all_sync(0xffffffffu, ok);
                             if (!ok) break;
@@ -835,24 +833,37 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                             }
                         }
                     }
-                    l0 = l1 = 0;
-                    exps(0, EARLY);
-                    tc_wait_st();
-                    tc_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(p_full + 8 * i);
-                    exps(EARLY, 4);
+                    // exponentials against the reference; 16 bits of each go over the scores, their 32-bit sums to l
+                    const float sub = C::OFF - (m == -INFINITY ? 0.0f : m);
+                    const f2 scl2 = pair(scl, scl), sub2 = pair(sub, sub);
+                    f2 l0 = 0, l1 = 0;
+#pragma unroll
+                    for (int q = 0; q < SUB / 32; ++q) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            float a, b;
+                            unpair(fma2(pair(s[32 * q + 2 * k], s[32 * q + 2 * k + 1]), scl2, sub2), a, b);
+                            a = ex2(a);
+                            b = ex2(b);
+                            if (k & 1) l1 = add2(l1, pair(a, b));
+                            else l0 = add2(l0, pair(a, b));
+                            pk[k] = pack2(a, b, T());
+                        }
+                        tc_st16(pk, s_at + 16 * q);
+                    }
                     float la, lb;
                     unpair(add2(l0, l1), la, lb);
                     l += la + lb;
                     tc_wait_st();
                     tc_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(p_late + 8 * i);
+                    if (lane == 0) mbar_arrive(p_full + 8 * (2 * i + u));
                     ++n_s;
                 }
                 if (!ok) break;
-                ok = mbar_wait(o_full + 8 * i, (n_s - 1) & 1, dead);
+                // (o_full would not do: two of its phases may be open here, and one bit does not tell them apart)
+                ok = mbar_wait(o_done + 8 * i, n_seg++ & 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_after();
