@@ -588,14 +588,22 @@ int tutti_kv_append_layer(tutti_ctx_t *ctx, uint32_t layer, const tutti_step_t *
  *     out = sum_j softmax_j(scale * q . k_j) v_j,   lse = ln sum_j exp(scale * q . k_j)
  * A row that sees no key (padding, or only blocks outside the pool) gets out = 0 and
  * lse = -infinity.  Cache bytes behind a sequence's last token are never used, whatever they
- * hold.  Sums and softmax statistics are 32-bit; probabilities are rounded to 16 bits for
- * the product with the values.
- * The handle holds the workspace in which parts of a long sequence are joined: calls on one
- * handle must be ordered after each other (one stream, or events; replays of captured graphs
- * too), calls that may overlap need a handle each.
+ * hold.  (A key that is NaN or infinite reaches only the rows that see it; a VALUE of one of the
+ * step's own tokens that is NaN or infinite may also reach rows of the same sequence's step that
+ * come before it, as 0 * NaN.)
+ * Sums and softmax statistics are 32-bit.  Probabilities are rounded to 16 bits for the product
+ * with the values; keys and values of an 8-bit pool are code * scale, without a rounding of their
+ * own for the scales that the append call makes (others may be rounded to the 16 bits of dtype).
+ * The result of a call does not depend on the order in which the GPU runs its parts.
+ * The handle holds the workspace in which parts of a long sequence are joined (about 40 MB): calls
+ * on one handle must be ordered after each other (one stream, or events; replays of captured
+ * graphs too), calls that may overlap need a handle each.  Destroy it before its context.  Every
+ * wait inside the kernels is bounded; one that runs out is reported as TUTTI_ETIMEDOUT in *status,
+ * the outputs are then incomplete and the handle must not be used again.
  * Asynchronous on `stream`, graph-capturable.  TUTTI_EINVAL for a layer that is not
  * registered, head_dim other than 64 or 128, elem_bytes other than 2, or 1 with registered
- * scales; n_q_heads not a multiple of n_kv_heads; a bad stride, alignment, type or scale.
+ * scales; n_q_heads not a multiple of n_kv_heads; out equal to q (they must not overlap); more
+ * than 2^31 - 1 rows (n_tok * n_q_heads); a bad stride, alignment, type or scale.
  */
 typedef struct tutti_attn tutti_attn_t;
 int tutti_attn_create(tutti_ctx_t *ctx, tutti_attn_t **out);

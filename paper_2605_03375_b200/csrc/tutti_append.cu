@@ -500,14 +500,9 @@ int tutti_kv_append_layer(tutti_ctx_t *ctx, uint32_t layer, const tutti_step_t *
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const bool bf = t->dtype == TUTTI_DTYPE_BF16;
     cudaStream_t st = (cudaStream_t)stream;
-    if (elem_bytes == 2) {
-        if (bf) append_kernel<__nv_bfloat16><<<grid, THREADS, 0, st>>>(p);
-        else append_kernel<__half><<<grid, THREADS, 0, st>>>(p);
-    } else {
-        if (bf) append8_kernel<__nv_bfloat16><<<grid, THREADS, 0, st>>>(p);
-        else append8_kernel<__half><<<grid, THREADS, 0, st>>>(p);
-    }
-    const cudaError_t e = cudaGetLastError();
+    const auto kernel = elem_bytes == 2 ? (bf ? append_kernel<__nv_bfloat16> : append_kernel<__half>)
+                                        : (bf ? append8_kernel<__nv_bfloat16> : append8_kernel<__half>);
+    const cudaError_t e = launch_plain(kernel, grid, THREADS, 0, st, p);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "append launch");
 }
 

@@ -38,7 +38,9 @@ int tutti_attend_check_(const tutti_geom_t *g, const tutti_step_t *step, const t
     if (io->dtype != TUTTI_DTYPE_BF16 && io->dtype != TUTTI_DTYPE_FP16) return TUTTI_EINVAL;
     if (!io->n_q_heads || io->n_q_heads % g->n_kv_heads || io->n_q_heads > 65536) return TUTTI_EINVAL;
     if (!std::isfinite(io->scale) || io->reserved) return TUTTI_EINVAL;
+    if ((uint64_t)step->n_tok * io->n_q_heads > 0x7fffffffull) return TUTTI_EINVAL;
     if (!step->n_tok || !step->n_seq) return TUTTI_OK;
+    if (io->q == io->out) return TUTTI_EINVAL;
     if (!rows_ok(io->q, io->q_stride, io->n_q_heads, g->head_dim) ||
         !rows_ok(io->out, io->out_stride, io->n_q_heads, g->head_dim) || ((uint64_t)io->lse & 3))
         return TUTTI_EINVAL;
@@ -102,7 +104,6 @@ int tutti_kv_attend_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *s
     p.out = io->out;
     p.lse = io->lse;
     p.scale = io->scale;
-    p.hnd = p.pool.head_stride > p.pool.tok_stride;
     OnDevice on(tutti_ctx_device_(a->ctx));
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const bool bf = io->dtype == TUTTI_DTYPE_BF16;

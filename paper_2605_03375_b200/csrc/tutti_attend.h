@@ -17,7 +17,6 @@ struct AttendParams {
     void *out;
     float *lse;
     float scale;
-    bool hnd;                         // head-major pool blocks
 };
 
 // Tile loads of the layer's keys and values.

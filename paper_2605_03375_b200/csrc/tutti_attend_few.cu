@@ -103,9 +103,10 @@ struct Few {
     static constexpr int CH = RB / 16;                               // 16-byte chunks of a row
     static constexpr uint32_t SCALES = C8 ? KW * 8 : 0;              // scales of the stage's keys, then values
     static constexpr uint32_t STAGE = STAGE_BYTES + SCALES;
-    // probabilities are kept 2^OFF times too large where they are rounded to f16: full precision
-    // down to 2^-28 of the largest instead of 2^-14
-    static constexpr float OFF = std::is_same<M, __half>::value ? 14.0f : 0.0f;
+    // f16 probabilities are kept 2^OFF times too large: full precision down to 2^-28 of the largest
+    // instead of 2^-14.  (8-bit: the products with the value scales are, see `unit` below.)
+    static constexpr float OFF = std::is_same<M, __half>::value && !C8 ? 14.0f : 0.0f;
+    static constexpr float UP = 16384.0f;
     static constexpr uint32_t OFF_MASK = WARPS * STAGES * STAGE;     // uint64 keys that exist, by warp and stage
     static constexpr uint32_t OFF_ML = OFF_MASK + WARPS * STAGES * 8;
     static constexpr uint32_t OFF_PLAN = OFF_ML + WARPS * ROWS * 8;
@@ -319,9 +320,13 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             }
         }
         float o[NB][F::DT][4], m[NB][2], l[NB][2];
-        float vtop = 0;                      // 8-bit: power of two at or above no value scale so far; O is in its units
+        // 8-bit: a row's O is kept in units of a power of two near its largest product of probability and
+        // value scale so far, so that the f16 products hold what counts in the row whatever the
+        // scales of other blocks are.
+        float unit[NB][2];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
+            unit[b][0] = unit[b][1] = 0;
             m[b][0] = m[b][1] = -INFINITY;
             l[b][0] = l[b][1] = 0;
 #pragma unroll
@@ -373,25 +378,13 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                     }
                 }
                 const bool masked = there != ALL || key0 + F::KW - 1 > last_all;
-                float vs[F::MT][2], vinv = 1.0f, vdown = 1.0f;      // 8-bit: value scales of the lane's keys
+                float vs[F::MT][2];                      // 8-bit: value scales of the lane's keys
                 if constexpr (C8) {
-                    float vmax = 0;
 #pragma unroll
                     for (int t = 0; t < F::MT; ++t)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
+                        for (int i = 0; i < 2; ++i)
                             vs[t][i] = *reinterpret_cast<const float *>(st + F::STAGE_BYTES + (F::KW + t * 16 + g + 8 * i) * 4);
-                            vmax = fmaxf(vmax, vs[t][i]);
-                        }
-                    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, 4));
-                    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, 8));
-                    vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, 16));
-                    vmax = __uint_as_float(min(max(__float_as_uint(vmax) >> 23, 1u), 253u) << 23);
-                    if (vmax > vtop) {
-                        vdown = vtop / vmax;
-                        vtop = vmax;
-                    }
-                    vinv = 1.0f / vtop;
                 }
                 uint32_t pf[NB][F::MT][2];
 #pragma unroll
@@ -419,8 +412,33 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                         alpha[r] = ex2(m[b][r] - sub[r]);
                         m[b][r] = m2;
                         l[b][r] *= alpha[r];
-                        alpha[r] *= vdown;
                         sub[r] -= F::OFF;
+                    }
+                    float up[2] = {1.0f, 1.0f}, most[2] = {0, 0};
+#pragma unroll
+                    for (int t = 0; t < F::MT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            s[b][t][e] = ex2(s[b][t][e] - sub[e & 1]);
+                            l[b][e & 1] += s[b][t][e];
+                            if constexpr (C8) {
+                                s[b][t][e] *= vs[t][e / 2];
+                                most[e & 1] = fmaxf(most[e & 1], s[b][t][e]);
+                            }
+                        }
+                    if constexpr (C8) {
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            most[r] = fmaxf(most[r], __shfl_xor_sync(0xffffffffu, most[r], 4));
+                            most[r] = fmaxf(most[r], __shfl_xor_sync(0xffffffffu, most[r], 8));
+                            most[r] = fmaxf(most[r], __shfl_xor_sync(0xffffffffu, most[r], 16));
+                            most[r] = fmaxf(most[r], unit[b][r] * alpha[r]);
+                            // the power of two at or below it, between 2^-100 and 2^126
+                            const float next = __uint_as_float(min(max(__float_as_uint(most[r]) >> 23, 27u), 253u) << 23);
+                            alpha[r] *= unit[b][r] / next;
+                            unit[b][r] = next;
+                            up[r] = F::UP / next;
+                        }
                     }
                     if (__any_sync(0xffffffffu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {
 #pragma unroll
@@ -431,17 +449,11 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                             o[b][i][3] *= alpha[1];
                         }
                     }
+                    // from (key g, rows 2 c and 2 c + 1) to (row g, keys 2 c and 2 c + 1)
 #pragma unroll
                     for (int t = 0; t < F::MT; ++t)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float x0_ = ex2(s[b][t][2 * i] - sub[0]), x1_ = ex2(s[b][t][2 * i + 1] - sub[1]);
-                            l[b][0] += x0_;
-                            l[b][1] += x1_;
-                            const float f = C8 ? vs[t][i] * vinv : 1.0f;
-                            // from (key g, rows 2 c and 2 c + 1) to (row g, keys 2 c and 2 c + 1)
-                            pf[b][t][i] = transpose8(C8 ? pack2(x0_ * f, x1_ * f, M()) : pack2(x0_, x1_, M()));
-                        }
+                        for (int i = 0; i < 2; ++i) pf[b][t][i] = transpose8(pack2(s[b][t][2 * i] * up[0], s[b][t][2 * i + 1] * up[1], M()));
                 }
                 // values
 #pragma unroll
@@ -510,7 +522,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 float top = -INFINITY;
 #pragma unroll
                 for (int i = 0; i < WARPS; ++i) top = fmaxf(top, ml[i * F::ROWS + row].x);
-                const float f = top == -INFINITY ? 0 : ex2(m[b][r] - top) * (C8 ? vtop : 1.0f);
+                const float f = top == -INFINITY ? 0 : ex2(m[b][r] - top) * (C8 ? unit[b][r] * (1.0f / F::UP) : 1.0f);
                 float *dst = mine_o + row * D;
 #pragma unroll
                 for (int i = 0; i < F::DT; ++i) {
@@ -606,8 +618,7 @@ template <typename T, bool C8, int D, int NB>
 cudaError_t launch_few(const AttendParams &p, Workspace ws, int sms, cudaStream_t st) {
     using F = Few<T, C8, D, NB>;
     ws.workers = sms * F::WORKERS_PER_SM;
-    attend_few_kernel<T, C8, D, NB><<<ws.workers, WARPS * 32, F::SMEM, st>>>(p, ws);
-    return cudaGetLastError();
+    return launch_plain(attend_few_kernel<T, C8, D, NB>, ws.workers, WARPS * 32, F::SMEM, st, p, ws);
 }
 
 template <typename T, bool C8, int D, int NB>

@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     if (my_part < PARTS) {
                         const int32_t token = (int32_t)p.pool.row_of(key0 + row);
                         tile_load(dst + my_part * ATOM + (half * 64 + row) * 128, kv ? &maps.v : &maps.k, bar, (int32_t)(my_part * (C8 ? 128 : 64)),
-                                  p.hnd ? token : (int32_t)head, p.hnd ? (int32_t)head : token, row < 32 ? lo : hi);
+                                  p.pool.hnd ? token : (int32_t)head, p.pool.hnd ? (int32_t)head : token, row < 32 ? lo : hi);
                     }
                 } else {
                     const uint64_t from = kv ? p.pool.v_base : p.pool.k_base;
@@ -946,8 +946,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 
 template <typename T, bool C8, int D>
 cudaError_t launch(const AttendParams &p, const PoolMaps &maps, const Workspace &ws, cudaStream_t st) {
-    attend_many_kernel<T, C8, D><<<ws.workers, THREADS, Many<T, C8, D>::SMEM, st>>>(p, maps, ws);
-    return cudaGetLastError();
+    return launch_plain(attend_many_kernel<T, C8, D>, ws.workers, THREADS, Many<T, C8, D>::SMEM, st, p, maps, ws);
 }
 
 template <typename T, bool C8>

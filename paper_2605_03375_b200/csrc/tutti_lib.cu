@@ -310,7 +310,7 @@ int tutti_ctx_pool_view_(tutti_ctx_t *ctx, uint32_t layer, PoolView *v, uint32_t
     *v = PoolView{p.k_base, p.v_base, p.block_stride, (uint32_t)p.n_blocks, g.block_tokens, g.n_kv_heads,
                   g.head_dim, ctx->pool_hnd ? row : ctx->layout.token_bytes,
                   ctx->pool_hnd ? row * g.block_tokens : row,
-                  ctx->scales[layer].first, ctx->scales[layer].second, 0, 0};
+                  ctx->scales[layer].first, ctx->scales[layer].second, ctx->pool_hnd, 0, 0};
     division_by(g.block_tokens, v->block_mul, v->block_shift);
     *elem_bytes = g.elem_bytes;
     return TUTTI_OK;

@@ -15,6 +15,7 @@ struct PoolView {
     uint32_t n_blocks, block_tokens, n_kv_heads, head_dim;
     uint64_t tok_stride, head_stride;       // bytes between tokens / heads of a block
     float *k_scale, *v_scale;               // [n_blocks][n_kv_heads], 8-bit pools only
+    bool hnd;                               // head-major blocks
     uint32_t block_mul, block_shift;        // key / block_tokens = key * block_mul >> block_shift, for keys below 2^31
 
     __host__ __device__ uint32_t block_of(uint32_t key) const { return (uint32_t)((uint64_t)key * block_mul >> block_shift); }
@@ -122,6 +123,18 @@ inline int check_step(const tutti_step_t *st) {
 // [n_tok][heads][head_dim] 16-bit elements at p, `stride` elements from token to token.
 inline bool rows_ok(const void *p, uint64_t stride, uint64_t heads, uint64_t head_dim) {
     return p && ((uint64_t)p & 15) == 0 && stride % 8 == 0 && stride >= heads * head_dim && stride < (1ull << 31);
+}
+
+// A launch whose own status is returned: an error that another call of the program left behind is
+// neither taken for this launch's nor cleared.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_plain(void (*kernel)(KArgs...), uint32_t grid, uint32_t block, size_t smem, cudaStream_t stream, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 // Makes a device current for a scope.

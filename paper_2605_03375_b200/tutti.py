@@ -300,6 +300,8 @@ def make_batch(hit_tokens, obj_start, obj_slot, blk_start, block_ids, plan_epoch
 
 def make_step(q_start, ctx_len, blk_start, block_ids, n_tok: int, max_new: int, status=None) -> Step:
     """Step struct over device tensors (int32): one step's tokens against the pool."""
+    if any(t.element_size() != 4 or not t.is_contiguous() for t in (q_start, ctx_len, blk_start, block_ids)):
+        raise TuttiError(EINVAL, "step tables (int32, contiguous)")
     s = Step(int(ctx_len.numel()), n_tok, int(block_ids.numel()), max_new, q_start.data_ptr(),
              ctx_len.data_ptr(), blk_start.data_ptr(), block_ids.data_ptr(),
              None if status is None else status.data_ptr())

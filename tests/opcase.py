@@ -130,6 +130,11 @@ class OpCase:
             out[b * self.bs:b * self.bs + m] = x[:m]
         return out
 
+    def key_scales(self, scale, half, s, n):
+        """The scales behind keys(), [n, head]."""
+        ids = self.block_ids[self.blk_start[s] + np.arange(n) // self.bs]
+        return scale[half].double().numpy()[ids] if scale is not None else np.ones((n, self.hk))
+
     def attend64(self, q, raw, scale, sm):
         """(out, lse, bound of |out error| for a 16-bit kernel, bound of |lse error|) for rows [0, q_start[-1])."""
         half_step, tiny = HALF[self.dtype]
@@ -142,6 +147,7 @@ class OpCase:
             total = int(self.ctx_len[s])
             first = total - n
             k, v = (self.keys(raw, scale, h, s, total) for h in range(2))
+            vs = self.key_scales(scale, 1, s, total)
             for i in range(n):
                 seen = first + i + 1
                 if seen <= 0:
@@ -152,6 +158,10 @@ class OpCase:
                     x = kk @ q[row, h] * sm
                     # 32-bit products and sums of a score; its exponential's argument and result
                     d = (self.dim * F32 * (np.abs(kk) @ np.abs(q[row, h]))).max() * abs(sm) + 4 * F32 * (np.abs(x).max() + 16)
+                    # fp16 over an 8-bit pool: keys and values may be rounded to f16 at half their size,
+                    # which is off by 2^-24 at most where that is below the normal range
+                    low = 2.0 ** -24 if self.cache == "8" and self.dtype == "fp16" else 0.0
+                    d += low * np.abs(q[row, h]).sum() * abs(sm)
                     m = x.max()
                     e = np.exp(x - m)
                     l = e.sum()
@@ -159,9 +169,14 @@ class OpCase:
                     out[row, h] = w @ vv
                     lse[row, h] = m + np.log(l)
                     size = w @ np.abs(vv)
+                    # Products of probability and value scale that are rounded to f16 are also off by half
+                    # its smallest step, 2^-25, in units that make the row's largest such product 2^6 at
+                    # least (2^14 where the rows of a step are few): 2^-31 of that product a key, times its code.
+                    f16 = self.dtype == "fp16" or self.cache == "8"
+                    floor = 2.0 ** -31 * (w * vs[:seen, h // g]).max() * (np.abs(vv) / vs[:seen, h // g, None]).sum(0) if f16 else 0.0
                     # the result rounded once, the probabilities rounded to 16 bits, the scores off by
                     # d, and 32-bit sums over the keys
-                    tol[row, h] = half_step * np.abs(out[row, h]) + tiny + (half_step + 2 * d + (seen + 64) * F32 + 2 ** -20) * size
+                    tol[row, h] = half_step * np.abs(out[row, h]) + tiny + low + floor + (half_step + 2 * d + (seen + 64) * F32 + 2 ** -20) * size
                     ltol[row, h] = 2 * d + (seen + 64) * F32 + 2 ** -20 + 4 * F32 * abs(lse[row, h])
         return out, lse, tol, ltol
 

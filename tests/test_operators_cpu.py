@@ -99,10 +99,15 @@ def test_geometries_that_attend_refuses(kw):
 
 
 @pytest.mark.parametrize("kw", [dict(dtype=3), dict(n_q_heads=0), dict(n_q_heads=5), dict(q_stride=1000), dict(out_stride=1020),
-                                dict(q=None), dict(out=None), dict(q=0x10008), dict(lse=0x30002), dict(scale=float("inf")),
+                                dict(q=None), dict(out=None), dict(out=0x10000), dict(q=0x10008), dict(lse=0x30002), dict(scale=float("inf")),
                                 dict(scale=float("nan")), dict(reserved=1)])
 def test_attends_that_are_refused(kw):
     assert attend_rc(a=attend(**kw)) == T.EINVAL
+
+
+def test_more_rows_than_are_counted_in_31_bits():
+    assert attend_rc(s=step(n_tok=1 << 28), a=attend(n_q_heads=8)) == T.EINVAL
+    assert attend_rc(s=step(n_tok=(1 << 28) - 1), a=attend(n_q_heads=8)) == T.OK
 
 
 def test_null_handles():
