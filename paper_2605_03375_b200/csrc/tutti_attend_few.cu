@@ -30,7 +30,7 @@ constexpr int WARPS = 4;
 constexpr int STAGES = 3, STAGES_8 = 2;
 constexpr int WORKERS_8 = 3;
 constexpr uint32_t BYTES_8 = 8192;
-constexpr int MIN_UNITS = 2;                // of a worker: a worker more costs joining its part
+constexpr int MIN_UNITS = 2;                // of a worker that takes a part of a tile: joining the parts costs, too
 
 __device__ inline void ldm4(uint32_t (&r)[4], uint32_t a) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
@@ -136,6 +136,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     // ---- this worker's share: a prefix sum over the sequences' units ----
     const uint32_t per = (p.step.n_seq + WARPS * 32 - 1) / (WARPS * 32);
     unsigned long long mine = 0;
+    uint32_t my_tiles = 0;
     Cursor own;                                    // the thread's last sequence (its only one, mostly)
     own.s = ~0u;
     for (uint32_t s = threadIdx.x * per; s < min((threadIdx.x + 1) * per, p.step.n_seq); ++s) {
@@ -143,6 +144,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         own.s = s;
         if (code != TUTTI_OK && blockIdx.x == 0) report(p.step, code);
         mine += (unsigned long long)own.n_tiles * own.n_units * p.pool.n_kv_heads;
+        my_tiles += own.n_tiles * p.pool.n_kv_heads;
     }
     unsigned long long incl = mine;
 #pragma unroll
@@ -151,15 +153,20 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         if (lane >= o) incl += x;
     }
     unsigned long long *sums = reinterpret_cast<unsigned long long *>(plan);
-    if (lane == 31) sums[warp] = incl;
+    my_tiles = __reduce_add_sync(0xffffffffu, my_tiles);
+    if (lane == 31) sums[warp] = incl, plan[2 * WARPS + warp] = my_tiles;
     __syncthreads();
+    uint32_t tiles = 0;
     unsigned long long total = 0, before = 0;
 #pragma unroll
     for (int i = 0; i < WARPS; ++i) {
         if (i < (int)warp) before += sums[i];
         total += sums[i];
+        tiles += plan[2 * WARPS + i];
     }
-    const unsigned long long wanted = (total + MIN_UNITS - 1) / MIN_UNITS, workers = wanted < ws.workers ? wanted : ws.workers;
+    unsigned long long workers = (total + MIN_UNITS - 1) / MIN_UNITS;
+    if (workers < tiles) workers = tiles;
+    if (workers > ws.workers) workers = ws.workers;
     const uint32_t w = blockIdx.x;
     if (w >= workers) return;
     const unsigned long long x0 = w * total / workers, x1 = (w + 1) * total / workers;

@@ -42,6 +42,8 @@ constexpr int HALF_ROWS = 128;
 constexpr int TILE_ROWS = 256;
 constexpr int BN = 128;                 // keys of a unit
 constexpr int RING = 4;                 // K and V tiles in flight
+constexpr uint32_t SNAP = 3;            // units
+constexpr int MIN_UNITS = 4;            // of a worker that takes a part of a tile
 constexpr int THREADS = 512;
 constexpr int MMA_WARP = 8, Q_WARP = 9, Q_WARPS = 3, KV_WARP = 12, KV_WARPS = 2;      // KV_WARPS: of a group
 constexpr uint32_t ATOM = BN * 128;     // 128 rows of 128 bytes
@@ -103,6 +105,11 @@ __host__ __device__ inline Rows rows_of(const SeqView &v, uint32_t group) {
     r.first = (int64_t)v.ctx - v.n_new;
     return r;
 }
+
+// Where a cut at unit u of a tile of n units goes: to its start below low(n), behind it from n -
+// high(n) on (a tile of 2 SNAP units or less is never cut).
+__host__ __device__ inline uint32_t snap_low(uint32_t n) { return n <= 2 * SNAP ? (n + 1) / 2 : SNAP; }
+__host__ __device__ inline uint32_t snap_high(uint32_t n) { return n <= 2 * SNAP ? n / 2 : SNAP; }
 
 struct Tile {
     uint32_t s, h, q, u, n_units;
@@ -296,7 +303,8 @@ struct Many {
     static constexpr uint32_t OFF_BAR = OFF_RAW + (C8 ? 2 * ATOM : 0);
     static constexpr uint32_t OFF_EXISTS = OFF_BAR + 288;   // [8 units][4]: keys that exist
     static constexpr uint32_t OFF_MISC = OFF_EXISTS + 128;
-    static constexpr uint32_t SMEM = OFF_MISC + 256 + 1024; // 1024: alignment of the dynamic part
+    static constexpr uint32_t OFF_TILE = OFF_MISC + 320;
+    static constexpr uint32_t SMEM = OFF_TILE + 128 + 1024; // 1024: alignment of the dynamic part
     // f16 codes are widened at half their value: scores and outputs make up for it
     static constexpr float VALUE = C8 && std::is_same<T, __half>::value ? 2.0f : 1.0f;
     // f16 probabilities are kept 2^6 times too large (at most 2^14): full precision down to 2^-20
@@ -319,7 +327,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     uint32_t *misc = reinterpret_cast<uint32_t *>(sm + C::OFF_MISC);
     uint32_t *exists = reinterpret_cast<uint32_t *>(sm + C::OFF_EXISTS);
-    volatile uint32_t *dead = misc + 60;
+    volatile uint32_t *dead = misc + 72;
     const uint32_t bars = base + C::OFF_BAR;
     const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, o_full = bars + 80, o_empty = bars + 96,
                    joined = bars + 112, drain = bars + 128, raw_full = bars + 136, s_full = bars + 200, p_full = bars + 232, o_done = bars + 264;
@@ -329,11 +337,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     const uint32_t per = (p.step.n_seq + THREADS - 1) / THREADS;
     const uint32_t s_lo = threadIdx.x * per, s_hi = min(s_lo + per, p.step.n_seq);
     unsigned long long mine = 0;
+    uint32_t my_tiles = 0;
     for (uint32_t s = s_lo; s < s_hi; ++s) {
         Tile t;
         const int code = tile_seq(p, s, t);
         if (code != TUTTI_OK && blockIdx.x == 0) report(p.step, code);
         mine += t.r.before(t.r.n_tiles) * p.pool.n_kv_heads;
+        my_tiles += t.r.n_tiles * p.pool.n_kv_heads;
     }
     unsigned long long incl = mine;
 #pragma unroll
@@ -341,33 +351,43 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         const unsigned long long x = __shfl_up_sync(0xffffffffu, incl, o);
         if (lane >= o) incl += x;
     }
-    if (lane == 31) sums[warp] = incl;
+    my_tiles = __reduce_add_sync(0xffffffffu, my_tiles);
+    if (lane == 31) sums[warp] = incl, misc[48 + warp] = my_tiles;
     __syncthreads();
+    uint32_t tiles = 0;
     unsigned long long total = 0, start = 0;
 #pragma unroll
     for (int i = 0; i < THREADS / 32; ++i) {
         if (i < (int)warp) start += sums[i];
         total += sums[i];
+        tiles += misc[48 + i];
     }
     start += incl - mine;
-    const unsigned long long workers = total < ws.workers ? total : ws.workers;
+    unsigned long long workers = (total + MIN_UNITS - 1) / MIN_UNITS;
+    if (workers < tiles) workers = tiles;
+    if (workers > ws.workers) workers = ws.workers;
+    if (workers > total) workers = total;
     const uint32_t w = blockIdx.x;
     if (w >= workers) return;
-    const unsigned long long x0 = w * total / workers, x1 = (w + 1) * total / workers;
-    if (x0 >= start && x0 < start + mine) {
-        unsigned long long at = start;
-        for (uint32_t s = s_lo; s < s_hi; ++s) {
-            Tile t;
-            tile_seq(p, s, t);
-            const unsigned long long n = t.r.before(t.r.n_tiles) * p.pool.n_kv_heads;
-            if (x0 < at + n) {
-                misc[40] = s;
-                sums[18] = x0 - at;
-                break;
+    // The share [x0, x1): cuts at multiples of total / workers, moved to a tile's end where one is near.
+    // Threads find the sequences of both cuts, warps 0 and 1 the tiles.
+    const unsigned long long cut[2] = {w * total / workers, (w + 1) * total / workers};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (cut[i] >= start && cut[i] < start + mine) {
+            unsigned long long at = start;
+            for (uint32_t s = s_lo; s < s_hi; ++s) {
+                Tile t;
+                tile_seq(p, s, t);
+                const unsigned long long n = t.r.before(t.r.n_tiles) * p.pool.n_kv_heads;
+                if (cut[i] < at + n) {
+                    misc[36 + i] = s;
+                    sums[20 + i] = cut[i] - at;
+                    break;
+                }
+                at += n;
             }
-            at += n;
         }
-    }
     if (threadIdx.x == 0) {
         for (int i = 0; i < RING; ++i) {
             mbar_init(full + 8 * i, KV_WARPS);
@@ -392,32 +412,49 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         fence_async();
     }
     if (warp == MMA_WARP) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(base + C::OFF_MISC + 61 * 4) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(base + C::OFF_MISC + 73 * 4) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         tc_before();
     }
     __syncthreads();
     tc_after();
-    const uint32_t tmem = misc[61];
-    Tile t;
-    tile_seq(p, misc[40], t);
-    {
-        const unsigned long long in_seq = sums[18], head = t.r.before(t.r.n_tiles);
-        t.h = (uint32_t)(in_seq / head);
-        const unsigned long long rest = in_seq % head;
-        const Rows r = t.r;
-        uint32_t lo = 0, len = r.n_tiles;               // last tile that starts at or before `rest`, 32 probes a round
-        while (len > 1) {
-            const uint32_t step = (len + 31) / 32;
-            const bool le = lane * step < len && r.before(lo + lane * step) <= rest;
-            const uint32_t last = 31 - __clz(__ballot_sync(0xffffffffu, le) | 1u);
-            lo += last * step;
-            len = min(len - last * step, step);
+    const uint32_t tmem = misc[73];
+    if (warp < 2) {
+        unsigned long long x = cut[warp];
+        Tile f;
+        f.s = f.h = f.q = f.u = f.n_units = 0;
+        if (x < total) {
+            tile_seq(p, misc[36 + warp], f);
+            const Rows r = f.r;
+            const unsigned long long in_seq = sums[20 + warp], head = r.before(r.n_tiles), rest = in_seq % head;
+            f.h = (uint32_t)(in_seq / head);
+            uint32_t lo = 0, len = r.n_tiles;           // last tile that starts at or before `rest`, 32 probes a round
+            while (len > 1) {
+                const uint32_t step = (len + 31) / 32;
+                const bool le = lane * step < len && r.before(lo + lane * step) <= rest;
+                const uint32_t last = 31 - __clz(__ballot_sync(0xffffffffu, le) | 1u);
+                lo += last * step;
+                len = min(len - last * step, step);
+            }
+            f.q = lo;
+            f.u = (uint32_t)(rest - r.before(lo));
+            f.n_units = r.units(lo);
+            if (f.u < snap_low(f.n_units)) {
+                x -= f.u;
+                f.u = 0;
+            } else if (f.u >= f.n_units - snap_high(f.n_units)) {
+                x += f.n_units - f.u;
+                if (x < total) next_tile(p, f);
+            }
         }
-        t.q = lo;
-        t.u = (uint32_t)(rest - r.before(lo));
-        t.n_units = r.units(lo);
+        if (lane == 0) {
+            sums[22 + warp] = x;
+            if (warp == 0) *reinterpret_cast<Tile *>(sm + C::OFF_TILE) = f;
+        }
     }
+    __syncthreads();
+    const unsigned long long x0 = sums[22], x1 = sums[23];
+    Tile t = *reinterpret_cast<const Tile *>(sm + C::OFF_TILE);
     // scores (and probabilities over them) of a half and step, then the halves' outputs
     auto S = [&](int i, int u) { return tmem + i * 128 + u * SUB; };
     auto O = [&](int i) { return tmem + 256 + i * D; };
@@ -880,8 +917,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if (lane == 0) mbar_arrive(o_empty + 8 * i);
                 if (!whole) {
                     const unsigned long long tile0 = x - t.u;
-                    const uint32_t w0 = (uint32_t)(((tile0 + 1) * workers - 1) / total);
-                    const uint32_t w1 = (uint32_t)(((tile0 + t.n_units) * workers - 1) / total);
+                    // the workers whose first and last cut before the tile's end lie in front of it and inside
+                    const uint32_t w0 = (uint32_t)(((tile0 + snap_low(t.n_units)) * workers - 1) / total);
+                    const uint32_t w1 = (uint32_t)(((tile0 + t.n_units - snap_high(t.n_units)) * workers - 1) / total);
                     auto slot = [&](uint32_t k) { return (k == w0 ? 2 * k + 1 : 2 * k) * 2 + i; };
                     float4 *part = reinterpret_cast<float4 *>(ws.part);
                     float2 *ml = reinterpret_cast<float2 *>(ws.part + (uint64_t)4 * ws.workers * HALF_ROWS * D);
@@ -894,10 +932,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     if (r == 0) {
                         const uint32_t old = atomicAdd(ws.count + 2 * w0 + i, 1);
                         if (old == w1 - w0) ws.count[2 * w0 + i] = 0;            // ready for the next call
-                        misc[42 + i] = old == w1 - w0;
+                        misc[74 + i] = old == w1 - w0;
                     }
                     if (!(ok = join())) break;
-                    write = *(volatile uint32_t *)(misc + 42 + i);
+                    write = *(volatile uint32_t *)(misc + 74 + i);
                     if (write) {
                         __threadfence();
                         m = -INFINITY;
@@ -984,6 +1022,28 @@ uint32_t many_workers(int sms) { return (uint32_t)sms; }
 size_t many_part_bytes(uint32_t workers) { return (size_t)4 * workers * HALF_ROWS * (128 + 2) * sizeof(float); }
 
 }  // namespace tutti
+
+// The kernel's own cuts, on the host, for tiles of n_units[i] units laid end to end: the share [x0, x1) of
+// worker w; and for a tile the first and the last worker that has a part of it.
+extern "C" void tutti_many_cut_(const uint32_t *n_units, uint32_t n_tiles, uint64_t workers, uint64_t w, uint64_t *out) {
+    uint64_t total = 0;
+    for (uint32_t i = 0; i < n_tiles; ++i) total += n_units[i];
+    for (int c = 0; c < 2; ++c) {
+        uint64_t x = (w + c) * total / workers, a = 0;
+        for (uint32_t i = 0; i < n_tiles; a += n_units[i++]) {
+            const uint32_t n = n_units[i];
+            if (x < a || x >= a + n) continue;
+            const uint32_t u = (uint32_t)(x - a);
+            x = u < tutti::snap_low(n) ? a : u >= n - tutti::snap_high(n) ? a + n : x;
+            break;
+        }
+        out[c] = x;
+    }
+}
+extern "C" void tutti_many_parts_(uint64_t tile0, uint32_t n, uint64_t workers, uint64_t total, uint64_t *out) {
+    out[0] = ((tile0 + tutti::snap_low(n)) * workers - 1) / total;
+    out[1] = ((tile0 + n - tutti::snap_high(n)) * workers - 1) / total;
+}
 
 // The kernel's own count of units, on the host: out2[0] units of tile q, out2[1] units of the tiles before it.
 extern "C" int tutti_many_units_(uint32_t ctx, uint32_t n_new, uint32_t group, uint32_t q, uint64_t *out2) {

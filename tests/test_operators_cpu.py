@@ -177,3 +177,31 @@ def test_units_of_causal_tiles_in_closed_form(group):
             total += want
         f(ctx, new, group, tiles, out)
         assert out[1] == total
+
+
+def test_shares_of_workers_cover_tiles_once_and_agree_on_their_parts():
+    """Cuts moved to tile ends: shares are consecutive, and the workers that a tile's formula names are the ones that hold its parts."""
+    lib = T.load()
+    cut, parts = lib.tutti_many_cut_, lib.tutti_many_parts_
+    cut.argtypes = [C.c_void_p, C.c_uint32, C.c_uint64, C.c_uint64, C.POINTER(C.c_uint64)]
+    parts.argtypes = [C.c_uint64, C.c_uint32, C.c_uint64, C.c_uint64, C.POINTER(C.c_uint64)]
+    rng = np.random.default_rng(5)
+    out = (C.c_uint64 * 2)()
+    for trial in range(300):
+        n = rng.integers(1, [3, 8, 40, 300][trial % 4], rng.integers(1, 60)).astype(np.uint32)
+        total = int(n.sum())
+        workers = int(rng.integers(1, min(148, total) + 1))
+        shares = []
+        for w in range(workers):
+            cut(n.ctypes.data, len(n), workers, w, out)
+            shares.append((out[0], out[1]))
+        assert shares[0][0] == 0 and shares[-1][1] == total
+        assert all(a[1] == b[0] and a[0] <= a[1] for a, b in zip(shares, shares[1:] + [(total, total)]))
+        start = 0
+        for k in n:
+            holders = [w for w, (a, b) in enumerate(shares) if max(a, start) < min(b, start + int(k))]
+            parts(start, int(k), workers, total, out)
+            assert holders == list(range(out[0], out[1] + 1)), (trial, start, k, holders, out[0], out[1])
+            if k <= 6:
+                assert len(holders) == 1
+            start += int(k)
