@@ -98,6 +98,7 @@ int tutti_kv_attend_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *s
                      step->blk_start, step->block_ids, step->status};
     p.n_q_heads = io->n_q_heads;
     p.group = io->n_q_heads / p.pool.n_kv_heads;
+    division_by(p.group, p.group_mul, p.group_shift);
     p.q_stride = io->q_stride;
     p.out_stride = io->out_stride;
     p.q = io->q;

@@ -17,6 +17,10 @@ struct AttendParams {
     void *out;
     float *lse;
     float scale;
+    uint32_t group_mul, group_shift;  // row / group = row * group_mul >> group_shift
+
+    __host__ __device__ uint32_t token_of(uint32_t row) const { return (uint32_t)((uint64_t)row * group_mul >> group_shift); }
+    __host__ __device__ uint32_t member_of(uint32_t row) const { return row - token_of(row) * group; }
 };
 
 // Tile loads of the layer's keys and values.

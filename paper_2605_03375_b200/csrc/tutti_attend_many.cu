@@ -53,26 +53,35 @@ constexpr float GROW = 8.0f;            // log2 of how far probabilities may exc
 constexpr long long WAIT_CLOCKS = 3000000000ll;   // about 1.5 s: a wait that takes longer is given up
 
 // sum over i in [0, n) of floor((a i + b) / m)  (a, b >= 0, m > 0)
-__host__ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+template <typename U>
+__host__ __device__ inline uint64_t floor_sum_in(U n, U m, U a, U b) {
     uint64_t ans = 0;
     while (n) {
         if (a >= m) {
-            ans += n * (n - 1) / 2 * (a / m);
-            a %= m;
+            const U q = a / m;
+            ans += (uint64_t)n * (n - 1) / 2 * q;
+            a -= q * m;
         }
         if (b >= m) {
-            ans += n * (b / m);
-            b %= m;
+            const U q = b / m;
+            ans += (uint64_t)n * q;
+            b -= q * m;
         }
-        const uint64_t y = a * n + b;
+        const U y = a * n + b;
         if (y < m) break;
         n = y / m;
-        b = y % m;
-        const uint64_t t = m;
+        b = y - n * m;
+        const U t = m;
         m = a;
         a = t;
     }
     return ans;
+}
+// In 32 bits where all of it fits (a n + b bounds every value on the way): their division is much faster.
+__host__ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a, uint64_t b) {
+    if (n < (1u << 20) && a < (1u << 11) && m < (1u << 31) && a * n + b < (1ull << 31))
+        return floor_sum_in<uint32_t>((uint32_t)n, (uint32_t)m, (uint32_t)a, (uint32_t)b);
+    return floor_sum_in<uint64_t>(n, m, a, b);
 }
 
 // The tiles of one sequence and head.
@@ -115,6 +124,12 @@ struct Tile {
     uint32_t s, h, q, u, n_units;
     SeqView v;
     Rows r;
+};
+
+// The sequence of a cut: units of one of its heads, units in front of the cut.
+struct Found {
+    Tile t;
+    unsigned long long head, in_seq;
 };
 
 __device__ inline int tile_seq(const AttendParams &p, uint32_t s, Tile &t) {
@@ -304,7 +319,7 @@ struct Many {
     static constexpr uint32_t OFF_EXISTS = OFF_BAR + 288;   // [8 units][4]: keys that exist
     static constexpr uint32_t OFF_MISC = OFF_EXISTS + 128;
     static constexpr uint32_t OFF_TILE = OFF_MISC + 320;
-    static constexpr uint32_t SMEM = OFF_TILE + 128 + 1024; // 1024: alignment of the dynamic part
+    static constexpr uint32_t SMEM = OFF_TILE + 256 + 1024; // 1024: alignment of the dynamic part
     // f16 codes are widened at half their value: scores and outputs make up for it
     static constexpr float VALUE = C8 && std::is_same<T, __half>::value ? 2.0f : 1.0f;
     // f16 probabilities are kept 2^6 times too large (at most 2^14): full precision down to 2^-20
@@ -327,6 +342,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     uint32_t *misc = reinterpret_cast<uint32_t *>(sm + C::OFF_MISC);
     uint32_t *exists = reinterpret_cast<uint32_t *>(sm + C::OFF_EXISTS);
+    Found *found = reinterpret_cast<Found *>(sm + C::OFF_TILE);
     volatile uint32_t *dead = misc + 72;
     const uint32_t bars = base + C::OFF_BAR;
     const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, o_full = bars + 80, o_empty = bars + 96,
@@ -338,12 +354,18 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     const uint32_t s_lo = threadIdx.x * per, s_hi = min(s_lo + per, p.step.n_seq);
     unsigned long long mine = 0;
     uint32_t my_tiles = 0;
+    Found own;                                     // the thread's last sequence (its only one, mostly)
+    own.t.s = ~0u;
+    auto look = [&](uint32_t s) {
+        const int code = tile_seq(p, s, own.t);
+        own.head = own.t.r.before(own.t.r.n_tiles);
+        return code;
+    };
     for (uint32_t s = s_lo; s < s_hi; ++s) {
-        Tile t;
-        const int code = tile_seq(p, s, t);
+        const int code = look(s);
         if (code != TUTTI_OK && blockIdx.x == 0) report(p.step, code);
-        mine += t.r.before(t.r.n_tiles) * p.pool.n_kv_heads;
-        my_tiles += t.r.n_tiles * p.pool.n_kv_heads;
+        mine += own.head * p.pool.n_kv_heads;
+        my_tiles += own.t.r.n_tiles * p.pool.n_kv_heads;
     }
     unsigned long long incl = mine;
 #pragma unroll
@@ -377,12 +399,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         if (cut[i] >= start && cut[i] < start + mine) {
             unsigned long long at = start;
             for (uint32_t s = s_lo; s < s_hi; ++s) {
-                Tile t;
-                tile_seq(p, s, t);
-                const unsigned long long n = t.r.before(t.r.n_tiles) * p.pool.n_kv_heads;
+                if (s != own.t.s) look(s);
+                const unsigned long long n = own.head * p.pool.n_kv_heads;
                 if (cut[i] < at + n) {
-                    misc[36 + i] = s;
-                    sums[20 + i] = cut[i] - at;
+                    own.in_seq = cut[i] - at;
+                    found[i] = own;
                     break;
                 }
                 at += n;
@@ -424,20 +445,23 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         Tile f;
         f.s = f.h = f.q = f.u = f.n_units = 0;
         if (x < total) {
-            tile_seq(p, misc[36 + warp], f);
+            f = found[warp].t;
             const Rows r = f.r;
-            const unsigned long long in_seq = sums[20 + warp], head = r.before(r.n_tiles), rest = in_seq % head;
-            f.h = (uint32_t)(in_seq / head);
+            const unsigned long long in_seq = found[warp].in_seq, head = found[warp].head;
+            f.h = in_seq < head ? 0 : (uint32_t)(in_seq / head);
+            const unsigned long long rest = in_seq - f.h * head;
+            unsigned long long at = 0;                  // units in front of tile `lo`
             uint32_t lo = 0, len = r.n_tiles;           // last tile that starts at or before `rest`, 32 probes a round
             while (len > 1) {
                 const uint32_t step = (len + 31) / 32;
-                const bool le = lane * step < len && r.before(lo + lane * step) <= rest;
-                const uint32_t last = 31 - __clz(__ballot_sync(0xffffffffu, le) | 1u);
+                const unsigned long long mine = lane * step < len ? r.before(lo + lane * step) : ~0ull;
+                const uint32_t last = 31 - __clz(__ballot_sync(0xffffffffu, mine <= rest) | 1u);
+                at = __shfl_sync(0xffffffffu, mine, last);
                 lo += last * step;
                 len = min(len - last * step, step);
             }
             f.q = lo;
-            f.u = (uint32_t)(rest - r.before(lo));
+            f.u = (uint32_t)(rest - at);
             f.n_units = r.units(lo);
             if (f.u < snap_low(f.n_units)) {
                 x -= f.u;
@@ -447,14 +471,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if (x < total) next_tile(p, f);
             }
         }
+        __syncwarp();
         if (lane == 0) {
             sums[22 + warp] = x;
-            if (warp == 0) *reinterpret_cast<Tile *>(sm + C::OFF_TILE) = f;
+            if (warp == 0) found[0].t = f;
         }
     }
     __syncthreads();
     const unsigned long long x0 = sums[22], x1 = sums[23];
-    Tile t = *reinterpret_cast<const Tile *>(sm + C::OFF_TILE);
+    Tile t = found[0].t;
     // scores (and probabilities over them) of a half and step, then the halves' outputs
     auto S = [&](int i, int u) { return tmem + i * 128 + u * SUB; };
     auto O = [&](int i) { return tmem + 256 + i * D; };
@@ -670,10 +695,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             bool ok = !segs || mbar_wait(q_empty, (segs - 1) & 1, dead);
             if (!__all_sync(0xffffffffu, ok)) break;
             constexpr int CH = D / 8;
+#pragma unroll 4
             for (uint32_t i = warp - Q_WARP; i < TILE_ROWS * CH / 32; i += Q_WARPS) {
                 const uint32_t r = (i * 32 + lane) / CH, ch = lane % CH, row = t.q * TILE_ROWS + r;
                 const bool in = row < t.r.n_rows;           // zeros behind the last row
-                const uint32_t k = in ? row / p.group : 0, h = t.h * p.group + (in ? row % p.group : 0);
+                const uint32_t k = in ? p.token_of(row) : 0, h = t.h * p.group + (in ? p.member_of(row) : 0);
                 const T *src = (const T *)p.q + (uint64_t)(t.v.q0 + k) * p.q_stride + (uint64_t)h * D + ch * 8;
                 const uint32_t dst = r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch);
                 cp16(base + dst, src, in);
@@ -799,7 +825,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             if (t.q * TILE_ROWS + i * HALF_ROWS < t.r.n_rows) {
                 const bool in = row < t.r.n_rows;
                 // rows behind the last take the last one's position: they are computed and dropped
-                const uint32_t tok = (in ? row : t.r.n_rows - 1) / p.group;
+                const uint32_t tok = p.token_of(in ? row : t.r.n_rows - 1);
                 const int64_t pos = t.r.first + tok;
                 const int64_t pos_low = __shfl_sync(0xffffffffu, pos, 0);
                 float m = -INFINITY, l = 0;
@@ -957,7 +983,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 }
                 if (write && in) {
                     const uint64_t token = t.v.q0 + tok;
-                    const uint32_t qh = t.h * p.group + row % p.group;
+                    const uint32_t qh = t.h * p.group + p.member_of(row);
                     const float inv = m == -INFINITY ? 0.0f : C::VALUE / l;
                     uint4 *out = reinterpret_cast<uint4 *>((T *)p.out + token * p.out_stride + (uint64_t)qh * D);
 #pragma unroll
