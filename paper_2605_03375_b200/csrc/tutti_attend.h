@@ -37,6 +37,10 @@ struct Workspace {
 };
 
 #ifdef __CUDACC__
+// a / b, by the much faster 32-bit division where both fit (they nearly always do)
+__device__ inline unsigned long long quotient(unsigned long long a, unsigned long long b) {
+    return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b;
+}
 __device__ inline float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

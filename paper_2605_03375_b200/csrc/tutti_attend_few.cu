@@ -169,7 +169,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     if (workers > ws.workers) workers = ws.workers;
     const uint32_t w = blockIdx.x;
     if (w >= workers) return;
-    const unsigned long long x0 = w * total / workers, x1 = (w + 1) * total / workers;
+    const unsigned long long x0 = quotient(w * total, workers), x1 = quotient((w + 1) * total, workers);
     before += incl - mine;
     __syncthreads();
     if (x0 >= before && x0 < before + mine) {      // one thread's sequences hold the first unit
@@ -179,10 +179,10 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             const unsigned long long n = (unsigned long long)own.n_tiles * own.n_units * p.pool.n_kv_heads;
             if (x0 < at + n) {
                 own.s = s;
-                const unsigned long long tile = (x0 - at) / own.n_units;
-                own.h = (uint32_t)(tile / own.n_tiles);
-                own.r = (uint32_t)(tile % own.n_tiles);
-                own.u = (uint32_t)((x0 - at) % own.n_units);
+                const unsigned long long tile = quotient(x0 - at, own.n_units);
+                own.h = (uint32_t)quotient(tile, own.n_tiles);
+                own.r = (uint32_t)(tile - (unsigned long long)own.h * own.n_tiles);
+                own.u = (uint32_t)(x0 - at - tile * own.n_units);
                 *reinterpret_cast<Cursor *>(plan) = own;
                 break;
             }
@@ -565,8 +565,8 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         bool write = whole;
         if (!whole) {
             // this worker's part, and whoever brings the last part of the tile joins them
-            const uint32_t w0 = (uint32_t)(((tile0 + 1) * workers - 1) / total);
-            const uint32_t w1 = (uint32_t)(((tile0 + get.n_units) * workers - 1) / total);
+            const uint32_t w0 = (uint32_t)quotient((tile0 + 1) * workers - 1, total);
+            const uint32_t w1 = (uint32_t)quotient((tile0 + get.n_units) * workers - 1, total);
             auto slot = [&](uint32_t i) { return i == w0 ? 2 * i + 1 : 2 * i; };
             float *part_o = ws.part, *part_ml = ws.part + (uint64_t)2 * ws.workers * F::ROWS * D;
             float4 *po = reinterpret_cast<float4 *>(part_o + ((uint64_t)slot(w) * F::ROWS + row) * D);

@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     if (w >= workers) return;
     // The share [x0, x1): cuts at multiples of total / workers, moved to a tile's end where one is near.
     // Threads find the sequences of both cuts, warps 0 and 1 the tiles.
-    const unsigned long long cut[2] = {w * total / workers, (w + 1) * total / workers};
+    const unsigned long long cut[2] = {quotient(w * total, workers), quotient((w + 1) * total, workers)};
 #pragma unroll
     for (int i = 0; i < 2; ++i)
         if (cut[i] >= start && cut[i] < start + mine) {
@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             f = found[warp].t;
             const Rows r = f.r;
             const unsigned long long in_seq = found[warp].in_seq, head = found[warp].head;
-            f.h = in_seq < head ? 0 : (uint32_t)(in_seq / head);
+            f.h = (uint32_t)quotient(in_seq, head);
             const unsigned long long rest = in_seq - f.h * head;
             unsigned long long at = 0;                  // units in front of tile `lo`
             uint32_t lo = 0, len = r.n_tiles;           // last tile that starts at or before `rest`, 32 probes a round
@@ -944,8 +944,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if (!whole) {
                     const unsigned long long tile0 = x - t.u;
                     // the workers whose first and last cut before the tile's end lie in front of it and inside
-                    const uint32_t w0 = (uint32_t)(((tile0 + snap_low(t.n_units)) * workers - 1) / total);
-                    const uint32_t w1 = (uint32_t)(((tile0 + t.n_units - snap_high(t.n_units)) * workers - 1) / total);
+                    const uint32_t w0 = (uint32_t)quotient((tile0 + snap_low(t.n_units)) * workers - 1, total);
+                    const uint32_t w1 = (uint32_t)quotient((tile0 + t.n_units - snap_high(t.n_units)) * workers - 1, total);
                     auto slot = [&](uint32_t k) { return (k == w0 ? 2 * k + 1 : 2 * k) * 2 + i; };
                     float4 *part = reinterpret_cast<float4 *>(ws.part);
                     float2 *ml = reinterpret_cast<float2 *>(ws.part + (uint64_t)4 * ws.workers * HALF_ROWS * D);
@@ -981,19 +981,48 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         }
                     }
                 }
-                if (write && in) {
+                if (write) {
                     const uint64_t token = t.v.q0 + tok;
-                    const uint32_t qh = t.h * p.group + p.member_of(row);
+                    const uint32_t qh = t.h * p.group + p.member_of(in ? row : t.r.n_rows - 1);
                     const float inv = m == -INFINITY ? 0.0f : C::VALUE / l;
-                    uint4 *out = reinterpret_cast<uint4 *>((T *)p.out + token * p.out_stride + (uint64_t)qh * D);
+                    const unsigned long long mine = in ? (unsigned long long)((T *)p.out + token * p.out_stride + (uint64_t)qh * D) : 0;
+                    unsigned long long to[4];               // the rows of the lane's quad
 #pragma unroll
-                    for (int d = 0; d < D / 8; ++d) {
-                        constexpr int B = C::ORDERED ? 1 : 2, E = C::ORDERED ? 2 : 1;      // where elements 1 and 2 of four are
-                        const float *e = o + 8 * d;
-                        out[d] = make_uint4(pack2(e[0] * inv, e[B] * inv, T()), pack2(e[E] * inv, e[3] * inv, T()),
-                                            pack2(e[4] * inv, e[4 + B] * inv, T()), pack2(e[4 + E] * inv, e[7] * inv, T()));
+                    for (int k = 0; k < 4; ++k) to[k] = __shfl_sync(0xffffffffu, mine, (lane & ~3u) + k);
+                    // A thread has a row, a store wants neighbouring lanes on neighbouring bytes: the four lanes
+                    // of a quad exchange 16-byte pieces, so that a store writes 64 bytes of a row (a piece of its
+                    // own row a lane made a store of 32 separate lines: 3 us a tile, and the load of the next
+                    // tile's queries behind it)
+#pragma unroll
+                    for (int d = 0; d < D / 8; d += 4) {
+                        uint32_t piece[4][4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            constexpr int B = C::ORDERED ? 1 : 2, E = C::ORDERED ? 2 : 1;      // where elements 1 and 2 of four are
+                            const float *e = o + 8 * (d + k);
+                            piece[k][0] = pack2(e[0] * inv, e[B] * inv, T()), piece[k][1] = pack2(e[E] * inv, e[3] * inv, T());
+                            piece[k][2] = pack2(e[4] * inv, e[4 + B] * inv, T()), piece[k][3] = pack2(e[4 + E] * inv, e[7] * inv, T());
+                        }
+                        // (row, piece) to (piece, row): the off-diagonal blocks change places, at distance 2 and 1
+#pragma unroll
+                        for (int dist = 2; dist; dist >>= 1)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                if (k & dist) continue;
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const bool up = lane & dist;
+                                    const uint32_t give = up ? piece[k][i] : piece[k + dist][i];
+                                    const uint32_t got = __shfl_xor_sync(0xffffffffu, give, dist);
+                                    if (up) piece[k][i] = got;
+                                    else piece[k + dist][i] = got;
+                                }
+                            }
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (to[k]) *reinterpret_cast<uint4 *>(to[k] + (d + (lane & 3)) * 16) = make_uint4(piece[k][0], piece[k][1], piece[k][2], piece[k][3]);
                     }
-                    if (p.lse) p.lse[token * p.n_q_heads + qh] = m == -INFINITY ? -INFINITY : (m - C::OFF + log2f(l)) * 0.6931471805599453f;
+                    if (p.lse && in) p.lse[token * p.n_q_heads + qh] = m == -INFINITY ? -INFINITY : (m - C::OFF + log2f(l)) * 0.6931471805599453f;
                 }
             }
             n_unit += n;
