@@ -275,7 +275,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         for (int b = 0; b < NB; ++b) {
             const uint32_t row = row0 + b * 8 + g;
             const bool ok = row < n_rows;
-            const uint32_t i = ok ? p.token_of(row) : 0, qh = h * p.group + (ok ? p.member_of(row) : 0);
+            const uint32_t i = ok ? row / p.group : 0, qh = h * p.group + (ok ? row % p.group : 0);
             const T *q = (const T *)p.q + (uint64_t)(get.v.q0 + i) * p.q_stride + (uint64_t)qh * D;
             float mul = p.scale * 1.4426950408889634f;
             if constexpr (!C8) {
@@ -322,7 +322,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 const uint32_t mine = row0 + b * 8 + 2 * c + r;
-                pos[b][r] = mine < n_rows ? first + p.token_of(mine) : -1;
+                pos[b][r] = mine < n_rows ? first + mine / p.group : -1;
                 rowscale[b][r] = __shfl_sync(0xffffffffu, mul, (2 * c + r) * 4);
             }
         }
@@ -339,7 +339,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
 #pragma unroll
             for (int i = 0; i < F::DT; ++i) o[b][i][0] = o[b][i][1] = o[b][i][2] = o[b][i][3] = 0;
         }
-        const int64_t last_all = first + p.token_of(row0);        // keys up to here are seen by every row of the tile
+        const int64_t last_all = first + row0 / p.group;        // keys up to here are seen by every row of the tile
 
         for (; x < seg_end; ++x) {
             cp_wait<F::STAGES - 2>();
@@ -603,7 +603,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             }
         }
         if (write && row0 + row < n_rows) {
-            const uint32_t i = p.token_of(row0 + row), qh = h * p.group + p.member_of(row0 + row);
+            const uint32_t i = (row0 + row) / p.group, qh = h * p.group + (row0 + row) % p.group;
             const uint64_t tok = get.v.q0 + i;
             const float inv = M_ == -INFINITY ? 0.0f : 1.0f / L;
             T *out = (T *)p.out + tok * p.out_stride + (uint64_t)qh * D;
