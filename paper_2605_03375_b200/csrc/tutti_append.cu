@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__
 }
 
 template <typename T>
-__global__ void __launch_bounds__(THREADS) append8_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(THREADS, 3) append8_kernel(const __grid_constant__ AppendParams p) {
     const uint32_t w = (blockIdx.x * (uint64_t)THREADS + threadIdx.x) / 32;
     if (w < p.n_row_warps)
         row_warp<T, false>(p, w);

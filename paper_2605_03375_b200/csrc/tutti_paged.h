@@ -76,17 +76,24 @@ __device__ inline void report(const StepDev &st, int code) {
     if (st.status) atomicCAS(st.status, TUTTI_OK, code);
 }
 
-// Largest s with start(s) <= x over s in [0, n): all lanes of a warp, 32 probes a round.
-// start(0) <= x is taken for granted; the caller checks what it found.
+// Largest s with start(s) <= x over s in [0, n): all lanes of a warp, 128 probes a round (one round of
+// loads for up to 128 sequences).  start(0) <= x is taken for granted; the caller checks what it found.
 template <typename F>
 __device__ inline uint32_t warp_find(uint32_t n, uint32_t x, F start) {
     const uint32_t lane = threadIdx.x & 31;
     uint32_t lo = 0, len = n;
     while (len > 1) {
-        const uint32_t step = (len + 31) / 32;
-        const uint32_t at = lo + lane * step;
-        const bool le = lane * step < len && start(at) <= x;
-        const uint32_t last = 31 - __clz(__ballot_sync(0xffffffffu, le) | 1u);
+        const uint32_t step = (len + 127) / 128;
+        bool le[4];
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+            const uint32_t at = (lane * 4 + k) * step;
+            le[k] = at < len && start(lo + at) <= x;
+        }
+        uint32_t n_le = 0;
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) n_le += __popc(__ballot_sync(0xffffffffu, le[k]));
+        const uint32_t last = n_le ? n_le - 1 : 0;
         lo += last * step;
         len = len - last * step < step ? len - last * step : step;
     }
