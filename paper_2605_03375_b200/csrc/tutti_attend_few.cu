@@ -27,7 +27,7 @@ namespace {
 // way round.  8-bit caches are multiplied as f16 codes (exact); the scale of a key goes onto
 // its score, the scale of a value onto its probability.
 constexpr int WARPS = 4;
-constexpr int STAGES = 3, STAGES_8 = 2;
+constexpr int STAGES = 3, STAGES_8 = 2;     // of a warp's ring; _8: 8-bit caches with 8 rows (below)
 constexpr int WORKERS_8 = 3;
 constexpr uint32_t BYTES_8 = 8192;
 constexpr int MIN_UNITS = 2;                // of a worker that takes a part of a tile: joining the parts costs, too
@@ -89,8 +89,9 @@ template <typename T, bool C8, int D, int NB>
 struct Few {
     using M = typename std::conditional<C8, __half, T>::type;        // type of the matrix instructions
     static constexpr int ROWS = 8 * NB;
-    // 8-bit caches take more instructions a byte (widening): with 8 rows 128 registers are enough for
-    // 16 warps an SM instead of 8, each with a stage less.
+    // 8-bit caches take more instructions a byte (widening): with 8 rows 168 registers are enough for
+    // 12 warps an SM instead of 8, each with a stage less (8 x 32768 keys: 108 us with 2 or 3 workers of
+    // 32 keys a step, 131-135 us with 3 or 4 of 16; 64-wide heads, ragged: 73 with 3, 81 with 2).
     static constexpr int WORKERS_PER_SM = C8 && NB == 1 ? WORKERS_8 : 2;
     static constexpr int STAGES = C8 && NB == 1 ? STAGES_8 : tutti::STAGES;
     static constexpr uint32_t STAGE_BYTES = C8 && NB == 1 ? BYTES_8 : 8192;  // keys and values of one warp's KW keys
@@ -588,20 +589,27 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             write = plan[0];
             if (write) {
                 __threadfence();
+                // in worker order, a running maximum along; the loads of eight parts are in flight at once
+                const float2 *parts_ml = reinterpret_cast<const float2 *>(part_ml);
                 M_ = -INFINITY;
                 L = 0;
-                for (uint32_t i = w0; i <= w1; ++i) M_ = fmaxf(M_, __ldcg(reinterpret_cast<const float2 *>(part_ml) + slot(i) * F::ROWS + row).x);
 #pragma unroll
                 for (int j = 0; j < GROUPS * 4; ++j) acc[j] = 0;
+#pragma unroll 8
                 for (uint32_t i = w0; i <= w1; ++i) {
-                    const float2 e = __ldcg(reinterpret_cast<const float2 *>(part_ml) + slot(i) * F::ROWS + row);
-                    const float f = M_ == -INFINITY ? 0 : ex2(e.x - M_);
-                    L += e.y * f;
+                    const float2 e = __ldcg(parts_ml + slot(i) * F::ROWS + row);
                     const float4 *src = reinterpret_cast<const float4 *>(part_o + ((uint64_t)slot(i) * F::ROWS + row) * D);
+                    float4 b[GROUPS];
+#pragma unroll
+                    for (int j = 0; j < GROUPS; ++j) b[j] = __ldcg(src + j * TPR + lanec);
+                    const float m2 = fmaxf(M_, e.x);
+                    const float was = m2 == -INFINITY ? 0 : ex2(M_ - m2), f = m2 == -INFINITY ? 0 : ex2(e.x - m2);
+                    M_ = m2;
+                    L = L * was + e.y * f;
 #pragma unroll
                     for (int j = 0; j < GROUPS; ++j) {
-                        const float4 b = __ldcg(src + j * TPR + lanec);
-                        acc[j * 4] += b.x * f, acc[j * 4 + 1] += b.y * f, acc[j * 4 + 2] += b.z * f, acc[j * 4 + 3] += b.w * f;
+                        acc[j * 4] = acc[j * 4] * was + b[j].x * f, acc[j * 4 + 1] = acc[j * 4 + 1] * was + b[j].y * f;
+                        acc[j * 4 + 2] = acc[j * 4 + 2] * was + b[j].z * f, acc[j * 4 + 3] = acc[j * 4 + 3] * was + b[j].w * f;
                     }
                 }
             }

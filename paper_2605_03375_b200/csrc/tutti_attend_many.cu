@@ -966,6 +966,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         __threadfence();
                         m = -INFINITY;
                         l = 0;
+#pragma unroll 4
                         for (uint32_t k = w0; k <= w1; ++k) m = fmaxf(m, __ldcg(ml + (uint64_t)slot(k) * HALF_ROWS + r).x);
 #pragma unroll
                         for (int d = 0; d < D; ++d) o[d] = 0;
