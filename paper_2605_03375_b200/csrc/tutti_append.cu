@@ -8,7 +8,11 @@
 // as two 16-byte vectors, chosen so that every pair is inside one job (half-split style: the
 // vectors at d and d + rot_dim / 2).  head_dim / 16 lanes cover a row, a warp 32 / (head_dim / 16)
 // rows at a time.  Every input is read once and every output written once; the bound is HBM
-// bandwidth for prompts and launch latency for a decode step.
+// bandwidth for prompts and latency for a decode step: the search of the sequence, its tables, the
+// block's id and the rows are loads that wait for each other.
+// On a B200 (6.45 TB/s copy): 16384 tokens of 48 rows of 128, bf16, 72 us = 5.7 TB/s; 12187 tokens of
+// 80 rows, fp16, into an 8-bit pool 106 us = 4.6 TB/s; 64 single tokens 4.0 and 6.6 us.  24 warps an SM
+// (80 registers, a few spilled) against 16: 72 against 75 us, 106 against 109; 32: 92 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -381,7 +385,7 @@ __device__ void block_warp(const AppendParams &p, uint32_t w) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(THREADS) append_kernel(const __grid_constant__ AppendParams p) {
+__global__ void __launch_bounds__(THREADS, 3) append_kernel(const __grid_constant__ AppendParams p) {
     const uint32_t w = (blockIdx.x * (uint64_t)THREADS + threadIdx.x) / 32;
     if (w < p.n_row_warps) row_warp<T, true>(p, w);
     // A copy kernel behind this one in the stream may be launched as soon as every CTA has ended

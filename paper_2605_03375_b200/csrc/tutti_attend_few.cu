@@ -1,4 +1,8 @@
-// Attention of few rows per sequence (a decode step).
+// Attention of few rows per sequence (a decode step).  Bound: HBM, the cache is read once.
+// On a B200 (6.45 TB/s copy), 128-wide heads: 64 ragged requests on 1-token pages (2.3 GB) 361 us =
+// 6.4 TB/s; one of 131072 tokens (0.54 GB) 93 us = 5.75 TB/s; 8 of 32768, 8-bit (0.54 GB), 108 us = 5.0
+// TB/s; 64-wide heads, 8-bit, 48 ragged (0.22 GB), 70 us = 3.1 TB/s (bound by instructions: 17 a byte).  One
+// request of 1 / 512 / 4096 tokens 5.2 / 9.0 / 12.5 us: three rounds of dependent loads, and the join.
 #include <type_traits>
 
 #include "tutti_attend.h"

@@ -28,8 +28,12 @@
 //             8-bit codes are widened to 16 bits (code * scale, exact for the powers of two that
 //             append writes): keys where they landed, values out of a buffer of their own, so that
 //             they are fetched before the place they go to is free.
-// Bound: the tensor cores (2 x 128 x 128 x D multiply-adds a half and unit) and, as close,
-// the 128 x 128 exponentials on 16 lanes a clock.
+// Bound: the tensor cores (2 x 128 x 128 x D multiply-adds a half and unit: 2048 clocks a unit for D = 128)
+// and, as close, the 2 x 128 x 128 exponentials on 16 lanes a clock; in a long loop the power limit
+// (1550 MHz at 1000 W).  What is reached: 3500 clocks a unit, set by the chain scores -> softmax -> P V
+// -> next scores of a half.  On a B200 (1676 TFLOP/s in short, 1389 in long runs of the library's product): 2048 new tokens
+// over 32768, 32 heads, bf16, 1040-1180 us = 960-1090 TFLOP/s; 1801 over 2 x 8192 256 us = 974; 8-bit, fp16, 64 heads, 4
+// ragged chunks over 2000-9000 280 us = 667 (the widening of the codes and shared memory).
 #include <type_traits>
 
 #include "tutti_attend.h"
