@@ -7,6 +7,7 @@ import torch
 
 from paper_2605_03375_b200 import tutti as T
 from tests.opcase import DTYPES, OpCase
+from tests.test_gpu_append import append, verify as append_verify
 from tests.test_gpu_attend import attend, fill_new, verify
 
 pytestmark = pytest.mark.gpu
@@ -292,5 +293,30 @@ def test_decode_and_prompt_rows_in_one_step(cache):
     try:
         fill_new(c)
         verify(c, attend(c))
+    finally:
+        c.close()
+
+
+def random_case(seed):
+    rng = np.random.default_rng(seed)
+    kv_heads = int(rng.choice([1, 2, 3, 4]))
+    new = int(rng.choice([1, 1, 3, 20, 150]))
+    lens = [(int(rng.integers(0, rng.choice([5, 60, 700]))), int(rng.integers(0, new + 1)) if new > 1 else 1) for _ in range(rng.integers(1, 7))]
+    block = int(rng.choice([1, 2, 7, 8, 16, 16, 33, 64, 100, 128]))
+    cache = str(rng.choice(["16", "8"]))
+    return OpCase(lens, heads=kv_heads * int(rng.choice([1, 2, 4, 5, 8, 13])), kv_heads=kv_heads, dim=int(rng.choice([64, 128])), block=block,
+                  dtype=str(rng.choice(["bf16", "fp16"])), cache=cache, hnd=bool(rng.random() < 0.4), interleaved=bool(rng.random() < 0.3),
+                  pad=16 * int(rng.integers(0, 5)), packed=bool(rng.random() < 0.5), spare_rows=int(rng.integers(0, 4)), seed=seed)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_steps(seed):
+    c = random_case(1000 + seed)
+    try:
+        style = "half" if seed % 2 else "pairs"
+        append_verify(c, append(c, style, c.dim // (1 + seed % 3 // 2)), style)
+        fill_new(c)
+        verify(c, attend(c))
+        assert int(c.status) == T.OK
     finally:
         c.close()
