@@ -582,24 +582,22 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
 #pragma unroll
             for (int j = 0; j < GROUPS; ++j) po[j * TPR + lanec] = make_float4(acc[j * 4], acc[j * 4 + 1], acc[j * 4 + 2], acc[j * 4 + 3]);
             if (lanec == 0) reinterpret_cast<float2 *>(part_ml)[slot(w) * F::ROWS + row] = make_float2(M_, L);
-            __threadfence();
             __syncthreads();
             if (threadIdx.x == 0) {
-                const uint32_t old = atomicAdd(ws.count + w0, 1);
+                const uint32_t old = arrive_gpu(ws.count + w0);
                 if (old == w1 - w0) ws.count[w0] = 0;          // ready for the next call
                 plan[0] = old == w1 - w0;
             }
             __syncthreads();
             write = plan[0];
             if (write) {
-                __threadfence();
-                // in worker order, a running maximum along; the loads of eight parts are in flight at once
+                // in worker order, a running maximum along; the loads of sixteen parts are in flight at once
                 const float2 *parts_ml = reinterpret_cast<const float2 *>(part_ml);
                 M_ = -INFINITY;
                 L = 0;
 #pragma unroll
                 for (int j = 0; j < GROUPS * 4; ++j) acc[j] = 0;
-#pragma unroll 8
+#pragma unroll 16
                 for (uint32_t i = w0; i <= w1; ++i) {
                     const float2 e = __ldcg(parts_ml + slot(i) * F::ROWS + row);
                     const float4 *src = reinterpret_cast<const float4 *>(part_o + ((uint64_t)slot(i) * F::ROWS + row) * D);

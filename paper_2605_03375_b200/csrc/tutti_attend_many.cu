@@ -957,17 +957,15 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 #pragma unroll
                     for (int d = 0; d < D / 4; ++d) *at(w, d) = make_float4(o[4 * d], o[4 * d + 1], o[4 * d + 2], o[4 * d + 3]);
                     ml[(uint64_t)slot(w) * HALF_ROWS + r] = make_float2(m, l);
-                    __threadfence();
                     if (!(ok = join())) break;
                     if (r == 0) {
-                        const uint32_t old = atomicAdd(ws.count + 2 * w0 + i, 1);
+                        const uint32_t old = arrive_gpu(ws.count + 2 * w0 + i);
                         if (old == w1 - w0) ws.count[2 * w0 + i] = 0;            // ready for the next call
                         misc[74 + i] = old == w1 - w0;
                     }
                     if (!(ok = join())) break;
                     write = *(volatile uint32_t *)(misc + 74 + i);
                     if (write) {
-                        __threadfence();
                         m = -INFINITY;
                         l = 0;
 #pragma unroll 4
