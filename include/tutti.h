@@ -570,9 +570,9 @@ int tutti_scales_register(tutti_ctx_t *ctx, uint32_t layer, float *k_scale, floa
  * scale that the block has if it already holds earlier tokens of the sequence, and at least
  * 2^-100.  Where the scale grows, the block's earlier codes are rounded again to the new one.
  * Infinite values are stored as +-448 codes, NaN as NaN.
- * A block that receives tokens must belong to one sequence of the step only (prefix blocks that
- * several sequences share are only read by attention); two sequences that write the same rows,
- * or in an 8-bit pool the same block, race.  Padding rows are skipped.  TUTTI_EINVAL in
+ * A block that receives tokens must belong to one sequence of the step only, and be listed once in
+ * its row (prefix blocks that several sequences share are only read by attention); two writers
+ * of the same rows, or in an 8-bit pool of the same block, race.  Padding rows are skipped.  TUTTI_EINVAL in
  * *status also for a sequence with ctx_len > rope->n_pos.
  * Asynchronous on `stream`, graph-capturable.  TUTTI_EINVAL for a layer that is not registered,
  * elem_bytes other than 2, or 1 with registered scales; head_dim not a multiple of 16 or above

@@ -24,6 +24,7 @@ using namespace tutti;
 
 struct tutti_attn {
     tutti_ctx *ctx;
+    int device;
     Workspace few, many;     // they share the parts' memory
 };
 
@@ -57,6 +58,7 @@ int tutti_attn_create(tutti_ctx_t *ctx, tutti_attn_t **out) {
     tutti_attn *a = new (std::nothrow) tutti_attn();
     if (!a) return TUTTI_ENOMEM;
     a->ctx = ctx;
+    a->device = tutti_ctx_device_(ctx);
     const uint32_t n_few = few_workers(tutti_ctx_sms_(ctx)), n_many = many_workers(tutti_ctx_sms_(ctx));
     const size_t few_part = few_part_bytes(tutti_ctx_sms_(ctx)), many_part = many_part_bytes(n_many), part = few_part > many_part ? few_part : many_part;
     const size_t counts = (n_few + 2 * n_many) * sizeof(uint32_t);
@@ -78,7 +80,7 @@ int tutti_attn_create(tutti_ctx_t *ctx, tutti_attn_t **out) {
 
 int tutti_attn_destroy(tutti_attn_t *a) {
     if (!a) return TUTTI_EINVAL;
-    OnDevice on(tutti_ctx_device_(a->ctx));
+    OnDevice on(a->device);
     cudaDeviceSynchronize();
     cudaFree(a->few.part);
     cudaFree(a->few.count);

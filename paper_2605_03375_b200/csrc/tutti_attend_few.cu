@@ -31,9 +31,12 @@ namespace {
 // way round.  8-bit caches are multiplied as f16 codes (exact); the scale of a key goes onto
 // its score, the scale of a value onto its probability.
 constexpr int WARPS = 4;
-constexpr int STAGES = 3, STAGES_8 = 2;     // of a warp's ring; _8: 8-bit caches with 8 rows (below)
-constexpr int WORKERS_8 = 3;
-constexpr uint32_t BYTES_8 = 8192;
+// _8: 8-bit caches (the ring and the workers: with 8 rows), see below.
+constexpr int STAGES = 3, STAGES_8 = 2;     // of a warp's ring
+constexpr uint32_t BYTES_8 = 8192;          // of a stage
+constexpr int WORKERS_8 = 3;                // an SM
+constexpr int DEEP = 16, DEEP_8 = 4;        // parts whose loads are in flight while a tile is joined (registers: 16 cost
+                                            // the 8-bit loop 4 %)
 constexpr int MIN_UNITS = 2;                // of a worker that takes a part of a tile: joining the parts costs, too
 
 __device__ inline void ldm4(uint32_t (&r)[4], uint32_t a) {
@@ -591,13 +594,14 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             __syncthreads();
             write = plan[0];
             if (write) {
-                // in worker order, a running maximum along; the loads of sixteen parts are in flight at once
+                // in worker order, a running maximum along, the loads of several parts in flight at once
                 const float2 *parts_ml = reinterpret_cast<const float2 *>(part_ml);
                 M_ = -INFINITY;
                 L = 0;
 #pragma unroll
                 for (int j = 0; j < GROUPS * 4; ++j) acc[j] = 0;
-#pragma unroll 16
+                constexpr int IN_FLIGHT = C8 ? DEEP_8 : DEEP;
+#pragma unroll IN_FLIGHT
                 for (uint32_t i = w0; i <= w1; ++i) {
                     const float2 e = __ldcg(parts_ml + slot(i) * F::ROWS + row);
                     const float4 *src = reinterpret_cast<const float4 *>(part_o + ((uint64_t)slot(i) * F::ROWS + row) * D);
