@@ -1033,6 +1033,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             if (x < x1) next_tile(p, t);
         }
     }
+    if (*dead) {                                    // a wait was given up: copies in flight get 1 ms to land
+        const long long t0 = clock64();
+        while (clock64() - t0 < WAIT_CLOCKS / 1500) {}
+    }
     tc_before();
     __syncthreads();
     tc_after();

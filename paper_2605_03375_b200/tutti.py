@@ -322,23 +322,24 @@ def _dtype_code(dtype) -> int:
     return code
 
 
-def _rows(t, dtype) -> int:
-    """Token stride of a [tokens, heads, head_dim] tensor whose heads lie side by side."""
-    _, heads, dim = t.shape
+def _rows(t, dtype, dim: int) -> int:
+    """Token stride of a [tokens, heads, dim] tensor whose heads lie side by side."""
     by_token, by_head, by_dim = t.stride()
-    if t.dtype is not dtype or by_dim != 1 or (by_head != dim and heads > 1):
-        raise TuttiError(EINVAL, "token tensor (type or strides)")
+    if t.dtype is not dtype or by_dim != 1 or by_head != dim:
+        _, heads, own_dim = t.shape
+        if t.dtype is not dtype or own_dim != dim or by_dim != 1 or heads > 1:
+            raise TuttiError(EINVAL, "token tensor (type, shape or strides)")
     return by_token
 
 
 def make_tokens(k, v, q=None, q_out=None) -> Tokens:
     """Token struct over [tokens, heads, head_dim] device tensors (bf16 or fp16; views of a packed
     projection are fine).  The struct does not keep the tensors alive."""
-    dtype = k.dtype
+    dtype, dim = k.dtype, k.shape[2]
     code = _dtype_code(dtype)
     if q is None:
-        return Tokens(code, 0, 0, _rows(k, dtype), _rows(v, dtype), 0, None, k.data_ptr(), v.data_ptr(), None)
-    return Tokens(code, q.shape[1], _rows(q, dtype), _rows(k, dtype), _rows(v, dtype), _rows(q_out, dtype),
+        return Tokens(code, 0, 0, _rows(k, dtype, dim), _rows(v, dtype, dim), 0, None, k.data_ptr(), v.data_ptr(), None)
+    return Tokens(code, q.shape[1], _rows(q, dtype, dim), _rows(k, dtype, dim), _rows(v, dtype, dim), _rows(q_out, dtype, dim),
                   q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr())
 
 
@@ -367,7 +368,8 @@ def make_attend(q, out, lse=None) -> Attend:
     if lse is not None and not (_float32(lse) and lse.is_contiguous()):
         raise TuttiError(EINVAL, "lse (float32, contiguous)")
     dtype = q.dtype
-    return Attend(_dtype_code(dtype), q.shape[1], _rows(q, dtype), _rows(out, dtype), q.data_ptr(), out.data_ptr(),
+    _, heads, dim = q.shape
+    return Attend(_dtype_code(dtype), heads, _rows(q, dtype, dim), _rows(out, dtype, dim), q.data_ptr(), out.data_ptr(),
                   None if lse is None else lse.data_ptr(), 0.0, 0)
 
 

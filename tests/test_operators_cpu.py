@@ -205,3 +205,26 @@ def test_shares_of_workers_cover_tiles_once_and_agree_on_their_parts():
             if k <= 6:
                 assert len(holders) == 1
             start += int(k)
+
+
+def test_structs_from_tensors():
+    """The binding's own checks of types, shapes and strides."""
+    import torch
+    k, q = torch.zeros(4, 2, 64, dtype=torch.float16), torch.zeros(4, 8, 64, dtype=torch.float16)
+    t = T.make_tokens(k, k, q, q)
+    assert (t.dtype, t.n_q_heads, t.q_stride, t.k_stride, t.v_stride, t.q_out_stride) == (T.DTYPE_FP16, 8, 512, 128, 128, 512)
+    one = torch.zeros(4, 3, 64, dtype=torch.float16)[:, 1:2]               # one head of a packed row
+    assert T.make_tokens(one, one).k_stride == 192
+    a = T.make_attend(q, q, torch.zeros(4, 8))
+    assert (a.n_q_heads, a.q_stride, a.out_stride) == (8, 512, 512) and a.lse
+    assert T.make_rope(torch.zeros(10, 32), T.ROPE_PAIRS).rot_dim == 32
+    half = torch.float16
+    for bad in (lambda: T.make_tokens(k, k.float()), lambda: T.make_tokens(k.float(), k.float()),
+                lambda: T.make_tokens(k, k, torch.zeros(4, 8, 32, dtype=half), q), lambda: T.make_tokens(k.transpose(1, 2), k),
+                lambda: T.make_tokens(k, torch.zeros(4, 2, 128, dtype=half)[:, :, ::2]), lambda: T.make_tokens(one, torch.zeros(4, 1, 32, dtype=half)),
+                lambda: T.make_tokens(k, torch.zeros(2, 4, 64, dtype=half).transpose(0, 1)), lambda: T.make_attend(q, q.transpose(0, 1)),
+                lambda: T.make_attend(q, q, torch.zeros(4, 8, dtype=half)), lambda: T.make_rope(torch.zeros(10, 32, dtype=half)),
+                lambda: T.make_step(torch.zeros(2, dtype=torch.int64), torch.zeros(1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32),
+                                    torch.zeros(1, dtype=torch.int32), 1, 1)):
+        with pytest.raises(T.TuttiError):
+            bad()
