@@ -494,7 +494,8 @@ int tutti_kv_restore_layer_noalloc(const tutti_geom_t *geom, int device, uint32_
  * ctx_len - n + i; a row whose position comes out negative (ctx_len smaller than n, as in a
  * padded batch) is padding.  All five arrays are DEVICE pointers owned by the caller; they may
  * change between calls and between replays of a captured graph, within the host-known sizes:
- * n_tok rows in the token arrays (rows at and behind q_start[n_seq] are left as they are),
+ * n_tok rows in the token arrays (rows before q_start[0], and at and behind q_start[n_seq], are left
+ * as they are: slices of a step's tables are steps over the same arrays),
  * n_blk entries in block_ids, max_new rows of one sequence at most.
  * status (may be NULL): a device or mapped pinned int32 that the caller has set to 0; the first
  * problem found is written to it.  TUTTI_EINVAL: a sequence's numbers contradict each other or

@@ -140,6 +140,7 @@ __device__ void row_warp(const AppendParams &p, uint32_t w) {
     if (tok >= __ldg(p.step.q_start + p.step.n_seq)) return;      // behind the last sequence
     SeqView v;
     int code = seq_view(p.step, p.pool.block_tokens, s, v);
+    if (code == TUTTI_OK && s == 0 && tok < v.q0) return;         // before the first one
     if (code == TUTTI_OK && (tok < v.q0 || tok - v.q0 >= v.n_new)) code = TUTTI_EINVAL;
     if (code == TUTTI_OK && p.rope.rot_dim && v.ctx > p.rope.n_pos) code = TUTTI_EINVAL;
     if (code != TUTTI_OK) {

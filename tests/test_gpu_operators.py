@@ -7,7 +7,7 @@ import torch
 
 from paper_2605_03375_b200 import tutti as T
 from tests.opcase import DTYPES, OpCase
-from tests.test_gpu_append import append, verify as append_verify
+from tests.test_gpu_append import append, table_of, verify as append_verify
 from tests.test_gpu_attend import attend, fill_new, verify
 
 pytestmark = pytest.mark.gpu
@@ -293,6 +293,34 @@ def test_decode_and_prompt_rows_in_one_step(cache):
     try:
         fill_new(c)
         verify(c, attend(c))
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("cache", ["16", "8"])
+def test_a_step_in_two_calls_over_slices_of_its_tables(cache):
+    """Decoding and prompt sequences of one step apart: the second call's first row is not row 0."""
+    c = OpCase([(600, 1), (1000, 1), (90, 1), (0, 300), (130, 7), (700, 128)], heads=8, kv_heads=2, cache=cache, seed=74)
+    try:
+        steps = [T.make_step(c.t_q_start[a:b + 1], c.t_ctx[a:b], c.t_blk_start[a:b + 1], c.t_ids, c.n_tok, new, c.status)
+                 for a, b, new in ((3, 6, 300), (0, 3, 1))]
+        qr = torch.full((c.n_tok, c.heads, c.dim), 7.5, dtype=DTYPES[c.dtype], device=c.dev)
+        c.table = table_of(1001, c.dim)
+        for st in steps:
+            c.ctx.tutti_kv_append_layer(1, st, T.make_tokens(c.k, c.v, c.q, qr), T.make_rope(c.table))
+            assert int(c.status) == T.OK
+            if st is steps[0]:
+                assert (qr[:3] == 7.5).all()
+        append_verify(c, qr)
+        fill_new(c)
+        out = torch.full_like(qr, 7.5)
+        c.lse = torch.full((c.n_tok, c.heads), 7.5, dtype=torch.float32, device=c.dev)
+        for st in steps:
+            c.attn.tutti_kv_attend_layer(1, st, T.make_attend(c.q, out, c.lse), c.dim ** -0.5)
+            assert int(c.status) == T.OK
+            if st is steps[0]:
+                assert (out[:3] == 7.5).all() and (c.lse[:3] == 7.5).all()
+        verify(c, out)
     finally:
         c.close()
 
