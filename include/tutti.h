@@ -517,7 +517,7 @@ typedef struct tutti_step {
 /* A step's projections, device pointers to [n_tok][heads][head_dim] elements of dtype; strides
  * in elements from one token to the next, so that q, k and v may be parts of one packed row.
  * Base addresses are 16-byte aligned, strides multiples of 8.  q and q_out may be the same
- * array; both NULL (and n_q_heads 0) leaves the queries out. */
+ * array, with one stride; both NULL (and n_q_heads 0) leaves the queries out. */
 typedef struct tutti_tokens {
     uint32_t dtype; /* TUTTI_DTYPE_* */
     uint32_t n_q_heads;

@@ -437,6 +437,8 @@ int tutti_append_check_(const tutti_geom_t *g, const tutti_step_t *step, const t
         if (!rows_ok(t->q, t->q_stride, t->n_q_heads, g->head_dim) ||
             !rows_ok(t->q_out, t->q_out_stride, t->n_q_heads, g->head_dim))
             return TUTTI_EINVAL;
+        // in place means row by row: with another stride a row would land on one not read yet
+        if (t->q == t->q_out && t->q_stride != t->q_out_stride && step->n_tok > 1) return TUTTI_EINVAL;
     } else if (t->q || t->q_out) {
         return TUTTI_EINVAL;
     }

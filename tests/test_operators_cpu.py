@@ -82,6 +82,13 @@ def test_tokens_that_are_refused(kw):
     assert append_rc(t=tokens(**kw)) == T.EINVAL
 
 
+def test_queries_in_place_have_one_stride():
+    q = dict(q=0x10000, q_out=0x10000, q_stride=1536)
+    assert append_rc(t=tokens(q_out_stride=1536, **q)) == T.OK
+    assert append_rc(t=tokens(q_out_stride=1024, **q)) == T.EINVAL
+    assert append_rc(t=tokens(q_out_stride=1024, **q), s=step(n_tok=1)) == T.OK
+
+
 @pytest.mark.parametrize("kw", [dict(style=2), dict(rot_dim=0), dict(rot_dim=24), dict(rot_dim=144), dict(table=None),
                                 dict(table=0x50008), dict(n_pos=0)])
 def test_rotations_that_are_refused(kw):
