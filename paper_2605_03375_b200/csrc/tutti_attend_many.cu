@@ -34,6 +34,7 @@
 // -> next scores of a half.  On a B200 (1676 TFLOP/s in short, 1389 in long runs of the library's product): 2048 new tokens
 // over 32768, 32 heads, bf16, 1040-1180 us = 960-1090 TFLOP/s; 1801 over 2 x 8192 256 us = 974; 8-bit, fp16, 64 heads, 4
 // ragged chunks over 2000-9000 280 us = 667 (the widening of the codes and shared memory).
+#include <cstring>
 #include <type_traits>
 
 #include "tutti_attend.h"
@@ -285,27 +286,37 @@ __device__ inline uint2 spread(uint32_t w, __nv_bfloat16, uint32_t &top) {
     return make_uint2(even | ((w << 8) & 0x80008000u), odd | (w & 0x80008000u));
 }
 __device__ inline uint2 spread(uint32_t w, __half, uint32_t &) { return spread(w, __half()); }
-__device__ inline uint32_t twice(float x, __half) { return pack2(x, x, __half()); }
-__device__ inline uint32_t twice(float x, __nv_bfloat16) { return pack2(x, x, __nv_bfloat16()); }
-__device__ inline uint32_t times(uint32_t x, uint32_t s, __half) {
-    const __half2 y = __hmul2(*reinterpret_cast<const __half2 *>(&x), *reinterpret_cast<const __half2 *>(&s));
-    return *reinterpret_cast<const uint32_t *>(&y);
+template <typename P>
+__host__ __device__ inline uint32_t word(const P &x) {
+    uint32_t w;
+    memcpy(&w, &x, 4);
+    return w;
 }
-__device__ inline uint32_t times(uint32_t x, uint32_t s, __nv_bfloat16) {
-    const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&x), *reinterpret_cast<const __nv_bfloat162 *>(&s));
-    return *reinterpret_cast<const uint32_t *>(&y);
+template <typename P>
+__host__ __device__ inline P pair_of(uint32_t w) {
+    P x;
+    memcpy((void *)&x, &w, 4);
+    return x;
+}
+__host__ __device__ inline uint32_t twice(float x, __half) { return word(__float2half2_rn(x)); }
+__host__ __device__ inline uint32_t twice(float x, __nv_bfloat16) { return word(__float2bfloat162_rn(x)); }
+__host__ __device__ inline uint32_t times(uint32_t x, uint32_t s, __half) { return word(__hmul2(pair_of<__half2>(x), pair_of<__half2>(s))); }
+__host__ __device__ inline uint32_t times(uint32_t x, uint32_t s, __nv_bfloat16) {
+    return word(__hmul2(pair_of<__nv_bfloat162>(x), pair_of<__nv_bfloat162>(s)));
 }
 // A scale as the two factors that finish spread(), each rounded to the type (powers of two are
-// exact) and twice in a register; true if the second is not 1.  f16: half the value, so that
-// nothing that came from f16 overflows, and a second factor for what is below the normal range.
-__device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __half) {
+// exact) and twice in a register; true if the second is not 1.  f16: half the value, so that the scales of
+// f16 rows (2^8 at most) give nothing above 448 * 2^7; where half the scale is below the normal range it is
+// brought in 2^14 times too large, which is below 1, so the code times it stays below 448 and the second
+// factor rounds once, into the subnormal range where the product lies there.
+__host__ __device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __half) {
     s *= 0.5f;
-    const bool low = s != 0 && fabsf(s) < 6.103515625e-05f;
-    f1 = twice(low ? s * 16777216.0f : s, __half());
-    f2 = twice(low ? 5.9604644775390625e-08f : 1.0f, __half());               // 2^-24
+    const bool low = s != 0 && fabsf(s) < 0x1p-14f;
+    f1 = twice(low ? s * 0x1p14f : s, __half());
+    f2 = twice(low ? 0x1p-14f : 1.0f, __half());
     return low;
 }
-__device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __nv_bfloat16) {
+__host__ __device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __nv_bfloat16) {
     const bool high = fabsf(s) >= 128.0f;                                     // 2^120 * s would overflow
     f1 = twice(high ? 1.329227995784916e+36f : 1.329227995784916e+36f * s, __nv_bfloat16());
     f2 = twice(high ? s : 1.0f, __nv_bfloat16());
@@ -1114,4 +1125,20 @@ extern "C" int tutti_many_units_(uint32_t ctx, uint32_t n_new, uint32_t group, u
     out2[0] = q < r.n_tiles ? r.units(q) : 0;
     out2[1] = r.before(q);
     return (int)r.n_tiles;
+}
+
+// What a code becomes on its way into a many-row product, on the host: the two 16-bit elements of a pair (one
+// code twice) behind both factors, as `widen` multiplies them.  f16: half the value.
+template <typename T>
+static uint32_t widened(uint8_t code, float scale) {
+    __nv_fp8_e4m3 c;
+    c.__x = code;
+    const float start = std::is_same<T, __half>::value ? (float)c : (float)c * 0x1p-120f;      // see spread()
+    uint32_t f1, f2;
+    const bool two = tutti::factors(scale, f1, f2, T());
+    const uint32_t x = tutti::times(tutti::twice(start, T()), f1, T());
+    return two ? tutti::times(x, f2, T()) : x;
+}
+extern "C" uint32_t tutti_many_widen_(uint32_t code, float scale, uint32_t dtype) {
+    return dtype == TUTTI_DTYPE_BF16 ? widened<__nv_bfloat16>((uint8_t)code, scale) : widened<__half>((uint8_t)code, scale);
 }
