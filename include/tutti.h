@@ -593,8 +593,15 @@ int tutti_kv_append_layer(tutti_ctx_t *ctx, uint32_t layer, const tutti_step_t *
  * step's own tokens that is NaN or infinite may also reach rows of the same sequence's step that
  * come before it, as 0 * NaN.)
  * Sums and softmax statistics are 32-bit.  Probabilities are rounded to 16 bits for the product
- * with the values; keys and values of an 8-bit pool are code * scale, without a rounding of their
- * own for the scales that the append call makes (others may be rounded to the 16 bits of dtype).
+ * with the values: to dtype, over an 8-bit pool with up to 16 rows to fp16 (rows: max_new *
+ * n_q_heads / n_kv_heads).  An 8-bit pool's keys and values are code * scale; what is rounded there:
+ *   up to 16 rows: the scales are applied in 32 bits.  bf16 queries become fp16 in units of a power of
+ *   two of the row: exact but for elements below 2^-14 of its largest, which are off by up to 2^-25 of it.
+ *   more rows, bf16: nothing where scales are powers of two (append's are), else code * scale once.
+ *   more rows, fp16: code * scale in units of a power of two, one for 64 neighbouring keys.  Keys are exact
+ *   unless a scale among the 64 is more than 2^22 times larger; values of magnitude below 2^-13 are off by up
+ *   to 2^-24, the smallest step of an fp16 output.  (Scales that are not powers of two: rounded to 11 bits.)
+ *   Scales may be anything up to 2^70, beyond what fp16 rows bring.
  * The result of a call does not depend on the order in which the GPU runs its parts.
  * The handle holds the workspace in which parts of a long sequence are joined (about 40 MB): calls
  * on one handle must be ordered after each other (one stream, or events; replays of captured

@@ -25,9 +25,9 @@
 //             sequence ends inside the unit, a block is missing or blocks do not tile 64 rows, row
 //             by row with zeros in place of what is not there.  Two groups of two warps take the
 //             units in turn, so a group waits for its own loads while the other's are in flight.
-//             8-bit codes are widened to 16 bits (code * scale, exact for the powers of two that
-//             append writes): keys where they landed, values out of a buffer of their own, so that
-//             they are fetched before the place they go to is free.
+//             8-bit codes are widened to 16 bits (code * scale; f16 in units of a power of two for the 64 keys of
+//             a step, which the softmax warps undo): keys where they landed, values out of a buffer of their
+//             own, so that they are fetched before the place they go to is free.
 // Bound: the tensor cores (2 x 128 x 128 x D multiply-adds a half and unit: 2048 clocks a unit for D = 128)
 // and, as close, the 2 x 128 x 128 exponentials on 16 lanes a clock; in a long loop the power limit
 // (1550 MHz at 1000 W).  What is reached: 3500 clocks a unit, set by the chain scores -> softmax -> P V
@@ -55,6 +55,10 @@ constexpr uint32_t ATOM = BN * 128;     // 128 rows of 128 bytes
 constexpr int SUB_16 = 128, SUB_8 = 64;  // keys of a step, by the cache's bits
 constexpr int REGS_16 = 192, REGS_8 = 160;  // of a softmax thread; the other half of the threads has 256 less these
 constexpr float GROW = 8.0f;            // log2 of how far probabilities may exceed 1
+// Exponents of the units of f16 operands (see unit_of).  Keys: any.  Values: 2 at least, the unit of nearly every
+// cache (f16 rows give scales of 2^8 at most), so that the output's unit changes only for larger ones; what is
+// lost below is 2^-24, the smallest step that an f16 output has.  2^64 at most: parts are joined by 32-bit weights.
+constexpr int UNIT_LEAST_K = -120, UNIT_MOST_K = 120, UNIT_LEAST_V = 1, UNIT_MOST_V = 64;
 constexpr long long WAIT_CLOCKS = 3000000000ll;   // about 1.5 s: a wait that takes longer is given up
 
 // sum over i in [0, n) of floor((a i + b) / m)  (a, b >= 0, m > 0)
@@ -304,13 +308,24 @@ __host__ __device__ inline uint32_t times(uint32_t x, uint32_t s, __half) { retu
 __host__ __device__ inline uint32_t times(uint32_t x, uint32_t s, __nv_bfloat16) {
     return word(__hmul2(pair_of<__nv_bfloat162>(x), pair_of<__nv_bfloat162>(s)));
 }
+// f16 operands of an 8-bit cache are kept in units of a power of two, one for the keys and one for the values of
+// a step's 64 rows: the exponent that brings their largest scale (its bits) to 2^7 at most, so that no code
+// times scale passes 448 * 2^7, between `least` and `most`.
+__host__ __device__ inline int unit_of(uint32_t top, int least, int most) {
+    const int e = (int)((top + 0x7fffffu) >> 23) - 127 - 7;        // the power of two at or above it
+    return e < least ? least : e > most ? most : e;
+}
+__host__ __device__ inline float pow2(int e) {                     // -126 <= e <= 127
+    const uint32_t w = (uint32_t)(e + 127) << 23;
+    float x;
+    memcpy(&x, &w, 4);
+    return x;
+}
 // A scale as the two factors that finish spread(), each rounded to the type (powers of two are
-// exact) and twice in a register; true if the second is not 1.  f16: half the value, so that the scales of
-// f16 rows (2^8 at most) give nothing above 448 * 2^7; where half the scale is below the normal range it is
-// brought in 2^14 times too large, which is below 1, so the code times it stays below 448 and the second
-// factor rounds once, into the subnormal range where the product lies there.
+// exact) and twice in a register; true if the second is not 1.  f16 (a scale in its unit, 2^7 at most): one below
+// the normal range is brought in 2^14 times too large, which is below 1, so the code times it stays below 448
+// and the second factor rounds once, into the subnormal range where the product lies there.
 __host__ __device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __half) {
-    s *= 0.5f;
     const bool low = s != 0 && fabsf(s) < 0x1p-14f;
     f1 = twice(low ? s * 0x1p14f : s, __half());
     f2 = twice(low ? 0x1p-14f : 1.0f, __half());
@@ -332,11 +347,11 @@ struct Many {
     static constexpr uint32_t OFF_RAW = OFF_RING + RING * KV;          // 8-bit: codes of a group's values
     static constexpr uint32_t OFF_BAR = OFF_RAW + (C8 ? 2 * ATOM : 0);
     static constexpr uint32_t OFF_EXISTS = OFF_BAR + 288;   // [8 units][4]: keys that exist
-    static constexpr uint32_t OFF_MISC = OFF_EXISTS + 128;
+    static constexpr bool UNITS = C8 && std::is_same<T, __half>::value;
+    static constexpr uint32_t OFF_UNITS = OFF_EXISTS + 128; // [8 units][2 steps]: exponents of keys' and values' units
+    static constexpr uint32_t OFF_MISC = OFF_UNITS + (UNITS ? 128 : 0);
     static constexpr uint32_t OFF_TILE = OFF_MISC + 320;
     static constexpr uint32_t SMEM = OFF_TILE + 256 + 1024; // 1024: alignment of the dynamic part
-    // f16 codes are widened at half their value: scores and outputs make up for it
-    static constexpr float VALUE = C8 && std::is_same<T, __half>::value ? 2.0f : 1.0f;
     // f16 probabilities are kept 2^6 times too large (at most 2^14): full precision down to 2^-20
     static constexpr float OFF = std::is_same<T, __half>::value ? 6.0f : 0.0f;
     // whether widened codes keep their order
@@ -358,6 +373,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     uint32_t *misc = reinterpret_cast<uint32_t *>(sm + C::OFF_MISC);
     uint32_t *exists = reinterpret_cast<uint32_t *>(sm + C::OFF_EXISTS);
     Found *found = reinterpret_cast<Found *>(sm + C::OFF_TILE);
+    int2 *units = reinterpret_cast<int2 *>(sm + C::OFF_UNITS);
     volatile uint32_t *dead = misc + 72;
     const uint32_t bars = base + C::OFF_BAR;
     const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, o_full = bars + 80, o_empty = bars + 96,
@@ -564,10 +580,20 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             uint32_t fac[2][2], sec[2][2];              // 8-bit: the scales' two factors, twice 16 bits
             bool small = false;
             if constexpr (C8) {
+                float k_in = 1.0f, v_in = 1.0f;
+                if constexpr (C::UNITS) {
+                    auto most = [](const float (&x)[2]) {
+                        return __reduce_max_sync(0xffffffffu, max(__float_as_uint(fabsf(x[0])), __float_as_uint(fabsf(x[1]))));
+                    };
+                    const int ku = unit_of(most(ks), UNIT_LEAST_K, UNIT_MOST_K), vu = unit_of(most(vs), UNIT_LEAST_V, UNIT_MOST_V);
+                    if (lane == 0) units[(n & 7) * 2 + half] = make_int2(ku, vu);
+                    k_in = pow2(-ku);
+                    v_in = pow2(-vu);
+                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    small = factors(ks[i], fac[0][i], sec[0][i], T()) || small;
-                    small = factors(vs[i], fac[1][i], sec[1][i], T()) || small;
+                    small = factors(ks[i] * k_in, fac[0][i], sec[0][i], T()) || small;
+                    small = factors(vs[i] * v_in, fac[1][i], sec[1][i], T()) || small;
                 }
                 small = __any_sync(0xffffffffu, small);
             }
@@ -608,9 +634,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if (lane == 0) mbar_arrive(full + 8 * (2 * group + kv));
             };
             // 8-bit: four steps' codes are read before the rows they may lie in are written
-            auto widen = [&](int kv, auto two_factors) {
+            auto widen = [&](int kv, uint32_t fa, uint32_t fb, uint32_t sa, uint32_t sb, auto two_factors) {
                 constexpr int B = 4;
-                const unsigned char *src = sm + land[kv];
+                const unsigned char *src = sm + (kv ? land[1] : land[0]);
                 unsigned char *dst = sm + slot0 + kv * C::KV;
 #pragma unroll 1
                 for (int it0 = 0; it0 < 64 / RPI; it0 += B) {
@@ -625,7 +651,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 #pragma unroll
                     for (int k = 0; k < B; ++k) {
                         const uint32_t r = (it0 + k) * RPI + sub, row = half * 64 + r;
-                        const uint32_t f1 = __shfl_sync(0xffffffffu, r < 32 ? fac[kv][0] : fac[kv][1], r % 32);
+                        const uint32_t f1 = __shfl_sync(0xffffffffu, r < 32 ? fa : fb, r % 32);
                         const uint32_t w[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
                         uint32_t e[8];
 #pragma unroll
@@ -635,7 +661,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                             e[2 * i + 1] = times(x.y, f1, T());
                         }
                         if constexpr (two_factors.value) {
-                            const uint32_t f2 = __shfl_sync(0xffffffffu, r < 32 ? sec[kv][0] : sec[kv][1], r % 32);
+                            const uint32_t f2 = __shfl_sync(0xffffffffu, r < 32 ? sa : sb, r % 32);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) e[i] = times(e[i], f2, T());
                         }
@@ -680,7 +706,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 step_unit();
                 step_unit();
                 locate();
-#pragma unroll
+#pragma unroll 1                                        // the widening loops once in the code: 265 us against 293 on the 8-bit chunk of the header (fetching of instructions)
                 for (int kv = 0; kv < 2; ++kv) {
                     if (kv == 1) {
                         resolve();                      // the next unit's scales arrive while this one's values are widened
@@ -693,8 +719,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         cp_wait<0>();
                         __syncwarp();                   // the warp's rows, brought by all its lanes
                     }
-                    if (small) widen(kv, std::true_type());
-                    else widen(kv, std::false_type());
+                    const uint32_t fa = kv ? fac[1][0] : fac[0][0], fb = kv ? fac[1][1] : fac[0][1];
+                    const uint32_t sa = kv ? sec[1][0] : sec[0][0], sb = kv ? sec[1][1] : sec[0][1];
+                    if (small) widen(kv, fa, fb, sa, sb, std::true_type());
+                    else widen(kv, fa, fb, sa, sb, std::false_type());
                     arrive(kv);
                 }
                 if (!ok) break;
@@ -824,7 +852,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         setmaxnreg_inc<C::SOFT_REGS>();
         const int i = warp / 4;                                   // half
         const uint32_t lanes = (warp % 4) * 32 << 16, o_at = O(i) + lanes, r = (warp % 4) * 32 + lane;
-        const float scl = fmaxf(fabsf(p.scale) * 1.4426950408889634f * C::VALUE, 1e-30f);
+        const float scl_all = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 1e-30f);
         const bool negative = p.scale < 0;
         uint32_t n_s = 0, n_seg = 0, n_unit = 0, n_join = 0;                 // steps of this half; units of the worker
         bool ok = true;
@@ -844,6 +872,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 const int64_t pos = t.r.first + tok;
                 const int64_t pos_low = __shfl_sync(0xffffffffu, pos, 0);
                 float m = -INFINITY, l = 0;
+                int o_unit = UNIT_LEAST_V;                        // UNITS: exponent of the output's unit, the largest of its values'
                 const uint32_t steps = STEPS * n;
                 for (uint32_t j = 0; j < steps && ok; ++j) {
                     const int u = j % STEPS;
@@ -861,6 +890,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     for (int q = 0; q < SUB / 32; ++q) {
                         ex[q] = exists[((n_unit + j / STEPS) & 7) * 4 + SUB / 32 * u + q];
                         all &= ex[q];
+                    }
+                    float scl = scl_all;
+                    int below = 0;                                // of the values' unit to the output's
+                    if constexpr (C::UNITS) {
+                        const int2 unit = units[((n_unit + j / STEPS) & 7) * 2 + u];
+                        scl = fmaxf(scl * pow2(unit.x), 0x1p-126f);         // not zero, for the scores of -infinity
+                        below = o_unit - unit.y;
                     }
                     tc_wait_ld();
 #pragma unroll
@@ -889,10 +925,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     a1 = max3(a1, s[SUB - 2], s[SUB - 1]);
                     const float top = max3(a0, a1, fmaxf(a2, a3)) * scl;
                     const bool grow = top > m + GROW || (m == -INFINITY && top > m);
-                    if (__any_sync(0xffffffffu, grow)) {          // rare: the reference has to move
-                        const float alpha = grow ? ex2(m - top) : 1.0f;
+                    if (__any_sync(0xffffffffu, grow) || below != 0) {          // rare: the reference has to move, or the unit
+                        float alpha = grow ? ex2(m - top) : 1.0f;
                         if (grow) m = top;
                         l *= alpha;
+                        if (below != 0) {                         // exact, and far from the ends of the range
+                            alpha *= pow2(below);
+                            o_unit -= below;
+                        }
                         if (j > 0) {
                             // these scores were issued behind the product two steps back, so only the last one's may be open
                             ok = mbar_wait(o_full + 8 * i, (n_s - 1) & 1, dead);
@@ -945,6 +985,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_after();
+                if (C::UNITS && o_unit != UNIT_LEAST_V) {          // outputs 2^x too small: as much in the reference, out of the sum
+                    m += (float)(o_unit - UNIT_LEAST_V);
+                    l *= pow2(UNIT_LEAST_V - o_unit);
+                }
                 bool write = true;
                 const bool whole = t.u == 0 && n == t.n_units;
                 float o[D];
@@ -998,7 +1042,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if (write) {
                     const uint64_t token = t.v.q0 + tok;
                     const uint32_t qh = t.h * p.group + p.member_of(in ? row : t.r.n_rows - 1);
-                    const float inv = m == -INFINITY ? 0.0f : C::VALUE / l;
+                    const float inv = m == -INFINITY ? 0.0f : (C::UNITS ? pow2(UNIT_LEAST_V) : 1.0f) / l;
                     const unsigned long long mine = in ? (unsigned long long)((T *)p.out + token * p.out_stride + (uint64_t)qh * D) : 0;
                     unsigned long long to[4];               // the rows of the lane's quad
 #pragma unroll
@@ -1128,7 +1172,8 @@ extern "C" int tutti_many_units_(uint32_t ctx, uint32_t n_new, uint32_t group, u
 }
 
 // What a code becomes on its way into a many-row product, on the host: the two 16-bit elements of a pair (one
-// code twice) behind both factors, as `widen` multiplies them.  f16: half the value.
+// code twice) behind both factors, as `widen` multiplies them.  f16: in the unit that a step whose largest
+// scale is `top` has (its exponent goes to *unit; keys or values by their least one).
 template <typename T>
 static uint32_t widened(uint8_t code, float scale) {
     __nv_fp8_e4m3 c;
@@ -1139,6 +1184,11 @@ static uint32_t widened(uint8_t code, float scale) {
     const uint32_t x = tutti::times(tutti::twice(start, T()), f1, T());
     return two ? tutti::times(x, f2, T()) : x;
 }
-extern "C" uint32_t tutti_many_widen_(uint32_t code, float scale, uint32_t dtype) {
-    return dtype == TUTTI_DTYPE_BF16 ? widened<__nv_bfloat16>((uint8_t)code, scale) : widened<__half>((uint8_t)code, scale);
+extern "C" uint32_t tutti_many_widen_(uint32_t code, float scale, float top, uint32_t dtype, uint32_t is_v, int32_t *unit) {
+    *unit = 0;
+    if (dtype == TUTTI_DTYPE_BF16) return widened<__nv_bfloat16>((uint8_t)code, scale);
+    uint32_t bits;
+    memcpy(&bits, &top, 4);
+    *unit = is_v ? tutti::unit_of(bits, tutti::UNIT_LEAST_V, tutti::UNIT_MOST_V) : tutti::unit_of(bits, tutti::UNIT_LEAST_K, tutti::UNIT_MOST_K);
+    return widened<__half>((uint8_t)code, scale * tutti::pow2(-*unit));
 }

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2605_03375_b200 import tutti as T
-from tests.opcase import OpCase
+from tests.opcase import OpCase, check
 from tests.test_gpu_attend import attend, fill_new, verify
 
 pytestmark = pytest.mark.gpu
@@ -55,5 +55,64 @@ def test_small_values_are_appended_and_attended(dtype):
         used = torch.cat([s.log2().unique() for s in c.scale])
         assert {-15.0, -14.0} <= set(used.tolist())
         verify(c, attend(c))
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype,dim", [("fp16", 64), ("fp16", 128), ("bf16", 128)])
+def test_attend8_keys_at_scales_beyond_those_of_fp16_rows(dtype, dim, new):
+    """A pool that bf16 steps have filled: keys far beyond 65504, scores as small as any."""
+    c = OpCase([(60, new), (3, new), (700, new)], heads=4, kv_heads=2, dim=dim, cache="8", dtype=dtype, seed=84)
+    try:
+        fill_new(c)
+        for e in (9, 12, 17, 25, 40, 60):
+            set_scales(c, lambda s, b: e - b % 3)
+            c.scale[1].fill_(2.0 ** -7)
+            c.scale_dev[1].copy_(c.scale[1])
+            sm = 2.0 ** -e * 0.01
+            verify(c, attend(c, sm), sm)
+        assert int(c.status) == T.OK
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype,dim", [("fp16", 64), ("fp16", 128), ("bf16", 128)])
+@pytest.mark.parametrize("order", [0, 1, 2])
+def test_attend8_values_at_scales_beyond_those_of_fp16_rows(dtype, dim, new, order):
+    """Values of up to 2^20 among small ones, in every order; outputs stay finite.  One sequence is shared by many workers."""
+    c = OpCase([(60, new), (330, new), (3000, new)], heads=4, kv_heads=2, dim=dim, cache="8", dtype=dtype, seed=85)
+    try:
+        fill_new(c)
+        exps = [-7, 9, 20, -7, 12, 17, 10, -12]                  # of the values' scales, by block
+        least = {12: 8, 17: 8, 20: 2}                            # codes 0..7 are subnormal, 0 and 1 the two smallest
+        at = lambda s, b: 0 if order == 1 and s == 2 and b < 150 else (b * (1, 3, 5)[order] + s) % 8  # noqa: E731
+        set_scales(c, lambda s, b: exps[at(s, b)])
+        c.scale[0].fill_(2.0 ** -7)
+        c.scale_dev[0].copy_(c.scale[0])
+        for s in range(3):
+            for b in range(-(-int(c.ctx_len[s]) // c.bs)):
+                x = c.block(c.raw, 1, int(c.block_ids[c.blk_start[s] + b]))
+                n = min(c.bs, int(c.ctx_len[s]) - b * c.bs)
+                if exps[at(s, b)] in least:
+                    g = torch.Generator().manual_seed(b)
+                    codes = torch.randint(0, least[exps[at(s, b)]], x.shape, generator=g, dtype=torch.uint8) + 128 * torch.randint(0, 2, x.shape, generator=g, dtype=torch.uint8)
+                    x[:n] = codes.view(torch.float8_e4m3fn)[:n]
+        c.pool.copy_(c.raw)
+        out = attend(c)
+        want, lse, tol, ltol = c.attend64(c.q, c.raw, c.scale, c.dim ** -0.5)
+        if dtype == "fp16":
+            # Probabilities are kept in the unit of the largest value scale, 2^13 here (2^20 is 2^7 of it), 2^12 of the
+            # usual one: half f16's smallest step, 2^-25, against a largest probability of 2^6; and values as
+            # much below that unit are off by 2^-25 of it.
+            for s in range(3):
+                v = np.abs(c.keys(c.raw, c.scale, 1, s, int(c.ctx_len[s]))).sum(0)
+                tol[c.q_start[s]:c.q_start[s + 1]] += np.repeat(2.0 ** (-31 + 12) * v, 2, 0) + 2.0 ** (13 - 25)
+        n = int(c.q_start[-1])
+        assert np.abs(want).max() < 65504
+        check(out[:n].float().double().cpu().numpy(), want, tol, "out")
+        check(c.lse[:n].double().cpu().numpy(), lse, ltol, "lse")
+        assert int(c.status) == T.OK
     finally:
         c.close()
