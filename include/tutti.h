@@ -587,8 +587,8 @@ int tutti_kv_append_layer(tutti_ctx_t *ctx, uint32_t layer, const tutti_step_t *
  * head h / (n_q_heads / n_kv_heads); the row at position p attends to the keys at positions
  * 0..p of its sequence (its own key included: append first).
  *     out = sum_j softmax_j(scale * q . k_j) v_j,   lse = ln sum_j exp(scale * q . k_j)
- * A row that sees no key (padding, or only blocks outside the pool) gets out = 0 and
- * lse = -infinity.  Cache bytes behind a sequence's last token are never used, whatever they
+ * A row that sees no key (padding, or only blocks outside the pool), or whose scores are all
+ * -infinity, gets out = 0 and lse = -infinity; a score that is NaN makes both NaN.  Cache bytes behind a sequence's last token are never used, whatever they
  * hold.  (A key that is NaN or infinite reaches only the rows that see it; a VALUE of one of the
  * step's own tokens that is NaN or infinite may also reach rows of the same sequence's step that
  * come before it, as 0 * NaN.)

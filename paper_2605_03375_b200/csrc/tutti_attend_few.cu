@@ -560,7 +560,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
 #pragma unroll
         for (int i = 0; i < WARPS; ++i) {
             const float2 e = ml[i * F::ROWS + row];
-            L += M_ == -INFINITY ? 0 : e.y * ex2(e.x - M_);
+            L += e.y * (M_ == -INFINITY ? 0 : ex2(e.x - M_));     // a NaN sum stays one: scores of NaN move no maximum
         }
         float acc[GROUPS * 4];
 #pragma unroll
@@ -623,14 +623,14 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         if (write && row0 + row < n_rows) {
             const uint32_t i = token_of(row0 + row), qh = h * p.group + (row0 + row - i * p.group);
             const uint64_t tok = get.v.q0 + i;
-            const float inv = M_ == -INFINITY ? 0.0f : 1.0f / L;
+            const float inv = L == 0 ? 0.0f : 1.0f / L;
             T *out = (T *)p.out + tok * p.out_stride + (uint64_t)qh * D;
 #pragma unroll
             for (int j = 0; j < GROUPS; ++j)
                 *reinterpret_cast<uint2 *>(out + (j * TPR + lanec) * 4) =
                     make_uint2(pack2(acc[j * 4] * inv, acc[j * 4 + 1] * inv, T()), pack2(acc[j * 4 + 2] * inv, acc[j * 4 + 3] * inv, T()));
             if (p.lse && lanec == 0)
-                p.lse[tok * p.n_q_heads + qh] = M_ == -INFINITY ? -INFINITY : (M_ - F::OFF + log2f(L)) * 0.6931471805599453f;
+                p.lse[tok * p.n_q_heads + qh] = L == 0 ? -INFINITY : (M_ - F::OFF + log2f(L)) * 0.6931471805599453f;
         }
         __syncthreads();                     // the stage and the small arrays may be written again
         stage = stage + 1 == F::STAGES ? 0 : stage + 1;

@@ -1042,7 +1042,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if (write) {
                     const uint64_t token = t.v.q0 + tok;
                     const uint32_t qh = t.h * p.group + p.member_of(in ? row : t.r.n_rows - 1);
-                    const float inv = m == -INFINITY ? 0.0f : (C::UNITS ? pow2(UNIT_LEAST_V) : 1.0f) / l;
+                    // l, not m, tells a row that saw nothing: scores of NaN move no maximum, but make the sum NaN
+                    const float inv = l == 0 ? 0.0f : (C::UNITS ? pow2(UNIT_LEAST_V) : 1.0f) / l;
                     const unsigned long long mine = in ? (unsigned long long)((T *)p.out + token * p.out_stride + (uint64_t)qh * D) : 0;
                     unsigned long long to[4];               // the rows of the lane's quad
 #pragma unroll
@@ -1080,7 +1081,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         for (int k = 0; k < 4; ++k)
                             if (to[k]) *reinterpret_cast<uint4 *>(to[k] + (d + (lane & 3)) * 16) = make_uint4(piece[k][0], piece[k][1], piece[k][2], piece[k][3]);
                     }
-                    if (p.lse && in) p.lse[token * p.n_q_heads + qh] = m == -INFINITY ? -INFINITY : (m - C::OFF + log2f(l)) * 0.6931471805599453f;
+                    if (p.lse && in) p.lse[token * p.n_q_heads + qh] = l == 0 ? -INFINITY : (m - C::OFF + log2f(l)) * 0.6931471805599453f;
                 }
             }
             n_unit += n;

@@ -116,3 +116,49 @@ def test_attend8_values_at_scales_beyond_those_of_fp16_rows(dtype, dim, new, ord
         assert int(c.status) == T.OK
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("cache,dtype", [("16", "bf16"), ("16", "fp16"), ("8", "bf16"), ("8", "fp16")])
+@pytest.mark.parametrize("new", [1, 40])
+def test_nan_scores_make_out_and_lse_nan(cache, dtype, new):
+    """A query of NaN; keys of NaN in every block but the last, so that whole parts of a shared row have no other score."""
+    c = OpCase([(3000, new), (60, new), (0, new)], heads=4, kv_heads=2, dim=128, cache=cache, dtype=dtype, seed=86)
+    try:
+        fill_new(c)
+        row = int(c.q_start[1])
+        c.q[row, 2, 5] = float("nan")
+        out = attend(c)
+        got, lse = torch.isnan(out.float()), torch.isnan(c.lse)
+        assert got[row, 2].all() and lse[row, 2]
+        got[row, 2], lse[row, 2] = False, False
+        assert not got.any() and not lse.any() and torch.isfinite(c.lse[:int(c.q_start[-1])][~lse[:int(c.q_start[-1])]]).sum() == lse[:int(c.q_start[-1])].numel() - 1
+        c.q[row, 2, 5] = 1
+        for b in range(-(-3000 // c.bs) - 1):
+            x = c.block(c.raw, 0, int(c.block_ids[b]))[:, 1, 77]
+            x.copy_(torch.full(x.shape, float("nan")))
+        c.pool.copy_(c.raw)
+        out = attend(c)
+        verify(c, out, skip=(0,))
+        got, lse = torch.isnan(out[:new].float()), torch.isnan(c.lse[:new])
+        assert got[:, 2:].all() and lse[:, 2:].all() and not got[:, :2].any() and torch.isfinite(c.lse[:new, :2]).all()
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_scores_that_are_all_minus_infinity(new):
+    c = OpCase([(60, new), (5, new)], heads=4, kv_heads=2, dim=64, packed=False, seed=87)
+    try:
+        fill_new(c)
+        q = c.q.clone()
+        c.q.zero_()
+        c.q[:, :, 0] = 1
+        for b in range(-(-int(c.ctx_len[0]) // c.bs)):
+            c.block(c.raw, 0, int(c.block_ids[b]))[:, 0, 0] = float("-inf")
+        c.pool.copy_(c.raw)
+        out = attend(c)
+        assert (out[:new, :2] == 0).all() and (c.lse[:new, :2] == -float("inf")).all()
+        assert torch.isfinite(c.lse[:new, 2:]).all() and torch.isfinite(c.lse[new:2 * new]).all() and torch.isfinite(out[:2 * new].float()).all()
+        c.q.copy_(q)
+    finally:
+        c.close()
