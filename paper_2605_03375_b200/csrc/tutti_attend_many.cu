@@ -852,7 +852,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         setmaxnreg_inc<C::SOFT_REGS>();
         const int i = warp / 4;                                   // half
         const uint32_t lanes = (warp % 4) * 32 << 16, o_at = O(i) + lanes, r = (warp % 4) * 32 + lane;
-        const float scl_all = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 1e-30f);
+        // Scores are multiplied by a positive factor, so that masked ones stay -infinity and the largest stays the
+        // largest; the smallest number there is makes the largest score of a zero scale less than 2^-20.
+        const float scl_all = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 0x1p-149f);
         const bool negative = p.scale < 0;
         uint32_t n_s = 0, n_seg = 0, n_unit = 0, n_join = 0;                 // steps of this half; units of the worker
         bool ok = true;

@@ -162,3 +162,29 @@ def test_scores_that_are_all_minus_infinity(new):
         c.q.copy_(q)
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("new", [1, 40])
+@pytest.mark.parametrize("dtype,cache", [("bf16", "16"), ("bf16", "8"), ("fp16", "8")])
+def test_scales_of_zero_and_next_to_it(new, dtype, cache):
+    """Products of queries and keys of 2^60 and more, which a scale makes ordinary scores again, or nothing."""
+    c = OpCase([(60, new), (500, new)], heads=4, kv_heads=2, dim=64, dtype=dtype, cache=cache, packed=False, seed=88)
+    try:
+        fill_new(c)
+        q_up, k_up = (60, 55) if dtype == "bf16" else (0, 110)
+        c.q *= 2.0 ** q_up
+        if cache == "8":
+            set_scales(c, lambda s, b: k_up)
+            c.scale[1].fill_(2.0 ** -7)
+            c.scale_dev[1].copy_(c.scale[1])
+        else:
+            for s in range(2):
+                for b in range(-(-int(c.ctx_len[s]) // c.bs)):
+                    c.block(c.raw, 0, int(c.block_ids[c.blk_start[s] + b])).mul_(2.0 ** k_up)
+            c.pool.copy_(c.raw)
+        small = 2.0 ** -(q_up + k_up) / (100 if cache == "8" else 1)
+        for scale in (small, -small, 0.0, -0.0, 2.0 ** -149):
+            verify(c, attend(c, scale), scale)
+        assert int(c.status) == T.OK
+    finally:
+        c.close()
