@@ -36,6 +36,11 @@ struct Workspace {
     uint32_t workers;
 };
 
+// a / b, by the much faster 32-bit division where both fit (they nearly always do)
+__host__ __device__ inline unsigned long long quotient(unsigned long long a, unsigned long long b) {
+    return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b;
+}
+
 #ifdef __CUDACC__
 // One arrival: what this thread has seen of its CTA (behind a barrier) is released with it, and what the
 // earlier arrivals released is acquired.
@@ -43,10 +48,6 @@ __device__ inline uint32_t arrive_gpu(uint32_t *count) {
     uint32_t old;
     asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(old) : "l"(count) : "memory");
     return old;
-}
-// a / b, by the much faster 32-bit division where both fit (they nearly always do)
-__device__ inline unsigned long long quotient(unsigned long long a, unsigned long long b) {
-    return (a | b) >> 32 ? a / b : (uint32_t)a / (uint32_t)b;
 }
 __device__ inline float ex2(float x) {
     float y;

@@ -128,6 +128,17 @@ __host__ __device__ inline Rows rows_of(const SeqView &v, uint32_t group) {
 // high(n) on (a tile of 2 SNAP units or less is never cut).
 __host__ __device__ inline uint32_t snap_low(uint32_t n) { return n <= 2 * SNAP ? (n + 1) / 2 : SNAP; }
 __host__ __device__ inline uint32_t snap_high(uint32_t n) { return n <= 2 * SNAP ? n / 2 : SNAP; }
+__host__ __device__ inline uint32_t snapped(uint32_t u, uint32_t n) { return u < snap_low(n) ? 0 : u >= n - snap_high(n) ? n : u; }
+// Unit at which worker w's share starts, before it is moved.
+__host__ __device__ inline unsigned long long cut_of(unsigned long long w, unsigned long long workers, unsigned long long total) {
+    return quotient(w * total, workers);
+}
+// The first and the last worker that have a part of a tile of n units that starts at unit tile0: those whose
+// first and last cut before the tile's end lie in front of it and inside.
+__host__ __device__ inline void holders(unsigned long long tile0, uint32_t n, unsigned long long workers, unsigned long long total, uint32_t &w0, uint32_t &w1) {
+    w0 = (uint32_t)quotient((tile0 + snap_low(n)) * workers - 1, total);
+    w1 = (uint32_t)quotient((tile0 + n - snap_high(n)) * workers - 1, total);
+}
 
 struct Tile {
     uint32_t s, h, q, u, n_units;
@@ -424,7 +435,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     if (w >= workers) return;
     // The share [x0, x1): cuts at multiples of total / workers, moved to a tile's end where one is near.
     // Threads find the sequences of both cuts, warps 0 and 1 the tiles.
-    const unsigned long long cut[2] = {quotient(w * total, workers), quotient((w + 1) * total, workers)};
+    const unsigned long long cut[2] = {cut_of(w, workers, total), cut_of(w + 1, workers, total)};
 #pragma unroll
     for (int i = 0; i < 2; ++i)
         if (cut[i] >= start && cut[i] < start + mine) {
@@ -494,13 +505,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             f.q = lo;
             f.u = (uint32_t)(rest - at);
             f.n_units = r.units(lo);
-            if (f.u < snap_low(f.n_units)) {
-                x -= f.u;
-                f.u = 0;
-            } else if (f.u >= f.n_units - snap_high(f.n_units)) {
-                x += f.n_units - f.u;
-                if (x < total) next_tile(p, f);
-            }
+            const uint32_t u = snapped(f.u, f.n_units);
+            x = x - f.u + u;
+            f.u = u;
+            if (u == f.n_units && x < total) next_tile(p, f);
         }
         __syncwarp();
         if (lane == 0) {
@@ -1004,9 +1012,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 if (lane == 0) mbar_arrive(o_empty + 8 * i);
                 if (!whole) {
                     const unsigned long long tile0 = x - t.u;
-                    // the workers whose first and last cut before the tile's end lie in front of it and inside
-                    const uint32_t w0 = (uint32_t)quotient((tile0 + snap_low(t.n_units)) * workers - 1, total);
-                    const uint32_t w1 = (uint32_t)quotient((tile0 + t.n_units - snap_high(t.n_units)) * workers - 1, total);
+                    uint32_t w0, w1;
+                    holders(tile0, t.n_units, workers, total, w0, w1);
                     auto slot = [&](uint32_t k) { return (k == w0 ? 2 * k + 1 : 2 * k) * 2 + i; };
                     float4 *part = reinterpret_cast<float4 *>(ws.part);
                     float2 *ml = reinterpret_cast<float2 *>(ws.part + (uint64_t)4 * ws.workers * HALF_ROWS * D);
@@ -1143,26 +1150,25 @@ size_t many_part_bytes(uint32_t workers) { return (size_t)4 * workers * HALF_ROW
 
 }  // namespace tutti
 
-// The kernel's own cuts, on the host, for tiles of n_units[i] units laid end to end: the share [x0, x1) of
-// worker w; and for a tile the first and the last worker that has a part of it.
+// The kernel's functions for cuts and parts, on the host, over tiles of n_units[i] units laid end to end (the search
+// for the tile of a cut is the caller's): the share [x0, x1) of worker w; and for a tile the first and the last worker
+// that has a part of it.
 extern "C" void tutti_many_cut_(const uint32_t *n_units, uint32_t n_tiles, uint64_t workers, uint64_t w, uint64_t *out) {
     uint64_t total = 0;
     for (uint32_t i = 0; i < n_tiles; ++i) total += n_units[i];
     for (int c = 0; c < 2; ++c) {
-        uint64_t x = (w + c) * total / workers, a = 0;
-        for (uint32_t i = 0; i < n_tiles; a += n_units[i++]) {
-            const uint32_t n = n_units[i];
-            if (x < a || x >= a + n) continue;
-            const uint32_t u = (uint32_t)(x - a);
-            x = u < tutti::snap_low(n) ? a : u >= n - tutti::snap_high(n) ? a + n : x;
-            break;
-        }
-        out[c] = x;
+        const uint64_t x = tutti::cut_of(w + c, workers, total);
+        uint64_t at = 0;
+        uint32_t i = 0;
+        while (i < n_tiles && x >= at + n_units[i]) at += n_units[i++];
+        out[c] = i < n_tiles ? at + tutti::snapped((uint32_t)(x - at), n_units[i]) : x;
     }
 }
 extern "C" void tutti_many_parts_(uint64_t tile0, uint32_t n, uint64_t workers, uint64_t total, uint64_t *out) {
-    out[0] = ((tile0 + tutti::snap_low(n)) * workers - 1) / total;
-    out[1] = ((tile0 + n - tutti::snap_high(n)) * workers - 1) / total;
+    uint32_t w0, w1;
+    tutti::holders(tile0, n, workers, total, w0, w1);
+    out[0] = w0;
+    out[1] = w1;
 }
 
 // The kernel's own count of units, on the host: out2[0] units of tile q, out2[1] units of the tiles before it.
