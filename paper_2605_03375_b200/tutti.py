@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -50,23 +51,27 @@ class Step(C.Structure):
     _fields_ = [("n_seq", C.c_uint32), ("n_tok", C.c_uint32), ("n_blk", C.c_uint32),
                 ("max_new", C.c_uint32), ("q_start", C.c_void_p), ("ctx_len", C.c_void_p),
                 ("blk_start", C.c_void_p), ("block_ids", C.c_void_p), ("status", C.c_void_p)]
+    _at, _keep = None, ()                   # of a struct over tensors: their GPU (-1: not one), the tensors
 
 
 class Tokens(C.Structure):
     _fields_ = [("dtype", C.c_uint32), ("n_q_heads", C.c_uint32), ("q_stride", C.c_uint64),
                 ("k_stride", C.c_uint64), ("v_stride", C.c_uint64), ("q_out_stride", C.c_uint64),
                 ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_out", C.c_void_p)]
+    _of = None                              # of a struct over tensors: ((KV heads, head_dim), tokens, their GPU (-1: not one), the tensors)
 
 
 class Rope(C.Structure):
     _fields_ = [("style", C.c_uint32), ("rot_dim", C.c_uint32), ("n_pos", C.c_uint64),
                 ("table", C.c_void_p)]
+    _of = -1,                               # its GPU, the table
 
 
 class Attend(C.Structure):
     _fields_ = [("dtype", C.c_uint32), ("n_q_heads", C.c_uint32), ("q_stride", C.c_uint64),
                 ("out_stride", C.c_uint64), ("q", C.c_void_p), ("out", C.c_void_p),
                 ("lse", C.c_void_p), ("scale", C.c_float), ("reserved", C.c_uint32)]
+    _of = None                              # (head_dim, tokens, their GPU, the tensors)
 
 
 class Cqe(C.Structure):
@@ -245,6 +250,7 @@ class Context:
         _check(self.lib.tutti_ctx_create(C.byref(geom), device, C.byref(h)), "tutti_ctx_create")
         self.h = h
         self.device = device
+        self._row = (geom.n_kv_heads, geom.head_dim)
 
     def close(self):
         if self.h:
@@ -267,10 +273,23 @@ class Context:
 
     def tutti_kv_append_layer(self, layer: int, step: Step, tokens: Tokens, rope: Optional[Rope] = None,
                               stream=None, allow: Sequence[int] = ()) -> int:
-        """Write a step's keys and values into the pool, rotating queries and keys on the way."""
-        return _check(self.lib.tutti_kv_append_layer(self.h, layer, step, tokens, rope,
-                                                     _stream_ptr(stream)),
-                      "tutti_kv_append_layer", allow)
+        """Write a step's keys and values into the pool, rotating queries and keys on the way.  stream None is
+        the legacy default stream, not torch's current one, as in all calls here.  Structs over tensors
+        (make_step, make_tokens, make_rope) are compared with each other and with the geometry."""
+        at, of = self.device, tokens._of
+        if of is not None:
+            row, rows, dev, held = of
+            if row != self._row or rows < step.n_tok:
+                raise TuttiError(EINVAL, "tutti_kv_append_layer: keys and values are not [n_tok or more, n_kv_heads, head_dim]")
+            if dev != at:
+                _reachable(at, held)
+        if step._at != at:
+            _reachable(at, step._keep)
+        if rope is not None and rope._of[0] != at:
+            _reachable(at, rope._of[1:])
+        rc = self.lib.tutti_kv_append_layer(self.h, layer, step, tokens, rope,
+                                            None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_kv_append_layer", allow)
 
     def tutti_set_option(self, option: int, value: int):
         _check(self.lib.tutti_set_option(self.h, option, value), "tutti_set_option")
@@ -298,18 +317,15 @@ def make_batch(hit_tokens, obj_start, obj_slot, blk_start, block_ids, plan_epoch
     return b
 
 
-def make_step(q_start, ctx_len, blk_start, block_ids, n_tok: int, max_new: int, status=None) -> Step:
-    """Step struct over device tensors (int32): one step's tokens against the pool."""
-    if any(t.element_size() != 4 or not t.is_contiguous() for t in (q_start, ctx_len, blk_start, block_ids)):
-        raise TuttiError(EINVAL, "step tables (int32, contiguous)")
-    s = Step(int(ctx_len.numel()), n_tok, int(block_ids.numel()), max_new, q_start.data_ptr(),
-             ctx_len.data_ptr(), blk_start.data_ptr(), block_ids.data_ptr(),
-             None if status is None else status.data_ptr())
-    s._keep = (q_start, ctx_len, blk_start, block_ids, status)
-    return s
-
-
 _DTYPE_CODES = {}                           # torch dtype -> TUTTI_DTYPE_*
+_FLOAT32 = set()                            # torch.float32, once seen (torch itself is not imported here)
+
+
+def _float32(dtype) -> bool:
+    if str(dtype) == "torch.float32":
+        _FLOAT32.add(dtype)
+        return True
+    return False
 
 
 def _dtype_code(dtype) -> int:
@@ -322,6 +338,34 @@ def _dtype_code(dtype) -> int:
     return code
 
 
+def _reachable(device: int, tensors):
+    """Raises unless every tensor is on the context's GPU or in pinned host memory, which it reads and writes in place."""
+    for t in tensors:
+        if t is not None and t.get_device() != device and not (t.get_device() < 0 and t.is_pinned()):
+            raise TuttiError(EINVAL, f"tensor on {t.device}, context on GPU {device}")
+
+
+def make_step(q_start, ctx_len, blk_start, block_ids, n_tok: int, max_new: int, status=None) -> Step:
+    """Step struct over device tensors (int32): one step's tokens against the pool."""
+    n_seq = int(ctx_len.numel())
+    if any(str(t.dtype) not in ("torch.int32", "torch.uint32") or not t.is_contiguous() for t in (q_start, ctx_len, blk_start, block_ids)):
+        raise TuttiError(EINVAL, "step tables (int32, contiguous)")
+    if n_seq and (q_start.numel() <= n_seq or blk_start.numel() <= n_seq):
+        raise TuttiError(EINVAL, "step tables (q_start and blk_start have an entry more than ctx_len)")
+    held = q_start, ctx_len, blk_start, block_ids
+    if status is not None:
+        if str(status.dtype) != "torch.int32" or not status.numel():
+            raise TuttiError(EINVAL, "status (int32)")
+        held += (status,)
+    s = Step(n_seq, n_tok, int(block_ids.numel()), max_new, q_start.data_ptr(),
+             ctx_len.data_ptr(), blk_start.data_ptr(), block_ids.data_ptr(),
+             None if status is None else status.data_ptr())
+    s._at, s._keep = held[0].get_device(), held
+    if any(t.get_device() != s._at for t in held):
+        s._at = -1
+    return s
+
+
 def _rows(t, dtype, dim: int) -> int:
     """Token stride of a [tokens, heads, dim] tensor whose heads lie side by side."""
     by_token, by_head, by_dim = t.stride()
@@ -332,45 +376,73 @@ def _rows(t, dtype, dim: int) -> int:
     return by_token
 
 
+# The structs of a call from their values (the ctypes constructors cost a third more of a small call's time).
+_TOKENS, _ROPE, _ATTEND = struct.Struct("=2I8Q").pack, struct.Struct("=2I2Q").pack, struct.Struct("=2I5Qf4x").pack
+
+
 def make_tokens(k, v, q=None, q_out=None) -> Tokens:
     """Token struct over [tokens, heads, head_dim] device tensors (bf16 or fp16; views of a packed
-    projection are fine).  The struct does not keep the tensors alive."""
-    dtype, dim = k.dtype, k.shape[2]
-    code = _dtype_code(dtype)
+    projection are fine).  The struct keeps the tensors alive: the GPU may still use them when the call
+    has returned, which torch's allocator knows of on the stream that they were made on only."""
+    dtype, shape, dev = k.dtype, k.shape, k.get_device()
+    n, heads, dim = shape
+    if v.shape != shape:
+        raise TuttiError(EINVAL, "keys and values have one shape")
+    if v.get_device() != dev:
+        dev = -1
     if q is None:
-        return Tokens(code, 0, 0, _rows(k, dtype, dim), _rows(v, dtype, dim), 0, None, k.data_ptr(), v.data_ptr(), None)
-    return Tokens(code, q.shape[1], _rows(q, dtype, dim), _rows(k, dtype, dim), _rows(v, dtype, dim), _rows(q_out, dtype, dim),
-                  q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr())
-
-
-_FLOAT32 = []                               # torch.float32, once seen (torch itself is not imported here)
-
-
-def _float32(t) -> bool:
-    if _FLOAT32:
-        return t.dtype is _FLOAT32[0]
-    if str(t.dtype) == "torch.float32":
-        _FLOAT32.append(t.dtype)
-        return True
-    return False
+        t = Tokens(_dtype_code(dtype), 0, 0, _rows(k, dtype, dim), _rows(v, dtype, dim), 0, None, k.data_ptr(), v.data_ptr(), None)
+        t._of = (heads, dim), n, dev, (k, v)
+        return t
+    shape = q.shape
+    rows, q_heads, q_dim = shape
+    if rows != n or q_dim != dim or q_out is None or q_out.shape != shape:
+        raise TuttiError(EINVAL, "queries and their output have one shape, with the tokens and head_dim of the keys")
+    if q.get_device() != dev or q_out.get_device() != dev:
+        dev = -1
+    (qs, q1, q0), (ks, k1, k0), (vs, v1, v0), (rs, o1, o0) = q.stride(), k.stride(), v.stride(), q_out.stride()
+    if not (q1 == k1 == v1 == o1 == dim and q0 == k0 == v0 == o0 == 1 and q.dtype is v.dtype is q_out.dtype is dtype):
+        qs, ks, vs, rs = _rows(q, dtype, dim), _rows(k, dtype, dim), _rows(v, dtype, dim), _rows(q_out, dtype, dim)
+    code = _DTYPE_CODES.get(dtype)
+    t = Tokens.from_buffer_copy(_TOKENS(_dtype_code(dtype) if code is None else code, q_heads, qs, ks, vs, rs,
+                                        q.data_ptr(), k.data_ptr(), v.data_ptr(), q_out.data_ptr()))
+    t._of = (heads, dim), n, dev, (k, v, q, q_out)
+    return t
 
 
 def make_rope(table, style: int = ROPE_HALF) -> Rope:
-    """Rotation over a [positions, rot_dim] float32 device table: cosines, then sines."""
-    if not _float32(table) or not table.is_contiguous():
+    """Rotation over a [positions, rot_dim] float32 device table: cosines, then sines.  Keeps the table alive."""
+    if (table.dtype not in _FLOAT32 and not _float32(table.dtype)) or not table.is_contiguous():
         raise TuttiError(EINVAL, "rotation table (float32, contiguous)")
     n_pos, rot_dim = table.shape
-    return Rope(style, rot_dim, n_pos, table.data_ptr())
+    r = Rope.from_buffer_copy(_ROPE(style, rot_dim, n_pos, table.data_ptr()))
+    r._of = table.get_device(), table
+    return r
 
 
 def make_attend(q, out, lse=None) -> Attend:
-    """Attention struct over [tokens, heads, head_dim] queries and outputs; lse [tokens, heads] float32."""
-    if lse is not None and not (_float32(lse) and lse.is_contiguous()):
-        raise TuttiError(EINVAL, "lse (float32, contiguous)")
-    dtype = q.dtype
-    _, heads, dim = q.shape
-    return Attend(_dtype_code(dtype), heads, _rows(q, dtype, dim), _rows(out, dtype, dim), q.data_ptr(), out.data_ptr(),
-                  None if lse is None else lse.data_ptr(), 0.0, 0)
+    """Attention struct over [tokens, heads, head_dim] queries and outputs; lse [tokens, heads] float32.  Keeps
+    the tensors alive."""
+    dtype, shape, dev = q.dtype, q.shape, q.get_device()
+    n, heads, dim = shape
+    if out.shape != shape:
+        raise TuttiError(EINVAL, "queries and outputs have one shape")
+    if out.get_device() != dev:
+        dev = -1
+    lse_at = 0
+    if lse is not None:
+        if (lse.dtype not in _FLOAT32 and not _float32(lse.dtype)) or lse.shape != (n, heads) or not lse.is_contiguous():
+            raise TuttiError(EINVAL, "lse (float32, [tokens, heads], contiguous)")
+        if lse.get_device() != dev:
+            dev = -1
+        lse_at = lse.data_ptr()
+    (qs, q1, q0), (rs, o1, o0) = q.stride(), out.stride()
+    if not (q1 == o1 == dim and q0 == o0 == 1 and out.dtype is dtype):
+        qs, rs = _rows(q, dtype, dim), _rows(out, dtype, dim)
+    code = _DTYPE_CODES.get(dtype)
+    a = Attend.from_buffer_copy(_ATTEND(_dtype_code(dtype) if code is None else code, heads, qs, rs, q.data_ptr(), out.data_ptr(), lse_at, 0.0))
+    a._of = dim, n, dev, (q, out, lse)
+    return a
 
 
 class Attn:
@@ -390,10 +462,24 @@ class Attn:
 
     def tutti_kv_attend_layer(self, layer: int, step: Step, io: Attend, scale: float, stream=None,
                               allow: Sequence[int] = ()) -> int:
-        """Causal attention of the step's queries over the pool layer."""
+        """Causal attention of the step's queries over the pool layer.  stream None is the legacy default
+        stream, not torch's current one.  Structs over tensors (make_step, make_attend) are compared with each other and
+        with the geometry."""
+        ctx = self.ctx
+        if ctx.h is None or self.h is None:
+            raise TuttiError(EINVAL, "tutti_kv_attend_layer: the handle or its context is closed")
+        at, of = ctx.device, io._of
+        if of is not None:
+            dim, rows, dev, held = of
+            if dim != ctx._row[1] or rows < step.n_tok:
+                raise TuttiError(EINVAL, "tutti_kv_attend_layer: queries are not [n_tok or more, heads, head_dim]")
+            if dev != at:
+                _reachable(at, held)
+        if step._at != at:
+            _reachable(at, step._keep)
         io.scale = scale
-        return _check(self.lib.tutti_kv_attend_layer(self.h, layer, step, io, _stream_ptr(stream)),
-                      "tutti_kv_attend_layer", allow)
+        rc = self.lib.tutti_kv_attend_layer(self.h, layer, step, io, None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_kv_attend_layer", allow)
 
 
 class Ring:
