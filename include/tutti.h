@@ -557,8 +557,12 @@ typedef struct tutti_attend {
  * tutti_pool_register (call it first; registering the pool again forgets the scales).  A stored
  * key or value is code * scale of its block and head.  To move the scales with the blocks, give
  * them a context of their own: a pool of n_blocks blocks of one token of n_kv_heads 4-byte
- * elements (block_tokens 1, head_dim 1, n_kv_heads a multiple of 4) takes the same block ids.
+ * elements (block_tokens 1, head_dim 1) takes the same block ids.  Its tokens are multiples of 16 bytes:
+ * where n_kv_heads is not a multiple of 4, register rows of the next one, row floats from a block's
+ * scales to the next block's, of which the operators use the first n_kv_heads and leave the others alone.
  */
+int tutti_scales_register_rows(tutti_ctx_t *ctx, uint32_t layer, float *k_scale, float *v_scale,
+                               uint64_t n_blocks, uint32_t row);
 int tutti_scales_register(tutti_ctx_t *ctx, uint32_t layer, float *k_scale, float *v_scale,
                           uint64_t n_blocks);
 

@@ -262,7 +262,7 @@ __device__ void block_warp(const AppendParams &p, uint32_t w) {
     }
     const uint32_t lo = max(first, blk * bs), hi = min((uint64_t)v.ctx, ((uint64_t)blk + 1) * bs);
     char *rows = (char *)((is_v ? p.pool.v_base : p.pool.k_base) + at + h * p.pool.head_stride);
-    float *scale = (is_v ? p.pool.v_scale : p.pool.k_scale) + (uint64_t)id * hk + h;
+    float *scale = (is_v ? p.pool.v_scale : p.pool.k_scale) + (uint64_t)id * p.pool.scale_row + h;
     const uint64_t in_stride = is_v ? p.v_stride : p.k_stride;
     const char *in = (is_v ? p.v : p.k) + (uint64_t)h * p.pool.head_dim * 2;
     const uint32_t per = 32 / p.jobs, j = lane % p.jobs, sub = lane / p.jobs;

@@ -241,7 +241,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 if (held && !ok) report(p.step, TUTTI_EFAULT);
                 mask |= (uint64_t)__ballot_sync(0xffffffffu, ok) << (32 * i);
                 if (C8 && i * 32 + lane < F::KW) {
-                    const uint64_t at = ok ? (uint64_t)(uint32_t)u.id[i] * p.pool.n_kv_heads + u.h : 0;
+                    const uint64_t at = ok ? (uint64_t)(uint32_t)u.id[i] * p.pool.scale_row + u.h : 0;
                     cp4(kst + F::STAGE_BYTES + (i * 32 + lane) * 4, p.pool.k_scale + at, ok);
                     cp4(kst + F::STAGE_BYTES + (F::KW + i * 32 + lane) * 4, p.pool.v_scale + at, ok);
                 }

@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 tiled = tiled && __all_sync(0xffffffffu, there);
                 off[i] = there ? block_offset(p.pool, id[i]) + (int64_t)(p.pool.row_of(key) * p.pool.tok_stride + head * p.pool.head_stride) : -1;
                 if constexpr (C8) {
-                    const uint64_t at = there ? (uint64_t)id[i] * p.pool.n_kv_heads + head : 0;
+                    const uint64_t at = there ? (uint64_t)id[i] * p.pool.scale_row + head : 0;
                     ks[i] = there ? p.pool.k_scale[at] : 0.0f;
                     vs[i] = there ? p.pool.v_scale[at] : 0.0f;
                 }

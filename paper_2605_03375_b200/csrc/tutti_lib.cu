@@ -7,7 +7,6 @@
 #include <new>
 #include <string>
 #include <thread>
-#include <utility>
 #include <vector>
 
 #include "tutti_internal.h"
@@ -62,6 +61,12 @@ struct DeviceGuard {
 
 }  // namespace
 
+// K and V scales of an 8-bit pool layer, `row` floats from block to block.
+struct PoolScales {
+    float *k, *v;
+    uint32_t row;
+};
+
 struct tutti_ctx {
     tutti_geom_t geom;
     tutti_layout_t layout;
@@ -74,7 +79,7 @@ struct tutti_ctx {
     void *partition = nullptr;   // SM partition state (tutti_partition.cu)
     bool pool_hnd = false;       // pool blocks are [head][token][dim]
     StoreTensorMaps maps;        // for the transposing bulk copies
-    std::vector<std::pair<float *, float *>> scales;   // K, V scales of an 8-bit pool layer
+    std::vector<PoolScales> scales;                    // of 8-bit pool layers
     std::vector<PoolTensorMaps> pool_maps;             // for attention's tile loads
     PoolLayerDev *d_pools = nullptr;   // device copy of the pool table (multi-layer builds)
 };
@@ -195,7 +200,7 @@ int tutti_ctx_create(const tutti_geom_t *geom, int device, tutti_ctx_t **out) {
     c->device = device;
     c->device_sms = prop.multiProcessorCount;
     c->pool.assign(geom->n_layers, PoolLayer{0, 0, 0, 0, false});
-    c->scales.assign(geom->n_layers, {nullptr, nullptr});
+    c->scales.assign(geom->n_layers, PoolScales{nullptr, nullptr, 0});
     c->pool_maps.assign(geom->n_layers, PoolTensorMaps());
     for (auto &s : c->store) s = StoreDev{0, 0, 0, false, false};
     memset(&c->maps, 0, sizeof(c->maps));
@@ -282,7 +287,7 @@ int tutti_pool_register(tutti_ctx_t *ctx, uint32_t layer, void *k_base, void *v_
     if ((k | v | block_stride) & 15) return TUTTI_EINVAL;
     if (block_stride < ctx->layout.block_bytes || n_blocks > 0x7fffffffull) return TUTTI_EINVAL;
     ctx->pool[layer] = PoolLayer{k, v, block_stride, n_blocks, true};
-    ctx->scales[layer] = {nullptr, nullptr};
+    ctx->scales[layer] = PoolScales{nullptr, nullptr, 0};
     encode_pool_maps(ctx, layer);
     PoolLayerDev pl{k, v, block_stride, n_blocks};
     DeviceGuard guard(ctx->device);
@@ -290,27 +295,33 @@ int tutti_pool_register(tutti_ctx_t *ctx, uint32_t layer, void *k_base, void *v_
     return TUTTI_OK;
 }
 
-int tutti_scales_register(tutti_ctx_t *ctx, uint32_t layer, float *k_scale, float *v_scale,
-                          uint64_t n_blocks) {
+int tutti_scales_register_rows(tutti_ctx_t *ctx, uint32_t layer, float *k_scale, float *v_scale,
+                               uint64_t n_blocks, uint32_t row) {
     if (!ctx || layer >= ctx->geom.n_layers || !k_scale || !v_scale) return TUTTI_EINVAL;
     if (ctx->geom.elem_bytes != 1 || !ctx->pool[layer].registered) return TUTTI_EINVAL;
     if ((((uint64_t)k_scale | (uint64_t)v_scale) & 3) || n_blocks != ctx->pool[layer].n_blocks)
         return TUTTI_EINVAL;
-    ctx->scales[layer] = {k_scale, v_scale};
+    if (row < ctx->geom.n_kv_heads) return TUTTI_EINVAL;
+    ctx->scales[layer] = PoolScales{k_scale, v_scale, row};
     return TUTTI_OK;
+}
+
+int tutti_scales_register(tutti_ctx_t *ctx, uint32_t layer, float *k_scale, float *v_scale,
+                          uint64_t n_blocks) {
+    return ctx ? tutti_scales_register_rows(ctx, layer, k_scale, v_scale, n_blocks, ctx->geom.n_kv_heads) : TUTTI_EINVAL;
 }
 
 // The view that the operators on the pool compute with; TUTTI_EINVAL for a layer they cannot use.
 int tutti_ctx_pool_view_(tutti_ctx_t *ctx, uint32_t layer, PoolView *v, uint32_t *elem_bytes) {
     if (layer >= ctx->geom.n_layers || !ctx->pool[layer].registered) return TUTTI_EINVAL;
     const tutti_geom_t &g = ctx->geom;
-    if (g.elem_bytes != 2 && !(g.elem_bytes == 1 && ctx->scales[layer].first)) return TUTTI_EINVAL;
+    if (g.elem_bytes != 2 && !(g.elem_bytes == 1 && ctx->scales[layer].k)) return TUTTI_EINVAL;
     const PoolLayer &p = ctx->pool[layer];
     const uint64_t row = (uint64_t)g.head_dim * g.elem_bytes;
     *v = PoolView{p.k_base, p.v_base, p.block_stride, (uint32_t)p.n_blocks, g.block_tokens, g.n_kv_heads,
                   g.head_dim, ctx->pool_hnd ? row : ctx->layout.token_bytes,
                   ctx->pool_hnd ? row * g.block_tokens : row,
-                  ctx->scales[layer].first, ctx->scales[layer].second, ctx->pool_hnd, 0, 0};
+                  ctx->scales[layer].k, ctx->scales[layer].v, ctx->pool_hnd, ctx->scales[layer].row, 0, 0};
     division_by(g.block_tokens, v->block_mul, v->block_shift);
     *elem_bytes = g.elem_bytes;
     return TUTTI_OK;

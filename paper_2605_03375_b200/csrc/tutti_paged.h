@@ -14,8 +14,9 @@ struct PoolView {
     uint64_t k_base, v_base, block_stride;
     uint32_t n_blocks, block_tokens, n_kv_heads, head_dim;
     uint64_t tok_stride, head_stride;       // bytes between tokens / heads of a block
-    float *k_scale, *v_scale;               // [n_blocks][n_kv_heads], 8-bit pools only
+    float *k_scale, *v_scale;               // [n_blocks][scale_row], 8-bit pools only
     bool hnd;                               // head-major blocks
+    uint32_t scale_row;                     // n_kv_heads or more
     uint32_t block_mul, block_shift;        // key / block_tokens = key * block_mul >> block_shift, for keys below 2^31
 
     __host__ __device__ uint32_t block_of(uint32_t key) const { return (uint32_t)((uint64_t)key * block_mul >> block_shift); }

@@ -112,7 +112,7 @@ EXPORTS = [
     "tutti_stream_wait_iocb", "tutti_ring_last_launch_sms", "tutti_ring_poll_range",
     "tutti_ring_set_iocb_bytes", "tutti_sched_profile",
     "tutti_stage_plan", "tutti_stage_copy_layer", "tutti_build_sqes_staged",
-    "tutti_scales_register", "tutti_kv_append_layer", "tutti_attn_create", "tutti_attn_destroy",
+    "tutti_scales_register", "tutti_scales_register_rows", "tutti_kv_append_layer", "tutti_attn_create", "tutti_attn_destroy",
     "tutti_kv_attend_layer",
 ]
 
@@ -187,6 +187,7 @@ def load(path: Optional[str] = None) -> C.CDLL:
         "tutti_filepool_remove": (C.c_int, [vp, u64]),
         "tutti_filepool_stats": (C.c_int, [vp, P(u64), P(u64), P(u64), P(u64), P(u64)]),
         "tutti_scales_register": (C.c_int, [vp, u32, vp, vp, u64]),
+        "tutti_scales_register_rows": (C.c_int, [vp, u32, vp, vp, u64, u32]),
         "tutti_kv_append_layer": (C.c_int, [vp, u32, P(Step), P(Tokens), P(Rope), vp]),
         "tutti_attn_create": (C.c_int, [vp, P(vp)]),
         "tutti_attn_destroy": (C.c_int, [vp]),
@@ -270,6 +271,11 @@ class Context:
         """Scales [n_blocks][n_kv_heads] (float32) of an 8-bit pool layer."""
         _check(self.lib.tutti_scales_register(self.h, layer, k_scale, v_scale, n_blocks),
                "tutti_scales_register")
+
+    def tutti_scales_register_rows(self, layer: int, k_scale: int, v_scale: int, n_blocks: int, row: int):
+        """Scales [n_blocks][row] of which the first n_kv_heads are used (rows that a store can move are multiples of 4)."""
+        _check(self.lib.tutti_scales_register_rows(self.h, layer, k_scale, v_scale, n_blocks, row),
+               "tutti_scales_register_rows")
 
     def tutti_kv_append_layer(self, layer: int, step: Step, tokens: Tokens, rope: Optional[Rope] = None,
                               stream=None, allow: Sequence[int] = ()) -> int:

@@ -117,3 +117,8 @@ def test_structs_keep_their_tensors():
     assert there() is not None
     del io
     assert there() is None
+
+
+def test_scale_rows_of_no_context():
+    lib = T.load()
+    assert lib.tutti_scales_register_rows(None, 0, None, None, 0, 4) == T.EINVAL
