@@ -137,46 +137,59 @@ def _codes(shape, g):
 # ---------------------------------------------------------------------------- the library's calls
 
 _contexts = {}
+LAYERS = 64
 
 
 def _context(c):
-    """The library context of a geometry (one for the program's life) and a layer of it that is not in use."""
+    """The library context of a geometry (one for the program's life), its attention handle and how often a layer of it has
+    been registered: the layers are taken in turn."""
     from paper_2605_03375_b200 import tutti as T
     size = 1 if c["cache"] == "8" else 2
     key = (c["kv_heads"], c["dim"], size, c["block"], c["hnd"])
     if key not in _contexts:
-        ctx = T.Context(T.Geom(64, c["kv_heads"], c["dim"], size, c["block"], c["block"], 1, T.LAYOUT_LAYER_MAJOR, 1), 0)
+        ctx = T.Context(T.Geom(LAYERS, c["kv_heads"], c["dim"], size, c["block"], c["block"], 1, T.LAYOUT_LAYER_MAJOR, 1), 0)
         ctx.tutti_set_option(T.OPT_POOL_LAYOUT, T.POOL_HND if c["hnd"] else T.POOL_NHD)
         _contexts[key] = [T, ctx, T.Attn(ctx), 0]
-    entry = _contexts[key]
-    entry[3] = (entry[3] + 1) % 64
-    return entry
+    return _contexts[key]
 
 
 def _bind(s):
     """What a program sets up once for its pool and once for a step (all its layers share it): the registration and the step."""
     c = s["case"]
-    T, ctx, attn, layer = _context(c)
+    entry = _context(c)
+    T, ctx, attn, turn = entry
+    entry[3] += 1
+    layer = turn % LAYERS
     k, v = s["pools"]
     ctx.tutti_pool_register(layer, k.data_ptr(), v.data_ptr(), c["block"] * c["kv_heads"] * c["dim"] * k.element_size(), s["n_blocks"])
     if c["cache"] == "8":
         ctx.tutti_scales_register(layer, s["scales"][0].data_ptr(), s["scales"][1].data_ptr(), s["n_blocks"])
     step = T.make_step(s["q_start"], s["ctx_len"], s["blk_start"], s["block_ids"], s["n_tok"], s["max_q"])
-    s["bound"] = T, ctx, attn, layer, step
+    s["bound"], s["turn"] = (T, ctx, attn, layer, step), (entry, turn)
     return s["bound"]
+
+
+def _bound(s):
+    """The state's binding, made anew once its layer has been registered for another state."""
+    if "bound" in s:
+        entry, turn = s["turn"]
+        if entry[3] - turn <= LAYERS:
+            return s["bound"]
+    return _bind(s)
 
 
 def _own(s):
     c = s["case"]
-    T, ctx, attn, layer, step = s.get("bound") or _bind(s)
+    T, ctx, attn, layer, step = _bound(s)
+    stream = torch._C._cuda_getCurrentRawStream(0)          # torch.cuda.current_stream().cuda_stream takes 4 us more
     if c["op"] == "append":
         out = torch.empty((s["n_tok"], c["heads"], c["dim"]), dtype=s["q"].dtype, device=DEV)
         rope = T.make_rope(s["table"], T.ROPE_HALF if c["style"] == "half" else T.ROPE_PAIRS)
-        ctx.tutti_kv_append_layer(layer, step, T.make_tokens(s["k"], s["v"], s["q"], out), rope)
+        ctx.tutti_kv_append_layer(layer, step, T.make_tokens(s["k"], s["v"], s["q"], out), rope, stream)
         return {"q": out, "pools": s["pools"], "scales": s.get("scales")}
     out = torch.empty((s["n_tok"], c["heads"], c["dim"]), dtype=s["q"].dtype, device=DEV)
     lse = torch.empty((s["n_tok"], c["heads"]), dtype=torch.float32, device=DEV)
-    attn.tutti_kv_attend_layer(layer, step, T.make_attend(s["q"], out, lse), c["dim"] ** -0.5)
+    attn.tutti_kv_attend_layer(layer, step, T.make_attend(s["q"], out, lse), c["dim"] ** -0.5, stream)
     return {"out": out, "lse": lse}
 
 
