@@ -11,13 +11,9 @@
 // bandwidth for prompts and latency for a decode step: the search of the sequence, its tables, the
 // block's id and the rows are loads that wait for each other.
 // On a B200 (6.45 TB/s copy): 16384 tokens of 48 rows of 128, bf16, 72 us = 5.7 TB/s; 12187 tokens of
-// 80 rows, fp16, into an 8-bit pool 106 us = 4.6 TB/s; 64 single tokens 4.0 and 6.6 us.  24 warps an SM
+// 80 rows, fp16, into an 8-bit pool 107 us = 4.5 TB/s (blocks of 32 or 64 tokens, read twice: 114 and 115); 64 single tokens 4.0 and 6.6 us.  24 warps an SM
 // (80 registers, a few spilled) against 16: 72 against 75 us, 106 against 109; 32: 92 us.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 #include <cuda_fp8.h>
-
-#include <string>
 
 #include "tutti_paged.h"
 
@@ -64,15 +60,6 @@ __device__ inline void unpack(const uint4 &u, float *x) {
     const T *e = reinterpret_cast<const T *>(&u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = to_f(e[i]);
-}
-
-__device__ inline uint32_t pack2(float a, float b, __nv_bfloat16) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<uint32_t *>(&h);
-}
-__device__ inline uint32_t pack2(float a, float b, __half) {
-    __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<uint32_t *>(&h);
 }
 
 template <typename T>
@@ -402,11 +389,6 @@ __global__ void __launch_bounds__(THREADS, 3) append8_kernel(const __grid_consta
     else if (w - p.n_row_warps < p.blk_units * 2 * p.pool.n_kv_heads)
         block_warp<T>(p, w - p.n_row_warps);
     __threadfence();
-}
-
-int fail(cudaError_t e, const char *what) {
-    tutti_set_cuda_error_((std::string(what) + ": " + cudaGetErrorName(e) + " (" + cudaGetErrorString(e) + ")").c_str());
-    return TUTTI_ECUDA;
 }
 
 }  // namespace

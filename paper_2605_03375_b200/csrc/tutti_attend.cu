@@ -3,22 +3,8 @@
 // over the keys j <= position of the row.
 #include <cmath>
 #include <new>
-#include <string>
 
 #include "tutti_attend.h"
-
-namespace tutti {
-
-namespace {
-
-int fail(cudaError_t e, const char *what) {
-    tutti_set_cuda_error_((std::string(what) + ": " + cudaGetErrorName(e) + " (" + cudaGetErrorString(e) + ")").c_str());
-    return TUTTI_ECUDA;
-}
-
-}  // namespace
-
-}  // namespace tutti
 
 using namespace tutti;
 

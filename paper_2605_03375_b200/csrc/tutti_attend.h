@@ -1,7 +1,5 @@
 // Shared by the attention kernels: the call's parameters and a few instructions.
 #pragma once
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
 #include "tutti_paged.h"
@@ -67,14 +65,6 @@ template <int N> __device__ inline void cp_wait() { asm volatile("cp.async.wait_
 // four e4m3 codes as four f16
 __device__ inline void codes4(uint32_t w, uint32_t &lo, uint32_t &hi) {
     asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
-}
-__device__ inline uint32_t pack2(float a, float b, __nv_bfloat16) {
-    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<uint32_t *>(&h);
-}
-__device__ inline uint32_t pack2(float a, float b, __half) {
-    __half2 h = __floats2half2_rn(a, b);
-    return *reinterpret_cast<uint32_t *>(&h);
 }
 #endif
 

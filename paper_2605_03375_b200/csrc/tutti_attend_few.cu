@@ -1,7 +1,7 @@
 // Attention of few rows per sequence (a decode step).  Bound: HBM, the cache is read once.
-// On a B200 (6.45 TB/s copy), 128-wide heads: 64 ragged requests on 1-token pages (2.3 GB) 361 us =
-// 6.4 TB/s; one of 131072 tokens (0.54 GB) 93 us = 5.75 TB/s; 8 of 32768, 8-bit (0.54 GB), 108 us = 5.0
-// TB/s; 64-wide heads, 8-bit, 48 ragged (0.22 GB), 70 us = 3.1 TB/s (bound by instructions: 17 a byte).  One
+// On a B200 (6.45 TB/s copy), the kernel alone, 128-wide heads: 64 ragged requests on 1-token pages (2.3 GB) 360 us =
+// 6.4 TB/s; one of 131072 tokens (0.54 GB) 92 us = 5.8 TB/s; 8 of 32768, 8-bit (0.54 GB), 110 us = 4.9
+// TB/s; 64-wide heads, 16-bit, 48 ragged (0.44 GB), 87 us = 5.0 TB/s; 64-wide heads, 8-bit, 48 ragged (0.22 GB), 70 us = 3.1 TB/s (bound by instructions: 17 a byte).  One
 // request of 1 / 512 / 4096 tokens 5.2 / 9.0 / 12.5 us: three rounds of dependent loads, and the join.
 #include <type_traits>
 
@@ -313,8 +313,8 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                         top = fmaxf(top, fabsf(e16[d * 16 + j]));
                     }
                 }
-                // a row of bf16 queries is scaled by a power of two so that f16 holds it: exactly,
-                // but for elements below 2^-14 of the row's largest, which keep an error of 2^-25 of it
+                // a row of bf16 queries is scaled by a power of two so that f16, the type that holds the codes, holds
+                // it: exactly, but for elements below 2^-14 of the row's largest, which keep an error of 2^-25 of it
                 float down = 1.0f;
                 if constexpr (std::is_same<T, __nv_bfloat16>::value) {
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -468,7 +468,8 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                             o[b][i][3] *= alpha[1];
                         }
                     }
-                    // from (key g, rows 2 c and 2 c + 1) to (row g, keys 2 c and 2 c + 1)
+                    // From (key g, rows 2 c and 2 c + 1) to (row g, keys 2 c and 2 c + 1).  Probabilities are rounded to 16
+                    // bits, the type of the matrix instruction; l has summed them in 32.
 #pragma unroll
                     for (int t = 0; t < F::MT; ++t)
 #pragma unroll

@@ -12,12 +12,13 @@
 //             its probabilities back over them (16 bits), rescales the output when the running
 //             maximum has grown by more than 2^8, and writes the row out at the end;
 //   8         issues the matrix instructions: S = Q K^T (both operands in shared memory),
-//             O += P V (P from TMEM).  Units are taken in two steps of 64 keys, each with
-//             its own columns of scores: a step's scores are ready before the softmax of the step
-//             before it has ended, so the softmax warps never wait for a product that depends on
-//             them (with one set of 128 columns a half, whose probabilities lie over its scores, they
-//             did: 3900 clocks a unit).  An instruction of 128 x 64 x 16 reads 6 KB of shared
-//             memory in the time of 4 KB, which makes Q K^T 1.5 times as long; P V is not touched;
+//             O += P V (P from TMEM, over the scores it came from).  16-bit caches: a unit is one step of
+//             128 keys; a half's next scores wait for its P V, which waits for its softmax, while the other
+//             half has the tensor cores.  8-bit caches: two steps of 64 keys, each with its own columns of
+//             scores, so that a step's scores are ready before the softmax of the step before it has ended.
+//             An instruction of 128 x 64 x 16 reads 6 KB of shared memory in the time of 4 KB, which makes
+//             Q K^T 1.5 times as long: it costs a 16-bit cache more than the waiting (318 against 278 us),
+//             and an 8-bit one, where the widening warps are the bound, less (360 -> 311);
 //   9-11      bring the queries of the next tile;
 //   12-15     gather keys and values through the block table into a ring of four 128-row tiles
 //             in the 128-byte swizzle (K: K-major B operand, V: the same bytes read as an
@@ -31,9 +32,10 @@
 // Bound: the tensor cores (2 x 128 x 128 x D multiply-adds a half and unit: 2048 clocks a unit for D = 128)
 // and, as close, the 2 x 128 x 128 exponentials on 16 lanes a clock; in a long loop the power limit
 // (1550 MHz at 1000 W).  What is reached: 3500 clocks a unit, set by the chain scores -> softmax -> P V
-// -> next scores of a half.  On a B200 (1676 TFLOP/s in short, 1389 in long runs of the library's product): 2048 new tokens
-// over 32768, 32 heads, bf16, 1040-1180 us = 960-1090 TFLOP/s; 1801 over 2 x 8192 256 us = 974; 8-bit, fp16, 64 heads, 4
-// ragged chunks over 2000-9000 280 us = 667 (the widening of the codes and shared memory).
+// -> next scores of a half.  On a B200 (1676 TFLOP/s in short, 1389 in long runs of the library's product), the kernel
+// alone, 32 heads: 2048 new tokens over 32768, bf16, 1150-1210 us = 940-990 TFLOP/s; 1801 over 2 x 8192 255 us = 978
+// (281-287 us among other calls); 8-bit, fp16, 4 ragged chunks over 2000-9000 266 us = 700, bf16 317 us cool and
+// 380-420 us in long runs (the widening of the codes and shared memory); 64-wide heads 1801 over 2 x 8192 207 us = 603.
 #include <cstring>
 #include <type_traits>
 
@@ -61,7 +63,9 @@ constexpr float GROW = 8.0f;            // log2 of how far probabilities may exc
 constexpr int UNIT_LEAST_K = -120, UNIT_MOST_K = 120, UNIT_LEAST_V = 1, UNIT_MOST_V = 64;
 constexpr long long WAIT_CLOCKS = 3000000000ll;   // about 1.5 s: a wait that takes longer is given up
 
-// sum over i in [0, n) of floor((a i + b) / m)  (a, b >= 0, m > 0)
+// sum over i in [0, n) of floor((a i + b) / m)  (a, b >= 0, m > 0): whole parts of a / m and b / m in closed form, then
+// the reciprocity of such sums (Graham, Knuth and Patashnik, Concrete Mathematics, section 3.5), which exchanges a
+// and m as Euclid's algorithm does.
 template <typename U>
 __host__ __device__ inline uint64_t floor_sum_in(U n, U m, U a, U b) {
     uint64_t ans = 0;
@@ -961,7 +965,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                             }
                         }
                     }
-                    // exponentials against the reference; 16 bits of each go over the scores, their 32-bit sums to l
+                    // Exponentials against the reference; their 32-bit sums go to l, and 16 bits of each over the scores:
+                    // the matrix instruction takes P and V of one 16-bit type.  (bf16: the outputs of the chunk above
+                    // are off from 64-bit arithmetic by 0.0023 of their size instead of 0.0017, what rounding them costs.)
                     const float sub = C::OFF - (m == -INFINITY ? 0.0f : m);
                     const f2 scl2 = pair(scl, scl), sub2 = pair(sub, sub);
                     f2 l0 = 0, l1 = 0;
@@ -1048,6 +1054,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         }
                     }
                 }
+                // The compiler spills about 1 KB a thread here (o, the joined parts, the pieces below), none of it in the
+                // loop over units: it costs once a tile.
                 if (write) {
                     const uint64_t token = t.v.q0 + tok;
                     const uint32_t qh = t.h * p.group + p.member_of(in ? row : t.r.n_rows - 1);

@@ -3,8 +3,12 @@
 // them.  The checks are plain arithmetic, callable on the host too.
 #pragma once
 #include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <string>
 
 #include "../../include/tutti.h"
 
@@ -73,6 +77,16 @@ __host__ __device__ inline int64_t block_offset(const PoolView &p, int32_t id) {
 }
 
 #ifdef __CUDACC__
+// two 32-bit numbers, each rounded once
+__device__ inline uint32_t pack2(float a, float b, __nv_bfloat16) {
+    __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+__device__ inline uint32_t pack2(float a, float b, __half) {
+    __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+
 __device__ inline void report(const StepDev &st, int code) {
     if (st.status) atomicCAS(st.status, TUTTI_OK, code);
 }
@@ -131,6 +145,11 @@ inline int check_step(const tutti_step_t *st) {
 // [n_tok][heads][head_dim] 16-bit elements at p, `stride` elements from token to token.
 inline bool rows_ok(const void *p, uint64_t stride, uint64_t heads, uint64_t head_dim) {
     return p && ((uint64_t)p & 15) == 0 && stride % 8 == 0 && stride >= heads * head_dim && stride < (1ull << 31);
+}
+
+inline int fail(cudaError_t e, const char *what) {
+    tutti_set_cuda_error_((std::string(what) + ": " + cudaGetErrorName(e) + " (" + cudaGetErrorString(e) + ")").c_str());
+    return TUTTI_ECUDA;
 }
 
 // A launch whose own status is returned: an error that another call of the program left behind is
