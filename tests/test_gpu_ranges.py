@@ -188,3 +188,17 @@ def test_scales_of_zero_and_next_to_it(new, dtype, cache):
         assert int(c.status) == T.OK
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("cache,dtype", [("16", "bf16"), ("8", "fp16")])
+@pytest.mark.parametrize("most", [1, 3, 17, 5000])
+def test_a_generous_bound_on_new_rows(cache, dtype, most):
+    """max_new may be larger than any sequence's rows: single tokens then go through whichever kernel it selects."""
+    c = OpCase([(300, 1), (0, 1), (1000, 1), (5, 0), (63, 1)], heads=16, kv_heads=2, dim=128, cache=cache, dtype=dtype, seed=97)
+    try:
+        fill_new(c)
+        c.step = T.make_step(c.t_q_start, c.t_ctx, c.t_blk_start, c.t_ids, c.n_tok, most, c.status)
+        verify(c, attend(c))
+        assert int(c.status) == T.OK
+    finally:
+        c.close()
