@@ -623,6 +623,119 @@ int tutti_attn_destroy(tutti_attn_t *attn);
 int tutti_kv_attend_layer(tutti_attn_t *attn, uint32_t layer, const tutti_step_t *step,
                           const tutti_attend_t *io, void *stream);
 
+/*
+ * Attention with a sliding window and a few first tokens that stay visible: the row at position p attends to the
+ * keys j <= p of its sequence with j < sinks or p - j < window (window 1: its own key and the first ones).  All else is as for
+ * tutti_kv_attend_layer, which a window of the longest context equals.  Blocks of which no row of the step sees
+ * a key are not looked at: their ids may be anything (tutti_pages_trim leaves -1).  A VALUE that is NaN or infinite may
+ * reach rows of the same sequence's step that come before its token or see it no longer, as 0 * NaN.
+ * TUTTI_EINVAL also for a window of 0, or window or sinks above 2^31 - 1.
+ */
+typedef struct tutti_window {
+    uint32_t window; /* keys that a row sees, its own included */
+    uint32_t sinks;  /* first tokens that every row sees        */
+} tutti_window_t;
+int tutti_kv_attend_window_layer(tutti_attn_t *attn, uint32_t layer, const tutti_step_t *step,
+                                 const tutti_attend_t *io, const tutti_window_t *window, void *stream);
+
+/* ------------------------------------------------------------------------- */
+/* Pages: which sequences hold which blocks of the pool.  Tables and counts    */
+/* live in device memory; every call is one step of a stream, graph-capturable, */
+/* and never waits for the host.                                               */
+/* ------------------------------------------------------------------------- */
+
+/*
+ * Tables of sequences: row s is block_ids[blk_start[s] .. blk_start[s+1]), of which the first
+ * ceil(len[s] / block_tokens) entries are held (the others are spare room and are neither read nor
+ * changed, but by tutti_pages_extend).  The arrays serve a tutti_step_t as they are, with len as its ctx_len.  An entry
+ * of -1 is a block that has been freed behind a window.  All arrays are DEVICE pointers owned by
+ * the caller, rows do not overlap, n_seq is at most TUTTI_PAGES_MAX_SEQ.  status as in tutti_step_t: TUTTI_EINVAL, a
+ * row's numbers contradict each other or the sizes (the row is skipped); TUTTI_EFAULT, a held entry other than -1 is outside the pool.
+ */
+typedef struct tutti_tables {
+    uint32_t n_seq;
+    uint32_t n_blk;
+    const uint32_t *blk_start; /* [n_seq + 1] */
+    int32_t *block_ids;        /* [n_blk]     */
+    uint32_t *len;             /* [n_seq]     */
+    int32_t *status;
+} tutti_tables_t;
+
+#define TUTTI_PAGES_MAX_SEQ 65536
+
+/*
+ * Counts of a pool's blocks: refs is a device pointer to [n_blocks] int32, 16-byte aligned, owned by the caller: how many
+ * rows (of any table, or other holders of the caller's) hold a block; 0 is a free block.  A block's id is the same in all
+ * layers, so the counts go by block.  The handle holds workspace (16 bytes a block): calls on one handle must be
+ * ordered after each other (one stream, or events; replays of captured graphs too), as must calls over the same counts.
+ * Destroy it before its context.
+ */
+typedef struct tutti_pages tutti_pages_t;
+int tutti_pages_create(tutti_ctx_t *ctx, int32_t *refs, uint64_t n_blocks, tutti_pages_t **out);
+int tutti_pages_destroy(tutti_pages_t *pages);
+
+/*
+ * Rows handed on: row s of `to` becomes row parent[s] of `from` (its held entries and len), and every block
+ * counts each row that holds it.  parent[s] = -1 makes the row empty; so do, with TUTTI_EINVAL in to->status, any other
+ * parent outside `from`, a parent's row that is refused, and a row that is too short.  A parent may
+ * be named any number of times: a sequence forks, or the beams of a search go on from the ones that were chosen.  move: TUTTI_FORK_MOVE
+ * gives up the rows of `from` in the same step (their blocks are free where no child took them); the
+ * table itself is left as it is and must not be used as one that holds blocks.  No bytes of the pool move: the last,
+ * partly filled block is shared until tutti_pages_extend copies it.  TUTTI_EINVAL if `from` and `to` share an array.
+ */
+#define TUTTI_FORK_KEEP 0
+#define TUTTI_FORK_MOVE 1
+int tutti_pages_fork(tutti_pages_t *pages, const tutti_tables_t *from, const int32_t *parent,
+                     const tutti_tables_t *to, uint32_t move, void *stream);
+
+/*
+ * Room for a step's tokens: len[s] grows by n_new[s] (device, [n_seq]; 0 leaves the row as it is).  New blocks are the
+ * free ones with the lowest ids, given out in the order of the rows; each counts 1.  Where the first new
+ * token goes into a block that holds earlier tokens and that others hold too, the row gets a new block in its
+ * place, and pairs[2 s], pairs[2 s + 1] (device, [n_seq][2]) are the old and the new one, for tutti_kv_copy_blocks; all other pairs
+ * are -1.  Of the rows that share the block they write to, the last one keeps it if nobody else holds it.
+ * All rows or none: with too few free blocks nothing changes, all pairs are -1 and *status is TUTTI_EAGAIN.
+ * A row is skipped (TUTTI_EINVAL) that has no room for its blocks or passes 2^31 - 1 tokens, or whose written block has a count below 1;
+ * TUTTI_EFAULT, and skipped, if that block is outside the pool or -1.
+ */
+int tutti_pages_extend(tutti_pages_t *pages, const tutti_tables_t *tables, const uint32_t *n_new,
+                       int32_t *pairs, void *stream);
+
+/*
+ * Free the rows s with which[s] != 0 (device, [n_seq] bytes; NULL: all): their blocks count one less, their held entries become
+ * -1 and len 0.  TUTTI_EINVAL in *status for a block whose count is 0 already (it stays 0).
+ */
+int tutti_pages_release(tutti_pages_t *pages, const tutti_tables_t *tables, const uint8_t *which, void *stream);
+
+/*
+ * Free what no later row of a sequence sees under a window: the blocks of each row whose keys are all at positions
+ * sinks .. len - window (a row at position len or later sees none of them); their entries become -1.
+ */
+int tutti_pages_trim(tutti_pages_t *pages, const tutti_tables_t *tables, const tutti_window_t *window, void *stream);
+
+/*
+ * Blocks in use moved to the lowest ids: with n blocks in use, the highest id at or above n goes to the lowest free
+ * id, the next to the next, until max_pairs have moved or all are below n.  Counts move along, entries of `tables` (n_seq 0:
+ * none) are rewritten, pairs[2 k], pairs[2 k + 1] (device, [max_pairs][2]) are the old and the new id of move k, -1 behind
+ * the last, and *n_pairs (device) is their number; tutti_kv_copy_blocks then moves the bytes.  Every holder of a block has to
+ * follow the pairs: rows of other tables, and restores or saves that were built before, are not rewritten.
+ */
+int tutti_pages_compact(tutti_pages_t *pages, const tutti_tables_t *tables, int32_t *pairs, uint32_t max_pairs,
+                        uint32_t *n_pairs, void *stream);
+
+/*
+ * Copy blocks inside the pool, keys and values, in layers [first_layer, first_layer + n_layers), with the
+ * scales of an 8-bit pool where they are registered: block pairs[2 k] to block pairs[2 k + 1] (device, [max_pairs][2]) for
+ * k < max_pairs, or below *n_pairs (device; NULL: all of them) where that is less.  A pair whose first id is -1 is
+ * left out, as is one of equal ids.  No block may be written twice, or be both read and written, in one call.
+ * TUTTI_EFAULT in *status (may be NULL; as in tutti_step_t) for an id outside a layer's pool; that pair is not
+ * copied in that layer.  TUTTI_ETIMEDOUT: a bounded wait ran out, the copies are incomplete.
+ * Any registered layers, whatever their elements.  Asynchronous on `stream`, graph-capturable, one launch for
+ * every 64 layers.  TUTTI_EINVAL for layers out of range or not registered, or a bad pointer.
+ */
+int tutti_kv_copy_blocks(tutti_ctx_t *ctx, uint32_t first_layer, uint32_t n_layers, const int32_t *pairs,
+                         uint32_t max_pairs, const uint32_t *n_pairs, int32_t *status, void *stream);
+
 /* ------------------------------------------------------------------------- */
 /* Slack-aware I/O scheduler (Section 3.3).  Pure host logic.                  */
 /* ------------------------------------------------------------------------- */

@@ -9,7 +9,7 @@ _CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libtutti.so")
 SOURCES = ["tutti_lib.cu", "tutti_build.cu", "tutti_copy.cu", "tutti_partition.cu", "tutti_noalloc.cu",
            "tutti_append.cu", "tutti_attend.cu", "tutti_attend_few.cu",
-           "tutti_attend_many.cu",
+           "tutti_attend_many.cu", "tutti_pages.cu", "tutti_pages_copy.cu",
            "host_ring.cpp", "tutti_sched.cpp", "tutti_filepool.cpp"]
 
 
@@ -28,7 +28,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall"]
+           "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "--threads", "0"]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     tmp = f"{LIB_PATH}.{os.getpid()}.tmp"           # several processes may build at once

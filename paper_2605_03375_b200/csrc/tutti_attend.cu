@@ -16,7 +16,10 @@ struct tutti_attn {
 
 extern "C" {
 
-// What the call refuses, from the geometry and the arguments alone.
+// What the calls refuse, from the geometry and the arguments alone.
+int tutti_window_check_(const tutti_window_t *w) {
+    return w && w->window && w->window <= 0x7fffffffu && w->sinks <= 0x7fffffffu ? TUTTI_OK : TUTTI_EINVAL;
+}
 int tutti_attend_check_(const tutti_geom_t *g, const tutti_step_t *step, const tutti_attend_t *io) {
     if (!g || !io) return TUTTI_EINVAL;
     if (int rc = check_step(step)) return rc;
@@ -74,8 +77,10 @@ int tutti_attn_destroy(tutti_attn_t *a) {
     return TUTTI_OK;
 }
 
-int tutti_kv_attend_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *step,
-                          const tutti_attend_t *io, void *stream) {
+}  // extern "C"
+
+// window 0: every key up to the row's own.
+static int attend(tutti_attn_t *a, uint32_t layer, const tutti_step_t *step, const tutti_attend_t *io, uint32_t window, uint32_t sinks, void *stream) {
     if (!a) return TUTTI_EINVAL;
     if (int rc = tutti_attend_check_(tutti_ctx_geom_(a->ctx), step, io)) return rc;
     AttendParams p;
@@ -93,6 +98,8 @@ int tutti_kv_attend_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *s
     p.out = io->out;
     p.lse = io->lse;
     p.scale = io->scale;
+    p.window = window;
+    p.sinks = sinks;
     OnDevice on(tutti_ctx_device_(a->ctx));
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const bool bf = io->dtype == TUTTI_DTYPE_BF16;
@@ -102,6 +109,19 @@ int tutti_kv_attend_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *s
     const cudaError_t e = few ? few_launch(p, a->few, tutti_ctx_sms_(a->ctx), elem_bytes == 1, bf, (cudaStream_t)stream)
                               : many_launch(p, maps, a->many, elem_bytes == 1, bf, (cudaStream_t)stream);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "attend launch");
+}
+
+extern "C" {
+
+int tutti_kv_attend_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *step,
+                          const tutti_attend_t *io, void *stream) {
+    return attend(a, layer, step, io, 0, 0, stream);
+}
+
+int tutti_kv_attend_window_layer(tutti_attn_t *a, uint32_t layer, const tutti_step_t *step,
+                                 const tutti_attend_t *io, const tutti_window_t *window, void *stream) {
+    if (int rc = tutti_window_check_(window)) return rc;
+    return attend(a, layer, step, io, window->window, window->sinks, stream);
 }
 
 }  // extern "C"

@@ -16,6 +16,10 @@ struct AttendParams {
     float *lse;
     float scale;
     uint32_t group_mul, group_shift;  // row / group = row * group_mul >> group_shift
+    uint32_t window, sinks;           // window 0: every key up to the row's own
+
+    // The first key behind the first `sinks` that a row at position `first` (any row behind it) sees: 0 or less, all.
+    __host__ __device__ int64_t window_start(int64_t first) const { return first - window + 1; }
 
     __host__ __device__ uint32_t token_of(uint32_t row) const { return (uint32_t)((uint64_t)row * group_mul >> group_shift); }
     __host__ __device__ uint32_t member_of(uint32_t row) const { return row - token_of(row) * group; }

@@ -64,21 +64,43 @@ __device__ inline uint32_t transpose8(uint32_t x) {
     return y;
 }
 // A place in the step's units laid end to end: unit u of row tile r and KV head h of sequence s.
-struct Cursor {
+struct Place {
     uint32_t s, h, r, u;
     uint32_t n_tiles, n_units;      // of the sequence: row tiles, units of each
     SeqView v;
 };
+// WIN: units that no row of the sequence sees, between its first tokens and its window, are left out.
+template <bool WIN>
+struct Cursor : Place {};
+template <>
+struct Cursor<true> : Place {
+    uint32_t gap;                   // how many
+};
+__device__ inline uint32_t sink_units(const AttendParams &p, uint32_t unit_keys) { return (p.sinks + unit_keys - 1) / unit_keys; }
 
 // Row tiles and units of a sequence (0 tiles: nothing to do); the error code, if any.
-__device__ inline int seq_shape(const AttendParams &p, uint32_t rows, uint32_t unit_keys, uint32_t s, Cursor &k) {
+template <bool WIN>
+__device__ inline int seq_shape(const AttendParams &p, uint32_t rows, uint32_t unit_keys, uint32_t s, Cursor<WIN> &k) {
     const int code = seq_view(p.step, p.pool.block_tokens, s, k.v);
     k.n_tiles = code == TUTTI_OK ? (k.v.n_new * p.group + rows - 1) / rows : 0;
     k.n_units = code == TUTTI_OK && k.v.ctx ? (k.v.ctx + unit_keys - 1) / unit_keys : 1;
+    if constexpr (WIN) {
+        const int64_t start = p.window_start((int64_t)k.v.ctx - k.v.n_new);
+        const uint32_t behind = start > 0 ? (uint32_t)start / unit_keys : 0, front = sink_units(p, unit_keys);
+        k.gap = code == TUTTI_OK && behind > front ? behind - front : 0;
+        k.n_units -= k.gap;
+    }
     return code;
 }
+// Which unit of the sequence's keys unit u is.
+template <bool WIN>
+__device__ inline uint32_t key_unit(const AttendParams &p, uint32_t unit_keys, const Cursor<WIN> &k) {
+    if constexpr (WIN) return k.u + (k.u >= sink_units(p, unit_keys) ? k.gap : 0);
+    else return k.u;
+}
 
-__device__ inline void advance(const AttendParams &p, uint32_t rows, uint32_t unit_keys, Cursor &k) {
+template <bool WIN>
+__device__ inline void advance(const AttendParams &p, uint32_t rows, uint32_t unit_keys, Cursor<WIN> &k) {
     if (++k.u < k.n_units) return;
     k.u = 0;
     if (++k.r < k.n_tiles) return;
@@ -129,7 +151,7 @@ struct Few {
     }
 };
 
-template <typename T, bool C8, int D, int NB>
+template <typename T, bool C8, int D, int NB, bool WIN>
 __global__ void __launch_bounds__(WARPS * 32, Few<T, C8, D, NB>::WORKERS_PER_SM)
 attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     using F = Few<T, C8, D, NB>;
@@ -145,7 +167,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     const uint32_t per = (p.step.n_seq + WARPS * 32 - 1) / (WARPS * 32);
     unsigned long long mine = 0;
     uint32_t my_tiles = 0;
-    Cursor own;                                    // the thread's last sequence (its only one, mostly)
+    Cursor<WIN> own;                               // the thread's last sequence (its only one, mostly)
     own.s = ~0u;
     for (uint32_t s = threadIdx.x * per; s < min((threadIdx.x + 1) * per, p.step.n_seq); ++s) {
         const int code = seq_shape(p, F::ROWS, F::UNIT, s, own);
@@ -191,7 +213,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                 own.h = (uint32_t)quotient(tile, own.n_tiles);
                 own.r = (uint32_t)(tile - (unsigned long long)own.h * own.n_tiles);
                 own.u = (uint32_t)(x0 - at - tile * own.n_units);
-                *reinterpret_cast<Cursor *>(plan) = own;
+                *reinterpret_cast<Cursor<WIN> *>(plan) = own;
                 break;
             }
             at += n;
@@ -199,27 +221,33 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
         }
     }
     __syncthreads();
-    Cursor get = *reinterpret_cast<const Cursor *>(plan);
+    Cursor<WIN> get = *reinterpret_cast<const Cursor<WIN> *>(plan);
 
     // ---- gathering ----
     // The ids of a unit's blocks are looked up two units before its rows are fetched, and not touched
     // until then (the first use waits for the load).
     struct Pending {
         uint32_t key0, ctx, h;                     // of a unit: the warp's first key, keys that exist, KV head
+        uint32_t start;                            // WIN: keys from here on, and the first p.sinks, are seen
         int32_t id[F::KPL];                        // of the lane's keys
     } pend[2];
-    Cursor look = get;
+    auto in_sight = [&](const Pending &u, uint32_t key) { return key < u.ctx && (!WIN || key < p.sinks || key >= u.start); };
+    Cursor<WIN> look = get;
     unsigned long long look_x = x0, put_x = x0;
     auto locate = [&](Pending &u) {
-        u.key0 = (look.u * WARPS + warp) * F::KW;
+        u.key0 = (key_unit(p, F::UNIT, look) * WARPS + warp) * F::KW;
         u.ctx = look.v.ctx;
+        if constexpr (WIN) {
+            const int64_t start = p.window_start((int64_t)look.v.ctx - look.v.n_new);
+            u.start = start > 0 ? (uint32_t)start : 0;
+        }
         u.h = look.h;
         if (look_x < x1) {
 #pragma unroll
             for (int i = 0; i < F::KPL; ++i) {
                 const uint32_t key = u.key0 + i * 32 + lane;
                 u.id[i] = -1;
-                if (i * 32 + lane < F::KW && key < u.ctx) u.id[i] = __ldg(p.step.block_ids + look.v.b0 + p.pool.block_of(key));
+                if (i * 32 + lane < F::KW && in_sight(u, key)) u.id[i] = __ldg(p.step.block_ids + look.v.b0 + p.pool.block_of(key));
             }
             advance(p, F::ROWS, F::UNIT, look);
         }
@@ -237,7 +265,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
 #pragma unroll
             for (int i = 0; i < F::KPL; ++i) {
                 const uint32_t key = u.key0 + i * 32 + lane;
-                const bool held = i * 32 + lane < F::KW && key < u.ctx, ok = held && (uint32_t)u.id[i] < p.pool.n_blocks;
+                const bool held = i * 32 + lane < F::KW && in_sight(u, key), ok = held && (uint32_t)u.id[i] < p.pool.n_blocks;
                 if (held && !ok) report(p.step, TUTTI_EFAULT);
                 mask |= (uint64_t)__ballot_sync(0xffffffffu, ok) << (32 * i);
                 if (C8 && i * 32 + lane < F::KW) {
@@ -352,6 +380,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             for (int i = 0; i < F::DT; ++i) o[b][i][0] = o[b][i][1] = o[b][i][2] = o[b][i][3] = 0;
         }
         const int64_t last_all = first + token_of(row0);        // keys up to here are seen by every row of the tile
+        const int64_t hidden = WIN ? first + token_of(min(row0 + F::ROWS, n_rows) - 1) - p.window : 0;      // up to here not by every one
 
         for (; x < seg_end; ++x) {
             cp_wait<F::STAGES - 2>();
@@ -360,7 +389,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
             unsigned char *st = ring + stage * F::STAGE;
             const uint32_t kst = smem_addr(st), vst = kst + F::KW * F::RB;
             const uint64_t there = exists[stage];
-            const int64_t key0 = (int64_t)(get.u * WARPS + warp) * F::KW;
+            const int64_t key0 = (int64_t)(key_unit(p, F::UNIT, get) * WARPS + warp) * F::KW;
             constexpr uint64_t ALL = F::KW == 64 ? ~0ull : (1ull << (F::KW & 63)) - 1;
             if (there) {
                 // scores: fragment element e is key 16 t + g + 8 (e / 2), row 2 c + e % 2
@@ -396,7 +425,7 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                         }
                     }
                 }
-                const bool masked = there != ALL || key0 + F::KW - 1 > last_all;
+                const bool masked = there != ALL || key0 + F::KW - 1 > last_all || (WIN && key0 <= hidden);
                 float vs[F::MT][2];                      // 8-bit: value scales of the lane's keys
                 if constexpr (C8) {
 #pragma unroll
@@ -417,7 +446,9 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
                             const int key = t * 16 + g + 8 * (e / 2);
                             if constexpr (C8) ks *= *reinterpret_cast<const float *>(st + F::STAGE_BYTES + key * 4);
                             s[b][t][e] *= ks;
-                            if (masked && (!(there >> key & 1) || key0 + key > pos[b][e & 1])) s[b][t][e] = -INFINITY;
+                            if (masked && (!(there >> key & 1) || key0 + key > pos[b][e & 1] ||
+                                           (WIN && key0 + key <= pos[b][e & 1] - p.window && key0 + key >= p.sinks)))
+                                s[b][t][e] = -INFINITY;
                             top[e & 1] = fmaxf(top[e & 1], s[b][t][e]);
                         }
                     float alpha[2], sub[2];
@@ -640,23 +671,24 @@ attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     cp_wait<0>();
 }
 
-template <typename T, bool C8, int D, int NB>
+template <typename T, bool C8, int D, int NB, bool WIN>
 cudaError_t launch_few(const AttendParams &p, Workspace ws, int sms, cudaStream_t st) {
     using F = Few<T, C8, D, NB>;
     ws.workers = sms * F::WORKERS_PER_SM;
-    return launch_plain(attend_few_kernel<T, C8, D, NB>, ws.workers, WARPS * 32, F::SMEM, st, p, ws);
+    return launch_plain(attend_few_kernel<T, C8, D, NB, WIN>, ws.workers, WARPS * 32, F::SMEM, st, p, ws);
 }
 
-template <typename T, bool C8, int D, int NB>
+template <typename T, bool C8, int D, int NB, bool WIN>
 cudaError_t setup_few() {
-    return cudaFuncSetAttribute(attend_few_kernel<T, C8, D, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<T, C8, D, NB>::SMEM);
+    return cudaFuncSetAttribute(attend_few_kernel<T, C8, D, NB, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize, Few<T, C8, D, NB>::SMEM);
 }
 
-// f(type, 8-bit, head_dim, row blocks) for one or for every instance
+// f(type, 8-bit, head_dim, row blocks, window) for one or for every instance
 template <typename F>
-cudaError_t pick(bool bf, bool c8, bool wide, bool two, F f) {
+cudaError_t pick(bool bf, bool c8, bool wide, bool two, bool window, F f) {
+    auto win = [&](auto t, auto c, auto d, auto n) { return window ? f(t, c, d, n, std::true_type()) : f(t, c, d, n, std::false_type()); };
     auto nb = [&](auto t, auto c, auto d) {
-        return two ? f(t, c, d, std::integral_constant<int, 2>()) : f(t, c, d, std::integral_constant<int, 1>());
+        return two ? win(t, c, d, std::integral_constant<int, 2>()) : win(t, c, d, std::integral_constant<int, 1>());
     };
     auto dim = [&](auto t, auto c) {
         return wide ? nb(t, c, std::integral_constant<int, 128>()) : nb(t, c, std::integral_constant<int, 64>());
@@ -669,16 +701,16 @@ cudaError_t pick(bool bf, bool c8, bool wide, bool two, F f) {
 
 cudaError_t few_setup() {
     cudaError_t e = cudaSuccess;
-    for (int i = 0; i < 16 && e == cudaSuccess; ++i)
-        e = pick(i & 1, i & 2, i & 4, i & 8, [](auto t, auto c, auto d, auto nb) { return setup_few<decltype(t), c.value, d.value, nb.value>(); });
+    for (int i = 0; i < 32 && e == cudaSuccess; ++i)
+        e = pick(i & 1, i & 2, i & 4, i & 8, i & 16, [](auto t, auto c, auto d, auto nb, auto w) { return setup_few<decltype(t), c.value, d.value, nb.value, w.value>(); });
     return e;
 }
 
 cudaError_t few_launch(const AttendParams &p, const Workspace &ws, int sms, bool c8, bool bf, cudaStream_t st) {
     // one block of 8 rows where a step's tokens and the query heads of a KV head fit
     const bool two = (uint64_t)p.step.max_new * p.group > 8;
-    return pick(bf, c8, p.pool.head_dim == 128, two, [&](auto t, auto c, auto d, auto nb) {
-        return launch_few<decltype(t), c.value, d.value, nb.value>(p, ws, sms, st);
+    return pick(bf, c8, p.pool.head_dim == 128, two, p.window != 0, [&](auto t, auto c, auto d, auto nb, auto w) {
+        return launch_few<decltype(t), c.value, d.value, nb.value, w.value>(p, ws, sms, st);
     });
 }
 

@@ -118,14 +118,39 @@ struct Rows {
     }
 };
 
-__host__ __device__ inline Rows rows_of(const SeqView &v, uint32_t group) {
-    Rows r;
+// The same under a window: of a tile's units the ones that none of its rows sees, between the first tokens and the
+// window of its first row, are left out.
+struct WindowRows : Rows {
+    uint32_t front;                     // units of the first tokens that stay visible
+    int64_t start;                      // (keys in front of the first row's window, less those of `front`) * group
+    // how many are left out of tile q: floor((first + floor(256 q / group) - window + 1) / BN) - front, if positive
+    __host__ __device__ uint32_t gap(uint32_t q) const {
+        const int64_t x = start + (int64_t)q * TILE_ROWS;
+        return x > 0 ? (uint32_t)((uint64_t)x / ((uint64_t)BN * group)) : 0;
+    }
+    __host__ __device__ uint32_t units(uint32_t q) const { return Rows::units(q) - gap(q); }
+    __host__ __device__ uint64_t before(uint32_t q) const {
+        const uint64_t all = Rows::before(q);
+        // tiles in front of q0 leave nothing out
+        const uint64_t q0 = start >= 0 ? 0 : ((uint64_t)-start + TILE_ROWS - 1) / TILE_ROWS;
+        return q <= q0 ? all : all - floor_sum(q - q0, (uint64_t)BN * group, TILE_ROWS, (uint64_t)(start + (int64_t)q0 * TILE_ROWS));
+    }
+};
+template <bool WIN> struct RowsOf { typedef Rows type; };
+template <> struct RowsOf<true> { typedef WindowRows type; };
+
+__host__ __device__ inline void rows_of(const SeqView &v, uint32_t group, uint32_t, uint32_t, Rows &r) {
     r.n_rows = v.n_new * group;
     r.n_tiles = (r.n_rows + TILE_ROWS - 1) / TILE_ROWS;
     r.group = group;
     r.ctx = v.ctx;
     r.first = (int64_t)v.ctx - v.n_new;
-    return r;
+}
+__host__ __device__ inline void rows_of(const SeqView &v, uint32_t group, uint32_t window, uint32_t sinks, WindowRows &r) {
+    rows_of(v, group, 0, 0, static_cast<Rows &>(r));
+    r.front = (sinks + BN - 1) / BN;
+    // padding rows: every tile sees all
+    r.start = r.first < 0 ? -((int64_t)1 << 62) : (r.first - window + 1 - (int64_t)r.front * BN) * group;
 }
 
 // Where a cut at unit u of a tile of n units goes: to its start below low(n), behind it from n -
@@ -144,27 +169,43 @@ __host__ __device__ inline void holders(unsigned long long tile0, uint32_t n, un
     w1 = (uint32_t)quotient((tile0 + n - snap_high(n)) * workers - 1, total);
 }
 
+template <bool WIN>
 struct Tile {
     uint32_t s, h, q, u, n_units;
     SeqView v;
-    Rows r;
+    typename RowsOf<WIN>::type r;
 };
 
 // The sequence of a cut: units of one of its heads, units in front of the cut.
+template <bool WIN>
 struct Found {
-    Tile t;
+    Tile<WIN> t;
     unsigned long long head, in_seq;
 };
 
-__device__ inline int tile_seq(const AttendParams &p, uint32_t s, Tile &t) {
+// Which unit of the sequence's keys unit u of a tile is; `gap` of the tile.
+template <bool WIN>
+__device__ inline uint32_t gap_of(const Tile<WIN> &t) {
+    if constexpr (WIN) return t.r.gap(t.q);
+    else return 0;
+}
+template <bool WIN>
+__device__ inline uint32_t key_unit(const Tile<WIN> &t, uint32_t u, uint32_t gap) {
+    if constexpr (WIN) return u + (u >= t.r.front ? gap : 0);
+    else return u;
+}
+
+template <bool WIN>
+__device__ inline int tile_seq(const AttendParams &p, uint32_t s, Tile<WIN> &t) {
     t.s = s;
     const int code = seq_view(p.step, p.pool.block_tokens, s, t.v);
     if (code != TUTTI_OK) t.v.n_new = t.v.ctx = 0;
-    t.r = rows_of(t.v, p.group);
+    rows_of(t.v, p.group, p.window, p.sinks, t.r);
     return code;
 }
 
-__device__ inline void next_tile(const AttendParams &p, Tile &t) {
+template <bool WIN>
+__device__ inline void next_tile(const AttendParams &p, Tile<WIN> &t) {
     t.u = 0;
     if (++t.q == t.r.n_tiles) {
         t.q = 0;
@@ -377,7 +418,7 @@ struct Many {
     }
 };
 
-template <typename T, bool C8, int D>
+template <typename T, bool C8, int D, bool WIN>
 __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ PoolMaps maps, const Workspace ws) {
     using C = Many<T, C8, D>;
     constexpr int SUB = C::SUB, STEPS = C::STEPS;
@@ -387,7 +428,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31;
     uint32_t *misc = reinterpret_cast<uint32_t *>(sm + C::OFF_MISC);
     uint32_t *exists = reinterpret_cast<uint32_t *>(sm + C::OFF_EXISTS);
-    Found *found = reinterpret_cast<Found *>(sm + C::OFF_TILE);
+    Found<WIN> *found = reinterpret_cast<Found<WIN> *>(sm + C::OFF_TILE);
+    static_assert(2 * sizeof(Found<WIN>) <= 256, "two of them lie in front of the end");
     int2 *units = reinterpret_cast<int2 *>(sm + C::OFF_UNITS);
     volatile uint32_t *dead = misc + 72;
     const uint32_t bars = base + C::OFF_BAR;
@@ -400,7 +442,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     const uint32_t s_lo = threadIdx.x * per, s_hi = min(s_lo + per, p.step.n_seq);
     unsigned long long mine = 0;
     uint32_t my_tiles = 0;
-    Found own;                                     // the thread's last sequence (its only one, mostly)
+    Found<WIN> own;                                // the thread's last sequence (its only one, mostly)
     own.t.s = ~0u;
     auto look = [&](uint32_t s) {
         const int code = tile_seq(p, s, own.t);
@@ -488,11 +530,11 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     const uint32_t tmem = misc[73];
     if (warp < 2) {
         unsigned long long x = cut[warp];
-        Tile f;
+        Tile<WIN> f;
         f.s = f.h = f.q = f.u = f.n_units = 0;
         if (x < total) {
             f = found[warp].t;
-            const Rows r = f.r;
+            const auto r = f.r;
             const unsigned long long in_seq = found[warp].in_seq, head = found[warp].head;
             f.h = (uint32_t)quotient(in_seq, head);
             const unsigned long long rest = in_seq - f.h * head;
@@ -522,7 +564,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     }
     __syncthreads();
     const unsigned long long x0 = sums[22], x1 = sums[23];
-    Tile t = found[0].t;
+    Tile<WIN> t = found[0].t;
     // scores (and probabilities over them) of a half and step, then the halves' outputs
     auto S = [&](int i, int u) { return tmem + i * 128 + u * SUB; };
     auto O = [&](int i) { return tmem + 256 + i * D; };
@@ -551,19 +593,24 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         };
         // The next unit: block ids of rows lane and lane + 32 (locate), then what follows from them.
         int32_t id[2];
-        uint32_t key0 = 0, head = 0, ctx = 0;
+        uint32_t key0 = 0, head = 0, ctx = 0, start = 0;
+        auto in_sight = [&](uint32_t key) { return key < ctx && (!WIN || key < p.sinks || key >= start); };
         int64_t off[2];
         float ks[2], vs[2];
         uint32_t missing[2];
         bool tiled = false;
         auto locate = [&]() {
-            key0 = t.u * BN + half * 64;
+            key0 = key_unit(t, t.u, gap_of(t)) * BN + half * 64;
             head = t.h;
             ctx = fx < x1 ? t.v.ctx : 0;
+            if constexpr (WIN) {                        // of the sequence: no row sees a key in front of its first row's window
+                const int64_t x = p.window_start(t.r.first);
+                start = x > 0 ? (uint32_t)x : 0;
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint32_t key = key0 + i * 32 + lane;
-                id[i] = key < ctx ? __ldg(p.step.block_ids + t.v.b0 + p.pool.block_of(key)) : -1;
+                id[i] = in_sight(key) ? __ldg(p.step.block_ids + t.v.b0 + p.pool.block_of(key)) : -1;
             }
         };
         auto resolve = [&]() {
@@ -571,7 +618,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const uint32_t key = key0 + i * 32 + lane;
-                const bool there = (uint32_t)id[i] < p.pool.n_blocks, bad = !there && key < ctx;
+                const bool there = (uint32_t)id[i] < p.pool.n_blocks, bad = !there && in_sight(key);
                 if (bad) report(p.step, TUTTI_EFAULT);
                 missing[i] = __ballot_sync(0xffffffffu, bad);
                 tiled = tiled && __all_sync(0xffffffffu, there);
@@ -885,6 +932,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 const uint32_t tok = p.token_of(in ? row : t.r.n_rows - 1);
                 const int64_t pos = t.r.first + tok;
                 const int64_t pos_low = __shfl_sync(0xffffffffu, pos, 0);
+                const int64_t hidden = WIN ? __shfl_sync(0xffffffffu, pos, 31) - p.window : 0;      // keys up to here are not seen by every row
+                const uint32_t gap = gap_of(t);
                 float m = -INFINITY, l = 0;
                 int o_unit = UNIT_LEAST_V;                        // UNITS: exponent of the output's unit, the largest of its values'
                 const uint32_t steps = STEPS * n;
@@ -915,17 +964,23 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     tc_wait_ld();
 #pragma unroll
                     for (int q = 0; q < SUB / 32; ++q) tc_loaded(sr + 32 * q);
-                    const int64_t key0 = (int64_t)t.u * BN + j * SUB;
+                    const int64_t key0 = (int64_t)key_unit(t, t.u + j / STEPS, gap) * BN + j % STEPS * SUB;
                     if (negative) {
 #pragma unroll
                         for (int k = 0; k < SUB; ++k) s[k] = -s[k];
                     }
-                    if (key0 + SUB - 1 > pos_low || all != ~0u) {
+                    if (key0 + SUB - 1 > pos_low || all != ~0u || (WIN && key0 <= hidden)) {
                         const int64_t d = pos - key0;
                         const int lim = d < -1 ? -1 : d > SUB ? SUB : (int)d;
+                        int low = -1, front = 0;                  // WIN: keys up to `low`, but for those below `front`
+                        if constexpr (WIN) {
+                            const int64_t x = d - p.window, y = (int64_t)p.sinks - key0;
+                            low = x < -1 ? -1 : x > SUB ? SUB : (int)x;
+                            front = y < 0 ? 0 : y > SUB ? SUB : (int)y;
+                        }
 #pragma unroll
                         for (int k = 0; k < SUB; ++k)
-                            if (k > lim || !(ex[k / 32] >> (k % 32) & 1)) s[k] = -INFINITY;
+                            if (k > lim || (WIN && k <= low && k >= front) || !(ex[k / 32] >> (k % 32) & 1)) s[k] = -INFINITY;
                     }
                     float a0 = max3(s[0], s[4], s[8]), a1 = max3(s[1], s[5], s[9]), a2 = max3(s[2], s[6], s[10]), a3 = max3(s[3], s[7], s[11]);
 #pragma unroll
@@ -1119,7 +1174,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 
 template <typename T, bool C8, int D>
 cudaError_t launch(const AttendParams &p, const PoolMaps &maps, const Workspace &ws, cudaStream_t st) {
-    return launch_plain(attend_many_kernel<T, C8, D>, ws.workers, THREADS, Many<T, C8, D>::SMEM, st, p, maps, ws);
+    return p.window ? launch_plain(attend_many_kernel<T, C8, D, true>, ws.workers, THREADS, Many<T, C8, D>::SMEM, st, p, maps, ws)
+                    : launch_plain(attend_many_kernel<T, C8, D, false>, ws.workers, THREADS, Many<T, C8, D>::SMEM, st, p, maps, ws);
 }
 
 template <typename T, bool C8>
@@ -1129,7 +1185,8 @@ cudaError_t launch(const AttendParams &p, const PoolMaps &maps, const Workspace 
 
 template <typename T, bool C8, int D>
 cudaError_t setup() {
-    return cudaFuncSetAttribute(attend_many_kernel<T, C8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Many<T, C8, D>::SMEM);
+    const cudaError_t e = cudaFuncSetAttribute(attend_many_kernel<T, C8, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Many<T, C8, D>::SMEM);
+    return e == cudaSuccess ? cudaFuncSetAttribute(attend_many_kernel<T, C8, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Many<T, C8, D>::SMEM) : e;
 }
 
 template <typename T>
@@ -1182,9 +1239,21 @@ extern "C" void tutti_many_parts_(uint64_t tile0, uint32_t n, uint64_t workers, 
 // The kernel's own count of units, on the host: out2[0] units of tile q, out2[1] units of the tiles before it.
 extern "C" int tutti_many_units_(uint32_t ctx, uint32_t n_new, uint32_t group, uint32_t q, uint64_t *out2) {
     const tutti::SeqView v{0, n_new, ctx, 0};
-    const tutti::Rows r = tutti::rows_of(v, group);
+    tutti::Rows r;
+    tutti::rows_of(v, group, 0, 0, r);
     out2[0] = q < r.n_tiles ? r.units(q) : 0;
     out2[1] = r.before(q);
+    return (int)r.n_tiles;
+}
+// The same under a window; out4[2] the first units that stay, out4[3] the units left out behind them.
+extern "C" int tutti_many_window_units_(uint32_t ctx, uint32_t n_new, uint32_t group, uint32_t window, uint32_t sinks, uint32_t q, uint64_t *out4) {
+    const tutti::SeqView v{0, n_new, ctx, 0};
+    tutti::WindowRows r;
+    tutti::rows_of(v, group, window, sinks, r);
+    out4[0] = q < r.n_tiles ? r.units(q) : 0;
+    out4[1] = r.before(q);
+    out4[2] = r.front;
+    out4[3] = q < r.n_tiles ? r.gap(q) : 0;
     return (int)r.n_tiles;
 }
 

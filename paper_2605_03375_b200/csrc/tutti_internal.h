@@ -180,5 +180,6 @@ cudaError_t launch_copy(const RingDev &ring, uint32_t first_iocb, uint32_t n_ioc
 // library; called with the device current whenever a context is created on it.
 cudaError_t copy_kernels_setup();
 cudaError_t build_kernels_setup();
+cudaError_t copy_blocks_setup();
 
 }  // namespace tutti

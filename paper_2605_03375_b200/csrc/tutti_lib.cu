@@ -193,6 +193,7 @@ int tutti_ctx_create(const tutti_geom_t *geom, int device, tutti_ctx_t **out) {
         return TUTTI_ECUDA;
     }
     CK(copy_kernels_setup());
+    CK(copy_blocks_setup());
     tutti_ctx *c = new (std::nothrow) tutti_ctx();
     if (!c) return TUTTI_ENOMEM;
     c->geom = *geom;
@@ -325,6 +326,14 @@ int tutti_ctx_pool_view_(tutti_ctx_t *ctx, uint32_t layer, PoolView *v, uint32_t
     division_by(g.block_tokens, v->block_mul, v->block_shift);
     *elem_bytes = g.elem_bytes;
     return TUTTI_OK;
+}
+
+// A layer for copies of whole blocks; false for one that is not registered.
+bool tutti_ctx_layer_bytes_(tutti_ctx *ctx, uint32_t layer, LayerBytes *out) {
+    const PoolLayer &p = ctx->pool[layer];
+    const PoolScales &s = ctx->scales[layer];
+    *out = LayerBytes{p.k_base, p.v_base, p.block_stride, s.k, s.v, (uint32_t)p.n_blocks, s.row};
+    return p.registered;
 }
 
 // K and V tensor maps of a layer in the layout that is set now; false where there are none.

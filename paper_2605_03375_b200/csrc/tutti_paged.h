@@ -42,6 +42,13 @@ struct PoolTensorMaps {
     bool valid[2] = {false, false};
 };
 
+// A registered layer as bytes, with the scales of an 8-bit one (null where none are registered).
+struct LayerBytes {
+    uint64_t k_base, v_base, block_stride;
+    float *k_scale, *v_scale;
+    uint32_t n_blocks, scale_row;
+};
+
 struct StepDev {
     uint32_t n_seq, n_tok, n_blk, max_new;
     const uint32_t *q_start, *ctx_len, *blk_start;
@@ -122,10 +129,12 @@ __device__ inline uint32_t warp_find(uint32_t n, uint32_t x, F start) {
 struct tutti_ctx;
 extern "C" int tutti_ctx_pool_view_(tutti_ctx *ctx, uint32_t layer, tutti::PoolView *view, uint32_t *elem_bytes);
 extern "C" bool tutti_ctx_pool_maps_(tutti_ctx *ctx, uint32_t layer, CUtensorMap *k, CUtensorMap *v);
+extern "C" bool tutti_ctx_layer_bytes_(tutti_ctx *ctx, uint32_t layer, tutti::LayerBytes *out);
 extern "C" int tutti_ctx_device_(tutti_ctx *ctx);
 extern "C" int tutti_ctx_sms_(tutti_ctx *ctx);
 extern "C" const tutti_geom_t *tutti_ctx_geom_(tutti_ctx *ctx);
 extern "C" void tutti_set_cuda_error_(const char *msg);
+extern "C" int tutti_window_check_(const tutti_window_t *w);
 
 namespace tutti {
 

@@ -1,0 +1,607 @@
+// Pages of the pool: which rows hold which blocks.  Rows are handed on (fork), grow (extend), are freed (release,
+// trim), and blocks in use are moved to the lowest ids (compact); tables and counts live in device memory.
+#include <new>
+
+#include "tutti_attend.h"
+
+namespace tutti {
+
+namespace {
+
+constexpr uint32_t PLAN_THREADS = 1024;
+constexpr uint32_t TILE = 4 * PLAN_THREADS;     // counts that a CTA looks at in one round
+constexpr uint32_t ROW_THREADS = 256;
+constexpr uint32_t ROW_IDS = 8 * ROW_THREADS;   // ids of a row that a CTA takes at once
+constexpr uint32_t SEARCH = 4096;               // rows whose first ranks fit in shared memory
+
+struct TablesDev {
+    uint32_t n_seq, n_blk, block_tokens;
+    const uint32_t *blk_start;
+    int32_t *block_ids;
+    uint32_t *len;
+    int32_t *status;
+};
+
+// The handle's memory.  arrive, turn, writers and top are zero between calls.
+struct PagesDev {
+    int32_t *refs;
+    uint32_t n_blocks, n_tiles;
+    uint32_t *arrive;                           // CTAs of extend that have counted
+    uint32_t *turn;                             // [max rows] CTAs of release that have read a row's length
+    uint32_t *tile;                             // [n_tiles] free blocks, or blocks in use
+    uint32_t *moves;                            // of a compaction
+    uint32_t *writers, *top;                    // [n_blocks] rows that write to a shared block, and the last of them + 1
+    uint32_t *rank;                             // [n_blocks] a moved block's number
+    uint32_t *begin, *entry;                    // [max rows] rank of a row's first new block, and where it goes
+    int32_t *mark, *keep_id, *keep_count;       // [max rows] see extend_kernel
+};
+
+__device__ inline void report(int32_t *status, int code) {
+    if (status) atomicCAS(status, TUTTI_OK, code);
+}
+
+struct Row {
+    uint32_t b0, room, len, held;
+};
+
+__host__ __device__ inline uint32_t blocks_of(uint32_t tokens, uint32_t block_tokens) {
+    return tokens / block_tokens + (tokens % block_tokens != 0);
+}
+
+// The entries of row s, without its length.
+__device__ inline bool row_room(const TablesDev &t, uint32_t s, Row &r) {
+    const uint32_t b0 = t.blk_start[s], b1 = t.blk_start[s + 1];
+    if (b0 > b1 || b1 > t.n_blk) return false;
+    r.b0 = b0;
+    r.room = b1 - b0;
+    return true;
+}
+__device__ inline bool row_view(const TablesDev &t, uint32_t s, Row &r) {
+    r.len = t.len[s];
+    if (!row_room(t, s, r) || r.len > 0x7fffffffu) return false;
+    r.held = blocks_of(r.len, t.block_tokens);
+    return r.held <= r.room;
+}
+
+// One holder less; a count that is 0 stays 0.
+__device__ inline void drop(const PagesDev &p, int32_t id, int32_t *status) {
+    if (atomicAdd(p.refs + id, -1) <= 0) {
+        atomicAdd(p.refs + id, 1);
+        report(status, TUTTI_EINVAL);
+    }
+}
+
+// Sum over the CTA's threads before this one; `total` over all.  sums: [32] in shared memory.
+template <typename U>
+__device__ inline U scan(U x, U *sums, U &total) {
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, warps = blockDim.x / 32;
+    U incl = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const U y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+    }
+    __syncthreads();                            // the sums of an earlier scan have been read
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    U w = lane < warps ? sums[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const U y = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += y;
+    }
+    total = __shfl_sync(0xffffffffu, w, 31);
+    const U before = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
+    return incl - x + (warp ? before : 0);
+}
+
+// The four counts of a thread in a tile; blocks behind the last one read as `none`.
+__device__ inline int4 tile_counts(const PagesDev &p, uint32_t tile, int none) {
+    const uint32_t id = tile * TILE + threadIdx.x * 4;
+    if (id + 4 <= p.n_blocks) return *reinterpret_cast<const int4 *>(p.refs + id);
+    int4 v = make_int4(none, none, none, none);
+    if (id < p.n_blocks) v.x = p.refs[id];
+    if (id + 1 < p.n_blocks) v.y = p.refs[id + 1];
+    if (id + 2 < p.n_blocks) v.z = p.refs[id + 2];
+    return v;
+}
+__device__ inline uint32_t zeros(const int4 &v) { return (v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0); }
+
+// ---------------------------------------------------------------------------------------------
+// fork: CTAs [0, per * to.n_seq) copy the entries of the new rows, the ones behind change the counts of the old
+// rows' blocks, by as many as a row has children (less the row itself, where it is given up): a row with one
+// child that takes its place costs no atomics at all, and that is most of them.
+__global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, const TablesDev from, const int32_t *parent, const TablesDev to, uint32_t move, uint32_t per) {
+    const uint32_t row = blockIdx.x / per, part = blockIdx.x % per;
+    Row r, child;
+    if (row < to.n_seq) {
+        const int32_t f = parent[row];
+        bool ok = row_room(to, row, child);
+        if (f != -1) ok = ok && (uint32_t)f < from.n_seq && row_view(from, f, r) && r.held <= child.room;
+        if (part == 0 && threadIdx.x == 0) {
+            to.len[row] = ok && f != -1 ? r.len : 0;
+            if (!ok) report(to.status, TUTTI_EINVAL);
+        }
+        if (!ok || f == -1) return;
+        const int32_t *src = from.block_ids + r.b0;
+        int32_t *dst = to.block_ids + child.b0;
+        for (uint32_t i0 = part * ROW_IDS; i0 < r.held; i0 += per * ROW_IDS) {
+            int32_t id[ROW_IDS / ROW_THREADS];
+#pragma unroll
+            for (uint32_t k = 0; k < ROW_IDS / ROW_THREADS; ++k) {
+                const uint32_t i = i0 + k * ROW_THREADS + threadIdx.x;
+                if (i < r.held) id[k] = src[i];
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < ROW_IDS / ROW_THREADS; ++k) {
+                const uint32_t i = i0 + k * ROW_THREADS + threadIdx.x;
+                if (i < r.held) dst[i] = id[k];
+            }
+        }
+        return;
+    }
+    const uint32_t f = row - to.n_seq;
+    if (!row_view(from, f, r)) {
+        if (part == 0 && threadIdx.x == 0) report(from.status, TUTTI_EINVAL);
+        return;
+    }
+    if (part * ROW_IDS >= r.held) return;
+    int mine = 0;
+    for (uint32_t c = threadIdx.x; c < to.n_seq; c += ROW_THREADS)
+        if (parent[c] == (int32_t)f) mine += row_room(to, c, child) && r.held <= child.room;
+    __shared__ int sums[32];
+    int children;
+    scan(mine, sums, children);
+    const int by = children - (int)(move != 0);
+    if (by == 0) return;
+    for (uint32_t i0 = part * ROW_IDS; i0 < r.held; i0 += per * ROW_IDS)
+#pragma unroll
+        for (uint32_t k = 0; k < ROW_IDS / ROW_THREADS; ++k) {
+            const uint32_t i = i0 + k * ROW_THREADS + threadIdx.x;
+            const int32_t id = i < r.held ? from.block_ids[r.b0 + i] : -1;
+            if (id == -1) continue;
+            if ((uint32_t)id >= p.n_blocks) report(from.status, TUTTI_EFAULT);
+            else if (by > 0) atomicAdd(p.refs + id, by);
+            else drop(p, id, from.status);
+        }
+}
+
+// ---------------------------------------------------------------------------------------------
+// extend: every CTA counts the free blocks of a tile, and the last to arrive does the rest alone: decides which rows
+// copy, ranks the new blocks of all rows by a prefix sum, and goes through the tiles that have the lowest free ones.
+struct Growth {
+    Row r;
+    uint32_t add, more;
+    int32_t tail;                               // the partly filled block that is written to, or -1
+    int32_t count;                              // its count
+    int code;
+};
+__device__ inline Growth growth(const PagesDev &p, const TablesDev &t, const uint32_t *n_new, uint32_t s) {
+    Growth g;
+    g.add = n_new[s];
+    g.tail = -1;
+    g.count = 1;
+    g.more = 0;
+    g.code = TUTTI_EINVAL;
+    if (!row_view(t, s, g.r) || g.add > 0x7fffffffu - g.r.len) return g;
+    const uint32_t after = blocks_of(g.r.len + g.add, t.block_tokens);
+    if (after > g.r.room) return g;
+    if (g.add && g.r.len % t.block_tokens) {
+        const int32_t id = t.block_ids[g.r.b0 + g.r.len / t.block_tokens];
+        if ((uint32_t)id >= p.n_blocks) {
+            g.code = TUTTI_EFAULT;
+            return g;
+        }
+        g.count = p.refs[id];
+        if (g.count <= 0) return g;
+        g.tail = id;
+    }
+    g.more = after - g.r.held;
+    g.code = TUTTI_OK;
+    return g;
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS) extend_kernel(const PagesDev p, const TablesDev t, const uint32_t *n_new, int32_t *pairs) {
+    __shared__ unsigned long long sums[32];
+    __shared__ uint32_t sums32[32], masks[32], first[PLAN_THREADS], ranks[SEARCH];
+    __shared__ bool last;
+    uint32_t n;
+    scan(zeros(tile_counts(p, blockIdx.x, 1)), sums32, n);
+    if (threadIdx.x == 0) {
+        p.tile[blockIdx.x] = n;
+        last = arrive_gpu(p.arrive) == gridDim.x - 1;
+        if (last) *p.arrive = 0;                // ready for the next call
+    }
+    __syncthreads();
+    if (!last) return;
+
+    // Rows that write to a block that others hold: how many, and which is the last.
+    for (uint32_t s = threadIdx.x; s < t.n_seq; s += PLAN_THREADS) {
+        const Growth g = growth(p, t, n_new, s);
+        if (g.code == TUTTI_OK && g.count > 1) {
+            atomicAdd(p.writers + g.tail, 1);
+            atomicMax(p.top + g.tail, s + 1);
+        }
+        if (g.code != TUTTI_OK) report(t.status, g.code);
+    }
+    __syncthreads();
+    // mark: the block that a row copies, -1 none, -2 the row is skipped.  keep_id, keep_count: what a shared block's
+    // count becomes, at the last of its writers.
+    unsigned long long total = 0;
+    for (uint32_t s0 = 0; s0 < t.n_seq; s0 += PLAN_THREADS) {
+        const uint32_t s = s0 + threadIdx.x;
+        Growth g;
+        g.more = 0;
+        bool copies = false, ok = false;
+        if (s < t.n_seq) {
+            g = growth(p, t, n_new, s);
+            ok = g.code == TUTTI_OK;
+            int32_t keep = -1;
+            if (ok && g.count > 1) {
+                const int32_t w = (int32_t)__ldcg(p.writers + g.tail);
+                const bool is_last = __ldcg(p.top + g.tail) == s + 1;
+                copies = !(is_last && w >= g.count);
+                if (is_last) {
+                    keep = g.tail;
+                    p.keep_count[s] = w < g.count ? g.count - w : 1;
+                }
+            }
+            p.keep_id[s] = keep;
+            p.mark[s] = !ok ? -2 : copies ? g.tail : -1;
+        }
+        unsigned long long all;
+        const unsigned long long before = scan<unsigned long long>(ok ? g.more + copies : 0, sums, all);
+        if (s < t.n_seq) {
+            p.begin[s] = (uint32_t)(total + before);
+            if (s < SEARCH) ranks[s] = (uint32_t)(total + before);
+            p.entry[s] = ok ? g.r.b0 + g.r.held - copies : 0;
+        }
+        total += all;
+    }
+    unsigned long long n_free = 0, mine = 0;
+    for (uint32_t i = threadIdx.x; i < p.n_tiles; i += PLAN_THREADS) mine += __ldcg(p.tile + i);
+    scan(mine, sums, n_free);
+    const bool enough = total <= n_free;
+    if (!enough && threadIdx.x == 0) report(t.status, TUTTI_EAGAIN);
+    // The rows' new lengths and counts of the blocks that they shared.
+    for (uint32_t s = threadIdx.x; s < t.n_seq; s += PLAN_THREADS) {
+        const int32_t keep = p.keep_id[s], mark = p.mark[s];
+        if (keep >= 0) p.writers[keep] = p.top[keep] = 0;
+        if (keep >= 0 && enough) p.refs[keep] = p.keep_count[s];
+        if (mark != -2 && enough) t.len[s] += n_new[s];
+        pairs[2 * s] = enough && mark >= 0 ? mark : -1;
+        if (!enough || mark < 0) pairs[2 * s + 1] = -1;
+    }
+    if (!enough) return;
+    __syncthreads();
+    // Block number k of the step's new ones belongs to the last row whose first rank is k or less.
+    auto give = [&](uint32_t k, uint32_t id) {
+        uint32_t lo = 0, len = t.n_seq;
+        while (len > 1) {
+            const uint32_t half = len / 2;
+            const uint32_t b = t.n_seq <= SEARCH ? ranks[lo + half] : p.begin[lo + half];
+            if (b <= k) lo += half, len -= half;
+            else len = half;
+        }
+        const uint32_t j = k - (t.n_seq <= SEARCH ? ranks[lo] : p.begin[lo]);
+        t.block_ids[p.entry[lo] + j] = (int32_t)id;
+        if (j == 0 && p.mark[lo] >= 0) pairs[2 * lo + 1] = (int32_t)id;
+        p.refs[id] = 1;
+    };
+    uint32_t at = 0;                            // free blocks in front of the tiles in hand
+    for (uint32_t t0 = 0; t0 < p.n_tiles && at < total; t0 += PLAN_THREADS) {
+        const uint32_t c = t0 + threadIdx.x < p.n_tiles ? __ldcg(p.tile + t0 + threadIdx.x) : 0;
+        uint32_t in_all;
+        const uint32_t before = at + scan(c, sums32, in_all);
+        first[threadIdx.x] = before;
+        const uint32_t need = __ballot_sync(0xffffffffu, c && before < total);
+        if ((threadIdx.x & 31) == 0) masks[threadIdx.x / 32] = need;
+        __syncthreads();
+        for (uint32_t w = 0; w < PLAN_THREADS / 32; ++w)
+            for (uint32_t m = masks[w]; m; m &= m - 1) {
+                const uint32_t i = w * 32 + __ffs(m) - 1, id = (t0 + i) * TILE + threadIdx.x * 4;
+                const int4 v = tile_counts(p, t0 + i, 1);
+                uint32_t in_tile, k = first[i] + scan(zeros(v), sums32, in_tile);
+                if (v.x == 0 && k < total) give(k, id);
+                k += v.x == 0;
+                if (v.y == 0 && k < total) give(k, id + 1);
+                k += v.y == 0;
+                if (v.z == 0 && k < total) give(k, id + 2);
+                k += v.z == 0;
+                if (v.w == 0 && k < total) give(k, id + 3);
+            }
+        at += in_all;
+        __syncthreads();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// release and trim: `per` CTAs a row.  Release clears a row's length once all its CTAs have read it: the last to
+// say so does it, and the entries are independent of that.
+__global__ void __launch_bounds__(ROW_THREADS) release_kernel(const PagesDev p, const TablesDev t, const uint8_t *which, uint32_t per) {
+    const uint32_t s = blockIdx.x / per, part = blockIdx.x % per;
+    if (which && !which[s]) return;
+    Row r;
+    const bool ok = row_view(t, s, r);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        if (!ok && part == 0) report(t.status, TUTTI_EINVAL);
+        if (ok && (per == 1 || arrive_gpu(p.turn + s) == per - 1)) {
+            if (per > 1) p.turn[s] = 0;
+            t.len[s] = 0;
+        }
+    }
+    if (!ok) return;
+    for (uint32_t i = part * ROW_THREADS + threadIdx.x; i < r.held; i += per * ROW_THREADS) {
+        const int32_t id = t.block_ids[r.b0 + i];
+        if (id == -1) continue;
+        t.block_ids[r.b0 + i] = -1;
+        if ((uint32_t)id >= p.n_blocks) report(t.status, TUTTI_EFAULT);
+        else drop(p, id, t.status);
+    }
+}
+
+__global__ void __launch_bounds__(ROW_THREADS) trim_kernel(const PagesDev p, const TablesDev t, uint32_t window, uint32_t sinks, uint32_t per) {
+    const uint32_t s = blockIdx.x / per, part = blockIdx.x % per;
+    Row r;
+    if (!row_view(t, s, r)) {
+        if (part == 0 && threadIdx.x == 0) report(t.status, TUTTI_EINVAL);
+        return;
+    }
+    if (r.len < window) return;
+    const uint32_t end = (r.len - window + 1) / t.block_tokens;
+    for (uint32_t i = blocks_of(sinks, t.block_tokens) + part * ROW_THREADS + threadIdx.x; i < end; i += per * ROW_THREADS) {
+        const int32_t id = t.block_ids[r.b0 + i];
+        if (id == -1) continue;
+        t.block_ids[r.b0 + i] = -1;
+        if ((uint32_t)id >= p.n_blocks) report(t.status, TUTTI_EFAULT);
+        else drop(p, id, t.status);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// compact, with u(i) the blocks in use below i and n all of them: a free block f < n is the destination
+// number f - u(f), a block in use s >= n is the source number n - 1 - u(s), and there are n - u(n) of each.
+__global__ void __launch_bounds__(PLAN_THREADS) compact_count_kernel(const PagesDev p) {
+    __shared__ uint32_t sums[32];
+    uint32_t n;
+    scan(4 - zeros(tile_counts(p, blockIdx.x, 0)), sums, n);
+    if (threadIdx.x == 0) p.tile[blockIdx.x] = n;
+}
+
+__global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesDev p, int32_t *pairs, uint32_t max_pairs) {
+    __shared__ uint32_t sums[32];
+    uint32_t low = 0, all = 0, n, u, ignored;
+    for (uint32_t i = threadIdx.x; i < p.n_tiles; i += PLAN_THREADS) {
+        const uint32_t c = p.tile[i];
+        all += c;
+        if (i < blockIdx.x) low += c;
+    }
+    scan(all, sums, n);
+    scan(low, sums, u);
+    const int4 v = tile_counts(p, blockIdx.x, 0);
+    u += scan(4 - zeros(v), sums, ignored);
+    if (n == p.n_blocks && blockIdx.x == 0 && threadIdx.x == 0) *p.moves = 0;
+    const int count[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (uint32_t k = 0; k < 4; ++k) {
+        const uint32_t id = blockIdx.x * TILE + threadIdx.x * 4 + k;
+        if (id >= p.n_blocks) break;
+        if (id == n) *p.moves = n - u;
+        const bool used = count[k] != 0;
+        if (used && id >= n) {
+            const uint32_t r = n - 1 - u;
+            p.rank[id] = r;
+            if (r < max_pairs) pairs[2 * (uint64_t)r] = (int32_t)id;
+        } else if (!used && id < n) {
+            const uint32_t r = id - u;
+            if (r < max_pairs) pairs[2 * (uint64_t)r + 1] = (int32_t)id;
+        }
+        u += used;
+    }
+}
+
+__global__ void __launch_bounds__(ROW_THREADS) compact_apply_kernel(const PagesDev p, const TablesDev t, int32_t *pairs, uint32_t max_pairs, uint32_t *n_pairs, uint32_t per) {
+    const uint32_t n = min(*p.moves, max_pairs);
+    if (blockIdx.x >= per * t.n_seq) {          // the counts, and the pairs behind the last
+        const uint32_t first = blockIdx.x - per * t.n_seq, ctas = gridDim.x - per * t.n_seq;
+        if (first == 0 && threadIdx.x == 0) *n_pairs = n;
+        for (uint64_t r = first * ROW_THREADS + threadIdx.x; r < max_pairs; r += (uint64_t)ctas * ROW_THREADS) {
+            int2 *pair = reinterpret_cast<int2 *>(pairs) + r;
+            if (r >= n) {
+                *pair = make_int2(-1, -1);
+                continue;
+            }
+            const int2 m = *pair;
+            p.refs[m.y] = p.refs[m.x];
+            p.refs[m.x] = 0;
+        }
+        return;
+    }
+    const uint32_t s = blockIdx.x / per, part = blockIdx.x % per;
+    Row r;
+    if (!row_view(t, s, r)) {
+        if (part == 0 && threadIdx.x == 0) report(t.status, TUTTI_EINVAL);
+        return;
+    }
+    for (uint32_t i = part * ROW_THREADS + threadIdx.x; i < r.held; i += per * ROW_THREADS) {
+        const int32_t id = t.block_ids[r.b0 + i];
+        if (id == -1) continue;
+        if ((uint32_t)id >= p.n_blocks) {
+            report(t.status, TUTTI_EFAULT);
+            continue;
+        }
+        const uint32_t k = p.rank[id];          // of a block that does not move: of an earlier call, or none
+        if (k < n && pairs[2 * (uint64_t)k] == id) t.block_ids[r.b0 + i] = pairs[2 * (uint64_t)k + 1];
+    }
+}
+
+// CTAs a row, so that rows of average room are done in about one round and the GPU is filled a few times at most.
+uint32_t ctas_a_row(uint32_t n_seq, uint32_t n_blk, uint32_t ids, int sms) {
+    const uint32_t most = (uint32_t)sms * 8 / n_seq + 1, want = n_blk / n_seq / ids + 1;
+    return most < want ? most : want;
+}
+
+}  // namespace
+
+}  // namespace tutti
+
+using namespace tutti;
+
+struct tutti_pages {
+    tutti_ctx *ctx;
+    int device;
+    PagesDev dev;
+    uint32_t *memory;
+};
+
+namespace {
+
+int check_tables(const tutti_tables_t *t) {
+    if (!t || t->n_seq > TUTTI_PAGES_MAX_SEQ || t->n_blk > 0x7fffffffu) return TUTTI_EINVAL;
+    if (t->n_seq && (!t->blk_start || !t->len)) return TUTTI_EINVAL;
+    if (t->n_blk && !t->block_ids) return TUTTI_EINVAL;
+    if (((uint64_t)t->blk_start | (uint64_t)t->block_ids | (uint64_t)t->len | (uint64_t)t->status) & 3) return TUTTI_EINVAL;
+    return TUTTI_OK;
+}
+
+TablesDev on_device(const tutti_pages *pages, const tutti_tables_t *t) {
+    return TablesDev{t->n_seq, t->n_blk, tutti_ctx_geom_(pages->ctx)->block_tokens, t->blk_start, t->block_ids, t->len, t->status};
+}
+
+}  // namespace
+
+extern "C" {
+
+// What the calls refuse, from the arguments alone.
+int tutti_fork_check_(const tutti_tables_t *from, const int32_t *parent, const tutti_tables_t *to, uint32_t move) {
+    if (check_tables(from) || check_tables(to) || move > TUTTI_FORK_MOVE) return TUTTI_EINVAL;
+    if (to->n_seq && (!parent || ((uint64_t)parent & 3))) return TUTTI_EINVAL;
+    if ((from->block_ids && from->block_ids == to->block_ids) || (from->len && from->len == to->len)) return TUTTI_EINVAL;
+    return TUTTI_OK;
+}
+int tutti_extend_check_(const tutti_tables_t *t, const uint32_t *n_new, const int32_t *pairs) {
+    if (check_tables(t) || (t->n_seq && (!n_new || !pairs)) || (((uint64_t)n_new | (uint64_t)pairs) & 3)) return TUTTI_EINVAL;
+    return TUTTI_OK;
+}
+int tutti_compact_check_(const tutti_tables_t *t, const int32_t *pairs, uint32_t max_pairs, const uint32_t *n_pairs) {
+    if (check_tables(t) || !n_pairs || ((uint64_t)n_pairs & 3) || max_pairs > 0x7fffffffu) return TUTTI_EINVAL;
+    if (max_pairs && (!pairs || ((uint64_t)pairs & 7))) return TUTTI_EINVAL;
+    return TUTTI_OK;
+}
+int tutti_tables_check_(const tutti_tables_t *t) { return check_tables(t); }
+
+int tutti_pages_create(tutti_ctx_t *ctx, int32_t *refs, uint64_t n_blocks, tutti_pages_t **out) {
+    if (!ctx || !refs || ((uint64_t)refs & 15) || !n_blocks || n_blocks > 0x7fffffffull || !out) return TUTTI_EINVAL;
+    OnDevice on(tutti_ctx_device_(ctx));
+    if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
+    tutti_pages *p = new (std::nothrow) tutti_pages();
+    if (!p) return TUTTI_ENOMEM;
+    const uint32_t tiles = (uint32_t)((n_blocks + TILE - 1) / TILE);
+    const size_t words = 32 + (size_t)tiles + 3 * n_blocks + 6 * (size_t)TUTTI_PAGES_MAX_SEQ;
+    cudaError_t e = cudaMalloc((void **)&p->memory, words * 4);
+    if (e == cudaSuccess && ((e = cudaMemset(p->memory, 0, words * 4)) != cudaSuccess || (e = cudaDeviceSynchronize()) != cudaSuccess))
+        cudaFree(p->memory);
+    if (e != cudaSuccess) {
+        delete p;
+        fail(e, "workspace of the pages");
+        return TUTTI_ENOMEM;
+    }
+    p->ctx = ctx;
+    p->device = tutti_ctx_device_(ctx);
+    PagesDev &d = p->dev;
+    d.refs = refs;
+    d.n_blocks = (uint32_t)n_blocks;
+    d.n_tiles = tiles;
+    d.arrive = p->memory;
+    d.moves = p->memory + 1;
+    uint32_t *at = p->memory + 32;
+    auto take = [&](size_t n) {
+        uint32_t *a = at;
+        at += n;
+        return a;
+    };
+    d.turn = take(TUTTI_PAGES_MAX_SEQ);
+    d.begin = take(TUTTI_PAGES_MAX_SEQ);
+    d.entry = take(TUTTI_PAGES_MAX_SEQ);
+    d.mark = (int32_t *)take(TUTTI_PAGES_MAX_SEQ);
+    d.keep_id = (int32_t *)take(TUTTI_PAGES_MAX_SEQ);
+    d.keep_count = (int32_t *)take(TUTTI_PAGES_MAX_SEQ);
+    d.tile = take(tiles);
+    d.writers = take(n_blocks);
+    d.top = take(n_blocks);
+    d.rank = take(n_blocks);
+    *out = p;
+    return TUTTI_OK;
+}
+
+int tutti_pages_destroy(tutti_pages_t *p) {
+    if (!p) return TUTTI_EINVAL;
+    OnDevice on(p->device);
+    cudaDeviceSynchronize();
+    cudaFree(p->memory);
+    delete p;
+    return TUTTI_OK;
+}
+
+int tutti_pages_fork(tutti_pages_t *pages, const tutti_tables_t *from, const int32_t *parent, const tutti_tables_t *to, uint32_t move, void *stream) {
+    if (!pages) return TUTTI_EINVAL;
+    if (int rc = tutti_fork_check_(from, parent, to, move)) return rc;
+    const uint32_t rows = from->n_seq + to->n_seq;
+    if (!rows) return TUTTI_OK;
+    OnDevice on(pages->device);
+    if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
+    const uint32_t per = ctas_a_row(rows, from->n_blk / 2 + to->n_blk / 2, ROW_IDS, tutti_ctx_sms_(pages->ctx));
+    const cudaError_t e = launch_plain(fork_kernel, per * rows, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, from), parent, on_device(pages, to), move, per);
+    return e == cudaSuccess ? TUTTI_OK : fail(e, "fork launch");
+}
+
+int tutti_pages_extend(tutti_pages_t *pages, const tutti_tables_t *t, const uint32_t *n_new, int32_t *pairs, void *stream) {
+    if (!pages) return TUTTI_EINVAL;
+    if (int rc = tutti_extend_check_(t, n_new, pairs)) return rc;
+    if (!t->n_seq) return TUTTI_OK;
+    OnDevice on(pages->device);
+    if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
+    const cudaError_t e = launch_plain(extend_kernel, pages->dev.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), n_new, pairs);
+    return e == cudaSuccess ? TUTTI_OK : fail(e, "extend launch");
+}
+
+int tutti_pages_release(tutti_pages_t *pages, const tutti_tables_t *t, const uint8_t *which, void *stream) {
+    if (!pages) return TUTTI_EINVAL;
+    if (int rc = check_tables(t)) return rc;
+    if (!t->n_seq) return TUTTI_OK;
+    OnDevice on(pages->device);
+    if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
+    const uint32_t per = ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, tutti_ctx_sms_(pages->ctx));
+    const cudaError_t e = launch_plain(release_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), which, per);
+    return e == cudaSuccess ? TUTTI_OK : fail(e, "release launch");
+}
+
+int tutti_pages_trim(tutti_pages_t *pages, const tutti_tables_t *t, const tutti_window_t *window, void *stream) {
+    if (!pages) return TUTTI_EINVAL;
+    if (int rc = check_tables(t)) return rc;
+    if (int rc = tutti_window_check_(window)) return rc;
+    if (!t->n_seq) return TUTTI_OK;
+    OnDevice on(pages->device);
+    if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
+    const uint32_t per = ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, tutti_ctx_sms_(pages->ctx));
+    const cudaError_t e = launch_plain(trim_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), window->window, window->sinks, per);
+    return e == cudaSuccess ? TUTTI_OK : fail(e, "trim launch");
+}
+
+int tutti_pages_compact(tutti_pages_t *pages, const tutti_tables_t *t, int32_t *pairs, uint32_t max_pairs, uint32_t *n_pairs, void *stream) {
+    if (!pages) return TUTTI_EINVAL;
+    if (int rc = tutti_compact_check_(t, pairs, max_pairs, n_pairs)) return rc;
+    OnDevice on(pages->device);
+    if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
+    const PagesDev &d = pages->dev;
+    const int sms = tutti_ctx_sms_(pages->ctx);
+    const uint32_t per = t->n_seq ? ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, sms) : 1;
+    const uint32_t movers = max_pairs / ROW_THREADS + 1 < (uint32_t)sms ? max_pairs / ROW_THREADS + 1 : (uint32_t)sms;
+    cudaError_t e = launch_plain(compact_count_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d);
+    if (e == cudaSuccess) e = launch_plain(compact_plan_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d, pairs, max_pairs);
+    if (e == cudaSuccess) e = launch_plain(compact_apply_kernel, per * t->n_seq + movers, ROW_THREADS, 0, (cudaStream_t)stream, d, on_device(pages, t), pairs, max_pairs, n_pairs, per);
+    return e == cudaSuccess ? TUTTI_OK : fail(e, "compact launch");
+}
+
+}  // extern "C"

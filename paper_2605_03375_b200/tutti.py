@@ -26,6 +26,8 @@ OP_FLAG_HND = 0x100
 ENGINE_AUTO, ENGINE_LDST, ENGINE_BULK = 0, 1, 2
 DTYPE_BF16, DTYPE_FP16 = 0, 1
 ROPE_HALF, ROPE_PAIRS = 0, 1
+FORK_KEEP, FORK_MOVE = 0, 1
+PAGES_MAX_SEQ = 65536
 
 
 class Geom(C.Structure):
@@ -74,6 +76,16 @@ class Attend(C.Structure):
     _of = None                              # (head_dim, tokens, their GPU, the tensors)
 
 
+class Window(C.Structure):
+    _fields_ = [("window", C.c_uint32), ("sinks", C.c_uint32)]
+
+
+class Tables(C.Structure):
+    _fields_ = [("n_seq", C.c_uint32), ("n_blk", C.c_uint32), ("blk_start", C.c_void_p),
+                ("block_ids", C.c_void_p), ("len", C.c_void_p), ("status", C.c_void_p)]
+    _at, _keep = None, ()                   # of a struct over tensors: their GPU (-1: not one), the tensors
+
+
 class Cqe(C.Structure):
     _fields_ = [("iocb_idx", C.c_uint32), ("status", C.c_int32), ("bytes", C.c_uint64)]
 
@@ -113,7 +125,8 @@ EXPORTS = [
     "tutti_ring_set_iocb_bytes", "tutti_sched_profile",
     "tutti_stage_plan", "tutti_stage_copy_layer", "tutti_build_sqes_staged",
     "tutti_scales_register", "tutti_scales_register_rows", "tutti_kv_append_layer", "tutti_attn_create", "tutti_attn_destroy",
-    "tutti_kv_attend_layer",
+    "tutti_kv_attend_layer", "tutti_kv_attend_window_layer", "tutti_pages_create", "tutti_pages_destroy", "tutti_pages_fork",
+    "tutti_pages_extend", "tutti_pages_release", "tutti_pages_trim", "tutti_pages_compact", "tutti_kv_copy_blocks",
 ]
 
 _lib: Optional[C.CDLL] = None
@@ -192,6 +205,15 @@ def load(path: Optional[str] = None) -> C.CDLL:
         "tutti_attn_create": (C.c_int, [vp, P(vp)]),
         "tutti_attn_destroy": (C.c_int, [vp]),
         "tutti_kv_attend_layer": (C.c_int, [vp, u32, P(Step), P(Attend), vp]),
+        "tutti_kv_attend_window_layer": (C.c_int, [vp, u32, P(Step), P(Attend), P(Window), vp]),
+        "tutti_pages_create": (C.c_int, [vp, vp, u64, P(vp)]),
+        "tutti_pages_destroy": (C.c_int, [vp]),
+        "tutti_pages_fork": (C.c_int, [vp, P(Tables), vp, P(Tables), u32, vp]),
+        "tutti_pages_extend": (C.c_int, [vp, P(Tables), vp, vp, vp]),
+        "tutti_pages_release": (C.c_int, [vp, P(Tables), vp, vp]),
+        "tutti_pages_trim": (C.c_int, [vp, P(Tables), P(Window), vp]),
+        "tutti_pages_compact": (C.c_int, [vp, P(Tables), vp, u32, vp, vp]),
+        "tutti_kv_copy_blocks": (C.c_int, [vp, u32, u32, vp, u32, vp, vp, vp]),
         "tutti_kv_restore_layer_noalloc": (C.c_int, [P(Geom), C.c_int, u32, P(Batch), vp, vp, u64,
                                                      u64, P(vp), P(u64), vp, vp]),
     }
@@ -297,6 +319,18 @@ class Context:
                                             None if stream is None else _stream_ptr(stream))
         return rc if rc == OK else _check(rc, "tutti_kv_append_layer", allow)
 
+    def tutti_kv_copy_blocks(self, first_layer: int, n_layers: int, pairs, n_pairs=None, status=None, stream=None,
+                             allow: Sequence[int] = ()) -> int:
+        """Copy blocks (and scales) inside the layers' pools: `pairs` [n, 2] int32, from and to, as tutti_pages_extend and
+        tutti_pages_compact leave them; n_pairs (int32) is how many of them count, on the device."""
+        at = self.device
+        if len(pairs.shape) != 2 or pairs.shape[1] != 2:
+            raise TuttiError(EINVAL, "tutti_kv_copy_blocks: pairs are not [n, 2]")
+        rc = self.lib.tutti_kv_copy_blocks(self.h, first_layer, n_layers, _ints(pairs, at, "pairs"), pairs.shape[0],
+                                           None if n_pairs is None else _ints(n_pairs, at, "n_pairs", 1),
+                                           None if status is None else _ints(status, at, "status", 1), None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_kv_copy_blocks", allow)
+
     def tutti_set_option(self, option: int, value: int):
         _check(self.lib.tutti_set_option(self.h, option, value), "tutti_set_option")
 
@@ -370,6 +404,49 @@ def make_step(q_start, ctx_len, blk_start, block_ids, n_tok: int, max_new: int, 
     if any(t.get_device() != s._at for t in held):
         s._at = -1
     return s
+
+
+_INT32 = set()                              # torch.int32 and torch.uint32, once seen
+
+
+def _ints(t, device: int, what: str, least: int = 0) -> int:
+    """Address of a contiguous int32 tensor of `least` elements or more that the context's GPU reaches."""
+    if t.dtype not in _INT32:
+        if str(t.dtype) not in ("torch.int32", "torch.uint32"):
+            raise TuttiError(EINVAL, f"{what} (int32)")
+        _INT32.add(t.dtype)
+    if not t.is_contiguous() or t.numel() < least:
+        raise TuttiError(EINVAL, f"{what} (contiguous, {least} elements or more)")
+    if t.get_device() != device:
+        _reachable(device, (t,))
+    return t.data_ptr()
+
+
+def make_window(window: int, sinks: int = 0) -> Window:
+    """A row sees the last `window` keys, its own included, and the first `sinks` of its sequence."""
+    if not (0 < window < 1 << 31 and 0 <= sinks < 1 << 31):
+        raise TuttiError(EINVAL, "window (1 or more) and sinks (0 or more)")
+    return Window(window, sinks)
+
+
+def make_tables(blk_start, block_ids, length, status=None) -> Tables:
+    """Tables struct over device tensors (int32): rows of block ids and their tokens.  Keeps the tensors alive."""
+    n_seq = int(length.numel())
+    if any(str(t.dtype) not in ("torch.int32", "torch.uint32") or not t.is_contiguous() for t in (blk_start, block_ids, length)):
+        raise TuttiError(EINVAL, "tables (int32, contiguous)")
+    if n_seq and blk_start.numel() <= n_seq:
+        raise TuttiError(EINVAL, "tables (blk_start has an entry more than length)")
+    held = blk_start, block_ids, length
+    if status is not None:
+        if str(status.dtype) != "torch.int32" or not status.numel():
+            raise TuttiError(EINVAL, "status (int32)")
+        held += (status,)
+    t = Tables(n_seq, int(block_ids.numel()), blk_start.data_ptr(), block_ids.data_ptr(), length.data_ptr(),
+               None if status is None else status.data_ptr())
+    t._at, t._keep = held[0].get_device(), held
+    if any(x.get_device() != t._at for x in held):
+        t._at = -1
+    return t
 
 
 def _rows(t, dtype, dim: int) -> int:
@@ -466,26 +543,96 @@ class Attn:
             self.lib.tutti_attn_destroy(self.h)
             self.h = None
 
+    def _compare(self, step: Step, io: Attend, what: str):
+        ctx = self.ctx
+        if ctx.h is None or self.h is None:
+            raise TuttiError(EINVAL, f"{what}: the handle or its context is closed")
+        at, of = ctx.device, io._of
+        if of is not None:
+            dim, rows, dev, held = of
+            if dim != ctx._row[1] or rows < step.n_tok:
+                raise TuttiError(EINVAL, f"{what}: queries are not [n_tok or more, heads, head_dim]")
+            if dev != at:
+                _reachable(at, held)
+        if step._at != at:
+            _reachable(at, step._keep)
+
     def tutti_kv_attend_layer(self, layer: int, step: Step, io: Attend, scale: float, stream=None,
                               allow: Sequence[int] = ()) -> int:
         """Causal attention of the step's queries over the pool layer.  stream None is the legacy default
         stream, not torch's current one.  Structs over tensors (make_step, make_attend) are compared with each other and
         with the geometry."""
-        ctx = self.ctx
-        if ctx.h is None or self.h is None:
-            raise TuttiError(EINVAL, "tutti_kv_attend_layer: the handle or its context is closed")
-        at, of = ctx.device, io._of
-        if of is not None:
-            dim, rows, dev, held = of
-            if dim != ctx._row[1] or rows < step.n_tok:
-                raise TuttiError(EINVAL, "tutti_kv_attend_layer: queries are not [n_tok or more, heads, head_dim]")
-            if dev != at:
-                _reachable(at, held)
-        if step._at != at:
-            _reachable(at, step._keep)
+        self._compare(step, io, "tutti_kv_attend_layer")
         io.scale = scale
         rc = self.lib.tutti_kv_attend_layer(self.h, layer, step, io, None if stream is None else _stream_ptr(stream))
         return rc if rc == OK else _check(rc, "tutti_kv_attend_layer", allow)
+
+    def tutti_kv_attend_window_layer(self, layer: int, step: Step, io: Attend, scale: float, window: Window, stream=None,
+                                     allow: Sequence[int] = ()) -> int:
+        """The same with a window (make_window): a row sees its last keys and the sequence's first ones."""
+        self._compare(step, io, "tutti_kv_attend_window_layer")
+        io.scale = scale
+        rc = self.lib.tutti_kv_attend_window_layer(self.h, layer, step, io, window, None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_kv_attend_window_layer", allow)
+
+
+class Pages:
+    """tutti_pages_t: the rows of block tables and the counts `refs` (int32, a block each, on the context's GPU) of a pool."""
+
+    def __init__(self, ctx: Context, refs):
+        self.ctx = ctx
+        self.lib = ctx.lib
+        self.h = None
+        at = _ints(refs, ctx.device, "refs", 1)
+        h = C.c_void_p()
+        _check(self.lib.tutti_pages_create(ctx.h, at, refs.numel(), C.byref(h)), "tutti_pages_create")
+        self.h, self.refs = h, refs
+
+    def close(self):
+        if self.h:
+            self.lib.tutti_pages_destroy(self.h)
+            self.h = None
+
+    def _call(self, name: str, tables: Sequence[Tables], args, stream, allow: Sequence[int]) -> int:
+        at = self.ctx.device
+        if self.h is None or self.ctx.h is None:
+            raise TuttiError(EINVAL, f"{name}: the handle or its context is closed")
+        for t in tables:
+            if t._at != at:
+                _reachable(at, t._keep)
+        rc = getattr(self.lib, name)(self.h, *args, None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, name, allow)
+
+    def tutti_pages_fork(self, frm: Tables, parent, to: Tables, move: int = FORK_KEEP, stream=None, allow: Sequence[int] = ()) -> int:
+        """Row s of `to` becomes row parent[s] (int32; -1: empty) of `frm`; FORK_MOVE gives up the rows of `frm`."""
+        return self._call("tutti_pages_fork", (frm, to), (frm, _ints(parent, self.ctx.device, "parent", to.n_seq), to, move), stream, allow)
+
+    def tutti_pages_extend(self, tables: Tables, n_new, pairs, stream=None, allow: Sequence[int] = ()) -> int:
+        """Room for n_new[s] (int32) more tokens of every row; pairs [rows, 2] int32 receives the blocks to copy."""
+        at = self.ctx.device
+        return self._call("tutti_pages_extend", (tables,), (tables, _ints(n_new, at, "n_new", tables.n_seq), _ints(pairs, at, "pairs", 2 * tables.n_seq)), stream, allow)
+
+    def tutti_pages_release(self, tables: Tables, which=None, stream=None, allow: Sequence[int] = ()) -> int:
+        """Free the rows with which[s] (bool or uint8), or all of them."""
+        flags = None
+        if which is not None:
+            if str(which.dtype) not in ("torch.bool", "torch.uint8") or not which.is_contiguous() or which.numel() < tables.n_seq:
+                raise TuttiError(EINVAL, "which (bool or uint8, contiguous, an element a row)")
+            if which.get_device() != self.ctx.device:
+                _reachable(self.ctx.device, (which,))
+            flags = which.data_ptr()
+        return self._call("tutti_pages_release", (tables,), (tables, flags), stream, allow)
+
+    def tutti_pages_trim(self, tables: Tables, window: Window, stream=None, allow: Sequence[int] = ()) -> int:
+        """Free the blocks that no later row sees under the window."""
+        return self._call("tutti_pages_trim", (tables,), (tables, window), stream, allow)
+
+    def tutti_pages_compact(self, tables: Tables, pairs, n_pairs, stream=None, allow: Sequence[int] = ()) -> int:
+        """Move blocks in use to the lowest ids, at most len(pairs); pairs [n, 2] and n_pairs [1] (int32) receive the moves."""
+        at = self.ctx.device
+        if len(pairs.shape) != 2 or pairs.shape[1] != 2:
+            raise TuttiError(EINVAL, "tutti_pages_compact: pairs are not [n, 2]")
+        return self._call("tutti_pages_compact", (tables,), (tables, _ints(pairs, at, "pairs"), pairs.shape[0], _ints(n_pairs, at, "n_pairs", 1)), stream, allow)
 
 
 class Ring:
