@@ -696,7 +696,7 @@ int tutti_pages_fork(tutti_pages_t *pages, const tutti_tables_t *from, const int
  * are -1.  Of the rows that share the block they write to, the last one keeps it if nobody else holds it.
  * All rows or none: with too few free blocks nothing changes, all pairs are -1 and *status is TUTTI_EAGAIN.
  * A row is skipped (TUTTI_EINVAL) that has no room for its blocks or passes 2^31 - 1 tokens, or whose written block has a count below 1;
- * TUTTI_EFAULT, and skipped, if that block is outside the pool or -1.
+ * TUTTI_EFAULT, and skipped, if that block is outside the pool (an entry of -1 is no block: there is nothing to copy).
  */
 int tutti_pages_extend(tutti_pages_t *pages, const tutti_tables_t *tables, const uint32_t *n_new,
                        int32_t *pairs, void *stream);

@@ -172,6 +172,22 @@ inline cudaError_t launch_plain(void (*kernel)(KArgs...), uint32_t grid, uint32_
     cfg.stream = stream;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
+// The same for kernels that begin with griddepcontrol.wait: they become resident while the kernel in front of them in the
+// stream is still running, if that one lets them.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_behind(void (*kernel)(KArgs...), uint32_t grid, uint32_t block, size_t smem, cudaStream_t stream, const Args &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 // Makes a device current for a scope.
 struct OnDevice {

@@ -12,7 +12,9 @@ constexpr uint32_t PLAN_THREADS = 1024;
 constexpr uint32_t TILE = 4 * PLAN_THREADS;     // counts that a CTA looks at in one round
 constexpr uint32_t ROW_THREADS = 256;
 constexpr uint32_t ROW_IDS = 8 * ROW_THREADS;   // ids of a row that a CTA takes at once
+constexpr uint32_t GROUP = 16;                  // old rows whose counts a CTA of fork changes together
 constexpr uint32_t SEARCH = 4096;               // rows whose first ranks fit in shared memory
+constexpr uint32_t SMALL = 16;                  // tiles that every CTA of a compaction counts by itself
 
 struct TablesDev {
     uint32_t n_seq, n_blk, block_tokens;
@@ -26,14 +28,15 @@ struct TablesDev {
 struct PagesDev {
     int32_t *refs;
     uint32_t n_blocks, n_tiles;
-    uint32_t *arrive;                           // CTAs of extend that have counted
+    uint32_t *arrive;                           // CTAs of extend that are done
     uint32_t *turn;                             // [max rows] CTAs of release that have read a row's length
     uint32_t *tile;                             // [n_tiles] free blocks, or blocks in use
     uint32_t *moves;                            // of a compaction
+    unsigned long long *total;                  // new blocks of an extension
     uint32_t *writers, *top;                    // [n_blocks] rows that write to a shared block, and the last of them + 1
-    uint32_t *rank;                             // [n_blocks] a moved block's number
+    uint32_t *rank;                             // [n_blocks] a moved block's number; free blocks of extend, from each tile's start on
     uint32_t *begin, *entry;                    // [max rows] rank of a row's first new block, and where it goes
-    int32_t *mark, *keep_id, *keep_count;       // [max rows] see extend_kernel
+    int32_t *mark, *keep_id, *keep_count;       // [max rows] see plan_rows
 };
 
 __device__ inline void report(int32_t *status, int code) {
@@ -107,11 +110,19 @@ __device__ inline int4 tile_counts(const PagesDev &p, uint32_t tile, int none) {
 }
 __device__ inline uint32_t zeros(const int4 &v) { return (v.x == 0) + (v.y == 0) + (v.z == 0) + (v.w == 0); }
 
+// Every kernel here may be resident before the one in front of it in the stream has ended, and waits for it first.
+__device__ inline void after_predecessor() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // ---------------------------------------------------------------------------------------------
 // fork: CTAs [0, per * to.n_seq) copy the entries of the new rows, the ones behind change the counts of the old
-// rows' blocks, by as many as a row has children (less the row itself, where it is given up): a row with one
-// child that takes its place costs no atomics at all, and that is most of them.
-__global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, const TablesDev from, const int32_t *parent, const TablesDev to, uint32_t move, uint32_t per) {
+// rows' blocks, by as many as a row has children (less the row itself, where it is given up).  A CTA takes GROUP
+// old rows together and adds up what neighbours that hold the same block at the same place do to its count: the beams of
+// a request share their prompt, and what one loses there another gains, so that most blocks need no atomic at all.
+__global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, const TablesDev from, const int32_t *parent, const TablesDev to, uint32_t move, uint32_t per, uint32_t segs) {
+    after_predecessor();
     const uint32_t row = blockIdx.x / per, part = blockIdx.x % per;
     Row r, child;
     if (row < to.n_seq) {
@@ -140,35 +151,61 @@ __global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, con
         }
         return;
     }
-    const uint32_t f = row - to.n_seq;
-    if (!row_view(from, f, r)) {
-        if (part == 0 && threadIdx.x == 0) report(from.status, TUTTI_EINVAL);
-        return;
+    __shared__ uint32_t first[GROUP], held[GROUP], longest;
+    __shared__ int by[GROUP];
+    const uint32_t g = blockIdx.x - per * to.n_seq, f0 = g % ((from.n_seq + GROUP - 1) / GROUP) * GROUP, seg = g / ((from.n_seq + GROUP - 1) / GROUP);
+    if (threadIdx.x == 0) longest = 0;
+    __syncthreads();
+    if (threadIdx.x < GROUP) {
+        const uint32_t f = f0 + threadIdx.x;
+        const bool there = f < from.n_seq, ok = there && row_view(from, f, r);
+        if (there && !ok && seg == 0) report(from.status, TUTTI_EINVAL);
+        first[threadIdx.x] = ok ? r.b0 : 0;
+        held[threadIdx.x] = ok ? r.held : 0;
+        by[threadIdx.x] = move ? -1 : 0;
+        if (ok) atomicMax(&longest, r.held);
     }
-    if (part * ROW_IDS >= r.held) return;
-    int mine = 0;
-    for (uint32_t c = threadIdx.x; c < to.n_seq; c += ROW_THREADS)
-        if (parent[c] == (int32_t)f) mine += row_room(to, c, child) && r.held <= child.room;
-    __shared__ int sums[32];
-    int children;
-    scan(mine, sums, children);
-    const int by = children - (int)(move != 0);
-    if (by == 0) return;
-    for (uint32_t i0 = part * ROW_IDS; i0 < r.held; i0 += per * ROW_IDS)
+    __syncthreads();
+    if (seg * ROW_THREADS >= longest) return;
+    for (uint32_t c = threadIdx.x; c < to.n_seq; c += ROW_THREADS) {
+        const uint32_t k = (uint32_t)parent[c] - f0;
+        if (k < GROUP && row_room(to, c, child) && held[k] <= child.room) atomicAdd(by + k, 1);
+    }
+    __syncthreads();
+    for (uint32_t i = seg * ROW_THREADS + threadIdx.x; i < longest; i += segs * ROW_THREADS) {
+        int32_t id[GROUP];
 #pragma unroll
-        for (uint32_t k = 0; k < ROW_IDS / ROW_THREADS; ++k) {
-            const uint32_t i = i0 + k * ROW_THREADS + threadIdx.x;
-            const int32_t id = i < r.held ? from.block_ids[r.b0 + i] : -1;
-            if (id == -1) continue;
-            if ((uint32_t)id >= p.n_blocks) report(from.status, TUTTI_EFAULT);
-            else if (by > 0) atomicAdd(p.refs + id, by);
-            else drop(p, id, from.status);
+        for (uint32_t k = 0; k < GROUP; ++k) id[k] = i < held[k] ? from.block_ids[first[k] + i] : -1;
+        int32_t run = -1;
+        int sum = 0;
+        auto flush = [&]() {
+            if (run == -1 || sum == 0) return;
+            if ((uint32_t)run >= p.n_blocks) {
+                report(from.status, TUTTI_EFAULT);
+                return;
+            }
+            const int now = atomicAdd(p.refs + run, sum) + sum;
+            if (now < 0) {                      // a count does not pass 0
+                atomicAdd(p.refs + run, -now);
+                report(from.status, TUTTI_EINVAL);
+            }
+        };
+#pragma unroll
+        for (uint32_t k = 0; k < GROUP; ++k) {
+            if (id[k] != run) {
+                flush();
+                run = id[k];
+                sum = 0;
+            }
+            sum += by[k];
         }
+        flush();
+    }
 }
 
 // ---------------------------------------------------------------------------------------------
-// extend: every CTA counts the free blocks of a tile, and the last to arrive does the rest alone: decides which rows
-// copy, ranks the new blocks of all rows by a prefix sum, and goes through the tiles that have the lowest free ones.
+// extend: CTA 0 decides which rows copy and ranks the new blocks of all rows by a prefix sum, the others count the free
+// blocks of a tile each and list them; the last to arrive gives block number k to its row.
 struct Growth {
     Row r;
     uint32_t add, more;
@@ -188,76 +225,115 @@ __device__ inline Growth growth(const PagesDev &p, const TablesDev &t, const uin
     if (after > g.r.room) return g;
     if (g.add && g.r.len % t.block_tokens) {
         const int32_t id = t.block_ids[g.r.b0 + g.r.len / t.block_tokens];
-        if ((uint32_t)id >= p.n_blocks) {
-            g.code = TUTTI_EFAULT;
-            return g;
+        if (id != -1) {
+            if ((uint32_t)id >= p.n_blocks) {
+                g.code = TUTTI_EFAULT;
+                return g;
+            }
+            g.count = p.refs[id];
+            if (g.count <= 0) return g;
+            g.tail = id;
         }
-        g.count = p.refs[id];
-        if (g.count <= 0) return g;
-        g.tail = id;
     }
     g.more = after - g.r.held;
     g.code = TUTTI_OK;
     return g;
 }
 
+// mark: the block that a row copies, -1 none, -2 the row is skipped.  keep_id, keep_count: what a shared block's
+// count becomes, at the last of its writers.
+__device__ void plan_rows(const PagesDev &p, const TablesDev &t, const uint32_t *n_new, unsigned long long *sums) {
+    Growth own;                                 // the thread's last row (its only one, mostly)
+    uint32_t own_s = ~0u;
+    auto look = [&](uint32_t s) {
+        if (s != own_s) own = growth(p, t, n_new, s);
+        own_s = s;
+    };
+    // Rows that write to a block that others hold: how many, and which is the last.
+    bool shares = false;
+    for (uint32_t s = threadIdx.x; s < t.n_seq; s += PLAN_THREADS) {
+        look(s);
+        if (own.code != TUTTI_OK) report(t.status, own.code);
+        else if (own.count > 1) {
+            atomicAdd(p.writers + own.tail, 1);
+            atomicMax(p.top + own.tail, s + 1);
+            shares = true;
+        }
+    }
+    shares = __syncthreads_or(shares);
+    unsigned long long total = 0;
+    for (uint32_t s0 = 0; s0 < t.n_seq; s0 += PLAN_THREADS) {
+        const uint32_t s = s0 + threadIdx.x;
+        bool copies = false, ok = false;
+        if (s < t.n_seq) {
+            look(s);
+            ok = own.code == TUTTI_OK;
+            int32_t keep = -1;
+            if (shares && ok && own.count > 1) {
+                const int32_t w = (int32_t)__ldcg(p.writers + own.tail);
+                const bool is_last = __ldcg(p.top + own.tail) == s + 1;
+                copies = !(is_last && w >= own.count);
+                if (is_last) {
+                    keep = own.tail;
+                    p.keep_count[s] = w < own.count ? own.count - w : 1;
+                }
+            }
+            p.keep_id[s] = keep;
+            p.mark[s] = !ok ? -2 : copies ? own.tail : -1;
+        }
+        unsigned long long all;
+        const unsigned long long before = scan<unsigned long long>(ok ? own.more + copies : 0, sums, all);
+        if (s < t.n_seq) {
+            p.begin[s] = (uint32_t)(total + before);
+            p.entry[s] = ok ? own.r.b0 + own.r.held - copies : 0;
+        }
+        total += all;
+    }
+    if (threadIdx.x == 0) *p.total = total;
+}
+
+// The last of `begin`'s rows (ascending, begin[0] = 0) that starts at k or before.
+__device__ inline uint32_t last_at(const uint32_t *begin, uint32_t n, uint32_t k) {
+    uint32_t lo = 0;
+    while (n > 1) {
+        const uint32_t half = n / 2;
+        if (begin[lo + half] <= k) lo += half, n -= half;
+        else n = half;
+    }
+    return lo;
+}
+
 __global__ void __launch_bounds__(PLAN_THREADS) extend_kernel(const PagesDev p, const TablesDev t, const uint32_t *n_new, int32_t *pairs) {
     __shared__ unsigned long long sums[32];
-    __shared__ uint32_t sums32[32], masks[32], first[PLAN_THREADS], ranks[SEARCH];
+    __shared__ uint32_t sums32[32], first[PLAN_THREADS], ranks[SEARCH];
     __shared__ bool last;
-    uint32_t n;
-    scan(zeros(tile_counts(p, blockIdx.x, 1)), sums32, n);
+    after_predecessor();
+    if (blockIdx.x == 0) {
+        plan_rows(p, t, n_new, sums);
+    } else {
+        const uint32_t tile = blockIdx.x - 1, id = tile * TILE + threadIdx.x * 4;
+        const int4 v = tile_counts(p, tile, 1);
+        uint32_t n, k = scan(zeros(v), sums32, n);
+        // as many as all rows together may need
+        uint32_t *list = p.rank + (uint64_t)tile * TILE;
+        if (v.x == 0 && k < t.n_blk) list[k] = id;
+        k += v.x == 0;
+        if (v.y == 0 && k < t.n_blk) list[k] = id + 1;
+        k += v.y == 0;
+        if (v.z == 0 && k < t.n_blk) list[k] = id + 2;
+        k += v.z == 0;
+        if (v.w == 0 && k < t.n_blk) list[k] = id + 3;
+        if (threadIdx.x == 0) p.tile[tile] = n;
+    }
+    __syncthreads();
     if (threadIdx.x == 0) {
-        p.tile[blockIdx.x] = n;
         last = arrive_gpu(p.arrive) == gridDim.x - 1;
         if (last) *p.arrive = 0;                // ready for the next call
     }
     __syncthreads();
     if (!last) return;
 
-    // Rows that write to a block that others hold: how many, and which is the last.
-    for (uint32_t s = threadIdx.x; s < t.n_seq; s += PLAN_THREADS) {
-        const Growth g = growth(p, t, n_new, s);
-        if (g.code == TUTTI_OK && g.count > 1) {
-            atomicAdd(p.writers + g.tail, 1);
-            atomicMax(p.top + g.tail, s + 1);
-        }
-        if (g.code != TUTTI_OK) report(t.status, g.code);
-    }
-    __syncthreads();
-    // mark: the block that a row copies, -1 none, -2 the row is skipped.  keep_id, keep_count: what a shared block's
-    // count becomes, at the last of its writers.
-    unsigned long long total = 0;
-    for (uint32_t s0 = 0; s0 < t.n_seq; s0 += PLAN_THREADS) {
-        const uint32_t s = s0 + threadIdx.x;
-        Growth g;
-        g.more = 0;
-        bool copies = false, ok = false;
-        if (s < t.n_seq) {
-            g = growth(p, t, n_new, s);
-            ok = g.code == TUTTI_OK;
-            int32_t keep = -1;
-            if (ok && g.count > 1) {
-                const int32_t w = (int32_t)__ldcg(p.writers + g.tail);
-                const bool is_last = __ldcg(p.top + g.tail) == s + 1;
-                copies = !(is_last && w >= g.count);
-                if (is_last) {
-                    keep = g.tail;
-                    p.keep_count[s] = w < g.count ? g.count - w : 1;
-                }
-            }
-            p.keep_id[s] = keep;
-            p.mark[s] = !ok ? -2 : copies ? g.tail : -1;
-        }
-        unsigned long long all;
-        const unsigned long long before = scan<unsigned long long>(ok ? g.more + copies : 0, sums, all);
-        if (s < t.n_seq) {
-            p.begin[s] = (uint32_t)(total + before);
-            if (s < SEARCH) ranks[s] = (uint32_t)(total + before);
-            p.entry[s] = ok ? g.r.b0 + g.r.held - copies : 0;
-        }
-        total += all;
-    }
+    const unsigned long long total = __ldcg(p.total);
     unsigned long long n_free = 0, mine = 0;
     for (uint32_t i = threadIdx.x; i < p.n_tiles; i += PLAN_THREADS) mine += __ldcg(p.tile + i);
     scan(mine, sums, n_free);
@@ -265,51 +341,30 @@ __global__ void __launch_bounds__(PLAN_THREADS) extend_kernel(const PagesDev p, 
     if (!enough && threadIdx.x == 0) report(t.status, TUTTI_EAGAIN);
     // The rows' new lengths and counts of the blocks that they shared.
     for (uint32_t s = threadIdx.x; s < t.n_seq; s += PLAN_THREADS) {
-        const int32_t keep = p.keep_id[s], mark = p.mark[s];
+        const int32_t keep = __ldcg(p.keep_id + s), mark = __ldcg(p.mark + s);
+        if (s < SEARCH) ranks[s] = __ldcg(p.begin + s);
         if (keep >= 0) p.writers[keep] = p.top[keep] = 0;
-        if (keep >= 0 && enough) p.refs[keep] = p.keep_count[s];
+        if (keep >= 0 && enough) p.refs[keep] = __ldcg(p.keep_count + s);
         if (mark != -2 && enough) t.len[s] += n_new[s];
         pairs[2 * s] = enough && mark >= 0 ? mark : -1;
         if (!enough || mark < 0) pairs[2 * s + 1] = -1;
     }
     if (!enough) return;
-    __syncthreads();
-    // Block number k of the step's new ones belongs to the last row whose first rank is k or less.
-    auto give = [&](uint32_t k, uint32_t id) {
-        uint32_t lo = 0, len = t.n_seq;
-        while (len > 1) {
-            const uint32_t half = len / 2;
-            const uint32_t b = t.n_seq <= SEARCH ? ranks[lo + half] : p.begin[lo + half];
-            if (b <= k) lo += half, len -= half;
-            else len = half;
-        }
-        const uint32_t j = k - (t.n_seq <= SEARCH ? ranks[lo] : p.begin[lo]);
-        t.block_ids[p.entry[lo] + j] = (int32_t)id;
-        if (j == 0 && p.mark[lo] >= 0) pairs[2 * lo + 1] = (int32_t)id;
-        p.refs[id] = 1;
-    };
     uint32_t at = 0;                            // free blocks in front of the tiles in hand
     for (uint32_t t0 = 0; t0 < p.n_tiles && at < total; t0 += PLAN_THREADS) {
-        const uint32_t c = t0 + threadIdx.x < p.n_tiles ? __ldcg(p.tile + t0 + threadIdx.x) : 0;
         uint32_t in_all;
-        const uint32_t before = at + scan(c, sums32, in_all);
-        first[threadIdx.x] = before;
-        const uint32_t need = __ballot_sync(0xffffffffu, c && before < total);
-        if ((threadIdx.x & 31) == 0) masks[threadIdx.x / 32] = need;
+        const uint32_t c = t0 + threadIdx.x < p.n_tiles ? __ldcg(p.tile + t0 + threadIdx.x) : 0;
+        first[threadIdx.x] = at + scan(c, sums32, in_all);
         __syncthreads();
-        for (uint32_t w = 0; w < PLAN_THREADS / 32; ++w)
-            for (uint32_t m = masks[w]; m; m &= m - 1) {
-                const uint32_t i = w * 32 + __ffs(m) - 1, id = (t0 + i) * TILE + threadIdx.x * 4;
-                const int4 v = tile_counts(p, t0 + i, 1);
-                uint32_t in_tile, k = first[i] + scan(zeros(v), sums32, in_tile);
-                if (v.x == 0 && k < total) give(k, id);
-                k += v.x == 0;
-                if (v.y == 0 && k < total) give(k, id + 1);
-                k += v.y == 0;
-                if (v.z == 0 && k < total) give(k, id + 2);
-                k += v.z == 0;
-                if (v.w == 0 && k < total) give(k, id + 3);
-            }
+        for (uint32_t k = at + threadIdx.x; k < total && k < at + in_all; k += PLAN_THREADS) {
+            const uint32_t i = last_at(first, PLAN_THREADS, k);
+            const uint32_t id = __ldcg(p.rank + (uint64_t)(t0 + i) * TILE + (k - first[i]));
+            const uint32_t s = t.n_seq <= SEARCH ? last_at(ranks, t.n_seq, k) : last_at(p.begin, t.n_seq, k);
+            const uint32_t j = k - (t.n_seq <= SEARCH ? ranks[s] : p.begin[s]);
+            t.block_ids[__ldcg(p.entry + s) + j] = (int32_t)id;
+            if (j == 0 && __ldcg(p.mark + s) >= 0) pairs[2 * s + 1] = (int32_t)id;
+            p.refs[id] = 1;
+        }
         at += in_all;
         __syncthreads();
     }
@@ -319,6 +374,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) extend_kernel(const PagesDev p, 
 // release and trim: `per` CTAs a row.  Release clears a row's length once all its CTAs have read it: the last to
 // say so does it, and the entries are independent of that.
 __global__ void __launch_bounds__(ROW_THREADS) release_kernel(const PagesDev p, const TablesDev t, const uint8_t *which, uint32_t per) {
+    after_predecessor();
     const uint32_t s = blockIdx.x / per, part = blockIdx.x % per;
     if (which && !which[s]) return;
     Row r;
@@ -342,6 +398,7 @@ __global__ void __launch_bounds__(ROW_THREADS) release_kernel(const PagesDev p, 
 }
 
 __global__ void __launch_bounds__(ROW_THREADS) trim_kernel(const PagesDev p, const TablesDev t, uint32_t window, uint32_t sinks, uint32_t per) {
+    after_predecessor();
     const uint32_t s = blockIdx.x / per, part = blockIdx.x % per;
     Row r;
     if (!row_view(t, s, r)) {
@@ -363,6 +420,7 @@ __global__ void __launch_bounds__(ROW_THREADS) trim_kernel(const PagesDev p, con
 // compact, with u(i) the blocks in use below i and n all of them: a free block f < n is the destination
 // number f - u(f), a block in use s >= n is the source number n - 1 - u(s), and there are n - u(n) of each.
 __global__ void __launch_bounds__(PLAN_THREADS) compact_count_kernel(const PagesDev p) {
+    after_predecessor();
     __shared__ uint32_t sums[32];
     uint32_t n;
     scan(4 - zeros(tile_counts(p, blockIdx.x, 0)), sums, n);
@@ -371,15 +429,27 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_count_kernel(const Pages
 
 __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesDev p, int32_t *pairs, uint32_t max_pairs) {
     __shared__ uint32_t sums[32];
+    after_predecessor();
     uint32_t low = 0, all = 0, n, u, ignored;
-    for (uint32_t i = threadIdx.x; i < p.n_tiles; i += PLAN_THREADS) {
-        const uint32_t c = p.tile[i];
-        all += c;
-        if (i < blockIdx.x) low += c;
+    int4 v = make_int4(0, 0, 0, 0);
+    if (p.n_tiles <= SMALL) {
+#pragma unroll
+        for (uint32_t i = 0; i < SMALL; ++i) {
+            const int4 x = i < p.n_tiles ? tile_counts(p, i, 0) : make_int4(0, 0, 0, 0);
+            all += 4 - zeros(x);
+            if (i < blockIdx.x) low += 4 - zeros(x);
+            if (i == blockIdx.x) v = x;
+        }
+    } else {
+        for (uint32_t i = threadIdx.x; i < p.n_tiles; i += PLAN_THREADS) {
+            const uint32_t c = p.tile[i];
+            all += c;
+            if (i < blockIdx.x) low += c;
+        }
+        v = tile_counts(p, blockIdx.x, 0);
     }
     scan(all, sums, n);
     scan(low, sums, u);
-    const int4 v = tile_counts(p, blockIdx.x, 0);
     u += scan(4 - zeros(v), sums, ignored);
     if (n == p.n_blocks && blockIdx.x == 0 && threadIdx.x == 0) *p.moves = 0;
     const int count[4] = {v.x, v.y, v.z, v.w};
@@ -402,6 +472,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) compact_plan_kernel(const PagesD
 }
 
 __global__ void __launch_bounds__(ROW_THREADS) compact_apply_kernel(const PagesDev p, const TablesDev t, int32_t *pairs, uint32_t max_pairs, uint32_t *n_pairs, uint32_t per) {
+    after_predecessor();
     const uint32_t n = min(*p.moves, max_pairs);
     if (blockIdx.x >= per * t.n_seq) {          // the counts, and the pairs behind the last
         const uint32_t first = blockIdx.x - per * t.n_seq, ctas = gridDim.x - per * t.n_seq;
@@ -498,7 +569,7 @@ int tutti_pages_create(tutti_ctx_t *ctx, int32_t *refs, uint64_t n_blocks, tutti
     tutti_pages *p = new (std::nothrow) tutti_pages();
     if (!p) return TUTTI_ENOMEM;
     const uint32_t tiles = (uint32_t)((n_blocks + TILE - 1) / TILE);
-    const size_t words = 32 + (size_t)tiles + 3 * n_blocks + 6 * (size_t)TUTTI_PAGES_MAX_SEQ;
+    const size_t words = 32 + (size_t)tiles + 2 * n_blocks + (size_t)tiles * TILE + 6 * (size_t)TUTTI_PAGES_MAX_SEQ;
     cudaError_t e = cudaMalloc((void **)&p->memory, words * 4);
     if (e == cudaSuccess && ((e = cudaMemset(p->memory, 0, words * 4)) != cudaSuccess || (e = cudaDeviceSynchronize()) != cudaSuccess))
         cudaFree(p->memory);
@@ -515,6 +586,7 @@ int tutti_pages_create(tutti_ctx_t *ctx, int32_t *refs, uint64_t n_blocks, tutti
     d.n_tiles = tiles;
     d.arrive = p->memory;
     d.moves = p->memory + 1;
+    d.total = (unsigned long long *)(p->memory + 2);
     uint32_t *at = p->memory + 32;
     auto take = [&](size_t n) {
         uint32_t *a = at;
@@ -530,7 +602,7 @@ int tutti_pages_create(tutti_ctx_t *ctx, int32_t *refs, uint64_t n_blocks, tutti
     d.tile = take(tiles);
     d.writers = take(n_blocks);
     d.top = take(n_blocks);
-    d.rank = take(n_blocks);
+    d.rank = take((size_t)tiles * TILE);
     *out = p;
     return TUTTI_OK;
 }
@@ -551,8 +623,10 @@ int tutti_pages_fork(tutti_pages_t *pages, const tutti_tables_t *from, const int
     if (!rows) return TUTTI_OK;
     OnDevice on(pages->device);
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
+    const uint32_t groups = (from->n_seq + GROUP - 1) / GROUP;
     const uint32_t per = ctas_a_row(rows, from->n_blk / 2 + to->n_blk / 2, ROW_IDS, tutti_ctx_sms_(pages->ctx));
-    const cudaError_t e = launch_plain(fork_kernel, per * rows, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, from), parent, on_device(pages, to), move, per);
+    const uint32_t segs = groups ? ctas_a_row(groups, from->n_blk / GROUP, ROW_THREADS, tutti_ctx_sms_(pages->ctx)) : 0;
+    const cudaError_t e = launch_behind(fork_kernel, per * to->n_seq + segs * groups, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, from), parent, on_device(pages, to), move, per, segs);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "fork launch");
 }
 
@@ -562,7 +636,7 @@ int tutti_pages_extend(tutti_pages_t *pages, const tutti_tables_t *t, const uint
     if (!t->n_seq) return TUTTI_OK;
     OnDevice on(pages->device);
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
-    const cudaError_t e = launch_plain(extend_kernel, pages->dev.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), n_new, pairs);
+    const cudaError_t e = launch_behind(extend_kernel, pages->dev.n_tiles + 1, PLAN_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), n_new, pairs);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "extend launch");
 }
 
@@ -573,7 +647,7 @@ int tutti_pages_release(tutti_pages_t *pages, const tutti_tables_t *t, const uin
     OnDevice on(pages->device);
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const uint32_t per = ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, tutti_ctx_sms_(pages->ctx));
-    const cudaError_t e = launch_plain(release_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), which, per);
+    const cudaError_t e = launch_behind(release_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), which, per);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "release launch");
 }
 
@@ -585,7 +659,7 @@ int tutti_pages_trim(tutti_pages_t *pages, const tutti_tables_t *t, const tutti_
     OnDevice on(pages->device);
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const uint32_t per = ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, tutti_ctx_sms_(pages->ctx));
-    const cudaError_t e = launch_plain(trim_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), window->window, window->sinks, per);
+    const cudaError_t e = launch_behind(trim_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), window->window, window->sinks, per);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "trim launch");
 }
 
@@ -598,9 +672,10 @@ int tutti_pages_compact(tutti_pages_t *pages, const tutti_tables_t *t, int32_t *
     const int sms = tutti_ctx_sms_(pages->ctx);
     const uint32_t per = t->n_seq ? ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, sms) : 1;
     const uint32_t movers = max_pairs / ROW_THREADS + 1 < (uint32_t)sms ? max_pairs / ROW_THREADS + 1 : (uint32_t)sms;
-    cudaError_t e = launch_plain(compact_count_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d);
-    if (e == cudaSuccess) e = launch_plain(compact_plan_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d, pairs, max_pairs);
-    if (e == cudaSuccess) e = launch_plain(compact_apply_kernel, per * t->n_seq + movers, ROW_THREADS, 0, (cudaStream_t)stream, d, on_device(pages, t), pairs, max_pairs, n_pairs, per);
+    cudaError_t e = cudaSuccess;
+    if (d.n_tiles > SMALL) e = launch_behind(compact_count_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d);
+    if (e == cudaSuccess) e = launch_behind(compact_plan_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d, pairs, max_pairs);
+    if (e == cudaSuccess) e = launch_behind(compact_apply_kernel, per * t->n_seq + movers, ROW_THREADS, 0, (cudaStream_t)stream, d, on_device(pages, t), pairs, max_pairs, n_pairs, per);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "compact launch");
 }
 

@@ -84,10 +84,11 @@ def extend(t, refs, n_new):
         tail = -1
         if add and r[2] % t.bs:
             tail = t.ids[r[0] + r[2] // t.bs]
-            if not 0 <= tail < len(refs) or refs[tail] <= 0:
-                t.status.add(T.EFAULT if not 0 <= tail < len(refs) else T.EINVAL)
-                continue
-            writers.setdefault(tail, []).append(s)
+            if tail != -1:
+                if not 0 <= tail < len(refs) or refs[tail] <= 0:
+                    t.status.add(T.EFAULT if not 0 <= tail < len(refs) else T.EINVAL)
+                    continue
+                writers.setdefault(tail, []).append(s)
         rows[s] = (*r, add, tail)
     need = []
     for s in range(n_seq):

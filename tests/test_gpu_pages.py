@@ -105,6 +105,21 @@ def test_extend_shares_of_one_block(contexts):
             b.close()
 
 
+def test_extend_behind_an_entry_without_a_block(contexts):
+    """A row whose partly filled block is gone grows: nothing is copied, nobody shares it."""
+    book = P.Book([0, 3, 6], [0, -1, -7, 0, -1, -7], [6, 7], 4)
+    refs = [2, 0, 0, 0]
+    b = P.Bound(contexts(4), [book], refs)
+    pairs = torch.zeros(2, 2, dtype=torch.int32, device=b.dev)
+    try:
+        b.pages.tutti_pages_extend(b.tables(), ints([1, 2]), pairs)
+        assert pairs.tolist() == [list(p) for p in P.extend(book, refs, [1, 2])] and not book.status
+        assert book.lens == [7, 9] and book.ids[5] == 1
+        b.same(refs)
+    finally:
+        b.close()
+
+
 @pytest.mark.parametrize("n_free", [0, 1, 6, 7])
 def test_extend_takes_all_or_nothing(contexts, n_free):
     bs = 4
