@@ -100,12 +100,14 @@ __host__ __device__ inline uint64_t floor_sum(uint64_t n, uint64_t m, uint64_t a
 // The tiles of one sequence and head.
 struct Rows {
     uint32_t n_rows, n_tiles, group, ctx;
+    uint32_t group_mul, group_shift;    // row / group = row * group_mul >> group_shift
     int64_t first;                      // position of the first new token
+    __host__ __device__ uint32_t token_of(uint32_t row) const { return (uint32_t)((uint64_t)row * group_mul >> group_shift); }
     // units of tile q: up to the key of its last row
     __host__ __device__ uint32_t units(uint32_t q) const {
         if (first < 0 || ctx == 0) return ctx ? (ctx + BN - 1) / BN : 1;     // padding rows: every tile sees all
-        const uint64_t end = (uint64_t)(q + 1) * TILE_ROWS < n_rows ? (uint64_t)(q + 1) * TILE_ROWS : n_rows;
-        return (uint32_t)(((uint64_t)first + (end - 1) / group) / BN) + 1;
+        const uint32_t end = q + 1 < n_tiles ? (q + 1) * TILE_ROWS : n_rows;
+        return ((uint32_t)first + token_of(end - 1)) / BN + 1;
     }
     // units of tiles [0, q)
     __host__ __device__ uint64_t before(uint32_t q) const {
@@ -122,35 +124,38 @@ struct Rows {
 // window of its first row, are left out.
 struct WindowRows : Rows {
     uint32_t front;                     // units of the first tokens that stay visible
-    int64_t start;                      // (keys in front of the first row's window, less those of `front`) * group
-    // how many are left out of tile q: floor((first + floor(256 q / group) - window + 1) / BN) - front, if positive
+    int64_t start;                      // keys in front of the first row's window, less those of `front`
+    // how many are left out of tile q: those in front of its first row's window, less `front`, if positive
     __host__ __device__ uint32_t gap(uint32_t q) const {
-        const int64_t x = start + (int64_t)q * TILE_ROWS;
-        return x > 0 ? (uint32_t)((uint64_t)x / ((uint64_t)BN * group)) : 0;
+        const int64_t x = start + token_of(q * TILE_ROWS);
+        return x > 0 ? (uint32_t)x / BN : 0;
     }
     __host__ __device__ uint32_t units(uint32_t q) const { return Rows::units(q) - gap(q); }
     __host__ __device__ uint64_t before(uint32_t q) const {
         const uint64_t all = Rows::before(q);
-        // tiles in front of q0 leave nothing out
-        const uint64_t q0 = start >= 0 ? 0 : ((uint64_t)-start + TILE_ROWS - 1) / TILE_ROWS;
-        return q <= q0 ? all : all - floor_sum(q - q0, (uint64_t)BN * group, TILE_ROWS, (uint64_t)(start + (int64_t)q0 * TILE_ROWS));
+        // floor((start + floor(x / group)) / BN) = floor((start group + x) / (BN group)), x = 256 i; tiles in front of q0 leave nothing out
+        const int64_t b = start * (int64_t)group;
+        const uint64_t q0 = b >= 0 ? 0 : ((uint64_t)-b + TILE_ROWS - 1) / TILE_ROWS;
+        return q <= q0 ? all : all - floor_sum(q - q0, (uint64_t)BN * group, TILE_ROWS, (uint64_t)(b + (int64_t)q0 * TILE_ROWS));
     }
 };
 template <bool WIN> struct RowsOf { typedef Rows type; };
 template <> struct RowsOf<true> { typedef WindowRows type; };
 
-__host__ __device__ inline void rows_of(const SeqView &v, uint32_t group, uint32_t, uint32_t, Rows &r) {
+__host__ __device__ inline void rows_of(const SeqView &v, uint32_t group, uint32_t group_mul, uint32_t group_shift, uint32_t, uint32_t, Rows &r) {
     r.n_rows = v.n_new * group;
     r.n_tiles = (r.n_rows + TILE_ROWS - 1) / TILE_ROWS;
     r.group = group;
+    r.group_mul = group_mul;
+    r.group_shift = group_shift;
     r.ctx = v.ctx;
     r.first = (int64_t)v.ctx - v.n_new;
 }
-__host__ __device__ inline void rows_of(const SeqView &v, uint32_t group, uint32_t window, uint32_t sinks, WindowRows &r) {
-    rows_of(v, group, 0, 0, static_cast<Rows &>(r));
+__host__ __device__ inline void rows_of(const SeqView &v, uint32_t group, uint32_t group_mul, uint32_t group_shift, uint32_t window, uint32_t sinks, WindowRows &r) {
+    rows_of(v, group, group_mul, group_shift, 0, 0, static_cast<Rows &>(r));
     r.front = (sinks + BN - 1) / BN;
     // padding rows: every tile sees all
-    r.start = r.first < 0 ? -((int64_t)1 << 62) : (r.first - window + 1 - (int64_t)r.front * BN) * group;
+    r.start = r.first < 0 ? -((int64_t)1 << 40) : r.first - window + 1 - (int64_t)r.front * BN;
 }
 
 // Where a cut at unit u of a tile of n units goes: to its start below low(n), behind it from n -
@@ -200,7 +205,7 @@ __device__ inline int tile_seq(const AttendParams &p, uint32_t s, Tile<WIN> &t) 
     t.s = s;
     const int code = seq_view(p.step, p.pool.block_tokens, s, t.v);
     if (code != TUTTI_OK) t.v.n_new = t.v.ctx = 0;
-    rows_of(t.v, p.group, p.window, p.sinks, t.r);
+    rows_of(t.v, p.group, p.group_mul, p.group_shift, p.window, p.sinks, t.r);
     return code;
 }
 
@@ -872,6 +877,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 for (int u = 0; u < STEPS; ++u)
                     for (int i = 0; i < halves; ++i) qk(i, u, slot(n_unit, 0));
                 commit(empty + 8 * slot(n_unit, 0));
+                if (n == 1) commit(q_empty);            // behind the last Q K^T of the tile
+                x += n;
+                if (x < x1) next_tile(p, t);            // while the softmax has the first scores
                 for (uint32_t j = 0; j < n && ok; ++j, ++n_unit) {
                     const bool more = j + 1 < n;
                     ok = all(landed(n_unit, 1) && (!more || landed(n_unit + 1, 0)));
@@ -888,16 +896,14 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     if (!ok) break;
                     commit(empty + 8 * slot(n_unit, 1));
                     if (more) commit(empty + 8 * slot(n_unit + 1, 0));
+                    if (j + 2 == n) commit(q_empty);
                 }
                 if (!ok) break;
                 for (int i = 0; i < halves; ++i) {
                     commit(o_done + 8 * i);
                     ++ns[i];
                 }
-                commit(q_empty);
                 ++segs;
-                x += n;
-                if (x < x1) next_tile(p, t);
             }
             // every matrix instruction has ended before TMEM is given back
             commit(drain);
@@ -970,17 +976,18 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                         for (int k = 0; k < SUB; ++k) s[k] = -s[k];
                     }
                     if (key0 + SUB - 1 > pos_low || all != ~0u || (WIN && key0 <= hidden)) {
-                        const int64_t d = pos - key0;
-                        const int lim = d < -1 ? -1 : d > SUB ? SUB : (int)d;
-                        int low = -1, front = 0;                  // WIN: keys up to `low`, but for those below `front`
-                        if constexpr (WIN) {
-                            const int64_t x = d - p.window, y = (int64_t)p.sinks - key0;
-                            low = x < -1 ? -1 : x > SUB ? SUB : (int)x;
-                            front = y < 0 ? 0 : y > SUB ? SUB : (int)y;
-                        }
+                        // A bit a key, and two instructions a score: this code runs once or twice a tile, so that it is fetched
+                        // each time (with three comparisons a score a masked unit took 9 us instead of 2).
+                        auto ahead = [](int64_t n) { return n < 0 ? 0 : n > SUB ? SUB : (int)n; };
+                        auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };       // bits 0 .. n - 1
+                        const int seen = ahead(pos - key0 + 1), gone = WIN ? ahead(pos - p.window - key0 + 1) : 0, first = WIN ? ahead((int64_t)p.sinks - key0) : 0;
 #pragma unroll
-                        for (int k = 0; k < SUB; ++k)
-                            if (k > lim || (WIN && k <= low && k >= front) || !(ex[k / 32] >> (k % 32) & 1)) s[k] = -INFINITY;
+                        for (int q = 0; q < SUB / 32; ++q) {
+                            uint32_t bits = ex[q] & below(seen - 32 * q);
+                            if constexpr (WIN) bits &= ~below(gone - 32 * q) | below(first - 32 * q);
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) s[32 * q + k] = bits & 1u << k ? s[32 * q + k] : -INFINITY;
+                        }
                     }
                     float a0 = max3(s[0], s[4], s[8]), a1 = max3(s[1], s[5], s[9]), a2 = max3(s[2], s[6], s[10]), a3 = max3(s[3], s[7], s[11]);
 #pragma unroll
@@ -1240,7 +1247,9 @@ extern "C" void tutti_many_parts_(uint64_t tile0, uint32_t n, uint64_t workers, 
 extern "C" int tutti_many_units_(uint32_t ctx, uint32_t n_new, uint32_t group, uint32_t q, uint64_t *out2) {
     const tutti::SeqView v{0, n_new, ctx, 0};
     tutti::Rows r;
-    tutti::rows_of(v, group, 0, 0, r);
+    uint32_t mul, shift;
+    tutti::division_by(group, mul, shift);
+    tutti::rows_of(v, group, mul, shift, 0, 0, r);
     out2[0] = q < r.n_tiles ? r.units(q) : 0;
     out2[1] = r.before(q);
     return (int)r.n_tiles;
@@ -1249,7 +1258,9 @@ extern "C" int tutti_many_units_(uint32_t ctx, uint32_t n_new, uint32_t group, u
 extern "C" int tutti_many_window_units_(uint32_t ctx, uint32_t n_new, uint32_t group, uint32_t window, uint32_t sinks, uint32_t q, uint64_t *out4) {
     const tutti::SeqView v{0, n_new, ctx, 0};
     tutti::WindowRows r;
-    tutti::rows_of(v, group, window, sinks, r);
+    uint32_t mul, shift;
+    tutti::division_by(group, mul, shift);
+    tutti::rows_of(v, group, mul, shift, window, sinks, r);
     out4[0] = q < r.n_tiles ? r.units(q) : 0;
     out4[1] = r.before(q);
     out4[2] = r.front;
