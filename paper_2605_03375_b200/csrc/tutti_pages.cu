@@ -155,6 +155,15 @@ __global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, con
     __shared__ int by[GROUP];
     const uint32_t g = blockIdx.x - per * to.n_seq, f0 = g % ((from.n_seq + GROUP - 1) / GROUP) * GROUP, seg = g / ((from.n_seq + GROUP - 1) / GROUP);
     if (threadIdx.x == 0) longest = 0;
+    // the thread's first child, and its room, are fetched along with the old rows
+    int32_t parent0 = -1;
+    bool room0 = false;
+    Row child0;
+    child0.room = 0;
+    if (threadIdx.x < to.n_seq) {
+        parent0 = parent[threadIdx.x];
+        room0 = row_room(to, threadIdx.x, child0);
+    }
     __syncthreads();
     if (threadIdx.x < GROUP) {
         const uint32_t f = f0 + threadIdx.x;
@@ -168,8 +177,10 @@ __global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, con
     __syncthreads();
     if (seg * ROW_THREADS >= longest) return;
     for (uint32_t c = threadIdx.x; c < to.n_seq; c += ROW_THREADS) {
-        const uint32_t k = (uint32_t)parent[c] - f0;
-        if (k < GROUP && row_room(to, c, child) && held[k] <= child.room) atomicAdd(by + k, 1);
+        const bool is_first = c == threadIdx.x;
+        const uint32_t k = (uint32_t)(is_first ? parent0 : parent[c]) - f0;
+        if (k >= GROUP || !(is_first ? room0 : row_room(to, c, child))) continue;
+        if (held[k] <= (is_first ? child0.room : child.room)) atomicAdd(by + k, 1);
     }
     __syncthreads();
     for (uint32_t i = seg * ROW_THREADS + threadIdx.x; i < longest; i += segs * ROW_THREADS) {
@@ -305,8 +316,8 @@ __device__ inline uint32_t last_at(const uint32_t *begin, uint32_t n, uint32_t k
 
 __global__ void __launch_bounds__(PLAN_THREADS) extend_kernel(const PagesDev p, const TablesDev t, const uint32_t *n_new, int32_t *pairs) {
     __shared__ unsigned long long sums[32];
-    __shared__ uint32_t sums32[32], first[PLAN_THREADS], ranks[SEARCH];
-    __shared__ bool last;
+    __shared__ uint32_t sums32[32], first[PLAN_THREADS], ranks[SEARCH], entries[PLAN_THREADS];
+    __shared__ bool last, copies[PLAN_THREADS];
     after_predecessor();
     if (blockIdx.x == 0) {
         plan_rows(p, t, n_new, sums);
@@ -333,36 +344,57 @@ __global__ void __launch_bounds__(PLAN_THREADS) extend_kernel(const PagesDev p, 
     __syncthreads();
     if (!last) return;
 
+    // Everything that the end needs is fetched in one go: the thread's row and tile are its only ones, mostly.
     const unsigned long long total = __ldcg(p.total);
-    unsigned long long n_free = 0, mine = 0;
-    for (uint32_t i = threadIdx.x; i < p.n_tiles; i += PLAN_THREADS) mine += __ldcg(p.tile + i);
-    scan(mine, sums, n_free);
+    const uint32_t me = threadIdx.x;
+    int32_t keep = -1, mark = -2, keep_count = 0;
+    uint32_t begin = 0, len = 0, add = 0, entry = 0, mine = 0;
+    auto fetch = [&](uint32_t s) {
+        keep = __ldcg(p.keep_id + s), mark = __ldcg(p.mark + s), keep_count = __ldcg(p.keep_count + s);
+        begin = __ldcg(p.begin + s), entry = __ldcg(p.entry + s), len = t.len[s], add = n_new[s];
+    };
+    if (me < t.n_seq) fetch(me);
+    const uint32_t c0 = me < p.n_tiles ? __ldcg(p.tile + me) : 0;
+    for (uint32_t i = me + PLAN_THREADS; i < p.n_tiles; i += PLAN_THREADS) mine += __ldcg(p.tile + i);
+    uint32_t in_first, n_free;                  // in the first tiles, and in all
+    const uint32_t before0 = scan(c0, sums32, in_first);
+    n_free = in_first;
+    if (p.n_tiles > PLAN_THREADS) {
+        scan(mine, sums32, n_free);
+        n_free += in_first;
+    }
     const bool enough = total <= n_free;
-    if (!enough && threadIdx.x == 0) report(t.status, TUTTI_EAGAIN);
+    if (!enough && me == 0) report(t.status, TUTTI_EAGAIN);
     // The rows' new lengths and counts of the blocks that they shared.
-    for (uint32_t s = threadIdx.x; s < t.n_seq; s += PLAN_THREADS) {
-        const int32_t keep = __ldcg(p.keep_id + s), mark = __ldcg(p.mark + s);
-        if (s < SEARCH) ranks[s] = __ldcg(p.begin + s);
+    for (uint32_t s = me; s < t.n_seq; s += PLAN_THREADS) {
+        if (s != me) fetch(s);
+        if (s < SEARCH) ranks[s] = begin;
+        if (s < PLAN_THREADS) entries[s] = entry, copies[s] = mark >= 0;
         if (keep >= 0) p.writers[keep] = p.top[keep] = 0;
-        if (keep >= 0 && enough) p.refs[keep] = __ldcg(p.keep_count + s);
-        if (mark != -2 && enough) t.len[s] += n_new[s];
+        if (keep >= 0 && enough) p.refs[keep] = keep_count;
+        if (mark != -2 && enough) t.len[s] = len + add;
         pairs[2 * s] = enough && mark >= 0 ? mark : -1;
         if (!enough || mark < 0) pairs[2 * s + 1] = -1;
     }
     if (!enough) return;
     uint32_t at = 0;                            // free blocks in front of the tiles in hand
     for (uint32_t t0 = 0; t0 < p.n_tiles && at < total; t0 += PLAN_THREADS) {
-        uint32_t in_all;
-        const uint32_t c = t0 + threadIdx.x < p.n_tiles ? __ldcg(p.tile + t0 + threadIdx.x) : 0;
-        first[threadIdx.x] = at + scan(c, sums32, in_all);
+        uint32_t in_all = in_first;
+        if (t0 == 0) {
+            first[me] = before0;
+        } else {
+            const uint32_t c = t0 + me < p.n_tiles ? __ldcg(p.tile + t0 + me) : 0;
+            first[me] = at + scan(c, sums32, in_all);
+        }
         __syncthreads();
         for (uint32_t k = at + threadIdx.x; k < total && k < at + in_all; k += PLAN_THREADS) {
             const uint32_t i = last_at(first, PLAN_THREADS, k);
             const uint32_t id = __ldcg(p.rank + (uint64_t)(t0 + i) * TILE + (k - first[i]));
             const uint32_t s = t.n_seq <= SEARCH ? last_at(ranks, t.n_seq, k) : last_at(p.begin, t.n_seq, k);
             const uint32_t j = k - (t.n_seq <= SEARCH ? ranks[s] : p.begin[s]);
-            t.block_ids[__ldcg(p.entry + s) + j] = (int32_t)id;
-            if (j == 0 && __ldcg(p.mark + s) >= 0) pairs[2 * s + 1] = (int32_t)id;
+            const bool here = s < PLAN_THREADS;
+            t.block_ids[(here ? entries[s] : __ldcg(p.entry + s)) + j] = (int32_t)id;
+            if (j == 0 && (here ? copies[s] : __ldcg(p.mark + s) >= 0)) pairs[2 * s + 1] = (int32_t)id;
             p.refs[id] = 1;
         }
         at += in_all;
