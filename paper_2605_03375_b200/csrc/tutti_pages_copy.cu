@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(THREADS, 1) copy_blocks_kernel(const __grid_co
 
     // ---- this warp's walk over the CTA's tickets, and over its units of each ----
     uint32_t ticket = blockIdx.x, n_tickets = 0, round = ~0u, n = 0;
-    bool open = true, dead = false;
+    bool open = true;
     bool asks = gridDim.x > p.width;            // or the CTAs of the grid are the only tickets
     if (threadIdx.x == 0 && asks) ask(base + OFF_SLOT, full);
     // Pieces of `piece` bytes (the last of a block the rest), `per` of them a unit; the ticket's units.
@@ -99,7 +99,6 @@ __global__ void __launch_bounds__(THREADS, 1) copy_blocks_kernel(const __grid_co
     uint64_t pieces = 0, at = 0, end = 0;
     auto give_up = [&]() {
         if (p.status) atomicCAS(p.status, TUTTI_OK, TUTTI_ETIMEDOUT);
-        dead = true;
         open = false;
     };
     // The pairs of a round that are copied, in order: all CTAs make the same list.  All warps of the CTA come here together.

@@ -323,10 +323,8 @@ class Context:
                              allow: Sequence[int] = ()) -> int:
         """Copy blocks (and scales) inside the layers' pools: `pairs` [n, 2] int32, from and to, as tutti_pages_extend and
         tutti_pages_compact leave them; n_pairs (int32) is how many of them count, on the device."""
-        at = self.device
-        if len(pairs.shape) != 2 or pairs.shape[1] != 2:
-            raise TuttiError(EINVAL, "tutti_kv_copy_blocks: pairs are not [n, 2]")
-        rc = self.lib.tutti_kv_copy_blocks(self.h, first_layer, n_layers, _ints(pairs, at, "pairs"), pairs.shape[0],
+        at, n = self.device, _pairs(pairs, "tutti_kv_copy_blocks")
+        rc = self.lib.tutti_kv_copy_blocks(self.h, first_layer, n_layers, _ints(pairs, at, "pairs"), n,
                                            None if n_pairs is None else _ints(n_pairs, at, "n_pairs", 1),
                                            None if status is None else _ints(status, at, "status", 1), None if stream is None else _stream_ptr(stream))
         return rc if rc == OK else _check(rc, "tutti_kv_copy_blocks", allow)
@@ -409,12 +407,21 @@ def make_step(q_start, ctx_len, blk_start, block_ids, n_tok: int, max_new: int, 
 _INT32 = set()                              # torch.int32 and torch.uint32, once seen
 
 
+def _pairs(t, what: str) -> int:
+    """The rows of an [n, 2] tensor."""
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != 2:
+        raise TuttiError(EINVAL, f"{what}: pairs are not [n, 2]")
+    return shape[0]
+
+
 def _ints(t, device: int, what: str, least: int = 0) -> int:
     """Address of a contiguous int32 tensor of `least` elements or more that the context's GPU reaches."""
-    if t.dtype not in _INT32:
-        if str(t.dtype) not in ("torch.int32", "torch.uint32"):
+    dtype = t.dtype
+    if dtype not in _INT32:
+        if str(dtype) not in ("torch.int32", "torch.uint32"):
             raise TuttiError(EINVAL, f"{what} (int32)")
-        _INT32.add(t.dtype)
+        _INT32.add(dtype)
     if not t.is_contiguous() or t.numel() < least:
         raise TuttiError(EINVAL, f"{what} (contiguous, {least} elements or more)")
     if t.get_device() != device:
@@ -543,26 +550,23 @@ class Attn:
             self.lib.tutti_attn_destroy(self.h)
             self.h = None
 
-    def _compare(self, step: Step, io: Attend, what: str):
-        ctx = self.ctx
-        if ctx.h is None or self.h is None:
-            raise TuttiError(EINVAL, f"{what}: the handle or its context is closed")
-        at, of = ctx.device, io._of
-        if of is not None:
-            dim, rows, dev, held = of
-            if dim != ctx._row[1] or rows < step.n_tok:
-                raise TuttiError(EINVAL, f"{what}: queries are not [n_tok or more, heads, head_dim]")
-            if dev != at:
-                _reachable(at, held)
-        if step._at != at:
-            _reachable(at, step._keep)
-
     def tutti_kv_attend_layer(self, layer: int, step: Step, io: Attend, scale: float, stream=None,
                               allow: Sequence[int] = ()) -> int:
         """Causal attention of the step's queries over the pool layer.  stream None is the legacy default
         stream, not torch's current one.  Structs over tensors (make_step, make_attend) are compared with each other and
         with the geometry."""
-        self._compare(step, io, "tutti_kv_attend_layer")
+        ctx = self.ctx
+        if ctx.h is None or self.h is None:
+            raise TuttiError(EINVAL, "tutti_kv_attend_layer: the handle or its context is closed")
+        at, of = ctx.device, io._of
+        if of is not None:
+            dim, rows, dev, held = of
+            if dim != ctx._row[1] or rows < step.n_tok:
+                raise TuttiError(EINVAL, "tutti_kv_attend_layer: queries are not [n_tok or more, heads, head_dim]")
+            if dev != at:
+                _reachable(at, held)
+        if step._at != at:
+            _reachable(at, step._keep)
         io.scale = scale
         rc = self.lib.tutti_kv_attend_layer(self.h, layer, step, io, None if stream is None else _stream_ptr(stream))
         return rc if rc == OK else _check(rc, "tutti_kv_attend_layer", allow)
@@ -570,7 +574,18 @@ class Attn:
     def tutti_kv_attend_window_layer(self, layer: int, step: Step, io: Attend, scale: float, window: Window, stream=None,
                                      allow: Sequence[int] = ()) -> int:
         """The same with a window (make_window): a row sees its last keys and the sequence's first ones."""
-        self._compare(step, io, "tutti_kv_attend_window_layer")
+        ctx = self.ctx
+        if ctx.h is None or self.h is None:
+            raise TuttiError(EINVAL, "tutti_kv_attend_window_layer: the handle or its context is closed")
+        at, of = ctx.device, io._of
+        if of is not None:
+            dim, rows, dev, held = of
+            if dim != ctx._row[1] or rows < step.n_tok:
+                raise TuttiError(EINVAL, "tutti_kv_attend_window_layer: queries are not [n_tok or more, heads, head_dim]")
+            if dev != at:
+                _reachable(at, held)
+        if step._at != at:
+            _reachable(at, step._keep)
         io.scale = scale
         rc = self.lib.tutti_kv_attend_window_layer(self.h, layer, step, io, window, None if stream is None else _stream_ptr(stream))
         return rc if rc == OK else _check(rc, "tutti_kv_attend_window_layer", allow)
@@ -593,46 +608,53 @@ class Pages:
             self.lib.tutti_pages_destroy(self.h)
             self.h = None
 
-    def _call(self, name: str, tables: Sequence[Tables], args, stream, allow: Sequence[int]) -> int:
-        at = self.ctx.device
-        if self.h is None or self.ctx.h is None:
-            raise TuttiError(EINVAL, f"{name}: the handle or its context is closed")
-        for t in tables:
-            if t._at != at:
-                _reachable(at, t._keep)
-        rc = getattr(self.lib, name)(self.h, *args, None if stream is None else _stream_ptr(stream))
-        return rc if rc == OK else _check(rc, name, allow)
+    def _at(self, tables: Tables) -> int:
+        """The GPU of the handle, which is open and reaches the tables."""
+        ctx = self.ctx
+        if self.h is None or ctx.h is None:
+            raise TuttiError(EINVAL, "pages: the handle or its context is closed")
+        at = ctx.device
+        if tables._at != at:
+            _reachable(at, tables._keep)
+        return at
 
     def tutti_pages_fork(self, frm: Tables, parent, to: Tables, move: int = FORK_KEEP, stream=None, allow: Sequence[int] = ()) -> int:
         """Row s of `to` becomes row parent[s] (int32; -1: empty) of `frm`; FORK_MOVE gives up the rows of `frm`."""
-        return self._call("tutti_pages_fork", (frm, to), (frm, _ints(parent, self.ctx.device, "parent", to.n_seq), to, move), stream, allow)
+        at = self._at(frm)
+        if to._at != at:
+            _reachable(at, to._keep)
+        rc = self.lib.tutti_pages_fork(self.h, frm, _ints(parent, at, "parent", to.n_seq), to, move, None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_pages_fork", allow)
 
     def tutti_pages_extend(self, tables: Tables, n_new, pairs, stream=None, allow: Sequence[int] = ()) -> int:
         """Room for n_new[s] (int32) more tokens of every row; pairs [rows, 2] int32 receives the blocks to copy."""
-        at = self.ctx.device
-        return self._call("tutti_pages_extend", (tables,), (tables, _ints(n_new, at, "n_new", tables.n_seq), _ints(pairs, at, "pairs", 2 * tables.n_seq)), stream, allow)
+        at, n = self._at(tables), tables.n_seq
+        rc = self.lib.tutti_pages_extend(self.h, tables, _ints(n_new, at, "n_new", n), _ints(pairs, at, "pairs", 2 * n), None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_pages_extend", allow)
 
     def tutti_pages_release(self, tables: Tables, which=None, stream=None, allow: Sequence[int] = ()) -> int:
         """Free the rows with which[s] (bool or uint8), or all of them."""
-        flags = None
+        at, flags = self._at(tables), None
         if which is not None:
             if str(which.dtype) not in ("torch.bool", "torch.uint8") or not which.is_contiguous() or which.numel() < tables.n_seq:
                 raise TuttiError(EINVAL, "which (bool or uint8, contiguous, an element a row)")
-            if which.get_device() != self.ctx.device:
-                _reachable(self.ctx.device, (which,))
+            if which.get_device() != at:
+                _reachable(at, (which,))
             flags = which.data_ptr()
-        return self._call("tutti_pages_release", (tables,), (tables, flags), stream, allow)
+        rc = self.lib.tutti_pages_release(self.h, tables, flags, None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_pages_release", allow)
 
     def tutti_pages_trim(self, tables: Tables, window: Window, stream=None, allow: Sequence[int] = ()) -> int:
         """Free the blocks that no later row sees under the window."""
-        return self._call("tutti_pages_trim", (tables,), (tables, window), stream, allow)
+        self._at(tables)
+        rc = self.lib.tutti_pages_trim(self.h, tables, window, None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_pages_trim", allow)
 
     def tutti_pages_compact(self, tables: Tables, pairs, n_pairs, stream=None, allow: Sequence[int] = ()) -> int:
         """Move blocks in use to the lowest ids, at most len(pairs); pairs [n, 2] and n_pairs [1] (int32) receive the moves."""
-        at = self.ctx.device
-        if len(pairs.shape) != 2 or pairs.shape[1] != 2:
-            raise TuttiError(EINVAL, "tutti_pages_compact: pairs are not [n, 2]")
-        return self._call("tutti_pages_compact", (tables,), (tables, _ints(pairs, at, "pairs"), pairs.shape[0], _ints(n_pairs, at, "n_pairs", 1)), stream, allow)
+        at, n = self._at(tables), _pairs(pairs, "tutti_pages_compact")
+        rc = self.lib.tutti_pages_compact(self.h, tables, _ints(pairs, at, "pairs"), n, _ints(n_pairs, at, "n_pairs", 1), None if stream is None else _stream_ptr(stream))
+        return rc if rc == OK else _check(rc, "tutti_pages_compact", allow)
 
 
 class Ring:
