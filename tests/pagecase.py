@@ -99,6 +99,9 @@ def extend(t, refs, n_new):
             need.append((s, b0 + held - 1, True))
         need += [(s, b0 + k, False) for k in range(held, blocks_of(n + add, t.bs))]
     free = [i for i, x in enumerate(refs) if x == 0]
+    if len(need) > t.n_blk:                                     # rows that lie over each other
+        t.status.add(T.EINVAL)
+        return pairs
     if len(need) > len(free):
         t.status.add(T.EAGAIN)
         return pairs

@@ -269,3 +269,34 @@ def test_rows_of_two_tables_share_counts():
         assert int(m.status) == T.OK
     finally:
         m.close()
+
+
+def test_a_save_behind_a_copy_sees_what_was_copied():
+    """The kernels of a save may start while the kernel in front of them runs, if that one lets them: it does not."""
+    n, bs, hk, dim = 3000, 16, 8, 128
+    bb = bs * hk * dim * 2
+    ctx = T.Context(T.Geom(1, hk, dim, 2, bs, bs, 1, T.LAYOUT_LAYER_MAJOR, n // 2), 0)
+    pool, store = torch.empty(2, n, bb, dtype=torch.uint8, device=DEV), torch.empty(int(ctx.layout.dev_bytes), dtype=torch.uint8, device=DEV)
+    ring = T.Ring(ctx, 16, 2048, n, n)
+    try:
+        ctx.tutti_pool_register(0, pool[0].data_ptr(), pool[1].data_ptr(), bb, n)
+        ctx.tutti_store_register(0, store.data_ptr(), store.numel())
+        half = n // 2
+        to = list(range(half, n))
+        batch = T.make_batch(ints([half * bs]), ints([0, half]), ints(list(range(half))), ints([0, half]), ints(to))
+        pairs = ints([[i, half + i] for i in range(half)])
+        for i in range(5):
+            pool.fill_(0)
+            store.fill_(0)
+            pool[:, :half] = torch.arange(half, device=DEV).remainder(200).add(1 + i).to(torch.uint8)[None, :, None]
+            _, first, k = ring.tutti_build_sqes(batch, 0, T.OP_WRITE)
+            torch.cuda.synchronize()
+            ctx.tutti_kv_copy_blocks(0, 1, pairs)
+            ring.tutti_kv_save_layer(first, k)
+            rc, _, err, _ = ring.tutti_ring_poll_range(first, k, 5_000_000_000)
+            assert rc == T.OK and err == T.OK
+            assert torch.equal(store.view(half, 2, bb), pool[:, :half].transpose(0, 1))
+    finally:
+        torch.cuda.synchronize()
+        ring.close()
+        ctx.close()

@@ -151,6 +151,21 @@ def test_extend_takes_all_or_nothing(contexts, n_free):
         b.close()
 
 
+def test_extend_rows_that_lie_over_each_other(contexts):
+    """Starts that go back make rows of the same entries: more new blocks than entries are refused, before any list runs out."""
+    book = P.Book([0, 5, 0, 5], [-7] * 5, [0, 0, 0], 4)
+    refs = [0] * 20
+    b = P.Bound(contexts(4), [book], refs)
+    pairs = torch.zeros(3, 2, dtype=torch.int32, device=b.dev)
+    try:
+        b.pages.tutti_pages_extend(b.tables(), ints([20, 0, 20]), pairs)
+        assert pairs.tolist() == [list(p) for p in P.extend(book, refs, [20, 0, 20])]
+        assert not any(refs) and book.status == {T.EINVAL}
+        b.same(refs)
+    finally:
+        b.close()
+
+
 def test_extend_among_millions_of_blocks(contexts):
     """More tiles of counts than threads; the lowest free ids are far behind."""
     bs, n = 16, 5_000_000
