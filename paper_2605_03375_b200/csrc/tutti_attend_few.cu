@@ -156,6 +156,7 @@ __global__ void __launch_bounds__(WARPS * 32, Few<T, C8, D, NB>::WORKERS_PER_SM)
 attend_few_kernel(const __grid_constant__ AttendParams p, const Workspace ws) {
     using F = Few<T, C8, D, NB>;
     using M = typename F::M;
+    if constexpr (WIN) asm volatile("griddepcontrol.wait;" ::: "memory");
     extern __shared__ __align__(128) unsigned char smem[];
     const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x & 31, g = lane / 4, c = lane % 4;
     unsigned char *ring = smem + warp * F::STAGES * F::STAGE;
@@ -675,7 +676,8 @@ template <typename T, bool C8, int D, int NB, bool WIN>
 cudaError_t launch_few(const AttendParams &p, Workspace ws, int sms, cudaStream_t st) {
     using F = Few<T, C8, D, NB>;
     ws.workers = sms * F::WORKERS_PER_SM;
-    return launch_plain(attend_few_kernel<T, C8, D, NB, WIN>, ws.workers, WARPS * 32, F::SMEM, st, p, ws);
+    if constexpr (WIN) return launch_behind(attend_few_kernel<T, C8, D, NB, WIN>, ws.workers, WARPS * 32, F::SMEM, st, p, ws);
+    else return launch_plain(attend_few_kernel<T, C8, D, NB, WIN>, ws.workers, WARPS * 32, F::SMEM, st, p, ws);
 }
 
 template <typename T, bool C8, int D, int NB, bool WIN>

@@ -427,6 +427,7 @@ template <typename T, bool C8, int D, bool WIN>
 __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_constant__ AttendParams p, const __grid_constant__ PoolMaps maps, const Workspace ws) {
     using C = Many<T, C8, D>;
     constexpr int SUB = C::SUB, STEPS = C::STEPS;
+    if constexpr (WIN) asm volatile("griddepcontrol.wait;" ::: "memory");
     extern __shared__ unsigned char raw[];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
     unsigned char *sm = raw + (base - smem_addr(raw));
@@ -1181,7 +1182,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 
 template <typename T, bool C8, int D>
 cudaError_t launch(const AttendParams &p, const PoolMaps &maps, const Workspace &ws, cudaStream_t st) {
-    return p.window ? launch_plain(attend_many_kernel<T, C8, D, true>, ws.workers, THREADS, Many<T, C8, D>::SMEM, st, p, maps, ws)
+    return p.window ? launch_behind(attend_many_kernel<T, C8, D, true>, ws.workers, THREADS, Many<T, C8, D>::SMEM, st, p, maps, ws)
                     : launch_plain(attend_many_kernel<T, C8, D, false>, ws.workers, THREADS, Many<T, C8, D>::SMEM, st, p, maps, ws);
 }
 

@@ -116,6 +116,7 @@ __device__ inline uint32_t zeros(const int4 &v) { return (v.x == 0) + (v.y == 0)
 // old rows together and adds up what neighbours that hold the same block at the same place do to its count: the beams of
 // a request share their prompt, and what one loses there another gains, so that most blocks need no atomic at all.
 __global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, const TablesDev from, const int32_t *parent, const TablesDev to, uint32_t move, uint32_t per, uint32_t segs) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t row = blockIdx.x / per, part = blockIdx.x % per;
     Row r, child;
     if (row < to.n_seq) {
@@ -308,6 +309,7 @@ __device__ inline uint32_t last_at(const uint32_t *begin, uint32_t n, uint32_t k
 }
 
 __global__ void __launch_bounds__(PLAN_THREADS) extend_kernel(const PagesDev p, const TablesDev t, const uint32_t *n_new, int32_t *pairs) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     __shared__ unsigned long long sums[32];
     __shared__ uint32_t sums32[32], first[PLAN_THREADS], ranks[SEARCH], entries[PLAN_THREADS];
     __shared__ bool last, copies[PLAN_THREADS];
@@ -399,6 +401,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) extend_kernel(const PagesDev p, 
 // release and trim: `per` CTAs a row.  Release clears a row's length once all its CTAs have read it: the last to
 // say so does it, and the entries are independent of that.
 __global__ void __launch_bounds__(ROW_THREADS) release_kernel(const PagesDev p, const TablesDev t, const uint8_t *which, uint32_t per) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t s = blockIdx.x / per, part = blockIdx.x % per;
     if (which && !which[s]) return;
     Row r;
@@ -422,6 +425,7 @@ __global__ void __launch_bounds__(ROW_THREADS) release_kernel(const PagesDev p, 
 }
 
 __global__ void __launch_bounds__(ROW_THREADS) trim_kernel(const PagesDev p, const TablesDev t, uint32_t window, uint32_t sinks, uint32_t per) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t s = blockIdx.x / per, part = blockIdx.x % per;
     Row r;
     if (!row_view(t, s, r)) {
@@ -443,6 +447,7 @@ __global__ void __launch_bounds__(ROW_THREADS) trim_kernel(const PagesDev p, con
 // compact, with u(i) the blocks in use below i and n all of them: a free block f < n is the destination
 // number f - u(f), a block in use s >= n is the source number n - 1 - u(s), and there are n - u(n) of each.
 __global__ void __launch_bounds__(PLAN_THREADS) compact_count_kernel(const PagesDev p) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     __shared__ uint32_t sums[32];
     uint32_t n;
@@ -650,7 +655,7 @@ int tutti_pages_fork(tutti_pages_t *pages, const tutti_tables_t *from, const int
     const uint32_t groups = (from->n_seq + GROUP - 1) / GROUP;
     const uint32_t per = ctas_a_row(rows, from->n_blk / 2 + to->n_blk / 2, ROW_IDS, tutti_ctx_sms_(pages->ctx));
     const uint32_t segs = groups ? ctas_a_row(groups, from->n_blk / GROUP, ROW_THREADS, tutti_ctx_sms_(pages->ctx)) : 0;
-    const cudaError_t e = launch_plain(fork_kernel, per * to->n_seq + segs * groups, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, from), parent, on_device(pages, to), move, per, segs);
+    const cudaError_t e = launch_behind(fork_kernel, per * to->n_seq + segs * groups, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, from), parent, on_device(pages, to), move, per, segs);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "fork launch");
 }
 
@@ -660,7 +665,7 @@ int tutti_pages_extend(tutti_pages_t *pages, const tutti_tables_t *t, const uint
     if (!t->n_seq) return TUTTI_OK;
     OnDevice on(pages->device);
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
-    const cudaError_t e = launch_plain(extend_kernel, pages->dev.n_tiles + 1, PLAN_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), n_new, pairs);
+    const cudaError_t e = launch_behind(extend_kernel, pages->dev.n_tiles + 1, PLAN_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), n_new, pairs);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "extend launch");
 }
 
@@ -671,7 +676,7 @@ int tutti_pages_release(tutti_pages_t *pages, const tutti_tables_t *t, const uin
     OnDevice on(pages->device);
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const uint32_t per = ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, tutti_ctx_sms_(pages->ctx));
-    const cudaError_t e = launch_plain(release_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), which, per);
+    const cudaError_t e = launch_behind(release_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), which, per);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "release launch");
 }
 
@@ -683,7 +688,7 @@ int tutti_pages_trim(tutti_pages_t *pages, const tutti_tables_t *t, const tutti_
     OnDevice on(pages->device);
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const uint32_t per = ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, tutti_ctx_sms_(pages->ctx));
-    const cudaError_t e = launch_plain(trim_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), window->window, window->sinks, per);
+    const cudaError_t e = launch_behind(trim_kernel, per * t->n_seq, ROW_THREADS, 0, (cudaStream_t)stream, pages->dev, on_device(pages, t), window->window, window->sinks, per);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "trim launch");
 }
 
@@ -697,9 +702,7 @@ int tutti_pages_compact(tutti_pages_t *pages, const tutti_tables_t *t, int32_t *
     const uint32_t per = t->n_seq ? ctas_a_row(t->n_seq, t->n_blk, ROW_THREADS, sms) : 1;
     const uint32_t movers = max_pairs / ROW_THREADS + 1 < (uint32_t)sms ? max_pairs / ROW_THREADS + 1 : (uint32_t)sms;
     cudaError_t e = cudaSuccess;
-    // The kernels of this call may be resident before the one in front has ended, and wait for it.  The last one lets nothing
-    // start early: what a program launches behind it may not wait.
-    if (d.n_tiles > SMALL) e = launch_plain(compact_count_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d);
+    if (d.n_tiles > SMALL) e = launch_behind(compact_count_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d);
     if (e == cudaSuccess) e = launch_behind(compact_plan_kernel, d.n_tiles, PLAN_THREADS, 0, (cudaStream_t)stream, d, pairs, max_pairs);
     if (e == cudaSuccess) e = launch_behind(compact_apply_kernel, per * t->n_seq + movers, ROW_THREADS, 0, (cudaStream_t)stream, d, on_device(pages, t), pairs, max_pairs, n_pairs, per);
     return e == cudaSuccess ? TUTTI_OK : fail(e, "compact launch");

@@ -84,6 +84,7 @@ __global__ void __launch_bounds__(THREADS, 1) copy_blocks_kernel(const __grid_co
         fence_proxy_async();
     }
     __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const uint32_t n_pairs = p.n_pairs ? min(*p.n_pairs, p.max_pairs) : p.max_pairs;
     const uint32_t a_round = p.width * p.levels;
 
@@ -267,6 +268,7 @@ __global__ void __launch_bounds__(THREADS, 1) copy_blocks_kernel(const __grid_co
         }
         bulk_wait_all();
     }
+    __threadfence();
 }
 
 }  // namespace
@@ -320,7 +322,7 @@ int tutti_kv_copy_blocks(tutti_ctx_t *ctx, uint32_t first_layer, uint32_t n_laye
         // Halved as long as the last tickets have LAST_TICKET bytes, if all pairs of a round count; not for a few us of work.
         uint64_t share = 2 * p.block_bytes * p.n_layers * (max_pairs < LIST ? max_pairs : LIST) / p.width;
         for (share = share < 16 * LAST_TICKET ? 0 : share; share > LAST_TICKET && p.levels < most; share = share * 3 / 5) ++p.levels;
-        const cudaError_t e = launch_plain(copy_blocks_kernel, rounds * p.levels * p.width, THREADS, SMEM, (cudaStream_t)stream, p);
+        const cudaError_t e = launch_behind(copy_blocks_kernel, rounds * p.levels * p.width, THREADS, SMEM, (cudaStream_t)stream, p);
         if (e != cudaSuccess) return fail(e, "copy launch");
     }
     return TUTTI_OK;
