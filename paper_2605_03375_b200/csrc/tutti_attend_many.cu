@@ -399,6 +399,16 @@ __host__ __device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __n
     return high;
 }
 
+// The units [u, u + n) of a tile of n_units that a worker has: published by the warps that bring the queries, so that the
+// walk over tiles stands in the code of fewer roles.  SHARES: one that is published, one whose products run, one that the softmax may not
+// have taken yet, and one to spare.
+constexpr uint32_t SHARES = 4;
+struct Share {
+    uint32_t n, u, n_units, gap;        // gap: units left out behind the first tokens'
+    uint32_t q, h, q0, n_rows;          // tile of the head, KV head, first row of the sequence in the step, rows of a head
+    int64_t first;                      // position of the first new token
+};
+
 template <typename T, bool C8, int D>
 struct Many {
     static constexpr int SUB = C8 ? SUB_8 : SUB_16, STEPS = BN / SUB;
@@ -407,12 +417,13 @@ struct Many {
     static constexpr uint32_t OFF_RING = 2 * KV;            // behind the two halves of Q
     static constexpr uint32_t OFF_RAW = OFF_RING + RING * KV;          // 8-bit: codes of a group's values
     static constexpr uint32_t OFF_BAR = OFF_RAW + (C8 ? 2 * ATOM : 0);
-    static constexpr uint32_t OFF_EXISTS = OFF_BAR + 288;   // [8 units][4]: keys that exist
+    static constexpr uint32_t OFF_EXISTS = OFF_BAR + 320;   // [8 units][4]: keys that exist
     static constexpr bool UNITS = C8 && std::is_same<T, __half>::value;
     static constexpr uint32_t OFF_UNITS = OFF_EXISTS + 128; // [8 units][2 steps]: exponents of keys' and values' units
     static constexpr uint32_t OFF_MISC = OFF_UNITS + (UNITS ? 128 : 0);
     static constexpr uint32_t OFF_TILE = OFF_MISC + 320;
-    static constexpr uint32_t SMEM = OFF_TILE + 256 + 1024; // 1024: alignment of the dynamic part
+    static constexpr uint32_t OFF_SHARE = OFF_TILE + 256;   // [SHARES] what the worker has of its tiles
+    static constexpr uint32_t SMEM = OFF_SHARE + SHARES * sizeof(Share) + 1024;     // 1024: alignment of the dynamic part
     // f16 probabilities are kept 2^6 times too large (at most 2^14): full precision down to 2^-20
     static constexpr float OFF = std::is_same<T, __half>::value ? 6.0f : 0.0f;
     // whether widened codes keep their order
@@ -440,7 +451,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     volatile uint32_t *dead = misc + 72;
     const uint32_t bars = base + C::OFF_BAR;
     const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, o_full = bars + 80, o_empty = bars + 96,
-                   joined = bars + 112, drain = bars + 128, raw_full = bars + 136, s_full = bars + 200, p_full = bars + 232, o_done = bars + 264;
+                   joined = bars + 112, drain = bars + 128, raw_full = bars + 136, s_full = bars + 200, p_full = bars + 232, o_done = bars + 264, share_full = bars + 280;
+    Share *shares = reinterpret_cast<Share *>(sm + C::OFF_SHARE);
 
     // ---- this worker's share ----
     unsigned long long *sums = reinterpret_cast<unsigned long long *>(misc);
@@ -521,6 +533,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             mbar_init(p_full + 8 * i, 4);
         }
         mbar_init(drain, 1);
+        for (uint32_t i = 0; i < SHARES; ++i) mbar_init(share_full + 8 * i, 1);
         for (int i = 0; i < 2 * RING; ++i) mbar_init(raw_full + 8 * i, 1);
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -754,8 +767,8 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 fetch(0);
                 if (!(ok = room(1))) break;
                 fetch(1);
-                step_unit();
-                step_unit();
+#pragma unroll 1
+                for (int k = 0; k < 2; ++k) step_unit();
                 locate();                               // the next unit's ids arrive while this one's rows do
                 if (!by_tile) {                         // tensor copies arrive at `full` by themselves
                     cp_wait<1>();
@@ -800,23 +813,35 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         uint32_t segs = 0;
         for (unsigned long long x = x0; x < x1; ++segs) {
             const uint32_t n = (uint32_t)min(x1 - x, (unsigned long long)(t.n_units - t.u));
+            if (warp == Q_WARP && lane == 0) {
+                shares[segs % SHARES] = Share{n, t.u, t.n_units, gap_of(t), t.q, t.h, t.v.q0, t.r.n_rows, t.r.first};
+                mbar_arrive(share_full + 8 * (segs % SHARES));
+            }
             bool ok = !segs || mbar_wait(q_empty, (segs - 1) & 1, dead);
             if (!__all_sync(0xffffffffu, ok)) break;
-            constexpr int CH = D / 8;
-#pragma unroll 4
-            for (uint32_t i = warp - Q_WARP; i < TILE_ROWS * CH / 32; i += Q_WARPS) {
-                const uint32_t r = (i * 32 + lane) / CH, ch = lane % CH, row = t.q * TILE_ROWS + r;
-                const bool in = row < t.r.n_rows;           // zeros behind the last row
-                const uint32_t k = in ? p.token_of(row) : 0, h = t.h * p.group + (in ? p.member_of(row) : 0);
-                const T *src = (const T *)p.q + (uint64_t)(t.v.q0 + k) * p.q_stride + (uint64_t)h * D + ch * 8;
-                const uint32_t dst = r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch);
-                cp16(base + dst, src, in);
+            constexpr int CH = D / 8, RPI = 32 / CH;        // 16-byte chunks of a row; rows a warp takes at once
+            const uint32_t ch = lane % CH, sub = lane / CH;
+#pragma unroll 1
+            for (uint32_t b = warp - Q_WARP; b < TILE_ROWS / 32; b += Q_WARPS) {
+                const uint32_t mine = t.q * TILE_ROWS + b * 32 + lane;
+                const bool in = mine < t.r.n_rows;          // zeros behind the last row
+                const uint32_t k = in ? p.token_of(mine) : 0, h = t.h * p.group + (in ? p.member_of(mine) : 0);
+                const uint64_t src = in ? (uint64_t)((const T *)p.q + (uint64_t)(t.v.q0 + k) * p.q_stride + (uint64_t)h * D) : 0;
+#pragma unroll
+                for (uint32_t it = 0; it < CH; ++it) {
+                    const uint32_t r = b * 32 + it * RPI + sub;
+                    const uint64_t from = __shfl_sync(0xffffffffu, src, r % 32);
+                    cp16(base + r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch), (const void *)((from ? from : (uint64_t)p.q) + ch * 16), from != 0);
+                }
             }
             cp_commit();
             cp_wait<0>();
             if constexpr (!C::ORDERED) {                    // each lane what it brought itself
-                for (uint32_t i = warp - Q_WARP; i < TILE_ROWS * CH / 32; i += Q_WARPS) {
-                    const uint32_t r = (i * 32 + lane) / CH, ch = lane % CH;
+#pragma unroll 1
+                for (uint32_t b = warp - Q_WARP; b < TILE_ROWS / 32; b += Q_WARPS)
+#pragma unroll 4
+                for (uint32_t it = 0; it < CH; ++it) {
+                    const uint32_t r = b * 32 + it * RPI + sub;
                     uint4 *at = reinterpret_cast<uint4 *>(sm + r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch));
                     const uint4 u = *at;
                     *at = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.x, u.y, 0x7632),
@@ -870,17 +895,17 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             auto all = [](bool x) { return (bool)__all_sync(0xffffffffu, x); };
             auto landed = [&](uint32_t u, uint32_t kv) { return mbar_wait(full + 8 * slot(u, kv), (u / 2) & 1, dead); };
             for (unsigned long long x = x0; x < x1 && ok;) {
-                const uint32_t n = (uint32_t)min(x1 - x, (unsigned long long)(t.n_units - t.u));
-                const int halves = t.r.n_rows - t.q * TILE_ROWS > HALF_ROWS ? 2 : 1;
                 ok = all(mbar_wait(q_full, segs & 1, dead) && landed(n_unit, 0));
                 if (!ok) break;
+                const Share &t = shares[segs % SHARES];         // published before the queries were brought
+                const uint32_t n = t.n;
+                const int halves = t.n_rows - t.q * TILE_ROWS > HALF_ROWS ? 2 : 1;
                 tc_after();
                 for (int u = 0; u < STEPS; ++u)
                     for (int i = 0; i < halves; ++i) qk(i, u, slot(n_unit, 0));
                 commit(empty + 8 * slot(n_unit, 0));
                 if (n == 1) commit(q_empty);            // behind the last Q K^T of the tile
                 x += n;
-                if (x < x1) next_tile(p, t);            // while the softmax has the first scores
                 for (uint32_t j = 0; j < n && ok; ++j, ++n_unit) {
                     const bool more = j + 1 < n;
                     ok = all(landed(n_unit, 1) && (!more || landed(n_unit + 1, 0)));
@@ -892,6 +917,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                             tc_after();
                             pv(i, u, slot(n_unit, 1), j > 0 || u > 0);
                             if (more) qk(i, u, slot(n_unit + 1, 0));
+                            else if (u == STEPS - 1) commit(o_done + 8 * i);
                             np[i] += u == STEPS - 1;
                         }
                     if (!ok) break;
@@ -900,10 +926,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     if (j + 2 == n) commit(q_empty);
                 }
                 if (!ok) break;
-                for (int i = 0; i < halves; ++i) {
-                    commit(o_done + 8 * i);
-                    ++ns[i];
-                }
+                for (int i = 0; i < halves; ++i) ++ns[i];
                 ++segs;
             }
             // every matrix instruction has ended before TMEM is given back
@@ -922,7 +945,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         // largest; the smallest number there is makes the largest score of a zero scale less than 2^-20.
         const float scl_all = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 0x1p-149f);
         const bool negative = p.scale < 0;
-        uint32_t n_s = 0, n_seg = 0, n_unit = 0, n_join = 0;                 // steps of this half; units of the worker
+        uint32_t n_s = 0, n_seg = 0, n_unit = 0, n_join = 0, n_share = 0;    // steps of this half; units of the worker
         bool ok = true;
         auto join = [&]() {                                       // the half's four warps
             __syncwarp();
@@ -931,16 +954,20 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             return (bool)__all_sync(0xffffffffu, there);
         };
         for (unsigned long long x = x0; x < x1 && ok;) {
-            const uint32_t n = (uint32_t)min(x1 - x, (unsigned long long)(t.n_units - t.u));
+            ok = mbar_wait(share_full + 8 * (n_share % SHARES), n_share / SHARES & 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const Share t = shares[n_share++ % SHARES];
+            const uint32_t n = t.n;
             const uint32_t row = t.q * TILE_ROWS + i * HALF_ROWS + r;
-            if (t.q * TILE_ROWS + i * HALF_ROWS < t.r.n_rows) {
-                const bool in = row < t.r.n_rows;
+            if (t.q * TILE_ROWS + i * HALF_ROWS < t.n_rows) {
+                const bool in = row < t.n_rows;
                 // rows behind the last take the last one's position: they are computed and dropped
-                const uint32_t tok = p.token_of(in ? row : t.r.n_rows - 1);
-                const int64_t pos = t.r.first + tok;
+                const uint32_t tok = p.token_of(in ? row : t.n_rows - 1);
+                const int64_t pos = t.first + tok;
                 const int64_t pos_low = __shfl_sync(0xffffffffu, pos, 0);
                 const int64_t hidden = WIN ? __shfl_sync(0xffffffffu, pos, 31) - p.window : 0;      // keys up to here are not seen by every row
-                const uint32_t gap = gap_of(t);
+                const uint32_t front = WIN ? (p.sinks + BN - 1) / BN : 0;
                 float m = -INFINITY, l = 0;
                 int o_unit = UNIT_LEAST_V;                        // UNITS: exponent of the output's unit, the largest of its values'
                 const uint32_t steps = STEPS * n;
@@ -971,7 +998,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     tc_wait_ld();
 #pragma unroll
                     for (int q = 0; q < SUB / 32; ++q) tc_loaded(sr + 32 * q);
-                    const int64_t key0 = (int64_t)key_unit(t, t.u + j / STEPS, gap) * BN + j % STEPS * SUB;
+                    const int64_t key0 = (int64_t)(t.u + j / STEPS + (WIN && t.u + j / STEPS >= front ? t.gap : 0)) * BN + j % STEPS * SUB;
                     if (negative) {
 #pragma unroll
                         for (int k = 0; k < SUB; ++k) s[k] = -s[k];
@@ -1068,105 +1095,123 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     m += (float)(o_unit - UNIT_LEAST_V);
                     l *= pow2(UNIT_LEAST_V - o_unit);
                 }
-                bool write = true;
                 const bool whole = t.u == 0 && n == t.n_units;
-                float o[D];
-#pragma unroll
-                for (int q = 0; q < D / 32; ++q) tc_ld32(reinterpret_cast<uint32_t *>(o) + 32 * q, o_at + 32 * q);
+                uint32_t w0 = 0, w1 = 0;
+                if (!whole) holders(x - t.u, t.n_units, workers, total, w0, w1);
+            // Outputs in pieces of 32 dimensions, by loops that are not unrolled: a tile's end is code that has to be fetched, and
+            // all 128 at once spilled 1 KB a thread (8 us from a tile's last score to the next one's first; so 5).
+            auto outputs = [&](uint32_t q, float (&o)[32]) {
+                tc_ld32(reinterpret_cast<uint32_t *>(o), o_at + 32 * q);
                 tc_wait_ld();
-#pragma unroll
-                for (int q = 0; q < D / 32; ++q) tc_loaded(reinterpret_cast<uint32_t *>(o) + 32 * q);
+                tc_loaded(reinterpret_cast<uint32_t *>(o));
+            };
+            auto given_back = [&]() {                              // the outputs' place
                 tc_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(o_empty + 8 * i);
-                if (!whole) {
-                    const unsigned long long tile0 = x - t.u;
-                    uint32_t w0, w1;
-                    holders(tile0, t.n_units, workers, total, w0, w1);
-                    auto slot = [&](uint32_t k) { return (k == w0 ? 2 * k + 1 : 2 * k) * 2 + i; };
-                    float4 *part = reinterpret_cast<float4 *>(ws.part);
-                    float2 *ml = reinterpret_cast<float2 *>(ws.part + (uint64_t)4 * ws.workers * HALF_ROWS * D);
-                    auto at = [&](uint32_t k, int d4) { return part + ((uint64_t)slot(k) * (D / 4) + d4) * HALF_ROWS + r; };
+            };
+            bool write = true;
+            auto slot = [&](uint32_t k) { return (k == w0 ? 2 * k + 1 : 2 * k) * 2 + i; };
+            float4 *part = reinterpret_cast<float4 *>(ws.part);
+            float2 *ml = reinterpret_cast<float2 *>(ws.part + (uint64_t)4 * ws.workers * HALF_ROWS * D);
+            auto at = [&](uint32_t k, uint32_t d4) { return part + ((uint64_t)slot(k) * (D / 4) + d4) * HALF_ROWS + r; };
+            if (!whole) {
+#pragma unroll 1
+                for (uint32_t q = 0; q < D / 32; ++q) {
+                    float o[32];
+                    outputs(q, o);
 #pragma unroll
-                    for (int d = 0; d < D / 4; ++d) *at(w, d) = make_float4(o[4 * d], o[4 * d + 1], o[4 * d + 2], o[4 * d + 3]);
-                    ml[(uint64_t)slot(w) * HALF_ROWS + r] = make_float2(m, l);
-                    if (!(ok = join())) break;
-                    if (r == 0) {
-                        const uint32_t old = arrive_gpu(ws.count + 2 * w0 + i);
-                        if (old == w1 - w0) ws.count[2 * w0 + i] = 0;            // ready for the next call
-                        misc[74 + i] = old == w1 - w0;
-                    }
-                    if (!(ok = join())) break;
-                    write = *(volatile uint32_t *)(misc + 74 + i);
-                    if (write) {
-                        m = -INFINITY;
-                        l = 0;
-#pragma unroll 4
-                        for (uint32_t k = w0; k <= w1; ++k) m = fmaxf(m, __ldcg(ml + (uint64_t)slot(k) * HALF_ROWS + r).x);
-#pragma unroll
-                        for (int d = 0; d < D; ++d) o[d] = 0;
-                        for (uint32_t k = w0; k <= w1; ++k) {
-                            const float2 e = __ldcg(ml + (uint64_t)slot(k) * HALF_ROWS + r);
-                            const float c = m == -INFINITY ? 0.0f : ex2(e.x - m);
-                            l += e.y * c;
-#pragma unroll
-                            for (int d = 0; d < D / 4; ++d) {
-                                const float4 b = __ldcg(at(k, d));
-                                o[4 * d] += b.x * c, o[4 * d + 1] += b.y * c, o[4 * d + 2] += b.z * c, o[4 * d + 3] += b.w * c;
-                            }
-                        }
-                    }
+                    for (uint32_t d = 0; d < 8; ++d) *at(w, 8 * q + d) = make_float4(o[4 * d], o[4 * d + 1], o[4 * d + 2], o[4 * d + 3]);
                 }
-                // The compiler spills about 1 KB a thread here (o, the joined parts, the pieces below), none of it in the
-                // loop over units: it costs once a tile.
+                ml[(uint64_t)slot(w) * HALF_ROWS + r] = make_float2(m, l);
+                given_back();
+                if (!(ok = join())) break;
+                if (r == 0) {
+                    const uint32_t old = arrive_gpu(ws.count + 2 * w0 + i);
+                    if (old == w1 - w0) ws.count[2 * w0 + i] = 0;            // ready for the next call
+                    misc[74 + i] = old == w1 - w0;
+                }
+                if (!(ok = join())) break;
+                write = *(volatile uint32_t *)(misc + 74 + i);
                 if (write) {
-                    const uint64_t token = t.v.q0 + tok;
-                    const uint32_t qh = t.h * p.group + p.member_of(in ? row : t.r.n_rows - 1);
-                    // l, not m, tells a row that saw nothing: scores of NaN move no maximum, but make the sum NaN
-                    const float inv = l == 0 ? 0.0f : (C::UNITS ? pow2(UNIT_LEAST_V) : 1.0f) / l;
-                    const unsigned long long mine = in ? (unsigned long long)((T *)p.out + token * p.out_stride + (uint64_t)qh * D) : 0;
-                    unsigned long long to[4];               // the rows of the lane's quad
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) to[k] = __shfl_sync(0xffffffffu, mine, (lane & ~3u) + k);
-                    // A thread has a row, a store wants neighbouring lanes on neighbouring bytes: the four lanes
-                    // of a quad exchange 16-byte pieces, so that a store writes 64 bytes of a row (a piece of its
-                    // own row a lane made a store of 32 separate lines: 3 us a tile, and the load of the next
-                    // tile's queries behind it)
-#pragma unroll
-                    for (int d = 0; d < D / 8; d += 4) {
-                        uint32_t piece[4][4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            constexpr int B = C::ORDERED ? 1 : 2, E = C::ORDERED ? 2 : 1;      // where elements 1 and 2 of four are
-                            const float *e = o + 8 * (d + k);
-                            piece[k][0] = pack2(e[0] * inv, e[B] * inv, T()), piece[k][1] = pack2(e[E] * inv, e[3] * inv, T());
-                            piece[k][2] = pack2(e[4] * inv, e[4 + B] * inv, T()), piece[k][3] = pack2(e[4 + E] * inv, e[7] * inv, T());
-                        }
-                        // (row, piece) to (piece, row): the off-diagonal blocks change places, at distance 2 and 1
-#pragma unroll
-                        for (int dist = 2; dist; dist >>= 1)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) {
-                                if (k & dist) continue;
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) {
-                                    const bool up = lane & dist;
-                                    const uint32_t give = up ? piece[k][i] : piece[k + dist][i];
-                                    const uint32_t got = __shfl_xor_sync(0xffffffffu, give, dist);
-                                    if (up) piece[k][i] = got;
-                                    else piece[k + dist][i] = got;
-                                }
-                            }
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (to[k]) *reinterpret_cast<uint4 *>(to[k] + (d + (lane & 3)) * 16) = make_uint4(piece[k][0], piece[k][1], piece[k][2], piece[k][3]);
-                    }
-                    if (p.lse && in) p.lse[token * p.n_q_heads + qh] = l == 0 ? -INFINITY : (m - C::OFF + log2f(l)) * 0.6931471805599453f;
+                m = -INFINITY;
+                l = 0;
+#pragma unroll 4
+                for (uint32_t k = w0; k <= w1; ++k) m = fmaxf(m, __ldcg(ml + (uint64_t)slot(k) * HALF_ROWS + r).x);
+#pragma unroll 4
+                for (uint32_t k = w0; k <= w1; ++k) {
+                    const float2 e = __ldcg(ml + (uint64_t)slot(k) * HALF_ROWS + r);
+                    l += e.y * (m == -INFINITY ? 0.0f : ex2(e.x - m));
                 }
+                }
+            }
+            if (write) {
+            const uint64_t token = t.q0 + tok;
+            const uint32_t qh = t.h * p.group + p.member_of(in ? row : t.n_rows - 1);
+            const unsigned long long out_row = in ? (unsigned long long)((T *)p.out + token * p.out_stride + (uint64_t)qh * D) : 0;
+            float *lse_at = p.lse && in ? p.lse + token * p.n_q_heads + qh : nullptr;
+            // l, not m, tells a row that saw nothing: scores of NaN move no maximum, but make the sum NaN
+            const float inv = l == 0 ? 0.0f : (C::UNITS ? pow2(UNIT_LEAST_V) : 1.0f) / l;
+            unsigned long long to[4];                              // the rows of the lane's quad
+#pragma unroll
+            for (int k = 0; k < 4; ++k) to[k] = __shfl_sync(0xffffffffu, out_row, (lane & ~3u) + k);
+#pragma unroll 1
+            for (uint32_t q = 0; q < D / 32; ++q) {
+                float o[32];
+                if (whole) {
+                    outputs(q, o);
+                } else {                                           // the parts in worker order
+#pragma unroll
+                    for (int d = 0; d < 32; ++d) o[d] = 0;
+#pragma unroll 2
+                    for (uint32_t k = w0; k <= w1; ++k) {
+                        float4 b[8];
+                        const float2 e = __ldcg(ml + (uint64_t)slot(k) * HALF_ROWS + r);
+#pragma unroll
+                        for (uint32_t d = 0; d < 8; ++d) b[d] = __ldcg(at(k, 8 * q + d));
+                        const float c = m == -INFINITY ? 0.0f : ex2(e.x - m);
+#pragma unroll
+                        for (uint32_t d = 0; d < 8; ++d)
+                            o[4 * d] += b[d].x * c, o[4 * d + 1] += b[d].y * c, o[4 * d + 2] += b[d].z * c, o[4 * d + 3] += b[d].w * c;
+                    }
+                }
+                // A thread has a row, a store wants neighbouring lanes on neighbouring bytes: the four lanes
+                // of a quad exchange 16-byte pieces, so that a store writes 64 bytes of a row (a piece of its
+                // own row a lane made a store of 32 separate lines: 3 us a tile, and the load of the next
+                // tile's queries behind it)
+                uint32_t piece[4][4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    constexpr int B = C::ORDERED ? 1 : 2, E = C::ORDERED ? 2 : 1;      // where elements 1 and 2 of four are
+                    const float *e = o + 8 * k;
+                    piece[k][0] = pack2(e[0] * inv, e[B] * inv, T()), piece[k][1] = pack2(e[E] * inv, e[3] * inv, T());
+                    piece[k][2] = pack2(e[4] * inv, e[4 + B] * inv, T()), piece[k][3] = pack2(e[4 + E] * inv, e[7] * inv, T());
+                }
+                // (row, piece) to (piece, row): the off-diagonal blocks change places, at distance 2 and 1
+#pragma unroll
+                for (int dist = 2; dist; dist >>= 1)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (k & dist) continue;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const bool up = lane & dist;
+                            const uint32_t give = up ? piece[k][e] : piece[k + dist][e];
+                            const uint32_t got = __shfl_xor_sync(0xffffffffu, give, dist);
+                            if (up) piece[k][e] = got;
+                            else piece[k + dist][e] = got;
+                        }
+                    }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (to[k]) *reinterpret_cast<uint4 *>(to[k] + (4 * q + (lane & 3)) * 16) = make_uint4(piece[k][0], piece[k][1], piece[k][2], piece[k][3]);
+            }
+            if (lse_at) *lse_at = l == 0 ? -INFINITY : (m - C::OFF + log2f(l)) * 0.6931471805599453f;
+            if (whole) given_back();
+            }
             }
             n_unit += n;
             x += n;
-            if (x < x1) next_tile(p, t);
         }
     }
     if (*dead) {                                    // a wait was given up: copies in flight get 1 ms to land
