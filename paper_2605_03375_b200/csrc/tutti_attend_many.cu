@@ -697,10 +697,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     }
                 } else {
                     const uint64_t from = kv ? p.pool.v_base : p.pool.k_base;
-#pragma unroll
+#pragma unroll 4
                     for (int it = 0; it < 64 / RPI; ++it) {
                         const uint32_t r = it * RPI + sub, row = half * 64 + r;
-                        const int64_t o = __shfl_sync(0xffffffffu, off[it * RPI / 32], r % 32);
+                        const int64_t o = __shfl_sync(0xffffffffu, it * RPI < 32 ? off[0] : off[1], r % 32);
                         cp16(dst + (C8 ? row * 128 + (((ch ^ row) & (CH - 1)) << 4) : C::place(row, ch)), (const void *)(from + (o >= 0 ? o : 0) + ch * 16), o >= 0);
                     }
                     cp_commit();
@@ -763,10 +763,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 }
             };
             if constexpr (!C8) {
-                if (!(ok = room(0))) break;
-                fetch(0);
-                if (!(ok = room(1))) break;
-                fetch(1);
+#pragma unroll 1
+                for (int kv = 0; kv < 2 && (ok = room(kv)); ++kv) fetch(kv);
+                if (!ok) break;
 #pragma unroll 1
                 for (int k = 0; k < 2; ++k) step_unit();
                 locate();                               // the next unit's ids arrive while this one's rows do
@@ -836,17 +835,19 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             }
             cp_commit();
             cp_wait<0>();
-            if constexpr (!C::ORDERED) {                    // each lane what it brought itself
+            if (!C::ORDERED || p.scale < 0) {               // each lane what it brought itself
+                const uint32_t sign = p.scale < 0 ? 0x80008000u : 0;
 #pragma unroll 1
                 for (uint32_t b = warp - Q_WARP; b < TILE_ROWS / 32; b += Q_WARPS)
 #pragma unroll 4
-                for (uint32_t it = 0; it < CH; ++it) {
-                    const uint32_t r = b * 32 + it * RPI + sub;
-                    uint4 *at = reinterpret_cast<uint4 *>(sm + r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch));
-                    const uint4 u = *at;
-                    *at = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.x, u.y, 0x7632),
-                                     __byte_perm(u.z, u.w, 0x5410), __byte_perm(u.z, u.w, 0x7632));
-                }
+                    for (uint32_t it = 0; it < CH; ++it) {
+                        const uint32_t r = b * 32 + it * RPI + sub;
+                        uint4 *at = reinterpret_cast<uint4 *>(sm + r / HALF_ROWS * C::KV + C::place(r % HALF_ROWS, ch));
+                        uint4 u = *at;
+                        if constexpr (!C::ORDERED)
+                            u = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.x, u.y, 0x7632), __byte_perm(u.z, u.w, 0x5410), __byte_perm(u.z, u.w, 0x7632));
+                        *at = make_uint4(u.x ^ sign, u.y ^ sign, u.z ^ sign, u.w ^ sign);
+                    }
             }
             fence_async();
             __syncwarp();
@@ -941,10 +942,9 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         setmaxnreg_inc<C::SOFT_REGS>();
         const int i = warp / 4;                                   // half
         const uint32_t lanes = (warp % 4) * 32 << 16, o_at = O(i) + lanes, r = (warp % 4) * 32 + lane;
-        // Scores are multiplied by a positive factor, so that masked ones stay -infinity and the largest stays the
-        // largest; the smallest number there is makes the largest score of a zero scale less than 2^-20.
+        // Scores are multiplied by a positive factor (a negative scale's sign is on the queries), so that masked ones stay
+        // -infinity and the largest stays the largest; the smallest number there is makes the largest score of a zero scale less than 2^-20.
         const float scl_all = fmaxf(fabsf(p.scale) * 1.4426950408889634f, 0x1p-149f);
-        const bool negative = p.scale < 0;
         uint32_t n_s = 0, n_seg = 0, n_unit = 0, n_join = 0, n_share = 0;    // steps of this half; units of the worker
         bool ok = true;
         auto join = [&]() {                                       // the half's four warps
@@ -999,10 +999,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
 #pragma unroll
                     for (int q = 0; q < SUB / 32; ++q) tc_loaded(sr + 32 * q);
                     const int64_t key0 = (int64_t)(t.u + j / STEPS + (WIN && t.u + j / STEPS >= front ? t.gap : 0)) * BN + j % STEPS * SUB;
-                    if (negative) {
-#pragma unroll
-                        for (int k = 0; k < SUB; ++k) s[k] = -s[k];
-                    }
                     if (key0 + SUB - 1 > pos_low || all != ~0u || (WIN && key0 <= hidden)) {
                         // A bit a key, and two instructions a score: this code runs once or twice a tile, so that it is fetched
                         // each time (with three comparisons a score a masked unit took 9 us instead of 2).
@@ -1043,7 +1039,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                             ok = __all_sync(0xffffffffu, ok);
                             if (!ok) break;
                             tc_after();
-#pragma unroll
+#pragma unroll 1
                             for (int q = 0; q < D / 16; ++q) {
                                 uint32_t o[16];
                                 tc_ld16(o, o_at + 16 * q);
