@@ -197,6 +197,7 @@ __global__ void __launch_bounds__(THREADS, 1) copy_blocks_kernel(const __grid_co
                 }
             }
         } while (next_ticket());
+        if (p.scales) __threadfence();
     } else {
         unsigned long long *to = reinterpret_cast<unsigned long long *>(smem + OFF_TO) + warp * STAGES * 32 + lane;
         uint32_t *bytes = reinterpret_cast<uint32_t *>(smem + OFF_BYTES) + warp * STAGES * 32 + lane;
@@ -266,9 +267,8 @@ __global__ void __launch_bounds__(THREADS, 1) copy_blocks_kernel(const __grid_co
             bulk_wait_read_1();
             __syncwarp();
         }
-        bulk_wait_all();
+        bulk_wait_all();                        // the copies have been written, not only read
     }
-    __threadfence();
 }
 
 }  // namespace
