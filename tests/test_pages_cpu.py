@@ -28,7 +28,7 @@ def call(name, *args):
     return f(*conv)
 
 
-BAD = [dict(blk_start=None), dict(block_ids=None), dict(len=None), dict(n_seq=65537), dict(n_blk=1 << 31), dict(blk_start=0x1002),
+BAD = [dict(blk_start=None), dict(block_ids=None), dict(len=None), dict(n_seq=T.PAGES_MAX_SEQ + 1), dict(n_blk=1 << 31), dict(blk_start=0x1002),
        dict(block_ids=0x2001), dict(len=0x3003), dict(status=0x4002)]
 
 
@@ -42,7 +42,7 @@ def test_tables_that_are_refused(kw):
 
 
 def test_calls_that_are_taken():
-    assert call("tutti_tables_check_", tables()) == T.OK and call("tutti_tables_check_", tables(status=0x4000, n_seq=65536)) == T.OK
+    assert call("tutti_tables_check_", tables()) == T.OK and call("tutti_tables_check_", tables(status=0x4000, n_seq=T.PAGES_MAX_SEQ)) == T.OK
     assert call("tutti_tables_check_", T.Tables()) == T.OK
     assert call("tutti_fork_check_", tables(), 0x5000, other(), 0) == T.OK and call("tutti_fork_check_", tables(), 0x5000, other(), 1) == T.OK
     assert call("tutti_fork_check_", tables(), None, T.Tables(), 1) == T.OK
