@@ -19,7 +19,7 @@
 //             An instruction of 128 x 64 x 16 reads 6 KB of shared memory in the time of 4 KB, which makes
 //             Q K^T 1.5 times as long: it costs a 16-bit cache more than the waiting (318 against 278 us),
 //             and an 8-bit one, where the widening warps are the bound, less (360 -> 311);
-//   9-11      bring the queries of the next tile;
+//   9-11      bring the queries of the next tile; 9 also walks over the worker's tiles and publishes them (Share);
 //   12-15     gather keys and values through the block table into a ring of four 128-row tiles
 //             in the 128-byte swizzle (K: K-major B operand, V: the same bytes read as an
 //             MN-major B operand): one tensor copy per block and 128 bytes of its rows, or, where a
@@ -31,11 +31,20 @@
 //             own, so that they are fetched before the place they go to is free.
 // Bound: the tensor cores (2 x 128 x 128 x D multiply-adds a half and unit: 2048 clocks a unit for D = 128)
 // and, as close, the 2 x 128 x 128 exponentials on 16 lanes a clock; in a long loop the power limit
-// (1550 MHz at 1000 W).  What is reached: 3500 clocks a unit, set by the chain scores -> softmax -> P V
-// -> next scores of a half.  On a B200 (1676 TFLOP/s in short, 1389 in long runs of the library's product), the kernel
-// alone, 32 heads: 2048 new tokens over 32768, bf16, 1150-1210 us = 940-990 TFLOP/s; 1801 over 2 x 8192 255 us = 978
-// (281-287 us among other calls); 8-bit, fp16, 4 ragged chunks over 2000-9000 266 us = 700, bf16 317 us cool and
-// 380-420 us in long runs (the widening of the codes and shared memory); 64-wide heads 1801 over 2 x 8192 207 us = 603.
+// (1550 MHz at 1000 W).  What is reached: 3500-4000 clocks a unit, set by the chain scores -> softmax -> P V
+// -> next scores of a half.  A tile's start and end cost about two units more: they are code that runs once a tile, and the
+// roles' code together does not fit the instruction cache, so that what is rare is kept small (masks as bits, outputs in
+// pieces, one walk over the tiles; 2048 tokens without a prefix 97 -> 61 us).
+// On a B200 (1694 TFLOP/s in short, 1395 in long runs of the library's product), the kernel
+// alone, 32 heads: 2048 new tokens over 32768, bf16, 1133 us = 1000 TFLOP/s; 1801 over 2 x 8192 235-265 us = 950-1070
+// (264 us among other calls); 8-bit, fp16, 4 ragged chunks over 2000-9000 236 us = 800, bf16 292 us (the widening of the codes
+// and shared memory); 64-wide heads 1801 over 2 x 8192 197 us = 640.
+//
+// Under a window (WIN) a tile's units are the ones of the first tokens, if they lie in front of it, and the ones from its first
+// row's window on; the number of units of many tiles is still a closed form (a second floor_sum), and the units in
+// between are in no worker's share.  A masked unit is one of the first tokens, of the window's start or of the tile's end: 3 of
+// 10 under a window of 1024, all of them under one of 128.  8192 tokens without a prefix, 4 first tokens, bf16: window 128 94 us, 1024 190 us = 680
+// TFLOP/s, 4096 over 24576 518-528 us = 1050; 8-bit, fp16, 4 chunks of 300-700 under a window of 1024 87 us, bf16 102 us.
 #include <cstring>
 #include <type_traits>
 

@@ -1,5 +1,10 @@
 // Pages of the pool: which rows hold which blocks.  Rows are handed on (fork), grow (extend), are freed (release,
 // trim), and blocks in use are moved to the lowest ids (compact); tables and counts live in device memory.
+//
+// Bound: latency.  The bytes are few (a table of 128 rows of 8192 ids is 4 MB, counts of a million blocks 4 MB, all in L2), each
+// kernel is a launch and three to six rounds of loads that depend on each other.  On a B200, in a captured graph: fork of 64 rows
+// of 160 entries 4.7 us, of 128 rows of 8200 7.8; extend of 64 rows 5.0-6.4, of 1024 rows among a million blocks 7.4; trim of 64 rows of
+// 1040 entries 1.9, of 1024 of 520 3.7; release 1.7; compact of 5000 blocks 6.0.
 #include <new>
 
 #include "tutti_attend.h"
