@@ -409,8 +409,8 @@ __host__ __device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __n
 }
 
 // The units [u, u + n) of a tile of n_units that a worker has: published by the warps that bring the queries, so that the
-// walk over tiles stands in the code of fewer roles.  SHARES: one that is published, one whose products run, one that the softmax may not
-// have taken yet, and one to spare.
+// walk over tiles stands in the code of fewer roles.  The products' warp has read a share before the queries of the next are
+// brought; the softmax warps say when they have.
 constexpr uint32_t SHARES = 4;
 struct Share {
     uint32_t n, u, n_units, gap;        // gap: units left out behind the first tokens'
@@ -426,7 +426,7 @@ struct Many {
     static constexpr uint32_t OFF_RING = 2 * KV;            // behind the two halves of Q
     static constexpr uint32_t OFF_RAW = OFF_RING + RING * KV;          // 8-bit: codes of a group's values
     static constexpr uint32_t OFF_BAR = OFF_RAW + (C8 ? 2 * ATOM : 0);
-    static constexpr uint32_t OFF_EXISTS = OFF_BAR + 320;   // [8 units][4]: keys that exist
+    static constexpr uint32_t OFF_EXISTS = OFF_BAR + 352;   // [8 units][4]: keys that exist
     static constexpr bool UNITS = C8 && std::is_same<T, __half>::value;
     static constexpr uint32_t OFF_UNITS = OFF_EXISTS + 128; // [8 units][2 steps]: exponents of keys' and values' units
     static constexpr uint32_t OFF_MISC = OFF_UNITS + (UNITS ? 128 : 0);
@@ -460,7 +460,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
     volatile uint32_t *dead = misc + 72;
     const uint32_t bars = base + C::OFF_BAR;
     const uint32_t full = bars, empty = bars + 32, q_full = bars + 64, q_empty = bars + 72, o_full = bars + 80, o_empty = bars + 96,
-                   joined = bars + 112, drain = bars + 128, raw_full = bars + 136, s_full = bars + 200, p_full = bars + 232, o_done = bars + 264, share_full = bars + 280;
+                   joined = bars + 112, drain = bars + 128, raw_full = bars + 136, s_full = bars + 200, p_full = bars + 232, o_done = bars + 264, share_full = bars + 280, share_free = bars + 312;
     Share *shares = reinterpret_cast<Share *>(sm + C::OFF_SHARE);
 
     // ---- this worker's share ----
@@ -542,7 +542,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             mbar_init(p_full + 8 * i, 4);
         }
         mbar_init(drain, 1);
-        for (uint32_t i = 0; i < SHARES; ++i) mbar_init(share_full + 8 * i, 1);
+        for (uint32_t i = 0; i < SHARES; ++i) {
+            mbar_init(share_full + 8 * i, 1);
+            mbar_init(share_free + 8 * i, MMA_WARP);        // the softmax warps
+        }
         for (int i = 0; i < 2 * RING; ++i) mbar_init(raw_full + 8 * i, 1);
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -821,11 +824,13 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         uint32_t segs = 0;
         for (unsigned long long x = x0; x < x1; ++segs) {
             const uint32_t n = (uint32_t)min(x1 - x, (unsigned long long)(t.n_units - t.u));
+            bool ok = warp != Q_WARP || segs < SHARES || mbar_wait(share_free + 8 * (segs % SHARES), (segs / SHARES - 1) & 1, dead);
+            if (!__all_sync(0xffffffffu, ok)) break;
             if (warp == Q_WARP && lane == 0) {
                 shares[segs % SHARES] = Share{n, t.u, t.n_units, gap_of(t), t.q, t.h, t.v.q0, t.r.n_rows, t.r.first};
                 mbar_arrive(share_full + 8 * (segs % SHARES));
             }
-            bool ok = !segs || mbar_wait(q_empty, (segs - 1) & 1, dead);
+            ok = !segs || mbar_wait(q_empty, (segs - 1) & 1, dead);
             if (!__all_sync(0xffffffffu, ok)) break;
             constexpr int CH = D / 8, RPI = 32 / CH;        // 16-byte chunks of a row; rows a warp takes at once
             const uint32_t ch = lane % CH, sub = lane / CH;
@@ -966,7 +971,10 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             ok = mbar_wait(share_full + 8 * (n_share % SHARES), n_share / SHARES & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            const Share t = shares[n_share++ % SHARES];
+            const Share t = shares[n_share % SHARES];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(share_free + 8 * (n_share % SHARES));
+            ++n_share;
             const uint32_t n = t.n;
             const uint32_t row = t.q * TILE_ROWS + i * HALF_ROWS + r;
             if (t.q * TILE_ROWS + i * HALF_ROWS < t.n_rows) {

@@ -157,3 +157,13 @@ def test_refusals():
         assert c.attn.tutti_kv_attend_window_layer(0, c.step, io, 0.1, T.make_window(4), allow=(T.EINVAL,)) == T.EINVAL
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("cache", ["16", "8"])
+@pytest.mark.parametrize("most", [12, 40])
+def test_many_short_chunks(cache, most):
+    """Tiles of a few rows, of one half and of two, hundreds of them, most of one or two units."""
+    rng = np.random.default_rng(most)
+    lens = [(int(rng.integers(0, 300)), int(rng.integers(5, most))) for _ in range(90)]
+    run(lens, 60, 3, heads=8, kv_heads=2, dim=64, cache=cache, dtype="fp16", seed=most)
+    run(lens, 1 << 20, 0, heads=8, kv_heads=2, dim=64, cache=cache, dtype="fp16", seed=most, gone=None)
