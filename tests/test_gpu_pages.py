@@ -508,3 +508,67 @@ def test_copy_blocks_behind_four_gigabytes():
     finally:
         torch.cuda.synchronize()
         ctx.close()
+
+
+# ---------------------------------------------------------------------------- long runs of everything
+
+@pytest.mark.parametrize("seed", range(8))
+def test_random_runs_over_two_tables(contexts, seed):
+    """Forks there and back, extensions, rows freed, windows and compactions over the same counts, in a random order."""
+    rng = np.random.default_rng(seed)
+    bs = int(rng.choice([1, 4, 16]))
+    n_seq, n_blocks = int(rng.integers(1, 40)), int(rng.integers(30, 900))
+    cap = 24
+    books = [P.Book(np.arange(n_seq + 1) * cap, [-7] * (cap * n_seq), [0] * n_seq, bs) for _ in range(2)]
+    refs = [0] * n_blocks
+    b = P.Bound(contexts(bs), books, refs)
+    pairs = torch.zeros(n_seq, 2, dtype=torch.int32, device=b.dev)
+    moves, moved = torch.zeros(20, 2, dtype=torch.int32, device=b.dev), ints([0])
+    try:
+        for step in range(60):
+            k = int(rng.integers(0, 2))
+            t, book = b.tables(k), books[k]
+            what = rng.choice(["extend", "extend", "extend", "move", "keep", "release", "trim", "compact"])
+            if what == "extend":
+                n_new = rng.integers(0, rng.choice([2, 2, 3 * bs]), n_seq)
+                n_new = np.array([n if book.lens[s] + n <= cap * bs else 0 for s, n in enumerate(n_new)])
+                b.pages.tutti_pages_extend(t, ints(n_new), pairs)
+                assert pairs.tolist() == [list(p) for p in P.extend(book, refs, n_new)], (step, what)
+            elif what in ("move", "keep"):
+                # the other table's rows are given up first
+                b.pages.tutti_pages_release(b.tables(1 - k))
+                P.release(books[1 - k], refs, None)
+                parent = rng.integers(-1 if what == "keep" else 0, n_seq, n_seq)
+                b.pages.tutti_pages_fork(t, ints(parent), b.tables(1 - k), T.FORK_MOVE if what == "move" else T.FORK_KEEP)
+                P.fork(book, parent, books[1 - k], refs, what == "move")
+                if what == "move":                              # its rows hold nothing any longer
+                    book.lens = [0] * n_seq
+                    b.t[k][3].zero_()
+            elif what == "release":
+                which = rng.random(n_seq) < 0.3
+                b.pages.tutti_pages_release(t, torch.from_numpy(which).to(b.dev))
+                P.release(book, refs, which)
+            elif what == "trim":
+                w = int(rng.integers(1, 6 * bs + 2))
+                b.pages.tutti_pages_trim(t, T.make_window(w, 2))
+                P.trim(book, refs, w, 2)
+            else:
+                # rows of both tables: one call over arrays of their own would do; here the other table follows the pairs
+                other = books[1 - k]
+                b.pages.tutti_pages_compact(t, moves, moved)
+                place = dict(P.compact(book, refs, len(moves)))
+                for s in range(n_seq):
+                    a, _, _, h = other.row(s)
+                    other.ids[a:a + h] = [place.get(i, i) for i in other.ids[a:a + h]]
+                b.t[1 - k][2].copy_(ints(other.ids))
+                assert int(moved) == len(place)
+            for k in range(2):
+                status = books[k].status
+                b.same(refs, k)
+                assert status <= {T.EAGAIN}
+                status.clear()
+                b.t[k][4].zero_()
+            held = [i for book in books for s in range(n_seq) for i in book.ids[book.row(s)[0]:book.row(s)[0] + book.row(s)[3]] if i >= 0]
+            assert np.array_equal(np.bincount(held, minlength=n_blocks), refs)
+    finally:
+        b.close()
