@@ -100,6 +100,8 @@ static int attend(tutti_attn_t *a, uint32_t layer, const tutti_step_t *step, con
     p.scale = io->scale;
     p.window = window;
     p.sinks = sinks;
+    p.grain = grain_of(p.pool.block_tokens);
+    p.front = front_of(sinks, p.grain);
     OnDevice on(tutti_ctx_device_(a->ctx));
     if (!on.ok) return fail(cudaErrorInvalidDevice, "cudaSetDevice");
     const bool bf = io->dtype == TUTTI_DTYPE_BF16;

@@ -17,6 +17,9 @@ struct AttendParams {
     float scale;
     uint32_t group_mul, group_shift;  // row / group = row * group_mul >> group_shift
     uint32_t window, sinks;           // window 0: every key up to the row's own
+    // Many rows: a tile's keys are the first `front` of the sequence (the sinks, up to a multiple of `grain`) and the ones
+    // from its window on, which begins at a multiple of it; a tensor copy brings `grain` rows of one block or a multiple.
+    uint32_t front, grain;
 
     // The first key behind the first `sinks` that a row at position `first` (any row behind it) sees: 0 or less, all.
     __host__ __device__ int64_t window_start(int64_t first) const { return first - window + 1; }
@@ -24,6 +27,9 @@ struct AttendParams {
     __host__ __device__ uint32_t token_of(uint32_t row) const { return (uint32_t)((uint64_t)row * group_mul >> group_shift); }
     __host__ __device__ uint32_t member_of(uint32_t row) const { return row - token_of(row) * group; }
 };
+
+__host__ __device__ inline uint32_t grain_of(uint32_t block_tokens) { return 64 % block_tokens == 0 ? block_tokens : block_tokens % 64 == 0 ? 64 : 16; }
+__host__ __device__ inline uint32_t front_of(uint32_t sinks, uint32_t grain) { return (sinks + grain - 1) / grain * grain; }
 
 // Tile loads of the layer's keys and values.
 struct PoolMaps {

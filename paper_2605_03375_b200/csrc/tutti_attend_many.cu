@@ -129,42 +129,42 @@ struct Rows {
     }
 };
 
-// The same under a window: of a tile's units the ones that none of its rows sees, between the first tokens and the
-// window of its first row, are left out.
+// The same under a window.  From tile q0 on, where it saves a unit at least, a tile's keys are laid end to end without the ones
+// that none of its rows sees: the first `front` of the sequence, then the ones from its first row's window on (a
+// multiple of `grain`).  All such tiles have `per` units, what the longest of them needs, so that sums over tiles stay closed forms.
 struct WindowRows : Rows {
-    uint32_t front;                     // units of the first tokens that stay visible
-    int64_t start;                      // keys in front of the first row's window, less those of `front`
-    // how many are left out of tile q: those in front of its first row's window, less `front`, if positive
-    __host__ __device__ uint32_t gap(uint32_t q) const {
-        const int64_t x = start + token_of(q * TILE_ROWS);
-        return x > 0 ? (uint32_t)x / BN : 0;
-    }
-    __host__ __device__ uint32_t units(uint32_t q) const { return Rows::units(q) - gap(q); }
-    __host__ __device__ uint64_t before(uint32_t q) const {
-        const uint64_t all = Rows::before(q);
-        // floor((start + floor(x / group)) / BN) = floor((start group + x) / (BN group)), x = 256 i; tiles in front of q0 leave nothing out
-        const int64_t b = start * (int64_t)group;
-        const uint64_t q0 = b >= 0 ? 0 : ((uint64_t)-b + TILE_ROWS - 1) / TILE_ROWS;
-        return q <= q0 ? all : all - floor_sum(q - q0, (uint64_t)BN * group, TILE_ROWS, (uint64_t)(b + (int64_t)q0 * TILE_ROWS));
-    }
+    uint32_t q0, per, front, grain;
+    int64_t start;                      // first key of the first row's window
+    // Key number v of tile q is key v of the sequence below `front`, and key v + shift(q) from there on; 0: of a tile in front of q0.
+    __host__ __device__ uint32_t shift(uint32_t q) const { return q < q0 ? 0 : (uint32_t)(start + token_of(q * TILE_ROWS)) / grain * grain - front; }
+    __host__ __device__ uint32_t units(uint32_t q) const { return q < q0 ? Rows::units(q) : per; }
+    __host__ __device__ uint64_t before(uint32_t q) const { return q <= q0 ? Rows::before(q) : Rows::before(q0) + (uint64_t)(q - q0) * per; }
 };
 template <bool WIN> struct RowsOf { typedef Rows type; };
 template <> struct RowsOf<true> { typedef WindowRows type; };
 
-__host__ __device__ inline void rows_of(const SeqView &v, uint32_t group, uint32_t group_mul, uint32_t group_shift, uint32_t, uint32_t, Rows &r) {
-    r.n_rows = v.n_new * group;
+__host__ __device__ inline void rows_of(const SeqView &v, const AttendParams &p, Rows &r) {
+    r.n_rows = v.n_new * p.group;
     r.n_tiles = (r.n_rows + TILE_ROWS - 1) / TILE_ROWS;
-    r.group = group;
-    r.group_mul = group_mul;
-    r.group_shift = group_shift;
+    r.group = p.group;
+    r.group_mul = p.group_mul;
+    r.group_shift = p.group_shift;
     r.ctx = v.ctx;
     r.first = (int64_t)v.ctx - v.n_new;
 }
-__host__ __device__ inline void rows_of(const SeqView &v, uint32_t group, uint32_t group_mul, uint32_t group_shift, uint32_t window, uint32_t sinks, WindowRows &r) {
-    rows_of(v, group, group_mul, group_shift, 0, 0, static_cast<Rows &>(r));
-    r.front = (sinks + BN - 1) / BN;
-    // padding rows: every tile sees all
-    r.start = r.first < 0 ? -((int64_t)1 << 40) : r.first - window + 1 - (int64_t)r.front * BN;
+__host__ __device__ inline void rows_of(const SeqView &v, const AttendParams &p, WindowRows &r) {
+    rows_of(v, p, static_cast<Rows &>(r));
+    r.front = p.front;
+    r.grain = p.grain;
+    r.start = p.window_start(r.first);
+    // the first tile whose window begins a unit or more behind `front`: floor(256 q / group) tokens behind the first row's; padding rows: none
+    const int64_t x = (int64_t)p.front + BN - r.start;
+    const uint64_t q0 = x > 0 ? ((uint64_t)x * p.group + TILE_ROWS - 1) / TILE_ROWS : 0;
+    r.q0 = r.first < 0 || q0 > 0xffffffffu ? 0xffffffffu : (uint32_t)q0;
+    // tokens of a tile at most, and how far its window's start may lie behind a multiple of grain
+    const uint32_t tokens = TILE_ROWS % p.group ? (TILE_ROWS - 2 + p.group) / p.group + 1 : TILE_ROWS / p.group;
+    const uint32_t slack = TILE_ROWS % p.group || tokens % p.grain || r.start < 0 ? p.grain - 1 : (uint32_t)(r.start % p.grain);
+    r.per = (uint32_t)(((uint64_t)p.front + tokens + p.window - 1 + slack + BN - 1) / BN);
 }
 
 // Where a cut at unit u of a tile of n units goes: to its start below low(n), behind it from n -
@@ -197,16 +197,11 @@ struct Found {
     unsigned long long head, in_seq;
 };
 
-// Which unit of the sequence's keys unit u of a tile is; `gap` of the tile.
+// What is added to a key's number in the tile, from p.front on.
 template <bool WIN>
-__device__ inline uint32_t gap_of(const Tile<WIN> &t) {
-    if constexpr (WIN) return t.r.gap(t.q);
+__device__ inline uint32_t shift_of(const Tile<WIN> &t) {
+    if constexpr (WIN) return t.r.shift(t.q);
     else return 0;
-}
-template <bool WIN>
-__device__ inline uint32_t key_unit(const Tile<WIN> &t, uint32_t u, uint32_t gap) {
-    if constexpr (WIN) return u + (u >= t.r.front ? gap : 0);
-    else return u;
 }
 
 template <bool WIN>
@@ -214,7 +209,7 @@ __device__ inline int tile_seq(const AttendParams &p, uint32_t s, Tile<WIN> &t) 
     t.s = s;
     const int code = seq_view(p.step, p.pool.block_tokens, s, t.v);
     if (code != TUTTI_OK) t.v.n_new = t.v.ctx = 0;
-    rows_of(t.v, p.group, p.group_mul, p.group_shift, p.window, p.sinks, t.r);
+    rows_of(t.v, p, t.r);
     return code;
 }
 
@@ -413,7 +408,7 @@ __host__ __device__ inline bool factors(float s, uint32_t &f1, uint32_t &f2, __n
 // brought; the softmax warps say when they have.
 constexpr uint32_t SHARES = 4;
 struct Share {
-    uint32_t n, u, n_units, gap;        // gap: units left out behind the first tokens'
+    uint32_t n, u, n_units, shift;      // shift: see WindowRows
     uint32_t q, h, q0, n_rows;          // tile of the head, KV head, first row of the sequence in the step, rows of a head
     int64_t first;                      // position of the first new token
 };
@@ -624,14 +619,16 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
         };
         // The next unit: block ids of rows lane and lane + 32 (locate), then what follows from them.
         int32_t id[2];
-        uint32_t key0 = 0, head = 0, ctx = 0, start = 0;
+        uint32_t key0 = 0, head = 0, ctx = 0, start = 0, shift = 0;
+        auto key_of = [&](uint32_t v) { return WIN && v >= p.front ? v + shift : v; };
         auto in_sight = [&](uint32_t key) { return key < ctx && (!WIN || key < p.sinks || key >= start); };
         int64_t off[2];
         float ks[2], vs[2];
         uint32_t missing[2];
         bool tiled = false;
         auto locate = [&]() {
-            key0 = key_unit(t, t.u, gap_of(t)) * BN + half * 64;
+            key0 = t.u * BN + half * 64;
+            shift = shift_of(t);
             head = t.h;
             ctx = fx < x1 ? t.v.ctx : 0;
             if constexpr (WIN) {                        // of the sequence: no row sees a key in front of its first row's window
@@ -640,7 +637,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint32_t key = key0 + i * 32 + lane;
+                const uint32_t key = key_of(key0 + i * 32 + lane);
                 id[i] = in_sight(key) ? __ldg(p.step.block_ids + t.v.b0 + p.pool.block_of(key)) : -1;
             }
         };
@@ -648,7 +645,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             tiled = maps.valid;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const uint32_t key = key0 + i * 32 + lane;
+                const uint32_t key = key_of(key0 + i * 32 + lane);
                 const bool there = (uint32_t)id[i] < p.pool.n_blocks, bad = !there && in_sight(key);
                 if (bad) report(p.step, TUTTI_EFAULT);
                 missing[i] = __ballot_sync(0xffffffffu, bad);
@@ -703,7 +700,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     if (lane == 0) mbar_expect(bar, 64 * RB);
                     __syncwarp();
                     if (my_part < PARTS) {
-                        const int32_t token = (int32_t)p.pool.row_of(key0 + row);
+                        const int32_t token = (int32_t)p.pool.row_of(key_of(key0 + row));
                         tile_load(dst + my_part * ATOM + (half * 64 + row) * 128, kv ? &maps.v : &maps.k, bar, (int32_t)(my_part * (C8 ? 128 : 64)),
                                   p.pool.hnd ? token : (int32_t)head, p.pool.hnd ? (int32_t)head : token, row < 32 ? lo : hi);
                     }
@@ -827,7 +824,7 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
             bool ok = warp != Q_WARP || segs < SHARES || mbar_wait(share_free + 8 * (segs % SHARES), (segs / SHARES - 1) & 1, dead);
             if (!__all_sync(0xffffffffu, ok)) break;
             if (warp == Q_WARP && lane == 0) {
-                shares[segs % SHARES] = Share{n, t.u, t.n_units, gap_of(t), t.q, t.h, t.v.q0, t.r.n_rows, t.r.first};
+                shares[segs % SHARES] = Share{n, t.u, t.n_units, shift_of(t), t.q, t.h, t.v.q0, t.r.n_rows, t.r.first};
                 mbar_arrive(share_full + 8 * (segs % SHARES));
             }
             ok = !segs || mbar_wait(q_empty, (segs - 1) & 1, dead);
@@ -984,7 +981,6 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                 const int64_t pos = t.first + tok;
                 const int64_t pos_low = __shfl_sync(0xffffffffu, pos, 0);
                 const int64_t hidden = WIN ? __shfl_sync(0xffffffffu, pos, 31) - p.window : 0;      // keys up to here are not seen by every row
-                const uint32_t front = WIN ? (p.sinks + BN - 1) / BN : 0;
                 float m = -INFINITY, l = 0;
                 int o_unit = UNIT_LEAST_V;                        // UNITS: exponent of the output's unit, the largest of its values'
                 const uint32_t steps = STEPS * n;
@@ -1015,17 +1011,21 @@ __global__ void __launch_bounds__(THREADS, 1) attend_many_kernel(const __grid_co
                     tc_wait_ld();
 #pragma unroll
                     for (int q = 0; q < SUB / 32; ++q) tc_loaded(sr + 32 * q);
-                    const int64_t key0 = (int64_t)(t.u + j / STEPS + (WIN && t.u + j / STEPS >= front ? t.gap : 0)) * BN + j % STEPS * SUB;
+                    const int64_t v0 = (int64_t)t.u * BN + j * SUB, key0 = WIN ? v0 + t.shift : v0;    // (of numbers below p.front: v0)
                     if (key0 + SUB - 1 > pos_low || all != ~0u || (WIN && key0 <= hidden)) {
                         // A bit a key, and two instructions a score: this code runs once or twice a tile, so that it is fetched
                         // each time (with three comparisons a score a masked unit took 9 us instead of 2).
                         auto ahead = [](int64_t n) { return n < 0 ? 0 : n > SUB ? SUB : (int)n; };
                         auto below = [](int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; };       // bits 0 .. n - 1
-                        const int seen = ahead(pos - key0 + 1), gone = WIN ? ahead(pos - p.window - key0 + 1) : 0, first = WIN ? ahead((int64_t)p.sinks - key0) : 0;
+                        const int seen = ahead(pos - key0 + 1), gone = WIN ? ahead(pos - p.window - key0 + 1) : 0;
+                        // WIN: the sequence's first tokens, which all rows see; where a shift begins behind `front`, they are in front of it
+                        const int cut = WIN && t.shift ? ahead((int64_t)p.front - v0) : 0;
+                        const int first = WIN ? min(ahead((int64_t)p.sinks - v0), t.shift ? cut : seen) : 0;
 #pragma unroll
                         for (int q = 0; q < SUB / 32; ++q) {
-                            uint32_t bits = ex[q] & below(seen - 32 * q);
-                            if constexpr (WIN) bits &= ~below(gone - 32 * q) | below(first - 32 * q);
+                            uint32_t bits = below(seen - 32 * q);
+                            if constexpr (WIN) bits = (bits & ~below(gone - 32 * q) & ~below(cut - 32 * q)) | below(first - 32 * q);
+                            bits &= ex[q];
 #pragma unroll
                             for (int k = 0; k < 32; ++k) s[32 * q + k] = bits & 1u << k ? s[32 * q + k] : -INFINITY;
                         }
@@ -1303,27 +1303,35 @@ extern "C" void tutti_many_parts_(uint64_t tile0, uint32_t n, uint64_t workers, 
 }
 
 // The kernel's own count of units, on the host: out2[0] units of tile q, out2[1] units of the tiles before it.
+static void tile_params(tutti::AttendParams &p, uint32_t group, uint32_t window, uint32_t sinks, uint32_t block_tokens) {
+    p.group = group;
+    tutti::division_by(group, p.group_mul, p.group_shift);
+    p.window = window;
+    p.sinks = sinks;
+    p.grain = tutti::grain_of(block_tokens);
+    p.front = tutti::front_of(sinks, p.grain);
+}
 extern "C" int tutti_many_units_(uint32_t ctx, uint32_t n_new, uint32_t group, uint32_t q, uint64_t *out2) {
     const tutti::SeqView v{0, n_new, ctx, 0};
+    tutti::AttendParams p;
+    tile_params(p, group, 0, 0, 16);
     tutti::Rows r;
-    uint32_t mul, shift;
-    tutti::division_by(group, mul, shift);
-    tutti::rows_of(v, group, mul, shift, 0, 0, r);
+    tutti::rows_of(v, p, r);
     out2[0] = q < r.n_tiles ? r.units(q) : 0;
     out2[1] = r.before(q);
     return (int)r.n_tiles;
 }
-// The same under a window; out4[2] the first units that stay, out4[3] the units left out behind them.
-extern "C" int tutti_many_window_units_(uint32_t ctx, uint32_t n_new, uint32_t group, uint32_t window, uint32_t sinks, uint32_t q, uint64_t *out4) {
+// The same under a window; out4[2] the sequence's first keys that a tile has, out4[3] its shift of the others.
+extern "C" int tutti_many_window_units_(uint32_t ctx, uint32_t n_new, uint32_t group, uint32_t window, uint32_t sinks, uint32_t block_tokens, uint32_t q, uint64_t *out4) {
     const tutti::SeqView v{0, n_new, ctx, 0};
+    tutti::AttendParams p;
+    tile_params(p, group, window, sinks, block_tokens);
     tutti::WindowRows r;
-    uint32_t mul, shift;
-    tutti::division_by(group, mul, shift);
-    tutti::rows_of(v, group, mul, shift, window, sinks, r);
+    tutti::rows_of(v, p, r);
     out4[0] = q < r.n_tiles ? r.units(q) : 0;
     out4[1] = r.before(q);
     out4[2] = r.front;
-    out4[3] = q < r.n_tiles ? r.gap(q) : 0;
+    out4[3] = q < r.n_tiles ? r.shift(q) : 0;
     return (int)r.n_tiles;
 }
 

@@ -150,30 +150,39 @@ def test_binding():
     refused(lambda: p.tutti_pages_trim(t, T.make_window(4)), "closed")
 
 
-@pytest.mark.parametrize("group", [1, 2, 3, 5, 7, 8, 64, 300])
-def test_units_of_a_windows_tiles_in_closed_form(group):
-    """The 128-key units that 256-row tiles need under a window, against counting them."""
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 7, 8, 64, 300])
+def test_a_windows_tiles_have_every_key_that_a_row_sees_once(group):
+    """The keys of a tile, laid end to end without the ones that none of its rows sees: all that a row sees are among them, none
+    is there twice, a unit is at most lost to rounding, and the units of the tiles in front are counted in closed form."""
     f = check_fn("tutti_many_window_units_")
-    f.argtypes = [C.c_uint32] * 6 + [C.POINTER(C.c_uint64)]
+    f.argtypes = [C.c_uint32] * 7 + [C.POINTER(C.c_uint64)]
     rng = np.random.default_rng(group)
     out = (C.c_uint64 * 4)()
-    cases = [(1, 1, 1, 0), (5000, 700, 1024, 4), (2000, 2000, 1, 0), (2000, 2000, 128, 128), (40000, 3, 4096, 16), (10, 30, 5, 2), (0, 5, 7, 1),
-             (131072, 1000, 4096, 200), (5000, 5000, (1 << 31) - 1, (1 << 31) - 1), (5000, 5000, 100, (1 << 31) - 1), (5000, 5000, (1 << 31) - 1, 0)]
-    cases += [tuple(int(x) for x in c) for c in zip(rng.integers(0, 6000, 60), rng.integers(1, 900, 60), np.exp(rng.uniform(0, 9, 60)), rng.integers(0, 400, 60))]
-    for ctx, new, window, sinks in cases:
+    cases = [(1, 1, 1, 0, 16), (5000, 700, 1024, 4, 16), (2000, 2000, 1, 0, 1), (2000, 2000, 128, 128, 64), (40000, 3, 4096, 16, 128), (10, 30, 5, 2, 16), (0, 5, 7, 1, 16),
+             (131072, 1000, 4096, 200, 8), (5000, 5000, (1 << 31) - 1, (1 << 31) - 1, 16), (5000, 5000, 100, (1 << 31) - 1, 16), (5000, 5000, (1 << 31) - 1, 0, 24)]
+    cases += [tuple(int(x) for x in c) for c in zip(rng.integers(0, 6000, 60), rng.integers(1, 900, 60), np.exp(rng.uniform(0, 9, 60)), rng.integers(0, 400, 60),
+                                                   rng.choice([1, 2, 5, 8, 16, 24, 32, 64, 128, 192], 60))]
+    for ctx, new, window, sinks, bs in cases:
         rows, first = new * group, ctx - new
         tiles = -(-rows // 256)
-        total, front = 0, -(-sinks // 128)
+        grain = bs if 64 % bs == 0 else 64 if bs % 64 == 0 else 16
+        total, front = 0, -(-sinks // grain) * grain
         for q in range(tiles):
             a, b = first + q * 256 // group, first + (min(rows, (q + 1) * 256) - 1) // group
-            if first >= 0 and ctx:
-                behind = max(0, a - window + 1) // 128                        # the unit in which the first row's window begins
-                gap = max(0, behind - front)
-                want = b // 128 + 1 - gap
+            assert f(ctx, new, group, window, sinks, bs, q, out) == tiles
+            units, before, got_front, shift = tuple(out)
+            assert (before, got_front) == (total, front), (ctx, new, window, sinks, bs, q)
+            full = b // 128 + 1 if first >= 0 and ctx else max(1, -(-ctx // 128))
+            if shift:
+                assert first >= 0 and shift >= 128 and shift % grain == 0
+                v = np.arange(128 * units)
+                keys = np.where(v < front, v, v + shift)
+                lo = max(0, a - window + 1)
+                need = np.concatenate([np.arange(min(sinks, lo)), np.arange(lo, b + 1)])
+                assert len(np.unique(keys)) == len(keys) and np.isin(need, keys).all(), (ctx, new, window, sinks, bs, q)
+                assert units <= full and 128 * units < front + 256 // group + 3 + window + 2 * grain + 128
             else:
-                gap, want = 0, max(1, -(-ctx // 128))
-            assert f(ctx, new, group, window, sinks, q, out) == tiles
-            assert tuple(out) == (want, total, front, gap), (ctx, new, window, sinks, q, tuple(out))
-            total += want
-        f(ctx, new, group, window, sinks, tiles, out)
+                assert units == full
+            total += units
+        f(ctx, new, group, window, sinks, bs, tiles, out)
         assert out[1] == total
