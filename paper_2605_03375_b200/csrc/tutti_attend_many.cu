@@ -36,15 +36,15 @@
 // roles' code together does not fit the instruction cache, so that what is rare is kept small (masks as bits, outputs in
 // pieces, one walk over the tiles; 2048 tokens without a prefix 97 -> 61 us).
 // On a B200 (1694 TFLOP/s in short, 1395 in long runs of the library's product), the kernel
-// alone, 32 heads: 2048 new tokens over 32768, bf16, 1133 us = 1000 TFLOP/s; 1801 over 2 x 8192 235-265 us = 950-1070
-// (264 us among other calls); 8-bit, fp16, 4 ragged chunks over 2000-9000 236 us = 800, bf16 292 us (the widening of the codes
-// and shared memory); 64-wide heads 1801 over 2 x 8192 197 us = 640.
+// alone, 32 heads: 2048 new tokens over 32768, bf16, 1133 us = 1000 TFLOP/s; 1801 over 2 x 8192 235-270 us = 930-1070
+// (264 us among other calls); 8-bit, fp16, 4 ragged chunks over 2000-9000 232 us = 810, bf16 291 us (the widening of the codes
+// and shared memory); 64-wide heads 1801 over 2 x 8192 198 us = 640.
 //
-// Under a window (WIN) a tile's units are the ones of the first tokens, if they lie in front of it, and the ones from its first
-// row's window on; the number of units of many tiles is still a closed form (a second floor_sum), and the units in
-// between are in no worker's share.  A masked unit is one of the first tokens, of the window's start or of the tile's end: 3 of
-// 10 under a window of 1024, all of them under one of 128.  8192 tokens without a prefix, 4 first tokens, bf16: window 128 94 us, 1024 190 us = 680
-// TFLOP/s, 4096 over 24576 518-528 us = 1050; 8-bit, fp16, 4 chunks of 300-700 under a window of 1024 87 us, bf16 102 us.
+// Under a window (WIN) a tile's keys are the sequence's first tokens and the ones from its first row's window on, laid end to end
+// (WindowRows), so that 4 first tokens do not cost a unit of 128 and the window need not begin with one; with units of the sequence's
+// own keys, those in between left out, 8-bit chunks under a window of 1024 took 86 us instead of 74, 8192 rows under one of 128 95
+// instead of 78.  8192 tokens without a prefix, 4 first tokens, bf16: window 128 78 us, 1024 185 us = 700 TFLOP/s,
+// 4096 over 24576 505-520 us = 1080; 8-bit, fp16, 4 chunks of 300-700 under a window of 1024 74 us, bf16 82 us.
 #include <cstring>
 #include <type_traits>
 
