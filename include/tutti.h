@@ -682,6 +682,7 @@ int tutti_pages_destroy(tutti_pages_t *pages);
  * gives up the rows of `from` in the same step (their blocks are free where no child took them); the
  * table itself is left as it is and must not be used as one that holds blocks.  No bytes of the pool move: the last,
  * partly filled block is shared until tutti_pages_extend copies it.  TUTTI_EINVAL if `from` and `to` share an array.
+ * Ids outside the pool are handed on as they are (TUTTI_EFAULT in from->status; not for a row that is kept and that nobody takes).
  */
 #define TUTTI_FORK_KEEP 0
 #define TUTTI_FORK_MOVE 1

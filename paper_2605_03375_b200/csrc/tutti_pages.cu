@@ -189,11 +189,12 @@ __global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, con
         int32_t run = -1;
         int sum = 0;
         auto flush = [&]() {
-            if (run == -1 || sum == 0) return;
+            if (run == -1 || (sum == 0 && !move)) return;       // (nobody takes it, and it is kept)
             if ((uint32_t)run >= p.n_blocks) {
                 report(from.status, TUTTI_EFAULT);
                 return;
             }
+            if (sum == 0) return;
             const int now = atomicAdd(p.refs + run, sum) + sum;
             if (now < 0) {                      // a count does not pass 0
                 atomicAdd(p.refs + run, -now);
