@@ -683,6 +683,7 @@ int tutti_pages_destroy(tutti_pages_t *pages);
  * table itself is left as it is and must not be used as one that holds blocks.  No bytes of the pool move: the last,
  * partly filled block is shared until tutti_pages_extend copies it.  TUTTI_EINVAL if `from` and `to` share an array.
  * Ids outside the pool are handed on as they are (TUTTI_EFAULT in from->status; not for a row that is kept and that nobody takes).
+ * A count that says less than the rows that give the block up does not pass 0 (TUTTI_EINVAL in from->status).
  */
 #define TUTTI_FORK_KEEP 0
 #define TUTTI_FORK_MOVE 1

@@ -79,6 +79,10 @@ __device__ inline void drop(const PagesDev &p, int32_t id, int32_t *status) {
     }
 }
 
+// What goes back to a count that `sum` has taken to `now`: as much of `sum` as lies below 0.  (Not all that lies below 0: several
+// may take from one count at once, and each gives back its own part.)
+__host__ __device__ inline int given_back(int now, int sum) { return now >= 0 || sum >= 0 ? 0 : now > sum ? -now : -sum; }
+
 // Sum over the CTA's threads before this one; `total` over all.  sums: [32] in shared memory.
 template <typename U>
 __device__ inline U scan(U x, U *sums, U &total) {
@@ -197,7 +201,7 @@ __global__ void __launch_bounds__(ROW_THREADS) fork_kernel(const PagesDev p, con
             if (sum == 0) return;
             const int now = atomicAdd(p.refs + run, sum) + sum;
             if (now < 0) {                      // a count does not pass 0
-                atomicAdd(p.refs + run, -now);
+                if (const int back = given_back(now, sum)) atomicAdd(p.refs + run, back);
                 report(from.status, TUTTI_EINVAL);
             }
         };
@@ -597,6 +601,7 @@ int tutti_compact_check_(const tutti_tables_t *t, const int32_t *pairs, uint32_t
     return TUTTI_OK;
 }
 int tutti_tables_check_(const tutti_tables_t *t) { return check_tables(t); }
+int tutti_fork_given_back_(int now, int sum) { return given_back(now, sum); }
 
 int tutti_pages_create(tutti_ctx_t *ctx, int32_t *refs, uint64_t n_blocks, tutti_pages_t **out) {
     if (!ctx || !refs || ((uint64_t)refs & 15) || !n_blocks || n_blocks > 0x7fffffffull || !out) return TUTTI_EINVAL;

@@ -39,3 +39,22 @@ def test_ids_outside_the_pool_are_reported_whatever_becomes_of_the_counts(ctx, m
         b.same(refs, 1)
     finally:
         b.close()
+
+
+def test_counts_do_not_pass_zero(ctx):
+    """More rows hold a block than its count says, in groups that different CTAs see to."""
+    n_seq, n_blocks = 90, 40
+    for seed in range(6):
+        frm = P.Book([n_blocks * s for s in range(n_seq + 1)], list(range(n_blocks)) * n_seq, [n_blocks * BS - seed] * n_seq, BS)
+        to = P.Book([0, n_blocks], [-9] * n_blocks, [5], BS)
+        refs = [(7 * i + seed) % 120 for i in range(n_blocks)]
+        b = P.Bound(ctx, [frm, to], refs)
+        try:
+            b.pages.tutti_pages_fork(b.tables(0), ints([-1]), b.tables(1), T.FORK_MOVE)
+            P.fork(frm, [-1], to, refs, True)
+            held = frm.row(0)[3]
+            assert frm.status == {T.EINVAL} and refs == [max(0, (7 * i + seed) % 120 - n_seq * (i < held)) for i in range(n_blocks)]
+            b.same(refs, 0)
+            b.same(refs, 1)
+        finally:
+            b.close()
