@@ -681,7 +681,8 @@ int tutti_pages_destroy(tutti_pages_t *pages);
  * be named any number of times: a sequence forks, or the beams of a search go on from the ones that were chosen.  move: TUTTI_FORK_MOVE
  * gives up the rows of `from` in the same step (their blocks are free where no child took them); the
  * table itself is left as it is and must not be used as one that holds blocks.  No bytes of the pool move: the last,
- * partly filled block is shared until tutti_pages_extend copies it.  TUTTI_EINVAL if `from` and `to` share an array.
+ * partly filled block is shared until tutti_pages_extend copies it.  What rows of `to` held before is written over, not
+ * released.  TUTTI_EINVAL if block_ids or len of `to` lies over any other array of the call, in part or as a whole (the tables may have one blk_start).
  * Ids outside the pool are handed on as they are (TUTTI_EFAULT in from->status; not for a row that is kept and that nobody takes).
  * A count that says less than the rows that give the block up does not pass 0 (TUTTI_EINVAL in from->status).
  */

@@ -576,6 +576,16 @@ int check_tables(const tutti_tables_t *t) {
     return TUTTI_OK;
 }
 
+// `n` 32-bit words in memory
+struct Words {
+    const void *at;
+    uint64_t n;
+};
+bool lie_over(const Words &a, const Words &b) {
+    const uint64_t x = (uint64_t)a.at, y = (uint64_t)b.at;
+    return x && y && a.n && b.n && x < y + 4 * b.n && y < x + 4 * a.n;
+}
+
 TablesDev on_device(const tutti_pages *pages, const tutti_tables_t *t) {
     return TablesDev{t->n_seq, t->n_blk, tutti_ctx_geom_(pages->ctx)->block_tokens, t->blk_start, t->block_ids, t->len, t->status};
 }
@@ -589,7 +599,13 @@ int tutti_fork_check_(const tutti_tables_t *from, const int32_t *parent, const t
     if (check_tables(from) || check_tables(to) || move > TUTTI_FORK_MOVE) return TUTTI_EINVAL;
     if (to->n_seq && (!parent || ((uint64_t)parent & 3))) return TUTTI_EINVAL;
     if ((from->block_ids && from->block_ids == to->block_ids) || (from->len && from->len == to->len)) return TUTTI_EINVAL;
-    return TUTTI_OK;
+    // what is written lies over nothing that is read, nor over each other (what is read may: both tables may have one blk_start)
+    const Words ids{to->block_ids, to->n_blk}, len{to->len, to->n_seq};
+    const Words read[] = {{from->block_ids, from->n_blk}, {from->len, from->n_seq}, {from->blk_start, (uint64_t)from->n_seq + 1},
+                          {to->blk_start, (uint64_t)to->n_seq + 1}, {parent, to->n_seq}};
+    for (const Words &r : read)
+        if (lie_over(ids, r) || lie_over(len, r)) return TUTTI_EINVAL;
+    return lie_over(ids, len) ? TUTTI_EINVAL : TUTTI_OK;
 }
 int tutti_extend_check_(const tutti_tables_t *t, const uint32_t *n_new, const int32_t *pairs) {
     if (check_tables(t) || (t->n_seq && (!n_new || !pairs)) || (((uint64_t)n_new | (uint64_t)pairs) & 3)) return TUTTI_EINVAL;
