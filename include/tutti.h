@@ -661,12 +661,12 @@ typedef struct tutti_tables {
     int32_t *status;
 } tutti_tables_t;
 
-#define TUTTI_PAGES_MAX_SEQ 16384
+#define TUTTI_PAGES_MAX_SEQ 65536
 
 /*
  * Counts of a pool's blocks: refs is a device pointer to [n_blocks] int32, 16-byte aligned, owned by the caller: how many
  * rows (of any table, or other holders of the caller's) hold a block; 0 is a free block.  A block's id is the same in all
- * layers, so the counts go by block.  The handle holds workspace (12 bytes a block and 0.4 MB): calls on one handle must be
+ * layers, so the counts go by block.  The handle holds workspace (12 bytes a block and 1.6 MB): calls on one handle must be
  * ordered after each other (one stream, or events; replays of captured graphs too), as must calls over the same counts.
  * Destroy it before its context.
  */

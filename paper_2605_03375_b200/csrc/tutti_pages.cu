@@ -562,8 +562,8 @@ struct tutti_pages {
     tutti_ctx *ctx;
     int device;
     PagesDev dev;
-    // rows' arrays and tiles; writers; top; rank.  In pieces, because those below a megabyte are made in 15 us each instead of 400 and more.
-    uint32_t *memory[4];
+    // rows' arrays, two each (and tiles); writers; top; rank.  In pieces, because those below a megabyte are made in 15 us each instead of 400 and more.
+    uint32_t *memory[6];
 };
 
 namespace {
@@ -626,9 +626,9 @@ int tutti_pages_create(tutti_ctx_t *ctx, int32_t *refs, uint64_t n_blocks, tutti
     tutti_pages *p = new (std::nothrow) tutti_pages();
     if (!p) return TUTTI_ENOMEM;
     const uint32_t tiles = (uint32_t)((n_blocks + TILE - 1) / TILE);
-    const size_t words[4] = {32 + (size_t)tiles + 6 * (size_t)TUTTI_PAGES_MAX_SEQ, n_blocks, n_blocks, (size_t)tiles * TILE};
+    const size_t rows = 2 * (size_t)TUTTI_PAGES_MAX_SEQ, words[6] = {rows + 32 + tiles, rows, rows, n_blocks, n_blocks, (size_t)tiles * TILE};
     cudaError_t e = cudaSuccess;
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 6; ++i) {
         p->memory[i] = nullptr;
         if (e == cudaSuccess) e = cudaMalloc((void **)&p->memory[i], words[i] * 4);
         if (e == cudaSuccess) e = cudaMemset(p->memory[i], 0, words[i] * 4);
@@ -647,25 +647,19 @@ int tutti_pages_create(tutti_ctx_t *ctx, int32_t *refs, uint64_t n_blocks, tutti
     d.refs = refs;
     d.n_blocks = (uint32_t)n_blocks;
     d.n_tiles = tiles;
-    d.arrive = p->memory[0];
-    d.moves = p->memory[0] + 1;
-    d.total = (unsigned long long *)(p->memory[0] + 2);
-    uint32_t *at = p->memory[0] + 32;
-    auto take = [&](size_t n) {
-        uint32_t *a = at;
-        at += n;
-        return a;
-    };
-    d.turn = take(TUTTI_PAGES_MAX_SEQ);
-    d.begin = take(TUTTI_PAGES_MAX_SEQ);
-    d.entry = take(TUTTI_PAGES_MAX_SEQ);
-    d.mark = (int32_t *)take(TUTTI_PAGES_MAX_SEQ);
-    d.keep_id = (int32_t *)take(TUTTI_PAGES_MAX_SEQ);
-    d.keep_count = (int32_t *)take(TUTTI_PAGES_MAX_SEQ);
-    d.tile = take(tiles);
-    d.writers = p->memory[1];
-    d.top = p->memory[2];
-    d.rank = p->memory[3];
+    d.turn = p->memory[0];
+    d.begin = d.turn + TUTTI_PAGES_MAX_SEQ;
+    d.arrive = p->memory[0] + rows;
+    d.moves = d.arrive + 1;
+    d.total = (unsigned long long *)(d.arrive + 2);
+    d.tile = d.arrive + 32;
+    d.entry = p->memory[1];
+    d.mark = (int32_t *)d.entry + TUTTI_PAGES_MAX_SEQ;
+    d.keep_id = (int32_t *)p->memory[2];
+    d.keep_count = d.keep_id + TUTTI_PAGES_MAX_SEQ;
+    d.writers = p->memory[3];
+    d.top = p->memory[4];
+    d.rank = p->memory[5];
     *out = p;
     return TUTTI_OK;
 }

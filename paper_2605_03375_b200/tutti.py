@@ -27,7 +27,7 @@ ENGINE_AUTO, ENGINE_LDST, ENGINE_BULK = 0, 1, 2
 DTYPE_BF16, DTYPE_FP16 = 0, 1
 ROPE_HALF, ROPE_PAIRS = 0, 1
 FORK_KEEP, FORK_MOVE = 0, 1
-PAGES_MAX_SEQ = 16384
+PAGES_MAX_SEQ = 65536
 
 
 class Geom(C.Structure):
