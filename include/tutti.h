@@ -601,7 +601,7 @@ int tutti_kv_append_layer(tutti_ctx_t *ctx, uint32_t layer, const tutti_step_t *
  * n_q_heads / n_kv_heads).  An 8-bit pool's keys and values are code * scale; what is rounded there:
  *   up to 16 rows: the scales are applied in 32 bits.  bf16 queries become fp16 in units of a power of
  *   two of the row: exact but for elements below 2^-14 of its largest, which are off by up to 2^-25 of it.
- *   more rows, bf16: nothing where scales are powers of two (append's are), else code * scale once.
+ *   more rows, bf16: nothing where scales are powers of two (append's are), else the scale to bf16, and code * it once more.
  *   more rows, fp16: code * scale in units of a power of two, one for 64 neighbouring keys.  Keys are exact
  *   unless a scale among the 64 is more than 2^22 times larger; values of magnitude below 2^-13 are off by up
  *   to 2^-24, the smallest step of an fp16 output.  (Scales that are not powers of two: rounded to 11 bits.)
