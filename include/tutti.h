@@ -698,6 +698,7 @@ int tutti_pages_fork(tutti_pages_t *pages, const tutti_tables_t *from, const int
  * place, and pairs[2 s], pairs[2 s + 1] (device, [n_seq][2]) are the old and the new one, for tutti_kv_copy_blocks; all other pairs
  * are -1.  Of the rows that share the block they write to, the last one keeps it if nobody else holds it.
  * All rows or none: with too few free blocks nothing changes, all pairs are -1 and *status is TUTTI_EAGAIN.
+ * (A step's few blocks take 5-8 us; the blocks of whole prompts 1.1 us a thousand.)
  * A row is skipped (TUTTI_EINVAL) that has no room for its blocks or passes 2^31 - 1 tokens, or whose written block has a count below 1;
  * TUTTI_EFAULT, and skipped, if that block is outside the pool (an entry of -1 is no block: there is nothing to copy).
  */
@@ -734,7 +735,8 @@ int tutti_pages_compact(tutti_pages_t *pages, const tutti_tables_t *tables, int3
  * TUTTI_EFAULT in *status (may be NULL; as in tutti_step_t) for an id outside a layer's pool; that pair is not
  * copied in that layer.  TUTTI_ETIMEDOUT: a bounded wait ran out, the copies are incomplete.
  * Any registered layers, whatever their elements.  Asynchronous on `stream`, graph-capturable, one launch for
- * every 64 layers.  TUTTI_EINVAL for layers out of range or not registered, or a bad pointer.
+ * every 64 layers.  The launch is as large as max_pairs may need, also where *n_pairs is small (0.8 us a thousand): give the
+ * number of moves that a compaction may make, not of blocks.  TUTTI_EINVAL for layers out of range or not registered, or a bad pointer.
  */
 int tutti_kv_copy_blocks(tutti_ctx_t *ctx, uint32_t first_layer, uint32_t n_layers, const int32_t *pairs,
                          uint32_t max_pairs, const uint32_t *n_pairs, int32_t *status, void *stream);

@@ -44,7 +44,7 @@
 // (WindowRows), so that 4 first tokens do not cost a unit of 128 and the window need not begin with one; with units of the sequence's
 // own keys, those in between left out, 8-bit chunks under a window of 1024 took 86 us instead of 74, 8192 rows under one of 128 95
 // instead of 78.  8192 tokens without a prefix, 4 first tokens, bf16: window 128 78 us, 1024 185 us = 700 TFLOP/s,
-// 4096 over 24576 505-520 us = 1080; 8-bit, fp16, 4 chunks of 300-700 under a window of 1024 74 us, bf16 82 us.
+// 4096 over 24576 505-555 us = 990-1080; 8-bit, fp16, 4 chunks of 300-700 under a window of 1024 74 us, bf16 82 us.
 #include <cstring>
 #include <type_traits>
 

@@ -5,6 +5,8 @@
 // kernel is a launch and three to six rounds of loads that depend on each other.  On a B200, in a captured graph: fork of 64 rows
 // of 160 entries 4.7 us, of 128 rows of 8200 7.8; extend of 64 rows 5.0-6.4, of 1024 rows among a million blocks 7.4; trim of 64 rows of
 // 1040 entries 1.9, of 1024 of 520 3.7; release 1.7; compact of 5000 blocks 6.0.
+// Two things grow with the call: an extension's new blocks are given out by one CTA, 1.1 us a thousand (by 512 blocks 5.5 us, 4096 9.4,
+// 32768 43, 524288 597), and the rows are seen by every CTA of fork, or by one of extend (65536 rows: fork 500 us, extend 219, trim 42).
 #include <new>
 
 #include "tutti_attend.h"
